@@ -4,7 +4,9 @@
  * The library implements the query-time path of FROG ("FROG: Efficient
  * Range-Filtering Approximate Nearest Neighbor Search on GPUs", arxiv
  * 2608.16491) on one AMD GPU, plus the host-side index construction that
- * produces its input and an exhaustive filtered search used as ground truth.
+ * produces its input and an exhaustive filtered search used as ground truth;
+ * and attention over rows kept in attribute order, each query over one rank
+ * interval of them, with the upkeep of the cache that holds the rows.
  *
  * Conventions for every entry point:
  *   - Return value: FROG_OK (0) or a negative FROG_E* code.  frog_last_error()
@@ -293,6 +295,137 @@ int frog_bruteforce_filtered(const frog_index_t* idx, const float* d_queries, in
                              const double* d_lo, const double* d_hi, int k,
                              int32_t* d_ids, float* d_dists, int32_t* d_certified,
                              void* stream);
+
+/* ---------------------------------------------------------------- attention
+ *
+ * Attention over a store of rows in attribute order (token positions, time
+ * stamps, offsets in documents): the softmax counterpart of the filtered
+ * k-NN.  Query i of sequence b, head h, sees the keys of one rank interval
+ * [l, r] (as frog_rank_bounds writes them; clipped to the keys, empty when
+ * l > r), which says causal, window, document, prefix and padding masks.
+ * With x = scale q.k, kv head h' = h / (heads / kv_heads):
+ *   y = cap tanh(x / cap)  (cap > 0; else y = x)
+ *   z = y - slopes[h] |at_q[b, i] - at_k[b, h', j]|   (slopes given)
+ *   lse = log sum exp z,  p = exp(z - lse),  out = sum p v
+ * over the keys of the interval; out = 0 and lse = -inf for an empty one.
+ * Values are fp32, fp16 or bf16 (FROG_STORAGE_*); products, softmax
+ * statistics and sums are fp32.  With 16-bit values p (and in the gradient
+ * p's share of the score's) is rounded to the type as a factor of the second
+ * product, and each output once.
+ *
+ * Rows no interval meets are not read into any result: a cache's unused tail
+ * may hold anything.  Rows some interval meets must be finite (a NaN or
+ * infinite row may reach other queries of the same sequence).
+ *
+ * Strides count values; the last axis (d values) is contiguous.  Every row
+ * must start on a 16-byte boundary (pointers and strides), else FROG_EINVAL.
+ * d is 32, 64, 96 or 128 (FROG_EUNSUPPORTED otherwise: pad with zeros).
+ * Calls run on the current HIP device.  The structs may be zeroed first; a
+ * zero pointer leaves an optional argument out. */
+typedef struct {
+    /* [batch, token, head] strides */
+    const void* q; int64_t q_stride[3];
+    const void* k; int64_t k_stride[3];
+    const void* v; int64_t v_stride[3];
+    void* out; int64_t out_stride[3];  /* written (frog_attend_backward: read) */
+    const int32_t* lr;          /* [batch][queries][2] intervals; NULL: every key */
+    int64_t lr_stride;          /* values from one sequence's intervals to the next's; 0: shared */
+    const float* slopes;        /* [heads] slopes of the distance bias; NULL: none */
+    const float* at_q;          /* attributes of the queries (with slopes) */
+    int64_t at_q_stride;        /* per sequence */
+    const float* at_k;          /* attributes of the keys (with slopes) */
+    int64_t at_k_stride[2];     /* per sequence, per kv head */
+    float* lse;                 /* [batch][heads][queries]; NULL: not wanted (backward: read) */
+    const float* w_in;          /* [batch][kv_heads][keys] weights so far; NULL: 0 */
+    float* w_out;               /* w_in + the sum of p over queries and the group's heads
+                                   (may be w_in); NULL: not wanted */
+    /* frog_attend_backward only */
+    const void* dout; int64_t dout_stride[3];
+    void* dq; int64_t dq_stride[3];
+    void* dk; int64_t dk_stride[3];
+    void* dv; int64_t dv_stride[3];
+    /* workspace of at least frog_attend_workspace() bytes, 256-byte aligned,
+     * the caller's until `stream` has run the call; NULL: the library's
+     * buffer of (device, stream), as for frog_search_ex */
+    void* ws;
+    int64_t ws_bytes;
+    int64_t batch, queries, keys;
+    int32_t heads, kv_heads, d, type;
+    float scale, cap;
+} frog_attend_t;
+
+/* Bytes of workspace the call takes (0: none); a negative FROG_E* if it would
+ * be refused. */
+int64_t frog_attend_workspace(const frog_attend_t* a, int backward);
+
+/* Forward pass: out, and lse and w_out where wanted. */
+int frog_attend(const frog_attend_t* a, void* stream);
+
+/* Gradients of sum(dout * out): dq, dk, dv, from q, k, v, out, lse of the
+ * forward pass with the same arguments.  Rows without a query get 0, as do
+ * queries with an empty interval (their dout is not read into a result).
+ * Results do not depend on the order in which the device runs the work. */
+int frog_attend_backward(const frog_attend_t* a, void* stream);
+
+/* One query token per request over a prefix that all requests share, followed
+ * by the request's own tail in pages: key t of the tail of request b is row
+ * t % page of page pages[b][t / page] of k_pages / v_pages.  Keys count 0 ..
+ * prefix - 1 for the prefix, prefix + t for the tail; the query stands at
+ * prefix + lengths[b] - 1 (its distance to a key is the difference of these
+ * numbers).  lr (optional) limits what a request sees of the prefix.  The
+ * prefix is read once for all requests.  Page entries past a tail's length
+ * are not read; a length is clipped to pages_per_request * page, and an entry
+ * outside [0, num_pages) counts as no rows. */
+typedef struct {
+    const void* q; int64_t q_stride[2];        /* [batch, heads, d]: request, head */
+    const void* k; int64_t k_stride[2];        /* prefix: token, head */
+    const void* v; int64_t v_stride[2];
+    const void* k_pages; int64_t k_pages_stride[3]; /* page, row, head */
+    const void* v_pages; int64_t v_pages_stride[3];
+    const int32_t* pages;                      /* [batch][pages_per_request] */
+    const int32_t* lengths;                    /* [batch] */
+    const int32_t* lr;                         /* [batch][2] intervals of the prefix; NULL: all of it */
+    const float* slopes;                       /* [heads]; NULL: no distance bias */
+    void* out; int64_t out_stride[2];
+    float* lse;                                /* [batch][heads]; NULL: not wanted */
+    void* ws;
+    int64_t ws_bytes;
+    int64_t batch, prefix, num_pages, pages_per_request;
+    int32_t page, heads, kv_heads, d, type;
+    float scale, cap;
+} frog_attend_shared_t;
+
+int64_t frog_attend_shared_workspace(const frog_attend_shared_t* a);
+int frog_attend_shared(const frog_attend_shared_t* a, void* stream);
+
+/* Shorten the caches of a batch to the rows worth keeping: of the lengths[b]
+ * rows of every (sequence, head), the last `recent`, and of the others the
+ * keep - recent with the largest weight (equal weights: the lower slot; NaN
+ * counts as the smallest); all of them when lengths[b] <= keep.  Kept rows are
+ * copied in slot order (attribute order stays, so an interval of attributes
+ * stays an interval of slots); slots past them get 0, weight 0, position -1.
+ * The outputs must not overlap the inputs.  0 <= recent <= keep <= slots;
+ * lengths are clipped to [0, slots].  Any d whose rows are a multiple of 16
+ * bytes; row starts on 16-byte boundaries. */
+typedef struct {
+    const void* k; int64_t k_stride[3];        /* [batch, slots, heads, d]: sequence, slot, head */
+    const void* v; int64_t v_stride[3];
+    const float* weights;                      /* [batch][heads][slots] */
+    const int32_t* positions;                  /* [batch][heads][slots]; NULL: the slot itself */
+    const int32_t* lengths;                    /* [batch] */
+    void* k_out;                               /* [batch][keep][heads][d], packed */
+    void* v_out;
+    float* weights_out;                        /* [batch][heads][keep] */
+    int32_t* positions_out;                    /* [batch][heads][keep] */
+    int32_t* lengths_out;                      /* [batch] */
+    void* ws;
+    int64_t ws_bytes;
+    int64_t batch, slots, keep, recent;
+    int32_t heads, d, type;
+} frog_evict_t;
+
+int64_t frog_evict_workspace(const frog_evict_t* a);
+int frog_evict(const frog_evict_t* a, void* stream);
 
 /* Message of the last failure on this thread ("" if none). */
 const char* frog_last_error(void);

@@ -31,6 +31,8 @@ SYMBOLS = (
     "frog_index_load", "frog_index_upload", "frog_index_upload_ex", "frog_index_free",
     "frog_build_index_gpu", "frog_index_build_stats", "frog_rank_bounds", "frog_search",
     "frog_search_ex", "frog_search_noalloc", "frog_index_prepare_sample", "frog_bruteforce_filtered",
+    "frog_attend", "frog_attend_backward", "frog_attend_workspace", "frog_attend_shared",
+    "frog_attend_shared_workspace", "frog_evict", "frog_evict_workspace",
     "frog_last_error",
 )
 
@@ -108,6 +110,11 @@ def lib() -> C.CDLL:
     L.frog_index_prepare_sample.argtypes = [P, C.c_uint64]
     L.frog_bruteforce_filtered.restype = i32
     L.frog_bruteforce_filtered.argtypes = [P, P, i64, P, P, i32, P, P, P, P]
+    for name in ("frog_attend", "frog_attend_shared", "frog_evict"):
+        for fn, args, res in ((name, [P, P], i32), (name + "_workspace", [P] + [i32] * (name == "frog_attend"), i64)):
+            getattr(L, fn).argtypes, getattr(L, fn).restype = args, res
+    L.frog_attend_backward.restype = i32
+    L.frog_attend_backward.argtypes = [P, P]
     _lib = L
     return L
 
@@ -318,3 +325,17 @@ def bruteforce(index: Index, Q, lo, hi, k: int, stream=None):
                                           _dev(hi, torch.float64), k, _dev(ids, torch.int32),
                                           _dev(ds, torch.float32), _dev(cert, torch.int32), _stream(stream)))
     return ids, ds, cert
+
+
+# ------------------------------------------------------------------ attention
+
+_ATTENTION = ("attend", "attend_shared", "evict")
+
+
+def __getattr__(name):
+    # attend, attend_shared and evict need torch, which this module imports
+    # only where a call does
+    if name in _ATTENTION:
+        from . import attention
+        return getattr(attention, name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

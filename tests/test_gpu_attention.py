@@ -1,0 +1,258 @@
+"""Range attention on the GPU: forward, log sum, key weights and gradients
+against the formulas in 64 bits, each element within a bound derived from the
+rows' type and the sizes (attention_ref.py)."""
+import itertools
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+import paper_2608_16491_amd as F  # noqa: E402
+from tests.attention_ref import Attention, intervals, near  # noqa: E402
+
+TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+
+
+def make(kind, b, tq, tk, h, kv, d, mask, bias=False, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    t = TYPES[kind]
+
+    def normal(*shape, std=1.0):
+        return (torch.randn(shape, generator=g, device="cuda") * std).to(t)
+
+    s = dict(q=normal(b, tq, h, d, std=1.5), k=normal(b, tk, kv, d), v=normal(b, tk, kv, d))
+    lr = intervals(mask, b, tq, tk, seed)
+    s["lr"] = None if lr is None else lr.cuda()
+    opt = {}
+    if bias:
+        opt = dict(slopes=torch.exp2(-8.0 * torch.arange(1, h + 1, device="cuda") / h),
+                   at_q=torch.rand((b, tq), generator=g, device="cuda") * tk,
+                   at_k=torch.rand((b, kv, tk), generator=g, device="cuda") * tk)
+    return s, opt, normal(b, tq, h, d)
+
+
+def check(s, opt, dout, cap, what):
+    """Forward with lse and weights, and gradients, of one call."""
+    ref = Attention(s["q"], s["k"], s["v"], s["lr"], cap=cap, dout=dout, **opt)
+    b, tk, kv = s["k"].shape[:3]
+    w = torch.rand((b, kv, tk), device="cuda")
+    out, lse, w2 = F.attend(s["q"], s["k"], s["v"], s["lr"], cap=cap, return_lse=True, weights=w, **opt)
+    near(out, ref.out, ref.out_err, what + " out")
+    near(lse, ref.lse, ref.lse_err, what + " lse")
+    near(w2, w.double() + ref.weights, ref.weights_err + 4e-7 * (w.double() + ref.weights), what + " weights")
+    q, k, v = (s[x].detach().requires_grad_() for x in ("q", "k", "v"))
+    o = F.attend(q, k, v, s["lr"], cap=cap, **opt)
+    assert torch.equal(o, out)
+    dq, dk, dv = torch.autograd.grad(o, (q, k, v), dout)
+    near(dq, ref.dq, ref.dq_err, what + " dq")
+    near(dk, ref.dk, ref.dk_err, what + " dk")
+    near(dv, ref.dv, ref.dv_err, what + " dv")
+
+
+SHAPES = [  # b, tq, tk, h, kv, d
+    (1, 1, 1, 1, 1, 32), (2, 1, 77, 8, 2, 64), (1, 1, 1500, 8, 1, 128), (3, 2, 33, 6, 3, 96), (1, 5, 300, 14, 2, 128),
+    (2, 31, 31, 4, 4, 64), (1, 65, 200, 4, 2, 128), (2, 129, 129, 3, 1, 96), (1, 257, 257, 8, 8, 32), (1, 200, 333, 7, 1, 64),
+    (1, 500, 700, 4, 1, 128), (1, 17, 1000, 16, 2, 128),
+]
+MASKS = ["causal", "window", "prefix", "documents", "lengths", "wild", None]
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_attention(kind, shape):
+    print(f"[gpu] attention {kind} {shape}", flush=True)
+    at = SHAPES.index(shape)
+    for n, (cap, bias) in enumerate(itertools.product((0.0, 5.0), (False, True))):
+        mask = MASKS[(at + 2 * n) % len(MASKS)]
+        s, opt, dout = make(kind, *shape, mask, bias, seed=at * 10 + n)
+        check(s, opt, dout, cap, f"{mask} cap {cap} bias {bias}")
+
+
+@pytest.mark.parametrize("mask", ["wild", "empty", "documents"])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_masks(kind, mask):
+    s, opt, dout = make(kind, 2, 150, 190, 4, 2, 64, mask, seed=5)
+    check(s, opt, dout, 0.0, mask)
+    if mask == "empty":
+        out, lse = F.attend(s["q"], s["k"], s["v"], s["lr"], return_lse=True)
+        assert not out.any() and bool((lse == -math.inf).all())
+
+
+@pytest.mark.parametrize("tq", [1, 3, 70])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_rows_no_interval_meets_may_hold_anything(kind, tq):
+    s, opt, dout = make(kind, 2, tq, 130, 4, 2, 64, "lengths", seed=11)
+    s["lr"][0, :, 0], s["lr"][0, :, 1] = 37, 90 + torch.arange(tq, device="cuda") % 3
+    s["lr"][1, :, 0], s["lr"][1, :, 1] = 5, -1
+    for x in ("k", "v"):
+        s[x][0, :37], s[x][0, 93:], s[x][1] = math.nan, math.inf, math.nan
+        if tq < 3:
+            s[x][0, 90 + tq:] = math.nan
+    dout[1] = math.nan        # no query of it sees a key
+    check(s, opt, dout, 0.0, "nan")
+
+
+def test_intervals_shared_by_the_batch_and_no_keys_and_no_queries():
+    s, opt, dout = make("bf16", 3, 40, 60, 4, 2, 64, "causal")
+    a = F.attend(s["q"], s["k"], s["v"], s["lr"])
+    assert torch.equal(a, F.attend(s["q"], s["k"], s["v"], s["lr"][0].contiguous()))
+    w = torch.rand((3, 2, 0), device="cuda")
+    out, lse, w2 = F.attend(s["q"], s["k"][:, :0], s["v"][:, :0], return_lse=True, weights=w)
+    assert not out.any() and bool((lse == -math.inf).all()) and w2.numel() == 0
+    w = torch.rand((3, 2, 60), device="cuda")
+    out, w2 = F.attend(s["q"][:, :0], s["k"], s["v"], weights=w)
+    assert out.shape == (3, 0, 4, 64) and torch.equal(w, w2)
+    q, k, v = (x.detach().requires_grad_() for x in (s["q"][:, :0], s["k"], s["v"]))
+    F.attend(q, k, v).sum().backward()
+    assert not k.grad.any() and not v.grad.any()
+
+
+@pytest.mark.parametrize("tq", [1, 100])
+def test_strides(tq):
+    s, opt, dout = make("bf16", 2, tq, 140, 4, 2, 64, "causal", seed=3)
+    plain = F.attend(s["q"], s["k"], s["v"], s["lr"])
+    heads_first = {x: s[x].transpose(1, 2).contiguous().transpose(1, 2) for x in ("q", "k", "v")}
+    assert torch.equal(plain, F.attend(heads_first["q"], heads_first["k"], heads_first["v"], s["lr"]))
+    # q, k, v as slices of one wider tensor, and queries in reverse memory order of the batch
+    wide = torch.full((2, 140, 3, 2, 80), math.nan, device="cuda", dtype=torch.bfloat16)
+    wide[:, :, 1, :, 8:72], wide[:, :, 2, :, 8:72] = s["k"], s["v"]
+    k, v = wide[:, :, 1, :, 8:72], wide[:, :, 2, :, 8:72]
+    assert torch.equal(plain, F.attend(s["q"], k, v, s["lr"]))
+    # one kv head seen as two by a stride of 0, and its gradient
+    one = s["k"][:, :, :1]
+    both = one.expand(2, 140, 2, 64)
+    assert torch.equal(F.attend(s["q"], both, both, s["lr"]), F.attend(s["q"], one, one, s["lr"]))
+    a, b = one.detach().clone().requires_grad_(), one.detach().clone().requires_grad_()
+    F.attend(s["q"], a.expand(2, 140, 2, 64), s["v"], s["lr"]).backward(dout)
+    ref = Attention(s["q"], both, s["v"], s["lr"], dout=dout)
+    near(a.grad, ref.dk.sum(2, keepdim=True), ref.dk_err.sum(2, keepdim=True) + 2.0 ** -7 * ref.dk.abs().sum(2, keepdim=True), "dk")
+    # a gradient of the output that is one number spread by strides of 0
+    q = s["q"].detach().requires_grad_()
+    F.attend(q, s["k"], s["v"], s["lr"]).sum().backward()
+    ref = Attention(s["q"], s["k"], s["v"], s["lr"], dout=torch.ones_like(dout))
+    near(q.grad, ref.dq, ref.dq_err, "dq of the sum")
+
+
+def test_rows_past_32_bit_offsets():
+    # two sequences 2^31 values and more apart, tokens 2^22 values apart
+    big = torch.empty(2 ** 32 + 2 ** 20, dtype=torch.float16, device="cuda")
+    s, opt, dout = make("fp16", 2, 40, 900, 2, 1, 64, "causal", seed=9)
+    k = big.as_strided((2, 900, 1, 64), (2 ** 31 + 2 ** 16, 2 ** 21, 64, 1))
+    v = big.as_strided((2, 900, 1, 64), (2 ** 31 + 2 ** 16, 2 ** 21, 64, 1), 2 ** 19)
+    k.copy_(s["k"])
+    v.copy_(s["v"])
+    for tq in (1, 40):
+        q, lr = s["q"][:, -tq:].contiguous(), s["lr"][:, -tq:].contiguous()
+        assert torch.equal(F.attend(q, k, v, lr), F.attend(q, s["k"], s["v"], lr))
+    a = [x.detach().requires_grad_() for x in (s["q"], s["k"], s["v"])]
+    c = [x.detach().requires_grad_() for x in (s["q"], k, v)]
+    o, o2 = F.attend(*a, s["lr"]), F.attend(*c, s["lr"])
+    for x, y in zip(torch.autograd.grad(o, a, dout), torch.autograd.grad(o2, c, dout)):
+        assert torch.equal(x, y)
+
+
+def test_gradient_against_differences():
+    s, opt, dout = make("fp32", 2, 40, 50, 4, 2, 32, "documents", bias=True, seed=21)
+    x = [s[n].detach().requires_grad_() for n in ("q", "k", "v")]
+    grads = torch.autograd.grad(F.attend(*x, s["lr"], cap=3.0, **opt), x, dout)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for i, grad in enumerate(grads):
+        for _ in range(3):
+            way = torch.randn(grad.shape, generator=g, device="cuda")
+
+            def at(step):
+                y = [t.detach() for t in x]
+                y[i] = y[i] + step * way
+                return (F.attend(*y, s["lr"], cap=3.0, **opt).double() * dout.double()).sum().item()
+
+            # central differences of fourth order: the error is of the order step^4 + 1e-7 sqrt(outputs) / step
+            h = 0.02
+            slope = (8 * (at(h) - at(-h)) - (at(2 * h) - at(-2 * h))) / (12 * h)
+            exact = (grad.double() * way.double()).sum().item()
+            assert abs(slope - exact) < 2e-3 * (1 + abs(exact)), (i, slope, exact)
+
+
+def test_runs_repeat_bit_for_bit():
+    for shape in ((1, 1, 5000, 8, 2, 128), (1, 300, 300, 8, 2, 64)):
+        s, opt, dout = make("bf16", *shape, "causal", seed=2)
+        x = [s[n].detach().requires_grad_() for n in ("q", "k", "v")]
+        w = torch.zeros((1, 2, shape[2]), device="cuda")
+        o, w1 = F.attend(*x, s["lr"], weights=w)
+        grads = torch.autograd.grad(o, x, dout)
+        for _ in range(3):
+            o2, w2 = F.attend(*x, s["lr"], weights=w)
+            assert torch.equal(o, o2) and torch.equal(w1, w2)
+            assert all(torch.equal(a, b) for a, b in zip(grads, torch.autograd.grad(o2, x, dout)))
+
+
+def test_another_stream():
+    s, opt, dout = make("bf16", 2, 3, 4000, 8, 2, 128, "causal", seed=4)
+    want = F.attend(s["q"], s["k"], s["v"], s["lr"])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        got = F.attend(s["q"], s["k"], s["v"], s["lr"], stream=side)
+        side.synchronize()
+        assert torch.equal(got, want)
+    with torch.cuda.stream(side):
+        got = F.attend(s["q"], s["k"], s["v"], s["lr"])
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("shape", [(2, 1, 3000, 8, 2, 128), (1, 200, 200, 4, 2, 64)], ids=str)
+def test_graph(shape):
+    s, opt, dout = make("bf16", *shape, "causal", seed=6)
+    x = [s[n].detach().requires_grad_() for n in ("q", "k", "v")]
+    w = torch.zeros((shape[0], shape[4], shape[2]), device="cuda")
+
+    def step():
+        o, w2 = F.attend(*x, s["lr"], weights=w)
+        return (o, w2, *torch.autograd.grad(o, x, dout))
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for n in range(4):
+        with torch.no_grad():
+            x[0].normal_()
+            w.uniform_()
+        want = step()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert torch.equal(a, b), n
+
+
+def test_weights_in_place():
+    s, opt, dout = make("bf16", 2, 2, 100, 4, 2, 64, "causal")
+    w = torch.rand((2, 2, 100), device="cuda")
+    _, new = F.attend(s["q"], s["k"], s["v"], s["lr"], weights=w)
+    _, same = F.attend(s["q"], s["k"], s["v"], s["lr"], weights=w, weights_out=w)
+    assert same is w and torch.equal(w, new)
+
+
+def test_refusals():
+    s, opt, dout = make("bf16", 2, 3, 20, 4, 2, 64, "causal")
+    q, k, v, lr = (s[x] for x in ("q", "k", "v", "lr"))
+    sl, aq, ak = torch.ones(4, device="cuda"), torch.zeros((2, 3), device="cuda"), torch.zeros((2, 20), device="cuda")
+    for bad in (lambda: F.attend(q.cpu(), k, v), lambda: F.attend(q, k.float(), v), lambda: F.attend(q, k, v[:, :5]),
+                lambda: F.attend(q.double(), k.double(), v.double()), lambda: F.attend(q, k, v, lr.long()),
+                lambda: F.attend(q, k, v, lr[:, :2]), lambda: F.attend(q, k, v, lr, slopes=sl),
+                lambda: F.attend(q, k, v, slopes=sl, at_q=aq, at_k=ak[:, :3]), lambda: F.attend(q[0], k, v),
+                lambda: F.attend(q, k, v, weights=torch.zeros((2, 4, 20), device="cuda")),
+                lambda: F.attend(q.transpose(2, 3).contiguous().transpose(2, 3), k, v),
+                lambda: F.attend(q, k, v, weights_out=torch.zeros((2, 2, 20), device="cuda"))):
+        with pytest.raises(ValueError):
+            bad()
+    wide = torch.zeros((2, 3, 4, 70), dtype=torch.bfloat16, device="cuda")
+    for bad, code in ((lambda: F.attend(wide[..., 3:67], k, v), -1), (lambda: F.attend(wide[..., :64], k, v), -1),
+                      (lambda: F.attend(q[..., :48], k[..., :48], v[..., :48]), -7), (lambda: F.attend(q[:, :, :3], k, v), -1),
+                      (lambda: F.attend(q, k, v, cap=-1.0), -1), (lambda: F.attend(q, k, v, scale=math.nan), -1)):
+        with pytest.raises(F.FrogError) as e:
+            bad()
+        assert e.value.code == code
