@@ -19,6 +19,9 @@
 namespace frog {
 
 constexpr float kLog2e = 1.44269504088896340736f;
+// Largest distance of one key (query) row from the next, in bytes: 64 rows
+// stay within 32-bit offsets.
+constexpr int64_t kMaxTokenStride = (int64_t)1 << 24;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // element types of the rows

@@ -1,132 +1,142 @@
-// Range attention, forward (include/frog.h: frog_attend).
-//
-// One wavefront per (sequence, query, head): 64 keys a step, a lane each, the
-// running maximum and sum of the softmax in registers, then the lanes turn to
-// the values' columns.  The weights are summed per key in a second pass.
+// Range attention: how a call is cut and where its workspace lies, and the
+// dispatch by row type (include/frog.h: frog_attend, frog_attend_backward).
 
-#include "attend.h"
+#include <algorithm>
+
+#include "attend_launch.h"
 
 namespace frog {
 namespace {
 
-constexpr int kBlock = 256;
-
-__device__ inline float wave_max(float x) {
-    for (int o = 32; o; o >>= 1) x = fmaxf(x, __shfl_xor(x, o));
-    return x;
-}
-__device__ inline float wave_sum(float x) {
-    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
-    return x;
+int64_t take(int64_t* at, int64_t bytes) {
+    const int64_t here = *at;
+    *at = (here + bytes + 255) / 256 * 256;
+    return here;
 }
 
-template <typename T>
-__device__ inline float dot_row(const float* q, const T* k, int d) {
-    float s = 0.f;
-    for (int c = 0; c < d; ++c) s = fmaf(q[c], (float)k[c], s);
-    return s;
-}
-
-template <typename T, bool CAP>
-__global__ __launch_bounds__(kBlock) void attend_rows(frog_attend_t a, ScoreParams sp, float* lse) {
-    __shared__ float qs[4][128], ps[4][64];
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + w;
-    if (row >= a.batch * a.heads * a.queries) return;
-    const int64_t i = row % a.queries, bh = row / a.queries;
-    const int h = (int)(bh % a.heads);
-    const int64_t b = bh / a.heads;
-    const int hk = h / (a.heads / a.kv_heads);
-    const T* q = (const T*)a.q + b * a.q_stride[0] + i * a.q_stride[1] + h * a.q_stride[2];
-    const T* k = (const T*)a.k + b * a.k_stride[0] + hk * a.k_stride[2];
-    const T* v = (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2];
-    for (int c = lane; c < a.d; c += 64) qs[w][c] = (float)q[c];
-    int64_t lo = 0, hi = a.keys - 1;
-    if (a.lr) {
-        const int32_t* p = a.lr + b * a.lr_stride + 2 * i;
-        lo = max(lo, (int64_t)p[0]);
-        hi = min(hi, (int64_t)p[1]);
-    }
-    const float slope = a.slopes ? a.slopes[h] * kLog2e : 0.f;
-    const float aq = a.slopes ? a.at_q[b * a.at_q_stride + i] : 0.f;
-    const float* ak = a.slopes ? a.at_k + b * a.at_k_stride[0] + hk * a.at_k_stride[1] : nullptr;
-    float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
-    for (int64_t j0 = lo; j0 <= hi; j0 += 64) {
-        const int64_t j = j0 + lane;
-        float z = -INFINITY;
-        if (j <= hi) {
-            z = score2<CAP>(sp, dot_row(qs[w], k + j * a.k_stride[1], a.d));
-            if (ak) z -= slope * fabsf(aq - ak[j]);
-        }
-        const float mn = fmaxf(m, wave_max(z));
-        const float p = j <= hi ? exp2_fast(z - mn) : 0.f, scale = exp2_fast(m - mn);
-        l = l * scale + wave_sum(p);
-        m = mn;
-        ps[w][lane] = p;
-        const int cnt = (int)min((int64_t)64, hi - j0 + 1);
-        for (int u = 0; u < 2; ++u) {
-            const int c = lane + 64 * u;
-            if (c >= a.d) break;
-            float o = acc[u] * scale;
-            for (int t = 0; t < cnt; ++t) o = fmaf(ps[w][t], (float)v[(j0 + t) * a.v_stride[1] + c], o);
-            acc[u] = o;
-        }
-    }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    T* out = (T*)a.out + b * a.out_stride[0] + i * a.out_stride[1] + h * a.out_stride[2];
-    for (int u = 0; u < 2; ++u)
-        if (lane + 64 * u < a.d) out[lane + 64 * u] = (T)(acc[u] * inv);
-    if (lse && lane == 0) lse[bh * a.queries + i] = l > 0.f ? (m + __log2f(l)) * kLn2 : -INFINITY;
-}
-
-template <typename T, bool CAP>
-__global__ __launch_bounds__(kBlock) void weigh_keys(frog_attend_t a, ScoreParams sp, const float* lse) {
-    __shared__ float ks[4][128];
-    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * 4 + w;
-    if (row >= a.batch * a.kv_heads * a.keys) return;
-    const int64_t j = row % a.keys, bh = row / a.keys;
-    const int hk = (int)(bh % a.kv_heads), group = a.heads / a.kv_heads;
-    const int64_t b = bh / a.kv_heads;
-    const T* k = (const T*)a.k + b * a.k_stride[0] + hk * a.k_stride[2] + j * a.k_stride[1];
-    for (int c = lane; c < a.d; c += 64) ks[w][c] = (float)k[c];
-    const float ak = a.slopes ? a.at_k[b * a.at_k_stride[0] + hk * a.at_k_stride[1] + j] : 0.f;
-    float sum = 0.f;
-    for (int64_t r = lane; r < a.queries * group; r += 64) {
-        const int64_t i = r / group;
-        const int h = hk * group + (int)(r % group);
-        if (a.lr) {
-            const int32_t* p = a.lr + b * a.lr_stride + 2 * i;
-            if (j < p[0] || j > p[1]) continue;
-        }
-        const T* q = (const T*)a.q + b * a.q_stride[0] + i * a.q_stride[1] + h * a.q_stride[2];
-        float z = score2<CAP>(sp, dot_row(ks[w], q, a.d));
-        if (a.slopes) z -= a.slopes[h] * kLog2e * fabsf(a.at_q[b * a.at_q_stride + i] - ak);
-        sum += exp2_fast(z - lse[(b * a.heads + h) * a.queries + i] * kLog2e);
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) a.w_out[bh * a.keys + j] = (a.w_in ? a.w_in[bh * a.keys + j] : 0.f) + sum;
-}
-
-template <typename T, bool CAP>
-int run(const frog_attend_t& a, void* ws, hipStream_t stream) {
-    const ScoreParams sp = score_params(a.scale, a.cap);
-    float* lse = a.lse ? a.lse : (float*)ws;
-    const int64_t rows = a.batch * a.heads * a.queries, cols = a.batch * a.kv_heads * a.keys;
-    if (rows) attend_rows<T, CAP><<<dim3((unsigned)((rows + 3) / 4)), kBlock, 0, stream>>>(a, sp, lse);
-    if (a.w_out && cols) weigh_keys<T, CAP><<<dim3((unsigned)((cols + 3) / 4)), kBlock, 0, stream>>>(a, sp, lse);
+int launched(const char* what) {
     hipError_t e = hipGetLastError();
-    return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "attention launch: %s", hipGetErrorString(e));
+    return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+__global__ void copy_weights(const float* in, float* out, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) out[i] = in ? in[i] : 0.f;
+}
+
+// a tensor of rows set to 0: [batch][tokens][heads][d values], pieces of 16 bytes
+__global__ void clear_rows(char* p, int64_t s0, int64_t s1, int64_t s2, int64_t tokens, int heads, int pieces, int64_t total) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const int c = (int)(i % pieces);
+    const int64_t r = i / pieces, h = r % heads, t = r / heads % tokens, b = r / heads / tokens;
+    *(uint4*)(p + b * s0 + t * s1 + h * s2 + 16 * c) = make_uint4(0, 0, 0, 0);
+}
+
+void clear(void* p, const int64_t (&st)[3], int64_t batch, int64_t tokens, int heads, int d, int size, hipStream_t s) {
+    const int64_t total = batch * tokens * heads * (d * size / 16);
+    if (total)
+        clear_rows<<<dim3((unsigned)((total + 255) / 256)), 256, 0, s>>>((char*)p, st[0] * size, st[1] * size, st[2] * size, tokens, heads, d * size / 16,
+                                                                         total);
 }
 
 }  // namespace
 
-int64_t attend_ws(const frog_attend_t& a) { return a.w_out && !a.lse ? a.batch * a.heads * a.queries * 4 : 0; }
+ForwardPlan forward_plan(const frog_attend_t& a) {
+    ForwardPlan p{};
+    const int64_t group = a.heads / a.kv_heads, pairs = a.batch * a.kv_heads;
+    p.rows = a.queries * group;
+    p.few = p.rows <= 32;
+    p.groups = p.rows <= 16 ? 1 : 2;
+    p.tiles = (int)((p.rows + kTileRows - 1) / kTileRows);
+    // parts of the keys until the card's 256 CUs have four workgroups each
+    // (two of the larger tile's), none of less than a step of its wavefronts
+    // (128 keys; 256 of the tiles', whose parts cost 4 D bytes a row)
+    const int64_t blocks = pairs * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
+    p.splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / std::max<int64_t>(blocks, 1), (a.keys + least - 1) / least));
+    int64_t at = 0;
+    if (p.splits > 1) {
+        p.o = take(&at, p.splits * pairs * p.rows * a.d * 4);
+        p.ml = take(&at, p.splits * pairs * p.rows * 8);
+    }
+    if (a.w_out) {
+        if (!a.lse) p.lse = take(&at, a.batch * a.heads * a.queries * 4);
+        if (p.few) p.scores = take(&at, a.batch * a.heads * a.queries * a.keys * 4);
+        else p.pack = take(&at, pack_plan(a).bytes);
+    }
+    p.bytes = at;
+    return p;
+}
+
+PackPlan pack_plan(const frog_attend_t& a) {
+    PackPlan p{};
+    p.tiles = (a.queries * (a.heads / a.kv_heads) + 31) / 32;
+    int64_t at = 0;
+    p.rows = take(&at, a.batch * a.kv_heads * p.tiles * 192 * 4);
+    p.bounds = take(&at, a.batch * p.tiles * 16);
+    p.zeros = take(&at, 512);
+    p.bytes = at;
+    return p;
+}
+
+namespace {
+
+// a pass without a query or without a key
+bool empty(const frog_attend_t& a) { return a.batch == 0 || a.queries == 0 || a.keys == 0; }
+
+template <typename F>
+void by_type(int type, F&& f) {
+    if (type == FROG_STORAGE_F32) f(AttendLaunch<float>{});
+    else if (type == FROG_STORAGE_F16) f(AttendLaunch<f16_t>{});
+    else f(AttendLaunch<bf16_t>{});
+}
+
+// grids are one number of workgroups
+int check_grid(int64_t blocks) {
+    return blocks > 0x7fffffff ? fail(FROG_EUNSUPPORTED, "%lld workgroups: more than one launch takes", (long long)blocks) : FROG_OK;
+}
+
+__global__ void fill_lse(float* lse, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) lse[i] = -INFINITY;
+}
+
+}  // namespace
+
+int64_t attend_ws(const frog_attend_t& a) { return empty(a) ? 0 : forward_plan(a).bytes; }
 
 int launch_attend(const frog_attend_t& a, void* ws, hipStream_t stream) {
-    if (a.type == FROG_STORAGE_F32) return a.cap > 0.f ? run<float, true>(a, ws, stream) : run<float, false>(a, ws, stream);
-    if (a.type == FROG_STORAGE_F16) return a.cap > 0.f ? run<f16_t, true>(a, ws, stream) : run<f16_t, false>(a, ws, stream);
-    return a.cap > 0.f ? run<bf16_t, true>(a, ws, stream) : run<bf16_t, false>(a, ws, stream);
+    const int size = a.type == FROG_STORAGE_F32 ? 4 : 2;
+    if (empty(a)) {
+        clear(a.out, a.out_stride, a.batch, a.queries, a.heads, a.d, size, stream);
+        const int64_t rows = a.batch * a.heads * a.queries, cols = a.batch * a.kv_heads * a.keys;
+        if (a.lse && rows) fill_lse<<<dim3((unsigned)((rows + 255) / 256)), 256, 0, stream>>>(a.lse, rows);
+        if (a.w_out && a.w_out != a.w_in && cols) copy_weights<<<dim3((unsigned)((cols + 255) / 256)), 256, 0, stream>>>(a.w_in, a.w_out, cols);
+        return launched("attention launch");
+    }
+    const ForwardPlan p = forward_plan(a);
+    const int64_t pairs = a.batch * a.kv_heads;
+    int rc = check_grid(std::max(pairs * p.splits * (p.few ? 1 : p.tiles), std::max(pairs * p.rows / 4 + 1, a.w_out ? pairs * (a.keys / kTileRows + 1) : 0)));
+    if (rc != FROG_OK) return rc;
+    by_type(a.type, [&](auto l) { l.forward(a, p, (char*)ws, stream); });
+    return launched("attention launch");
+}
+
+int64_t attend_bwd_ws(const frog_attend_t& a) { return empty(a) ? 0 : pack_plan(a).bytes; }
+
+int launch_attend_bwd(const frog_attend_t& a, void* ws, hipStream_t stream) {
+    const int size = a.type == FROG_STORAGE_F32 ? 4 : 2;
+    if (empty(a)) {
+        clear(a.dq, a.dq_stride, a.batch, a.queries, a.heads, a.d, size, stream);
+        clear(a.dk, a.dk_stride, a.batch, a.keys, a.kv_heads, a.d, size, stream);
+        clear(a.dv, a.dv_stride, a.batch, a.keys, a.kv_heads, a.d, size, stream);
+        return launched("attention gradient launch");
+    }
+    const int64_t pairs = a.batch * a.kv_heads;
+    int rc = check_grid(pairs * std::max(a.keys / kTileRows + 1, pack_plan(a).tiles));
+    if (rc != FROG_OK) return rc;
+    by_type(a.type, [&](auto l) { l.backward(a, (char*)ws, stream); });
+    return launched("attention gradient launch");
 }
 
 }  // namespace frog

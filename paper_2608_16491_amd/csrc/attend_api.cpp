@@ -65,6 +65,8 @@ int check_attend(const frog_attend_t* a, bool backward) {
         TRY(check_rows("k", a->k, a->k_stride, cols, size));
         TRY(check_rows("v", a->v, a->v_stride, cols, size));
     }
+    const int64_t far = kMaxTokenStride / size;
+    if ((a->keys > 1 && (a->k_stride[1] > far || a->v_stride[1] > far))) return fail(FROG_EUNSUPPORTED, "k or v: rows more than 16 MiB apart");
     if (a->lr_stride < 0 || a->at_q_stride < 0 || a->at_k_stride[0] < 0 || a->at_k_stride[1] < 0) return fail(FROG_EINVAL, "negative stride");
     if (((uintptr_t)a->lr & 7) || (a->lr_stride & 1)) return fail(FROG_EINVAL, "lr: intervals must start on 8-byte boundaries");
     if (a->slopes && ((a->queries > 0 && !a->at_q) || (a->keys > 0 && !a->at_k))) return fail(FROG_EINVAL, "slopes need at_q and at_k");
@@ -102,6 +104,8 @@ int check_shared(const frog_attend_shared_t* a) {
         TRY(check_rows("k", a->k, a->k_stride, cols, size));
         TRY(check_rows("v", a->v, a->v_stride, cols, size));
     }
+    if (a->prefix > 1 && (a->k_stride[0] > kMaxTokenStride / size || a->v_stride[0] > kMaxTokenStride / size))
+        return fail(FROG_EUNSUPPORTED, "k or v: rows more than 16 MiB apart");
     if (a->pages_per_request > 0) {
         if (!a->pages || !a->lengths) return fail(FROG_EINVAL, "pages or lengths is NULL");
         if (a->num_pages > 0) {

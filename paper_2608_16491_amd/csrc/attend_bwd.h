@@ -1,0 +1,442 @@
+// Range attention, gradients and key weights (instantiated per row type by
+// attend_*.hip).
+#pragma once
+
+#include "attend_tile.h"
+
+namespace frog {
+
+// What the passes that own keys need of 32 query rows at a time, prepared once
+// per call: per (sequence, kv head) and tile of 32 rows a block of floats
+// (lse in log2 units, +inf for a row without keys; delta = dout . out; the
+// interval, as integers; bias slope and attribute), per (sequence, tile) the
+// least and largest key of the rows' intervals, and the keys all of them see
+// (z > w when a row has none), and a row of zeros that stands for the rows
+// without keys, whose memory may hold anything.
+struct RowPack {
+    static constexpr int kLse = 0, kDelta = 32, kLo = 64, kHi = 96, kSlope = 128, kAt = 160, kFloats = 192;
+    float* rows;       // [batch * kv_heads][tiles][kFloats]
+    int4* bounds;      // [batch][tiles]
+    void* zeros;       // 512 bytes
+    int tiles;
+};
+
+template <typename T, int D, bool GRAD>
+__global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, RowPack pack, const float* lse) {
+    const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
+    if (blockIdx.x == 0 && threadIdx.x < 128) ((float*)pack.zeros)[threadIdx.x] = 0.f;
+    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), pairs = a.batch * a.kv_heads;
+    if (at >= pairs * pack.tiles) return;
+    const int64_t x = at / pack.tiles, b = x / a.kv_heads;
+    const int tile = (int)(at % pack.tiles), hk = (int)(x % a.kv_heads);
+    const int64_t rows = a.queries * group, row = (int64_t)tile * 32 + i;
+    const QueryRow q(min(row, rows - 1), group, hk);
+    int lo, hi;
+    interval(a, b, q.token, &lo, &hi);
+    const bool some = row < rows && lo <= hi;
+    if (!some) lo = 1, hi = 0;
+    float* out = pack.rows + at * RowPack::kFloats;
+    const int64_t stat = (b * a.heads + q.head) * a.queries + q.token;
+    if constexpr (GRAD) {
+        // half a row a lane
+        const T* g = (const T*)a.dout + b * a.dout_stride[0] + q.token * a.dout_stride[1] + q.head * a.dout_stride[2] + h * (D / 2);
+        const T* o = (const T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2] + h * (D / 2);
+        float delta = 0.f;
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            const frag<T> u = load_frag(g + 8 * s), v = load_frag(o + 8 * s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = fmaf((float)u[e], (float)v[e], delta);
+        }
+        delta = half_sum(delta);
+        if (h == 0) out[RowPack::kDelta + i] = some ? delta : 0.f;
+    }
+    if (h == 0) {
+        out[RowPack::kLse + i] = some ? lse[stat] * kLog2e : INFINITY;
+        out[RowPack::kLo + i] = __int_as_float(lo);
+        out[RowPack::kHi + i] = __int_as_float(hi);
+        out[RowPack::kSlope + i] = a.slopes ? a.slopes[q.head] * kLog2e : 0.f;
+        out[RowPack::kAt + i] = a.slopes ? a.at_q[b * a.at_q_stride + q.token] : 0.f;
+    }
+    if (hk == 0) {
+        const int first = col_min(some ? lo : INT_MAX), last = col_max(some ? hi : -1);
+        const int flo = col_max(some ? lo : INT_MAX), fhi = col_min(some ? hi : -1);
+        if (lane == 0) pack.bounds[b * pack.tiles + tile] = make_int4(first, last, flo, fhi);
+    }
+}
+
+// The tiles of 32 query rows that see one of the keys first..last, in order;
+// 64 bounds are looked at together.  Every wavefront of a workgroup finds the
+// same ones.
+struct TileWalk {
+    const int4* bounds;
+    int tiles, first, last, base = -64, lane;
+    uint64_t left = 0;
+    __device__ inline TileWalk(const int4* b, int n, int first_, int last_, int lane_) : bounds(b), tiles(n), first(first_), last(last_), lane(lane_) {}
+    // the next tile, -1 after the last
+    __device__ inline int next() {
+        while (!left) {
+            base += 64;
+            if (base >= tiles) return -1;
+            bool in = false;
+            if (base + lane < tiles) {
+                const int4 x = bounds[base + lane];
+                in = x.x <= last && x.y >= first;
+            }
+            left = __ballot(in);
+        }
+        const int t = base + __builtin_ctzll(left);
+        left &= left - 1;
+        return t;
+    }
+};
+
+// 4 r (1 - r), r = 1 / (1 + exp2(c1 dot)): the derivative of the cap; *z2 the
+// capped score
+__device__ inline float cap_slope(const ScoreParams& sp, float dot, float* z2) {
+    const float r = rcp_fast(1.f + exp2_fast(dot * sp.mul));
+    *z2 = sp.cap2 - 2.f * sp.cap2 * r;
+    return 4.f * r * (1.f - r);
+}
+
+// One workgroup of W wavefronts, 32 keys each (a lane owns a key), over the
+// tiles of 32 query rows that see them, all heads of the group: the sums over
+// the group need no further pass, and no addition's order is left to chance.
+// Query and dout rows are double buffered in LDS, keys and values stay in
+// registers.
+//   GRAD: dk = sum dx q, dv = sum p dout.  Else: w_out = w_in + sum p.
+template <typename T, int D, bool PLAIN, bool GRAD, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(1)))
+void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack) {
+    constexpr int K = D / 16, M = D / 32;
+    using L = Tile<T, D>;
+    __shared__ __attribute__((aligned(16))) T q0[32 * D], q1[32 * D];
+    __shared__ __attribute__((aligned(16))) T g0[GRAD ? 32 * D : 8], g1[GRAD ? 32 * D : 8];
+    __shared__ __attribute__((aligned(16))) float p0[RowPack::kFloats], p1[RowPack::kFloats];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs;
+    const int tile = (int)(blockIdx.x / pairs);
+    const int64_t b = x / (uint32_t)a.kv_heads;
+    const int hk = (int)(x % (uint32_t)a.kv_heads), rows = (int)(a.queries * group);
+    const int first = tile * 32 * W, last = (int)min((int64_t)first + 32 * W, a.keys) - 1;
+    const int j = first + w * 32 + (lane & 31), jc = min(j, last);
+    const int wfirst = first + w * 32, wlast = wfirst + 31;
+    frag<T> kf[K], vf[GRAD ? K : 1];
+    {
+        const T* p = (const T*)a.k + b * a.k_stride[0] + hk * a.k_stride[2] + jc * a.k_stride[1] + 8 * h;
+#pragma unroll
+        for (int s = 0; s < K; ++s) kf[s] = load_frag(p + 16 * s);
+        if constexpr (GRAD) {
+            const T* p = (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2] + jc * a.v_stride[1] + 8 * h;
+#pragma unroll
+            for (int s = 0; s < K; ++s) vf[s] = load_frag(p + 16 * s);
+        }
+    }
+    const float ak = !PLAIN && a.slopes ? a.at_k[b * a.at_k_stride[0] + hk * a.at_k_stride[1] + jc] : 0.f;
+    acc16 dk[GRAD ? M : 1], dv[GRAD ? M : 1];
+    float sum = 0.f;
+    if constexpr (GRAD) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) dk[m] = dv[m] = acc16{};
+    }
+    const int4* bounds = pack.bounds + b * pack.tiles;
+    const float* blocks = pack.rows + (int64_t)x * pack.tiles * RowPack::kFloats;
+    TileWalk walk(bounds, pack.tiles, first, last, lane);
+
+    // returns whether every row of the tile sees some key (else rows of zeros
+    // stand in)
+    auto fetch = [&](T* qs, T* gs, float* ps, int t, const int4& bd) {
+        const T* zeros = (const T*)pack.zeros;
+        const bool gaps = bd.z > bd.w;
+        const float* blk = blocks + (int64_t)t * RowPack::kFloats;
+        auto row = [&](const void* p, const int64_t(&st)[3], int i) {
+            const QueryRow q(min(t * 32 + i, rows - 1), group, hk);
+            const T* r = (const T*)p + b * st[0] + q.token * st[1] + q.head * st[2];
+            if (gaps) r = blk[RowPack::kLse + i] < INFINITY ? r : zeros;
+            return r;
+        };
+        L::template load_rows<32, W>(qs, w, lane, [&](int i) { return row(a.q, a.q_stride, i); });
+        if constexpr (GRAD) L::template load_rows<32, W>(gs, w, lane, [&](int i) { return row(a.dout, a.dout_stride, i); });
+        if (w == 0 && lane < RowPack::kFloats / 4)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(blk + 4 * lane), (__attribute__((address_space(3))) void*)ps,
+                                             16, 0, 0);
+    };
+    auto step = [&](const T* qs, const T* gs, const float* ps, const int4& bd) {
+        if (bd.x > wlast || bd.y < wfirst) return;
+        acc16 z = acc16{};
+#pragma unroll
+        for (int s = 0; s < K; ++s) z = mma(L::rows(qs, 0, s, lane), kf[s], z);
+        acc16 dp = acc16{};
+        if constexpr (GRAD) {
+#pragma unroll
+            for (int s = 0; s < K; ++s) dp = mma(L::rows(gs, 0, s, lane), vf[s], dp);
+        }
+        acc16 p, dx;
+        const bool whole = bd.z <= wfirst && bd.w >= wlast;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = 8 * i + 4 * h;
+            const vec<float, 4> lse = *(const vec<float, 4>*)(ps + RowPack::kLse + at);
+            vec<float, 4> sl = {}, aq = {};
+            if (!PLAIN && a.slopes) {
+                sl = *(const vec<float, 4>*)(ps + RowPack::kSlope + at);
+                aq = *(const vec<float, 4>*)(ps + RowPack::kAt + at);
+            }
+            vec<float, 4> f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                float y;
+                if constexpr (PLAIN) {
+                    y = fmaf(z[4 * i + e], sp.mul, -lse[e]);
+                } else {
+                    f[e] = 1.f;
+                    if (sp.cap2 > 0.f) f[e] = cap_slope(sp, z[4 * i + e], &y);
+                    else y = z[4 * i + e] * sp.mul;
+                    if (a.slopes) y -= sl[e] * fabsf(aq[e] - ak);
+                    y -= lse[e];
+                }
+                p[4 * i + e] = exp2_fast(y);
+            }
+            if constexpr (GRAD) {
+                const vec<float, 4> delta = *(const vec<float, 4>*)(ps + RowPack::kDelta + at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    dx[4 * i + e] = p[4 * i + e] * (dp[4 * i + e] - delta[e]);
+                    if constexpr (!PLAIN) dx[4 * i + e] *= f[e];
+                }
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = 8 * i + 4 * h;
+                const vec<float, 4> lo = *(const vec<float, 4>*)(ps + RowPack::kLo + at), hi = *(const vec<float, 4>*)(ps + RowPack::kHi + at);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool in = j >= __float_as_int(lo[e]) && j <= __float_as_int(hi[e]);
+                    p[4 * i + e] = in ? p[4 * i + e] : 0.f;
+                    if constexpr (GRAD) dx[4 * i + e] = in ? dx[4 * i + e] : 0.f;
+                }
+            }
+        }
+        if constexpr (GRAD) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const frag<T> pf = to_frag<T>(p, t), xf = to_frag<T>(dx, t);
+#pragma unroll
+                for (int m = 0; m < M; ++m) {
+                    dv[m] = mma(L::cols(gs, 16 * t, m, lane), pf, dv[m]);
+                    dk[m] = mma(L::cols(qs, 16 * t, m, lane), xf, dk[m]);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sum += p[r];
+        }
+    };
+    auto ready = [&] {
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        __syncthreads();
+    };
+    int t = walk.next();
+    if (t >= 0) {
+        int4 bd = bounds[t];
+        fetch(q0, g0, p0, t, bd);
+        for (;;) {
+            ready();
+            t = walk.next();
+            int4 bn = bd;
+            if (t >= 0) {
+                bn = bounds[t];
+                fetch(q1, g1, p1, t, bn);
+            }
+            step(q0, g0, p0, bd);
+            if (t < 0) break;
+            ready();
+            t = walk.next();
+            if (t >= 0) {
+                bd = bounds[t];
+                fetch(q0, g0, p0, t, bd);
+            }
+            step(q1, g1, p1, bn);
+            if (t < 0) break;
+        }
+    }
+    if constexpr (GRAD) {
+        if (j > last) return;
+        T* pk = (T*)a.dk + b * a.dk_stride[0] + hk * a.dk_stride[2] + j * a.dk_stride[1];
+        T* pv = (T*)a.dv + b * a.dv_stride[0] + hk * a.dv_stride[2] + j * a.dv_stride[1];
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                vec<T, 4> y, z;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = (T)(dk[m][4 * i + e] * sp.scale);
+                    z[e] = (T)dv[m][4 * i + e];
+                }
+                *(vec<T, 4>*)(pk + 32 * m + 8 * i + 4 * h) = y;
+                *(vec<T, 4>*)(pv + 32 * m + 8 * i + 4 * h) = z;
+            }
+    } else {
+        sum = half_sum(sum);
+        if (j > last || lane >= 32) return;
+        const int64_t at = (int64_t)x * a.keys + j;
+        a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum;
+    }
+}
+
+// dq: one workgroup of W wavefronts, 32 query rows each (a lane owns a query),
+// over the keys of their intervals in tiles of N, double buffered.
+template <typename T, int D, bool PLAIN, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
+void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pack) {
+    constexpr int N = sizeof(T) == 2 ? 64 : 32, S = N / 32, K = D / 16, M = D / 32;
+    // (buffers by name: the compiler then knows that reads of one need not wait
+    // for the direct loads into the other)
+    __shared__ __attribute__((aligned(16))) T k0[N * D], k1[N * D], v0[N * D], v1[N * D];
+    __shared__ float a0[64], a1[64];
+    __shared__ int ends[4 * W];
+    __shared__ Gaps<32 * W> rows_of;
+    using L = Tile<T, D>;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs;
+    const int tile = tiles - 1 - (int)(blockIdx.x / pairs);
+    const int64_t b = x / (uint32_t)a.kv_heads;
+    const int hk = (int)(x % (uint32_t)a.kv_heads);
+    const int64_t rows = a.queries * group, row = ((int64_t)tile * W + w) * 32 + (lane & 31);
+    const QueryRow q(min(row, rows - 1), group, hk);
+    int lo, hi;
+    interval(a, b, q.token, &lo, &hi);
+    const bool some = row < rows && lo <= hi;
+    const int wlo = col_min(some ? lo : INT_MAX), whi = col_max(some ? hi : -1);
+    const int flo = col_max(some ? lo : 0), fhi = col_min(some ? hi : INT_MAX);
+    if (lane == 0) {
+        ends[w] = wlo;
+        ends[W + w] = whi;
+        ends[2 * W + w] = flo;
+        ends[3 * W + w] = fhi;
+    }
+    if (lane < 32) {
+        rows_of.lo[32 * w + lane] = some ? lo : 1;
+        rows_of.hi[32 * w + lane] = some ? hi : 0;
+    }
+    __syncthreads();
+    int first = INT_MAX, last = -1, inner_lo = 0, inner_hi = INT_MAX;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        first = min(first, ends[i]);
+        last = max(last, ends[W + i]);
+        inner_lo = max(inner_lo, ends[2 * W + i]);
+        inner_hi = min(inner_hi, ends[3 * W + i]);
+    }
+    // intervals that share a key leave no gap
+    const bool gaps = __builtin_amdgcn_readfirstlane(inner_lo > inner_hi);
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
+    const T* kp = (const T*)a.k + b * a.k_stride[0] + hk * a.k_stride[2];
+    const T* vp = (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2];
+    const float* akp = nullptr;
+    float slope = 0.f, aq = 0.f;
+    if (!PLAIN && a.slopes) {
+        akp = a.at_k + b * a.at_k_stride[0] + hk * a.at_k_stride[1];
+        slope = a.slopes[q.head] * kLog2e;
+        aq = a.at_q[b * a.at_q_stride + q.token];
+    }
+    frag<T> qf[K], gf[K];
+    {
+        const T* p = (const T*)a.q + b * a.q_stride[0] + q.token * a.q_stride[1] + q.head * a.q_stride[2] + (lane >> 5) * 8;
+        const T* g = (const T*)a.dout + b * a.dout_stride[0] + q.token * a.dout_stride[1] + q.head * a.dout_stride[2] + (lane >> 5) * 8;
+#pragma unroll
+        for (int s = 0; s < K; ++s) {
+            qf[s] = load_frag(p + 16 * s);
+            gf[s] = load_frag(g + 16 * s);
+        }
+    }
+    // (a wavefront past the last row reads the last tile's numbers)
+    const float* blk = pack.rows + ((int64_t)x * pack.tiles + min(tile * W + w, pack.tiles - 1)) * RowPack::kFloats + (lane & 31);
+    const float lse = some ? blk[RowPack::kLse] : INFINITY, delta = blk[RowPack::kDelta];
+    acc16 dq[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) dq[m] = acc16{};
+
+    auto fetch = [&](T* ks, T* vs, float* as, int j) {
+        L::template load<N, W>(ks, kp, a.k_stride[1], j, last, w, lane);
+        L::template load<N, W>(vs, vp, a.v_stride[1], j, last, w, lane);
+        if (!PLAIN && akp && w == 0)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(akp + min(j + lane, last)),
+                                             (__attribute__((address_space(3))) void*)as, 4, 0, 0);
+    };
+    auto step = [&](const T* ks, const T* vs, const float* as, int j0) {
+        if (j0 > whi || j0 + N <= wlo) return;
+#pragma unroll
+        for (int n = 0; n < S; ++n) {
+            const int j = j0 + 32 * n;
+            if (j > whi || j + 32 <= wlo) continue;
+            acc16 z[1] = {acc16{}};
+#pragma unroll
+            for (int s = 0; s < K; ++s) z[0] = mma(L::rows(ks, 32 * n, s, lane), qf[s], z[0]);
+            // p (times the cap's slope), before the other product needs registers
+            if (j < flo || j + 31 > fhi) mask_scores<1>(z, lo - j, hi - j, lane);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                if constexpr (PLAIN) {
+                    z[0][r] = exp2_fast(fmaf(z[0][r], sp.mul, -lse));
+                } else {
+                    float y, f = 1.f;
+                    if (sp.cap2 > 0.f) f = cap_slope(sp, z[0][r], &y);
+                    else y = z[0][r] * sp.mul;
+                    if (akp) y -= slope * fabsf(aq - as[32 * n + acc_row(r, lane)]);
+                    z[0][r] = exp2_fast(z[0][r] > -INFINITY ? y - lse : -INFINITY) * f;
+                }
+            }
+            acc16 dp = acc16{};
+#pragma unroll
+            for (int s = 0; s < K; ++s) dp = mma(L::rows(vs, 32 * n, s, lane), gf[s], dp);
+            // (a masked key's value row may hold anything: 0 times it is not 0)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[r] = z[0][r] == 0.f ? 0.f : z[0][r] * (dp[r] - delta);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const frag<T> xf = to_frag<T>(dp, t);
+#pragma unroll
+                for (int m = 0; m < M; ++m) dq[m] = mma(L::cols(ks, 32 * n + 16 * t, m, lane), xf, dq[m]);
+            }
+        }
+    };
+    auto ready = [&] {
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        __syncthreads();
+    };
+    auto turn = [&](T* ks, T* vs, float* as, T* kn, T* vn, float* an, int j) {
+        ready();
+        if (j + N <= last) fetch(kn, vn, an, j + N);
+        if (gaps) {
+            rows_of.template clear<N, D, W>(ks, j, w, lane);
+            __syncthreads();
+        }
+        step(ks, vs, as, j);
+    };
+    if (first <= last) {
+        fetch(k0, v0, a0, first);
+        for (int j = first; j <= last; j += 2 * N) {
+            turn(k0, v0, a0, k1, v1, a1, j);
+            if (j + N > last) break;
+            turn(k1, v1, a1, k0, v0, a0, j + N);
+        }
+    }
+    if (row >= rows) return;
+    T* out = (T*)a.dq + b * a.dq_stride[0] + q.token * a.dq_stride[1] + q.head * a.dq_stride[2];
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            vec<T, 4> y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = some ? (T)(dq[m][4 * i + e] * sp.scale) : (T)0.f;
+            *(vec<T, 4>*)(out + 32 * m + 8 * i + 4 * (lane >> 5)) = y;
+        }
+}
+
+}  // namespace frog

@@ -1,0 +1,7 @@
+// Attention, gradient and key-weight kernels of bf16 rows.
+#include "attend_launch_bwd.h"
+
+namespace frog {
+template void AttendLaunch<bf16_t>::weigh(const frog_attend_t&, const float*, char*, hipStream_t);
+template void AttendLaunch<bf16_t>::backward(const frog_attend_t&, char*, hipStream_t);
+}

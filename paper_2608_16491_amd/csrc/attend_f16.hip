@@ -1,0 +1,6 @@
+// Attention, forward kernels of f16 rows.
+#include "attend_launch_fwd.h"
+
+namespace frog {
+template void AttendLaunch<f16_t>::forward(const frog_attend_t&, const ForwardPlan&, char*, hipStream_t);
+}

@@ -1,0 +1,6 @@
+// Attention, forward kernels of f32 rows.
+#include "attend_launch_fwd.h"
+
+namespace frog {
+template void AttendLaunch<float>::forward(const frog_attend_t&, const ForwardPlan&, char*, hipStream_t);
+}

@@ -1,0 +1,633 @@
+// Range attention, forward kernels (instantiated per row type by attend_*.hip).
+#pragma once
+
+#include "attend_tile.h"
+
+namespace frog {
+
+// Partial results of a pass split along the keys: part s of query row i of
+// (sequence, kv head) x: maximum and sum at ml[(s * total + x * rows + i)],
+// unnormalised output of D floats at o[...] (total = rows of all)
+struct Parts {
+    float* o;
+    float2* ml;
+    int64_t total;
+    int splits;
+};
+
+constexpr float kLow = -FLT_MAX;   // running maximum of a row that has seen no key
+
+// One workgroup of W wavefronts, 32 query rows each, over the keys of their
+// intervals in tiles of N: scores transposed (keys x queries) so that a lane
+// owns a query, one pass with the running maximum and sum, keys and values
+// double buffered in LDS by direct loads.
+//   PLAIN: neither cap nor bias and a positive scale; the scale is then part
+//   of the exponent's multiply-add.
+template <typename T, int D, bool PLAIN, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
+void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts parts) {
+    constexpr int N = sizeof(T) == 2 ? 64 : 32, S = N / 32, K = D / 16, M = D / 32;
+    // (buffers by name: the compiler then knows that reads of one need not wait
+    // for the direct loads into the other)
+    __shared__ __attribute__((aligned(16))) T k0[N * D], k1[N * D], v0[N * D], v1[N * D];
+    __shared__ float a0[64], a1[64];
+    __shared__ int ends[4 * W];
+    __shared__ Gaps<32 * W> rows_of;
+    using L = Tile<T, D>;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // heads fastest (XCDs take workgroups in turn: with 8 heads or a multiple
+    // each XCD's L2 holds its own), later rows, which see more under a causal
+    // mask, first
+    const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs, rest = blockIdx.x / pairs;
+    const int split = (int)(rest % (uint32_t)parts.splits), tile = tiles - 1 - (int)(rest / (uint32_t)parts.splits);
+    const int64_t b = x / (uint32_t)a.kv_heads;
+    const int hk = (int)(x % (uint32_t)a.kv_heads);
+    const int64_t rows = a.queries * group, row = ((int64_t)tile * W + w) * 32 + (lane & 31);
+    const QueryRow q(min(row, rows - 1), group, hk);
+    int lo, hi;
+    interval(a, b, q.token, &lo, &hi);
+    const bool some = row < rows && lo <= hi;
+    // first and last key of the workgroup; of the wavefront; and the keys all its rows see
+    const int wlo = col_min(some ? lo : INT_MAX), whi = col_max(some ? hi : -1);
+    const int flo = col_max(some ? lo : 0), fhi = col_min(some ? hi : INT_MAX);
+    if (lane == 0) {
+        ends[w] = wlo;
+        ends[W + w] = whi;
+        ends[2 * W + w] = flo;
+        ends[3 * W + w] = fhi;
+    }
+    if (lane < 32) {
+        rows_of.lo[32 * w + lane] = some ? lo : 1;
+        rows_of.hi[32 * w + lane] = some ? hi : 0;
+    }
+    __syncthreads();
+    int first = INT_MAX, last = -1, inner_lo = 0, inner_hi = INT_MAX;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        first = min(first, ends[i]);
+        last = max(last, ends[W + i]);
+        inner_lo = max(inner_lo, ends[2 * W + i]);
+        inner_hi = min(inner_hi, ends[3 * W + i]);
+    }
+    // intervals that share a key leave no gap
+    const bool gaps = __builtin_amdgcn_readfirstlane(inner_lo > inner_hi);
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
+    if (parts.splits > 1 && last >= 0) {
+        const int each = ((last - first) / parts.splits / N + 1) * N;
+        const int64_t from = first + (int64_t)split * each;
+        last = (int)min((int64_t)last, from + each - 1);
+        first = (int)min(from, (int64_t)last + 1);
+    }
+    const T* kp = (const T*)a.k + b * a.k_stride[0] + hk * a.k_stride[2];
+    const T* vp = (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2];
+    const float* akp = nullptr;
+    float slope = 0.f, aq = 0.f;
+    if (!PLAIN && a.slopes) {
+        akp = a.at_k + b * a.at_k_stride[0] + hk * a.at_k_stride[1];
+        slope = a.slopes[q.head] * kLog2e;
+        aq = a.at_q[b * a.at_q_stride + q.token];
+    }
+    frag<T> qf[K];
+    {
+        const T* p = (const T*)a.q + b * a.q_stride[0] + q.token * a.q_stride[1] + q.head * a.q_stride[2] + (lane >> 5) * 8;
+#pragma unroll
+        for (int s = 0; s < K; ++s) qf[s] = load_frag(p + 16 * s);
+    }
+    acc16 o[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) o[m] = acc16{};
+    float top = kLow, sum = 0.f;
+
+    auto fetch = [&](T* ks, T* vs, float* as, int j) {
+        L::template load<N, W>(ks, kp, a.k_stride[1], j, last, w, lane);
+        L::template load<N, W>(vs, vp, a.v_stride[1], j, last, w, lane);
+        if (!PLAIN && akp && w == 0)
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(akp + min(j + lane, last)),
+                                             (__attribute__((address_space(3))) void*)as, 4, 0, 0);
+    };
+    auto step = [&](const T* ks, const T* vs, const float* as, int j) {
+        if (j > whi || j + N <= wlo) return;
+        acc16 z[S];
+#pragma unroll
+        for (int n = 0; n < S; ++n) {
+            z[n] = acc16{};
+#pragma unroll
+            for (int s = 0; s < K; ++s) z[n] = mma(L::rows(ks, 32 * n, s, lane), qf[s], z[n]);
+        }
+        if constexpr (!PLAIN) {
+            if (sp.cap2 > 0.f) {
+#pragma unroll
+                for (int n = 0; n < S; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) z[n][r] = score2<true>(sp, z[n][r]);
+            } else {
+#pragma unroll
+                for (int n = 0; n < S; ++n) z[n] *= sp.mul;
+            }
+            if (akp) {
+#pragma unroll
+                for (int n = 0; n < S; ++n)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) z[n][r] -= slope * fabsf(aq - as[32 * n + acc_row(r, lane)]);
+            }
+        }
+        // bit 16 n + r: some row of the wavefront sees the key of register r.
+        // The others' values, which may be anything, must not meet a weight
+        // of 0 in the second product.
+        if (j < flo || j + N - 1 > fhi) mask_scores<S>(z, lo - j, hi - j, lane);
+        float mx = z[0][0];
+#pragma unroll
+        for (int n = 0; n < S; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, z[n][r]);
+        mx = half_max(PLAIN ? mx * sp.mul : mx);
+        // the sums are scaled anew only when a row's maximum has grown by more
+        // than 2^8: weights up to 256 keep their precision in every type
+        if (__any(mx > top + 8.f)) {
+            const float up = fmaxf(top, mx), f = exp2_fast(top - up);
+            top = up;
+            sum *= f;
+#pragma unroll
+            for (int m = 0; m < M; ++m) o[m] *= f;
+        }
+#pragma unroll
+        for (int n = 0; n < S; ++n)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                z[n][r] = exp2_fast(PLAIN ? fmaf(z[n][r], sp.mul, -top) : z[n][r] - top);
+                sum += z[n][r];
+            }
+#pragma unroll
+        for (int n = 0; n < S; ++n)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const frag<T> p = to_frag<T>(z[n], t);
+#pragma unroll
+                for (int m = 0; m < M; ++m) o[m] = mma(L::cols(vs, 32 * n + 16 * t, m, lane), p, o[m]);
+            }
+    };
+    // barrier: the tile has arrived in LDS, and the other buffer is read no more
+    auto ready = [&] {
+        __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wavefront's own loads
+        __syncthreads();
+    };
+    auto turn = [&](T* ks, T* vs, float* as, T* kn, T* vn, float* an, int j) {
+        ready();
+        if (j + N <= last) fetch(kn, vn, an, j + N);
+        if (gaps) {
+            rows_of.template clear<N, D, W>(vs, j, w, lane);
+            __syncthreads();
+        }
+        step(ks, vs, as, j);
+    };
+    if (first <= last) {
+        fetch(k0, v0, a0, first);
+        for (int j = first; j <= last; j += 2 * N) {
+            turn(k0, v0, a0, k1, v1, a1, j);
+            if (j + N > last) break;
+            turn(k1, v1, a1, k0, v0, a0, j + N);
+        }
+    }
+    sum = half_sum(sum);
+    if (row >= rows) return;
+    if (!some) {
+        sum = 0.f;
+        top = kLow;
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    if (parts.splits > 1) {
+        const int64_t at = split * parts.total + x * rows + row;
+        if (lane < 32) parts.ml[at] = make_float2(top, sum);
+        if (sum > 0.f) {
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    *(vec<float, 4>*)(parts.o + at * D + 32 * m + 8 * i + 4 * (lane >> 5)) =
+                        vec<float, 4>{o[m][4 * i], o[m][4 * i + 1], o[m][4 * i + 2], o[m][4 * i + 3]};
+        }
+        return;
+    }
+    T* out = (T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2];
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            vec<T, 4> y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = sum > 0.f ? (T)(o[m][4 * i + e] * inv) : (T)0.f;
+            *(vec<T, 4>*)(out + 32 * m + 8 * i + 4 * (lane >> 5)) = y;
+        }
+    if (a.lse && lane < 32) a.lse[(b * a.heads + q.head) * a.queries + q.token] = sum > 0.f ? (top + __log2f(sum)) * kLn2 : -INFINITY;
+}
+
+// Keys of one sequence and kv head, in one piece or in pages.
+template <typename T>
+struct FlatKeys {
+    const T *k, *v;
+    int64_t ks, vs;
+    struct Where {
+        int j;
+    };
+    __device__ inline Where where(int j) const { return {j}; }
+    // row i (0 .. 31) of the 32 whose Where the lanes hold
+    __device__ static inline Where of(Where x, int i, int j, int last) { return {min(j + i, last)}; }
+    __device__ inline const T* key(Where x) const { return k + x.j * ks; }
+    __device__ inline const T* value(Where x) const { return v + x.j * vs; }
+    __device__ static inline bool real(Where) { return true; }
+};
+
+template <typename T>
+struct PagedKeys {
+    const T *k, *v;          // at the kv head
+    int64_t ks[2], vs[2];    // page, row
+    const int32_t* pages;    // of the request
+    uint32_t page;
+    int64_t num_pages;
+    const T* spare;          // D values that may be read, for rows without a page
+    struct Where {
+        int page, row;       // page -1: no such page
+    };
+    __device__ inline Where where(int j) const {
+        const uint32_t p = (uint32_t)j / page;
+        const int at = pages[p];
+        return {at >= 0 && at < num_pages ? at : -1, (int)((uint32_t)j - p * page)};
+    }
+    __device__ static inline Where of(Where x, int i, int, int) { return {__shfl(x.page, i), __shfl(x.row, i)}; }
+    __device__ inline const T* key(Where x) const { return x.page >= 0 ? k + x.page * ks[0] + x.row * ks[1] : spare; }
+    __device__ inline const T* value(Where x) const { return x.page >= 0 ? v + x.page * vs[0] + x.row * vs[1] : spare; }
+    __device__ static inline bool real(Where x) { return x.page >= 0; }
+};
+
+// The query rows of a wavefront's few-rows pass: column lane % 16 of each of
+// the RG groups of 16.
+template <int RG>
+struct FewRows {
+    int lo[RG], hi[RG];       // interval (lo > hi: no row, or an empty one)
+    float slope[RG], aq[RG];  // distance bias
+    float top[RG], sum[RG];
+};
+
+// Few query rows (at most 16 RG, a token's group of heads after another) over
+// the keys first..last of one (sequence, kv head), 32 keys a step and
+// wavefront, wavefront w of W taking every W-th step.  Nothing passes through
+// LDS: a lane loads 16 bytes of a key row as it stands in the left factor of
+// the scores, and D / 16 values each of 8 value rows, whose transposition is
+// a renaming of registers and one exchange of 16-bit halves; the output's
+// columns come out as d = 4 (L/16) + r times D/16 plus e.
+template <typename T, int D, int RG>
+struct FewPass {
+    static constexpr int K = D / 32, C = D / 16;
+    frag<T> q[RG][K];
+    acc4 o[RG][C];
+    FewRows<RG> row;
+
+    __device__ inline void reset() {
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            row.top[g] = kLow;
+            row.sum[g] = 0.f;
+#pragma unroll
+            for (int e = 0; e < C; ++e) o[g][e] = acc4{};
+        }
+    }
+
+    // at_key(j): attribute of key j (NULL functor result unused without bias);
+    // store(g, j, z): takes every score of key j <= last
+    template <typename Keys, typename At, typename Store>
+    __device__ inline void run(const Keys& keys, const ScoreParams& sp, bool bias, At&& at_key, Store&& store, int first, int last, int w,
+                               int W, int lane) {
+        const int c = lane & 15, h = lane >> 4;
+        int fit_lo = 0, fit_hi = INT_MAX;   // keys every real row sees
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            const bool some = row.lo[g] <= row.hi[g];
+            fit_lo = max(fit_lo, col_max(some ? row.lo[g] : 0));
+            fit_hi = min(fit_hi, col_min(some ? row.hi[g] : INT_MAX));
+        }
+        int64_t j0 = (int64_t)first + 32 * w;
+        if (j0 > last) return;
+        typename Keys::Where mine = keys.where(min((int)j0 + (lane & 31), last));
+        for (; j0 <= last; j0 += 32 * W) {
+            const int j = (int)j0;
+            // key rows c and 16 + c; value rows 4h .. 4h+3 and 16 + 4h ..
+            frag<T> kf[2][K];
+            vec<T, C> vv[8];
+            bool real[8];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const T* p = keys.key(Keys::of(mine, 16 * u + c, j, last)) + 8 * h;
+#pragma unroll
+                for (int s = 0; s < K; ++s) kf[u][s] = load_frag(p + 32 * s);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const auto x = Keys::of(mine, 16 * (e >> 2) + 4 * h + (e & 3), j, last);
+                vv[e] = load_piece(keys.value(x) + C * c);
+                real[e] = Keys::real(x);
+            }
+            const int64_t next = j0 + 32 * W;
+            if (next <= last) mine = keys.where((int)min(next + (lane & 31), (int64_t)last));
+            float ak[8];
+            if (bias) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ak[e] = at_key(min(j + 16 * (e >> 2) + 4 * h + (e & 3), last));
+            }
+            // keys that some row sees: the others' values, which may be anything,
+            // must not meet a weight of 0 in the second product
+            const bool whole = j >= fit_lo && j + 31 <= min(fit_hi, last);
+            if (!whole) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = j + 16 * (e >> 2) + 4 * h + (e & 3);
+                    bool in = false;
+#pragma unroll
+                    for (int g = 0; g < RG; ++g) in |= at >= row.lo[g] && at <= min(row.hi[g], last);
+                    real[e] = real[e] && ((__ballot(in) >> (16 * h)) & 0xffff) != 0;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!real[e]) vv[e] = vec<T, C>{};
+            frag<T> p[RG];
+#pragma unroll
+            for (int g = 0; g < RG; ++g) {
+                float z[8];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    acc4 s4 = acc4{};
+#pragma unroll
+                    for (int s = 0; s < K; ++s) s4 = mma(kf[u][s], q[g][s], s4);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[4 * u + r] = s4[r];
+                }
+                if (sp.cap2 > 0.f) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = score2<true>(sp, z[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] *= sp.mul;
+                }
+                if (bias) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] -= row.slope[g] * fabsf(row.aq[g] - ak[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) store(g, j + 16 * (e >> 2) + 4 * h + (e & 3), z[e]);
+                if (!whole) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int at = j + 16 * (e >> 2) + 4 * h + (e & 3);
+                        z[e] = at >= row.lo[g] && at <= min(row.hi[g], last) ? z[e] : -INFINITY;
+                    }
+                }
+                float mx = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    z[e] = real[e] ? z[e] : -INFINITY;
+                    mx = fmaxf(mx, z[e]);
+                }
+                mx = quarter_max(mx);
+                if (__any(mx > row.top[g] + 8.f)) {
+                    const float up = fmaxf(row.top[g], mx), f = exp2_fast(row.top[g] - up);
+                    row.top[g] = up;
+                    row.sum[g] *= f;
+#pragma unroll
+                    for (int e = 0; e < C; ++e) o[g][e] *= f;
+                }
+                vec<float, 8> y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    y[e] = exp2_fast(z[e] - row.top[g]);
+                    row.sum[g] += y[e];
+                }
+                if constexpr (sizeof(T) == 4) p[g] = y;
+                else p[g] = __builtin_convertvector(y, frag<T>);
+            }
+#pragma unroll
+            for (int e = 0; e < C; ++e) {
+                const frag<T> vf{vv[0][e], vv[1][e], vv[2][e], vv[3][e], vv[4][e], vv[5][e], vv[6][e], vv[7][e]};
+#pragma unroll
+                for (int g = 0; g < RG; ++g) o[g][e] = mma(vf, p[g], o[g][e]);
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < RG; ++g) row.sum[g] = quarter_sum(row.sum[g]);
+    }
+
+    // D / 16 values from an address of that alignment (4, 8, 12, 16 or 32 bytes)
+    __device__ static inline vec<T, C> load_piece(const T* p) {
+        vec<T, C> x;
+        constexpr int words = C * sizeof(T) / 4;
+        uint32_t r[words];
+        if constexpr (words % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < words / 4; ++i) *(uint4*)(r + 4 * i) = ((const uint4*)p)[i];
+        } else if constexpr (words % 2 == 0) {
+#pragma unroll
+            for (int i = 0; i < words / 2; ++i) *(uint2*)(r + 2 * i) = ((const uint2*)p)[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < words; ++i) r[i] = ((const uint32_t*)p)[i];
+        }
+        __builtin_memcpy(&x, r, sizeof(x));
+        return x;
+    }
+
+    // Joins the wavefronts' results in lds (16 RG rows of D floats, and W times
+    // as many maxima and sums); then every wavefront holds the joint top and
+    // sum, and the rows in LDS are the unnormalised output
+    template <int W>
+    __device__ inline void join(float* lds, float* tops, float* sums, int w, int lane) {
+        const int c = lane & 15, h = lane >> 4;
+#pragma unroll
+        for (int g = 0; g < RG; ++g)
+            if (h == 0) {
+                tops[(w * RG + g) * 16 + c] = row.top[g];
+                sums[(w * RG + g) * 16 + c] = row.sum[g];
+            }
+        __syncthreads();
+        float f[RG];
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            float top = kLow, sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < W; ++i) top = fmaxf(top, tops[(i * RG + g) * 16 + c]);
+#pragma unroll
+            for (int i = 0; i < W; ++i) sum += sums[(i * RG + g) * 16 + c] * exp2_fast(tops[(i * RG + g) * 16 + c] - top);
+            f[g] = exp2_fast(row.top[g] - top);
+            row.top[g] = top;
+            row.sum[g] = sum;
+        }
+        for (int i = 0; i < W; ++i) {
+            if (i == w) {
+#pragma unroll
+                for (int g = 0; g < RG; ++g)
+#pragma unroll
+                    for (int e = 0; e < C; ++e)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            float* p = lds + (16 * g + c) * (D + 4) + (4 * h + r) * C + e;
+                            const float y = o[g][e][r] * f[g];
+                            *p = i ? *p + y : y;
+                        }
+            }
+            __syncthreads();
+        }
+    }
+};
+
+// One workgroup per (sequence, kv head, part of the keys) for at most 16 RG
+// query rows; scores (optional) [batch][heads][queries][keys] receive every
+// score in log2 units for the key weights.
+template <typename T, int D, int RG>
+__global__ __launch_bounds__(256) void attend_few(frog_attend_t a, ScoreParams sp, int group, Parts parts, float* scores) {
+    constexpr int W = 4;
+    __shared__ float lds[16 * RG * (D + 4)], tops[W * RG * 16], sums[W * RG * 16];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs;
+    const int split = (int)(blockIdx.x / pairs);
+    const int64_t b = x / (uint32_t)a.kv_heads;
+    const int hk = (int)(x % (uint32_t)a.kv_heads), rows = (int)a.queries * group;
+    FewPass<T, D, RG> f;
+    f.reset();
+    int first = INT_MAX, last = -1;
+    float* zp[RG];
+#pragma unroll
+    for (int g = 0; g < RG; ++g) {
+        const int r = 16 * g + (lane & 15);
+        const QueryRow q(min(r, rows - 1), group, hk);
+        int lo, hi;
+        interval(a, b, q.token, &lo, &hi);
+        if (r >= rows) lo = 0, hi = -1;
+        f.row.lo[g] = lo;
+        f.row.hi[g] = hi;
+        first = min(first, col_min(lo <= hi ? lo : INT_MAX));
+        last = max(last, col_max(lo <= hi ? hi : -1));
+        f.row.slope[g] = a.slopes ? a.slopes[q.head] * kLog2e : 0.f;
+        f.row.aq[g] = a.slopes ? a.at_q[b * a.at_q_stride + q.token] : 0.f;
+        zp[g] = scores && r < rows ? scores + ((b * a.heads + q.head) * a.queries + q.token) * a.keys : nullptr;
+        const T* p = (const T*)a.q + b * a.q_stride[0] + q.token * a.q_stride[1] + q.head * a.q_stride[2] + (lane >> 4) * 8;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) f.q[g][s] = load_frag(p + 32 * s);
+    }
+    if (parts.splits > 1 && last >= 0) {
+        const int each = ((last - first) / parts.splits / (32 * W) + 1) * (32 * W);
+        const int64_t from = first + (int64_t)split * each;
+        last = (int)min((int64_t)last, from + each - 1);
+        first = (int)min(from, (int64_t)last + 1);
+    }
+    const FlatKeys<T> keys{(const T*)a.k + b * a.k_stride[0] + hk * a.k_stride[2], (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2],
+                           a.k_stride[1], a.v_stride[1]};
+    const float* akp = a.slopes ? a.at_k + b * a.at_k_stride[0] + hk * a.at_k_stride[1] : nullptr;
+    if (first <= last)
+        f.run(keys, sp, akp != nullptr, [&](int j) { return akp[j]; },
+              [&](int g, int j, float z) {
+                  if (zp[g] && j <= last) zp[g][j] = z;
+              },
+              first, last, w, W, lane);
+    f.template join<W>(lds, tops, sums, w, lane);
+    // joint rows: out, or this part's
+    if (w == 0 && lane < 16) {
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            sums[16 * g + lane] = f.row.lo[g] <= f.row.hi[g] ? f.row.sum[g] : 0.f;
+            tops[16 * g + lane] = f.row.top[g];
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * W) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
+        const float sum = sums[r], inv = sum > 0.f ? 1.f / sum : 0.f;
+        const acc4 y = *(const acc4*)(lds + r * (D + 4) + d);
+        if (parts.splits > 1) {
+            const int64_t at = split * parts.total + (int64_t)x * rows + r;
+            if (sum > 0.f) *(acc4*)(parts.o + at * D + d) = y;
+            if (d == 0) parts.ml[at] = make_float2(tops[r], sum);
+        } else {
+            const QueryRow q(r, group, hk);
+            vec<T, 4> t;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t[e] = sum > 0.f ? (T)(y[e] * inv) : (T)0.f;
+            *(vec<T, 4>*)((T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2] + d) = t;
+            if (a.lse && d == 0) a.lse[(b * a.heads + q.head) * a.queries + q.token] = sum > 0.f ? (tops[r] + __log2f(sum)) * kLn2 : -INFINITY;
+        }
+    }
+}
+
+// The parts of one query row, joined: one wavefront, D / 64 values a lane
+// (half the lanes of D = 32 idle).  Part s of row i is parts at(s).
+template <int D>
+struct Joined {
+    float y[D > 64 ? 2 : 1];
+    float top, sum;
+    __device__ inline Joined(const Parts& p, int64_t i, int lane) : top(kLow), sum(0.f) {
+        y[0] = y[D > 64 ? 1 : 0] = 0.f;
+        add(p, i, lane);
+    }
+    __device__ inline void add(const Parts& p, int64_t i, int lane) {
+        for (int s0 = 0; s0 < p.splits; s0 += 64) {
+            const float2 ml = s0 + lane < p.splits ? p.ml[(s0 + lane) * p.total + i] : make_float2(kLow, 0.f);
+            float up = ml.y > 0.f ? ml.x : kLow;
+            for (int o = 32; o; o >>= 1) up = fmaxf(up, __shfl_xor(up, o));
+            up = fmaxf(up, top);
+            const float f = exp2_fast(top - up), w = ml.y > 0.f ? exp2_fast(ml.x - up) : 0.f;
+            float all = ml.y * w;
+            for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
+            sum = sum * f + all;
+            y[0] *= f;
+            if (D > 64) y[D > 64 ? 1 : 0] *= f;
+            top = up;
+            const int n = min(64, p.splits - s0);
+            for (int s = 0; s < n; ++s) {
+                const float ws = __shfl(w, s);
+                const float* o = p.o + ((s0 + s) * p.total + i) * D;
+                // (a part without a key is not written)
+                if (ws > 0.f) {
+                    if (D >= 64 || lane < D) y[0] = fmaf(ws, o[lane], y[0]);
+                    if (D > 64 && lane + 64 < D) y[D > 64 ? 1 : 0] = fmaf(ws, o[lane + 64], y[D > 64 ? 1 : 0]);
+                }
+            }
+        }
+    }
+    template <typename T>
+    __device__ inline void write(T* out, int lane) const {
+        const float inv = sum > 0.f ? 1.f / sum : 0.f;
+        if (D >= 64 || lane < D) out[lane] = (T)(y[0] * inv);
+        if (D > 64 && lane + 64 < D) out[lane + 64] = (T)(y[D > 64 ? 1 : 0] * inv);
+    }
+    __device__ inline float lse() const { return sum > 0.f ? (top + __log2f(sum)) * kLn2 : -INFINITY; }
+};
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attend_join(frog_attend_t a, int group, Parts parts) {
+    const int lane = threadIdx.x & 63;
+    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), rows = a.queries * group;
+    if (i >= parts.total) return;
+    const int64_t x = i / rows, b = x / a.kv_heads;
+    const QueryRow q(i % rows, group, (int)(x % a.kv_heads));
+    const Joined<D> y(parts, i, lane);
+    y.write((T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2], lane);
+    if (a.lse && lane == 0) a.lse[(b * a.heads + q.head) * a.queries + q.token] = y.lse();
+}
+
+// The key weights of a few-rows pass, from the scores it kept: thread per key.
+static __global__ __launch_bounds__(256) void attend_weigh_few(frog_attend_t a, int group, const float* scores) {
+    const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs;
+    const int64_t b = x / (uint32_t)a.kv_heads, j = (int64_t)(blockIdx.x / pairs) * 256 + threadIdx.x;
+    const int hk = (int)(x % (uint32_t)a.kv_heads), rows = (int)a.queries * group;
+    if (j >= a.keys) return;
+    float sum = 0.f;
+    for (int r = 0; r < rows; ++r) {
+        const QueryRow q(r, group, hk);
+        int lo, hi;
+        interval(a, b, q.token, &lo, &hi);
+        const int64_t i = (b * a.heads + q.head) * a.queries + q.token;
+        if (j >= lo && j <= hi) sum += exp2_fast(scores[i * a.keys + j] - a.lse[i] * kLog2e);
+    }
+    const int64_t at = (int64_t)x * a.keys + j;
+    a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum;
+}
+
+}  // namespace frog

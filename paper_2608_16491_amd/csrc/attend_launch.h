@@ -1,0 +1,38 @@
+// Launches of the attention kernels of one row type (attend_bf16.hip,
+// attend_f16.hip, attend_f32.hip instantiate them) and the plan they share
+// with the workspace query.
+#pragma once
+
+#include "attend.h"
+
+namespace frog {
+
+// How a forward pass is cut, by sizes alone, and where its workspace lies
+// (byte offsets).
+struct ForwardPlan {
+    bool few;          // at most 32 query rows per kv head: no LDS tiles, 16-row products
+    int groups;        // few: groups of 16 rows
+    int tiles;         // else: workgroups' row tiles
+    int splits;        // parts of the keys
+    int64_t rows;      // query rows per (sequence, kv head)
+    int64_t lse, o, ml, scores, pack;   // workspace
+    int64_t bytes;
+};
+constexpr int kTileRows = 128;    // query rows (keys, in the passes that own keys) of a workgroup
+ForwardPlan forward_plan(const frog_attend_t& a);
+
+// What pack_rows prepares: offsets from the start of the region
+struct PackPlan {
+    int64_t tiles, rows, bounds, zeros, bytes;
+};
+PackPlan pack_plan(const frog_attend_t& a);
+
+template <typename T>
+struct AttendLaunch {
+    static void forward(const frog_attend_t& a, const ForwardPlan& p, char* ws, hipStream_t s);
+    // w_out from the log sums of a forward pass (natural logarithm)
+    static void weigh(const frog_attend_t& a, const float* lse, char* pack, hipStream_t s);
+    static void backward(const frog_attend_t& a, char* pack, hipStream_t s);
+};
+
+}  // namespace frog

@@ -12,7 +12,7 @@ import math
 
 import torch
 
-U = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -9}
+U = {t: torch.finfo(t).eps / 2 for t in (torch.float32, torch.float16, torch.bfloat16)}
 TINY = {torch.float32: 1e-36, torch.float16: 2.0 ** -24, torch.bfloat16: 1e-36}   # below it a value of the type is lost
 E = 2.0 ** -24
 
