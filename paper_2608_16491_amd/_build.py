@@ -26,7 +26,7 @@ HOST_SOURCES = ["build_index.cpp"]
 HIP_SOURCES = ["capi.cpp", "search.hip", "search_shared.hip", "search_scan.hip", "search_pool.hip", "search_trav.hip",
                "exact.hip", "bruteforce.hip", "build_gpu.hip", "attend_api.cpp", "attend.hip", "attend_bf16.hip",
                "attend_f16.hip", "attend_f32.hip", "attend_bwd_bf16.hip", "attend_bwd_f16.hip", "attend_bwd_f32.hip",
-               "attend_shared.hip", "evict.hip"]
+               "evict.hip"]
 
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -55,7 +55,7 @@ __device__ inline float score2(const ScoreParams& s, float dot) {
     return s.cap2 - 2.f * s.cap2 * rcp_fast(1.f + exp2_fast(dot * s.mul));
 }
 
-// launchers (attend.hip, attend_bwd.hip, attend_shared.hip, evict.hip).  The
+// launchers (attend.hip, evict.hip).  The
 // arguments have been checked (attend_api.cpp); ws holds the bytes of the
 // matching *_ws call.
 int64_t attend_ws(const frog_attend_t& a);

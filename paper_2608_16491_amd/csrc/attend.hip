@@ -139,4 +139,45 @@ int launch_attend_bwd(const frog_attend_t& a, void* ws, hipStream_t stream) {
     return launched("attention gradient launch");
 }
 
+SharedPlan shared_plan(const frog_attend_shared_t& a) {
+    SharedPlan p{};
+    const int64_t group = a.heads / a.kv_heads, rows = a.batch * group, all = a.batch * a.heads;
+    const int64_t most = a.pages_per_request * a.page;
+    // parts as in forward_plan
+    if (a.prefix > 0) {
+        p.few = rows <= 32;
+        p.tiles = (int)((rows + kTileRows - 1) / kTileRows);
+        const int64_t blocks = (int64_t)a.kv_heads * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
+        p.head_splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / blocks, (a.prefix + least - 1) / least));
+    }
+    p.groups = std::max(p.few ? rows : 0, std::min<int64_t>(group, 32)) <= 16 ? 1 : 2;
+    if (most > 0) {
+        const int64_t blocks = a.batch * a.kv_heads * ((group + 16 * p.groups - 1) / (16 * p.groups));
+        p.tail_splits = (int)std::max<int64_t>(1, std::min((1024 + blocks - 1) / blocks, (most + 127) / 128));
+        p.tail_blocks = blocks * p.tail_splits;
+    }
+    int64_t at = 0;
+    p.ho = take(&at, p.head_splits * all * a.d * 4);
+    p.hml = take(&at, p.head_splits * all * 8);
+    p.to = take(&at, p.tail_splits * all * a.d * 4);
+    p.tml = take(&at, p.tail_splits * all * 8);
+    if (a.slopes && p.head_splits && !p.few) {
+        p.at_q = take(&at, a.batch * 4);
+        p.at_k = take(&at, a.prefix * 4);
+    }
+    p.bytes = at;
+    return p;
+}
+
+int64_t attend_shared_ws(const frog_attend_shared_t& a) { return a.batch == 0 ? 0 : std::max<int64_t>(256, shared_plan(a).bytes); }
+
+int launch_attend_shared(const frog_attend_shared_t& a, void* ws, hipStream_t stream) {
+    if (a.batch == 0) return FROG_OK;
+    const SharedPlan p = shared_plan(a);
+    int rc = check_grid(std::max({p.tail_blocks + (int64_t)a.kv_heads * p.head_splits, (int64_t)a.kv_heads * p.head_splits * p.tiles, a.batch * a.heads / 4 + 1}));
+    if (rc != FROG_OK) return rc;
+    by_type(a.type, [&](auto l) { l.shared(a, p, (char*)ws, stream); });
+    return launched("shared attention launch");
+}
+
 }  // namespace frog

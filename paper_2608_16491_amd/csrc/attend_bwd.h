@@ -331,8 +331,8 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
         inner_lo = max(inner_lo, ends[2 * W + i]);
         inner_hi = min(inner_hi, ends[3 * W + i]);
     }
-    // intervals that share a key leave no gap
-    const bool gaps = __builtin_amdgcn_readfirstlane(inner_lo > inner_hi);
+    // (intervals that share a key leave no gap)
+    const bool gaps = inner_lo > inner_hi && rows_of.any(last, lane);
     first = __builtin_amdgcn_readfirstlane(first);
     last = __builtin_amdgcn_readfirstlane(last);
     const T* kp = (const T*)a.k + b * a.k_stride[0] + hk * a.k_stride[2];

@@ -3,4 +3,5 @@
 
 namespace frog {
 template void AttendLaunch<f16_t>::forward(const frog_attend_t&, const ForwardPlan&, char*, hipStream_t);
+template void AttendLaunch<f16_t>::shared(const frog_attend_shared_t&, const SharedPlan&, char*, hipStream_t);
 }

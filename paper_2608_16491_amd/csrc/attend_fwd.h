@@ -5,9 +5,10 @@
 
 namespace frog {
 
-// Partial results of a pass split along the keys: part s of query row i of
-// (sequence, kv head) x: maximum and sum at ml[(s * total + x * rows + i)],
-// unnormalised output of D floats at o[...] (total = rows of all)
+// Partial results of a pass split along the keys (o: null when the pass writes
+// its outputs itself): part s of query row i of (sequence, kv head) x: maximum
+// and sum at ml[(s * total + x * rows + i)], unnormalised output of D floats
+// at o[...] (total = rows of all)
 struct Parts {
     float* o;
     float2* ml;
@@ -69,8 +70,8 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
         inner_lo = max(inner_lo, ends[2 * W + i]);
         inner_hi = min(inner_hi, ends[3 * W + i]);
     }
-    // intervals that share a key leave no gap
-    const bool gaps = __builtin_amdgcn_readfirstlane(inner_lo > inner_hi);
+    // (intervals that share a key leave no gap)
+    const bool gaps = inner_lo > inner_hi && rows_of.any(last, lane);
     first = __builtin_amdgcn_readfirstlane(first);
     last = __builtin_amdgcn_readfirstlane(last);
     if (parts.splits > 1 && last >= 0) {
@@ -196,7 +197,7 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
         top = kLow;
     }
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    if (parts.splits > 1) {
+    if (parts.o) {
         const int64_t at = split * parts.total + x * rows + row;
         if (lane < 32) parts.ml[at] = make_float2(top, sum);
         if (sum > 0.f) {
@@ -541,7 +542,7 @@ __global__ __launch_bounds__(256) void attend_few(frog_attend_t a, ScoreParams s
         const int r = i / (D / 4), d = i % (D / 4) * 4;
         const float sum = sums[r], inv = sum > 0.f ? 1.f / sum : 0.f;
         const acc4 y = *(const acc4*)(lds + r * (D + 4) + d);
-        if (parts.splits > 1) {
+        if (parts.o) {
             const int64_t at = split * parts.total + (int64_t)x * rows + r;
             if (sum > 0.f) *(acc4*)(parts.o + at * D + d) = y;
             if (d == 0) parts.ml[at] = make_float2(tops[r], sum);
@@ -556,16 +557,104 @@ __global__ __launch_bounds__(256) void attend_few(frog_attend_t a, ScoreParams s
     }
 }
 
+// One token of each of many requests over their shared prefix and their own
+// tails, for few rows: workgroups below `head` take a part of the prefix for
+// the rows of all requests (at most 16 RG per kv head; none when the prefix is
+// left to attend_tile), the others a part of one request's tail for 16 RG rows
+// of a kv head's group.
+template <typename T, int D, int RG>
+__global__ __launch_bounds__(256) void shared_few(frog_attend_shared_t a, ScoreParams sp, int group, int head, Parts prefix, Parts tail) {
+    constexpr int W = 4;
+    __shared__ float lds[16 * RG * (D + 4)], tops[W * RG * 16], sums[W * RG * 16];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    FewPass<T, D, RG> f;
+    f.reset();
+    const bool own = (int)blockIdx.x >= head;    // a tail
+    const int row_groups = (group + 16 * RG - 1) / (16 * RG);
+    uint32_t x = own ? blockIdx.x - head : blockIdx.x;
+    const int hk = (int)(x % (uint32_t)a.kv_heads);
+    x /= (uint32_t)a.kv_heads;
+    int row0 = 0, split;
+    int64_t b = 0;
+    if (own) {
+        row0 = (int)(x % (uint32_t)row_groups) * 16 * RG;
+        x /= (uint32_t)row_groups;
+        b = x % (uint32_t)a.batch;
+        split = (int)(x / (uint32_t)a.batch);
+    } else {
+        split = (int)x;
+    }
+    const Parts& parts = own ? tail : prefix;
+    const int rows = own ? min(group - row0, 16 * RG) : (int)a.batch * group;
+    const int64_t most = a.pages_per_request * a.page;
+    int first = INT_MAX, last = -1;
+#pragma unroll
+    for (int g = 0; g < RG; ++g) {
+        const int r = min(16 * g + (lane & 15), rows - 1);
+        const int64_t req = own ? b : r / group;
+        const int h = hk * group + (own ? row0 + r : r % group);
+        const int len = a.pages_per_request > 0 ? (int)min((int64_t)max(a.lengths[req], 0), most) : 0;
+        int lo = 0, hi = own ? len - 1 : (int)a.prefix - 1;
+        if (!own && a.lr) {
+            const int2 p = *(const int2*)(a.lr + 2 * req);
+            lo = max(lo, p.x);
+            hi = min(hi, p.y);
+        }
+        if (16 * g + (lane & 15) >= rows) lo = 0, hi = -1;
+        f.row.lo[g] = lo;
+        f.row.hi[g] = hi;
+        first = min(first, col_min(lo <= hi ? lo : INT_MAX));
+        last = max(last, col_max(lo <= hi ? hi : -1));
+        f.row.slope[g] = a.slopes ? a.slopes[h] * kLog2e : 0.f;
+        f.row.aq[g] = (float)((own ? 0 : a.prefix) + len - 1);
+        const T* p = (const T*)a.q + req * a.q_stride[0] + h * a.q_stride[1] + (lane >> 4) * 8;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) f.q[g][s] = load_frag(p + 32 * s);
+    }
+    if (parts.splits > 1 && last >= 0) {
+        const int each = ((last - first) / parts.splits / (32 * W) + 1) * (32 * W);
+        const int64_t from = first + (int64_t)split * each;
+        last = (int)min((int64_t)last, from + each - 1);
+        first = (int)min(from, (int64_t)last + 1);
+    }
+    auto at_key = [](int j) { return (float)j; };
+    auto none = [](int, int, float) {};
+    if (first <= last) {
+        if (own) {
+            const PagedKeys<T> keys{(const T*)a.k_pages + hk * a.k_pages_stride[2], (const T*)a.v_pages + hk * a.v_pages_stride[2],
+                                    {a.k_pages_stride[0], a.k_pages_stride[1]}, {a.v_pages_stride[0], a.v_pages_stride[1]},
+                                    a.pages + b * a.pages_per_request, (uint32_t)a.page, a.num_pages,
+                                    (const T*)a.q + b * a.q_stride[0] + hk * group * a.q_stride[1]};
+            f.run(keys, sp, a.slopes != nullptr, at_key, none, first, last, w, W, lane);
+        } else {
+            const FlatKeys<T> keys{(const T*)a.k + hk * a.k_stride[1], (const T*)a.v + hk * a.v_stride[1], a.k_stride[0], a.v_stride[0]};
+            f.run(keys, sp, a.slopes != nullptr, at_key, none, first, last, w, W, lane);
+        }
+    }
+    f.template join<W>(lds, tops, sums, w, lane);
+    if (w == 0 && lane < 16) {
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            sums[16 * g + lane] = f.row.lo[g] <= f.row.hi[g] ? f.row.sum[g] : 0.f;
+            tops[16 * g + lane] = f.row.top[g];
+        }
+    }
+    __syncthreads();
+    const int64_t base = split * parts.total + (own ? (b * a.kv_heads + hk) * group + row0 : (int64_t)hk * rows);
+    for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * W) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4;
+        if (sums[r] > 0.f) *(acc4*)(parts.o + (base + r) * D + d) = *(const acc4*)(lds + r * (D + 4) + d);
+        if (d == 0) parts.ml[base + r] = make_float2(tops[r], sums[r]);
+    }
+}
+
 // The parts of one query row, joined: one wavefront, D / 64 values a lane
 // (half the lanes of D = 32 idle).  Part s of row i is parts at(s).
 template <int D>
 struct Joined {
     float y[D > 64 ? 2 : 1];
     float top, sum;
-    __device__ inline Joined(const Parts& p, int64_t i, int lane) : top(kLow), sum(0.f) {
-        y[0] = y[D > 64 ? 1 : 0] = 0.f;
-        add(p, i, lane);
-    }
+    __device__ inline Joined() : top(kLow), sum(0.f) { y[0] = y[D > 64 ? 1 : 0] = 0.f; }
     __device__ inline void add(const Parts& p, int64_t i, int lane) {
         for (int s0 = 0; s0 < p.splits; s0 += 64) {
             const float2 ml = s0 + lane < p.splits ? p.ml[(s0 + lane) * p.total + i] : make_float2(kLow, 0.f);
@@ -607,9 +696,34 @@ __global__ __launch_bounds__(256) void attend_join(frog_attend_t a, int group, P
     if (i >= parts.total) return;
     const int64_t x = i / rows, b = x / a.kv_heads;
     const QueryRow q(i % rows, group, (int)(x % a.kv_heads));
-    const Joined<D> y(parts, i, lane);
+    Joined<D> y;
+    y.add(parts, i, lane);
     y.write((T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2], lane);
     if (a.lse && lane == 0) a.lse[(b * a.heads + q.head) * a.queries + q.token] = y.lse();
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void shared_join(frog_attend_shared_t a, int group, Parts prefix, Parts tail) {
+    const int lane = threadIdx.x & 63;
+    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (i >= a.batch * a.heads) return;
+    const int64_t b = i / a.heads;
+    const int h = (int)(i % a.heads);
+    Joined<D> y;
+    y.add(prefix, (h / group * a.batch + b) * group + h % group, lane);
+    y.add(tail, i, lane);
+    y.write((T*)a.out + b * a.out_stride[0] + h * a.out_stride[1], lane);
+    if (a.lse && lane == 0) a.lse[i] = y.lse();
+}
+
+// The attributes of a biased pass over a shared prefix: keys stand at their
+// numbers, request b's query at prefix + its tail's length - 1.
+static __global__ __launch_bounds__(256) void shared_places(frog_attend_shared_t a, float* at_q, float* at_k) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < a.prefix) at_k[i] = (float)i;
+    if (i >= a.batch) return;
+    const int64_t len = a.pages_per_request > 0 ? min((int64_t)max(a.lengths[i], 0), a.pages_per_request * a.page) : 0;
+    at_q[i] = (float)(a.prefix + len - 1);
 }
 
 // The key weights of a few-rows pass, from the scores it kept: thread per key.

@@ -21,6 +21,18 @@ struct ForwardPlan {
 constexpr int kTileRows = 128;    // query rows (keys, in the passes that own keys) of a workgroup
 ForwardPlan forward_plan(const frog_attend_t& a);
 
+// The same of a pass over a shared prefix.
+struct SharedPlan {
+    bool few;                 // at most 32 query rows per kv head over the prefix
+    int groups;               // groups of 16 rows of the few-rows passes
+    int tiles;                // else: workgroups' row tiles over the prefix
+    int head_splits, tail_splits;
+    int64_t tail_blocks;      // workgroups of the tails
+    int64_t ho, hml, to, tml, at_q, at_k;
+    int64_t bytes;
+};
+SharedPlan shared_plan(const frog_attend_shared_t& a);
+
 // What pack_rows prepares: offsets from the start of the region
 struct PackPlan {
     int64_t tiles, rows, bounds, zeros, bytes;
@@ -30,6 +42,7 @@ PackPlan pack_plan(const frog_attend_t& a);
 template <typename T>
 struct AttendLaunch {
     static void forward(const frog_attend_t& a, const ForwardPlan& p, char* ws, hipStream_t s);
+    static void shared(const frog_attend_shared_t& a, const SharedPlan& p, char* ws, hipStream_t s);
     // w_out from the log sums of a forward pass (natural logarithm)
     static void weigh(const frog_attend_t& a, const float* lse, char* pack, hipStream_t s);
     static void backward(const frog_attend_t& a, char* pack, hipStream_t s);

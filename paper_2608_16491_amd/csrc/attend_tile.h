@@ -191,6 +191,18 @@ __device__ inline void mask_scores(acc16 (&z)[S], int lo, int hi, int lane) {
 template <int ROWS>
 struct Gaps {
     int lo[ROWS], hi[ROWS];
+    // whether there are any up to key `last`: a key after an interval's end
+    // that no interval holds
+    __device__ inline bool any(int last, int lane) const {
+        bool gap = false;
+        for (int i = lane; i < ROWS; i += 64) {
+            const int j = hi[i] + 1;
+            bool seen = lo[i] > hi[i] || j > last;
+            for (int r = 0; r < ROWS; ++r) seen |= j >= lo[r] && j <= hi[r];
+            gap |= !seen;
+        }
+        return __any(gap);
+    }
     // rows j .. j + N - 1 of a tile of D values in LDS, by W wavefronts (call
     // between barriers)
     template <int N, int D, int W, typename T>
