@@ -648,34 +648,50 @@ __global__ __launch_bounds__(256) void shared_few(frog_attend_shared_t a, ScoreP
     }
 }
 
-// The parts of one query row, joined: one wavefront, D / 64 values a lane
-// (half the lanes of D = 32 idle).  Part s of row i is parts at(s).
+// The parts of one query row, joined: one wavefront, D / 64 neighbouring
+// values a lane (half the lanes of D = 32 idle; D = 96 takes 1.5 as 2).
 template <int D>
 struct Joined {
-    float y[D > 64 ? 2 : 1];
+    static constexpr int V = D > 64 ? 2 : 1;
+    float y[V];
     float top, sum;
-    __device__ inline Joined() : top(kLow), sum(0.f) { y[0] = y[D > 64 ? 1 : 0] = 0.f; }
+    __device__ inline Joined() : top(kLow), sum(0.f) {
+        for (int v = 0; v < V; ++v) y[v] = 0.f;
+    }
+    // maxima and sums alone
+    __device__ inline float add_sums(const Parts& p, int64_t i, int s0, int lane) {
+        const float2 ml = s0 + lane < p.splits ? p.ml[(s0 + lane) * p.total + i] : make_float2(kLow, 0.f);
+        float up = ml.y > 0.f ? ml.x : kLow;
+        for (int o = 32; o; o >>= 1) up = fmaxf(up, __shfl_xor(up, o));
+        up = fmaxf(up, top);
+        const float f = exp2_fast(top - up), w = ml.y > 0.f ? exp2_fast(ml.x - up) : 0.f;
+        float all = ml.y * w;
+        for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
+        sum = sum * f + all;
+#pragma unroll
+        for (int v = 0; v < V; ++v) y[v] *= f;
+        top = up;
+        return w;
+    }
     __device__ inline void add(const Parts& p, int64_t i, int lane) {
+        const int d = min(lane * V, D - V);
         for (int s0 = 0; s0 < p.splits; s0 += 64) {
-            const float2 ml = s0 + lane < p.splits ? p.ml[(s0 + lane) * p.total + i] : make_float2(kLow, 0.f);
-            float up = ml.y > 0.f ? ml.x : kLow;
-            for (int o = 32; o; o >>= 1) up = fmaxf(up, __shfl_xor(up, o));
-            up = fmaxf(up, top);
-            const float f = exp2_fast(top - up), w = ml.y > 0.f ? exp2_fast(ml.x - up) : 0.f;
-            float all = ml.y * w;
-            for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o);
-            sum = sum * f + all;
-            y[0] *= f;
-            if (D > 64) y[D > 64 ? 1 : 0] *= f;
-            top = up;
+            const float w = add_sums(p, i, s0, lane);
             const int n = min(64, p.splits - s0);
-            for (int s = 0; s < n; ++s) {
-                const float ws = __shfl(w, s);
-                const float* o = p.o + ((s0 + s) * p.total + i) * D;
-                // (a part without a key is not written)
-                if (ws > 0.f) {
-                    if (D >= 64 || lane < D) y[0] = fmaf(ws, o[lane], y[0]);
-                    if (D > 64 && lane + 64 < D) y[D > 64 ? 1 : 0] = fmaf(ws, o[lane + 64], y[D > 64 ? 1 : 0]);
+            const float* o = p.o + (s0 * p.total + i) * D + d;
+            // eight parts' reads in flight; a part without a key is not
+            // written, and may hold anything
+            for (int s = 0; s < n; s += 8) {
+                vec<float, V> x[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] = *(const vec<float, V>*)(o + min(s + u, n - 1) * p.total * D);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const float ws = __shfl(w, (s + u) & 63);
+                    if (s + u < n && ws > 0.f) {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) y[v] = fmaf(ws, x[u][v], y[v]);
+                    }
                 }
             }
         }
@@ -683,8 +699,11 @@ struct Joined {
     template <typename T>
     __device__ inline void write(T* out, int lane) const {
         const float inv = sum > 0.f ? 1.f / sum : 0.f;
-        if (D >= 64 || lane < D) out[lane] = (T)(y[0] * inv);
-        if (D > 64 && lane + 64 < D) out[lane + 64] = (T)(y[D > 64 ? 1 : 0] * inv);
+        if (lane * V >= D) return;
+        vec<T, V> t;
+#pragma unroll
+        for (int v = 0; v < V; ++v) t[v] = (T)(y[v] * inv);
+        *(vec<T, V>*)(out + lane * V) = t;
     }
     __device__ inline float lse() const { return sum > 0.f ? (top + __log2f(sum)) * kLn2 : -INFINITY; }
 };
