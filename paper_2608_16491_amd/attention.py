@@ -6,10 +6,11 @@ only; the gradients go through ``torch.autograd``.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
-from . import STORAGE_BF16, STORAGE_F16, STORAGE_F32, FrogError, _check, lib
+from . import STORAGE_BF16, STORAGE_F16, STORAGE_F32, _check, lib
 
 _TYPES = {torch.float32: STORAGE_F32, torch.float16: STORAGE_F16, torch.bfloat16: STORAGE_BF16}
 _P, _I, _D = C.c_void_p, C.c_int64, C.c_int32
@@ -40,116 +41,134 @@ class EvictArgs(C.Structure):
                 ("slots", _I), ("keep", _I), ("recent", _I), ("heads", _D), ("d", _D), ("type", _D)]
 
 
+def _packer(cls):
+    """Writes the values of a struct's fields, arrays spread out, in order."""
+    codes = {_P: "P", _I: "q", _D: "i", C.c_float: "f"}
+    fmt = "".join(codes[t] if t in codes else codes[t._type_] * t._length_ for _, t in cls._fields_)
+    out = struct.Struct("@" + fmt + "0q")
+    assert out.size == C.sizeof(cls)
+    return out.pack
+
+
+_pack_attend, _pack_shared, _pack_evict = (_packer(c) for c in (AttendArgs, SharedArgs, EvictArgs))
+# the raw handle of the current stream, without the stream object built around it where torch offers that
+_current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _need(ok, text):
     if not ok:
         raise ValueError(text)
 
 
-def _tensor(name, t, dtype, shape, device, packed=True):
-    """`t` is None or a tensor of this type, shape and device (packed: contiguous)."""
-    if t is None:
-        return
-    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.device == device and (not packed or t.is_contiguous()),
-          f"{name}: {dtype} {tuple(shape)} on {device}{', contiguous' if packed else ''} is wanted, not {t.dtype} {tuple(t.shape)} on {t.device}")
+def _plain(name, t, dtype, shape, like):
+    """`t` is a contiguous tensor of this type and shape on the device of `like`."""
+    if t.dtype != dtype or t.shape != shape or t.get_device() != like.get_device() or not t.is_contiguous():
+        raise ValueError(f"{name}: {dtype} {tuple(shape)} on {like.device}, contiguous, is wanted, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
 
 
-def _values(name, t, dtype, dims, device):
-    """A tensor of rows: its last axis has no gaps."""
-    _need(t.dim() == dims and t.dtype == dtype and t.device == device, f"{name}: {dims} axes of {dtype} on {device} are wanted, "
-          f"not {t.dim()} of {t.dtype} on {t.device}")
-    _need(t.shape[-1] < 2 or t.stride(-1) == 1, f"{name}: the last axis must have stride 1")
+def _values(names, tensors, dims):
+    """Tensors of rows: of one supported type, on one GPU, their last axes without gaps."""
+    first = tensors[0]
+    dtype, device = first.dtype, first.get_device()
+    _need(device >= 0, f"{names[0]} is on {first.device}: a GPU tensor is wanted")
+    _need(dtype in _TYPES, f"{names[0]} is {dtype}: float32, float16 or bfloat16")
+    for name, t, n in zip(names, tensors, dims):
+        _need(t.dtype == dtype and t.get_device() == device and t.dim() == n, f"{name}: {n} axes of {dtype} on {first.device} are wanted, "
+              f"not {t.dim()} of {t.dtype} on {t.device}")
+        _need(t.stride(-1) == 1 or t.shape[-1] < 2, f"{name}: the last axis must have stride 1")
+    return _TYPES[dtype]
 
 
-def _start(q):
-    _need(q.is_cuda, f"q is on {q.device}: a GPU tensor is wanted")
-    _need(q.dtype in _TYPES, f"q is {q.dtype}: float32, float16 or bfloat16")
-
-
-def _put(a, name, t):
-    if t is not None:
-        setattr(a, name, t.data_ptr())
-        setattr(a, name + "_stride", t.stride()[:-1])
-
-
-def _at(t):
-    return None if t is None else t.data_ptr()
-
-
-def _workspace(a, bytes_, device):
-    """The call's workspace, from torch's allocator (so that a captured graph keeps it)."""
-    if bytes_ < 0:
-        _check(bytes_)
-    if bytes_ == 0:
-        return None
-    ws = torch.empty(bytes_, dtype=torch.uint8, device=device)
-    a.ws, a.ws_bytes = ws.data_ptr(), bytes_
-    return ws
-
-
-def _launch(fn, a, stream, device, tensors):
+def _launch(fn, args, stream, device, tensors):
     """Enqueue on `stream` (default: the current one of the device); memory that another stream's allocator pool holds is kept
     until `stream` is done with it."""
-    here = torch.cuda.current_stream(device)
-    s = here if stream is None else stream
-    _need(s.device == device, f"the stream is on {s.device}, the tensors on {device}")
-    with torch.cuda.device(device):
-        _check(fn(C.byref(a), s.cuda_stream))
-    if s != here:
+    index = device.index
+    here = _current(index)
+    handle = here if stream is None else stream.cuda_stream
+    _need(stream is None or stream.device == device, f"the stream is not on {device}")
+    if torch.cuda.current_device() == index:
+        rc = fn(args, handle)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(args, handle)
+    if rc:
+        _check(rc)
+    if handle != here:
         for t in tensors:
             if t is not None:
-                t.record_stream(s)
+                t.record_stream(stream)
+
+
+def _own_workspace(large):
+    """Whether a call takes its workspace from torch rather than the library's buffer of the stream: a captured graph has to
+    keep it, and the library would keep a large one for good."""
+    return large or torch.cuda.is_current_stream_capturing()
+
+
+def _workspace(query, args, device):
+    n = query(args)
+    if n < 0:
+        _check(n)
+    ws = torch.empty(n, dtype=torch.uint8, device=device) if n else None
+    return ws, (ws.data_ptr(), n) if n else (0, 0)
+
+
+_NONE4 = (0, 0, 0, 0)
+_NO_GRADS = _NONE4 * 4
 
 
 class _Call:
     """The checked arguments of one attention call, apart from its outputs."""
 
+    __slots__ = ("device", "shape", "extra", "rows", "masks", "tail")
+
     def __init__(self, q, k, v, lr, scale, cap, slopes, at_q, at_k):
-        _start(q)
-        _values("q", q, q.dtype, 4, q.device)
-        _values("k", k, q.dtype, 4, q.device)
-        _values("v", v, q.dtype, 4, q.device)
+        kind = _values(("q", "k", "v"), (q, k, v), (4, 4, 4))
         b, tq, h, d = q.shape
-        tk, kv = k.shape[1], k.shape[2]
-        _need(k.shape == (b, tk, kv, d) and v.shape == k.shape, f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}: "
+        _, tk, kv, _ = ks = k.shape
+        _need(ks == (b, tk, kv, d) and v.shape == ks, f"q {tuple(q.shape)}, k {tuple(ks)}, v {tuple(v.shape)}: "
               "[batch, queries, heads, d] and twice [batch, keys, kv_heads, d] are wanted")
-        _need((slopes is None) == (at_q is None) == (at_k is None), "slopes, at_q and at_k go together")
-        self.dev, self.shape, self.kv = q.device, (b, tq, h, d, tk), kv
-        self.extra = (lr, slopes, at_q, at_k)
-        a = self.a = AttendArgs()
+        self.device, self.shape, self.extra = q.device, (b, tq, h, d, tk, kv), (lr, slopes, at_q, at_k)
+        self.rows = (q.data_ptr(), *q.stride()[:3], k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3])
+        lrs = (0, 0)
         if lr is not None:
-            _tensor("lr", lr, torch.int32, (tq, 2) if lr.dim() == 2 else (b, tq, 2), q.device)
-            a.lr, a.lr_stride = lr.data_ptr(), 0 if lr.dim() == 2 else 2 * tq
+            one = lr.dim() == 2
+            lrs = (_plain("lr", lr, torch.int32, (tq, 2) if one else (b, tq, 2), q), 0 if one else 2 * tq)
+        bias = (0, 0, 0, 0, 0, 0)
         if slopes is not None:
-            _tensor("slopes", slopes, torch.float32, (h,), q.device)
-            _tensor("at_q", at_q, torch.float32, (b, tq), q.device)
-            _tensor("at_k", at_k, torch.float32, (b, tk) if at_k.dim() == 2 else (b, kv, tk), q.device)
+            _need(at_q is not None and at_k is not None, "slopes, at_q and at_k go together")
             _need(not slopes.requires_grad, "slopes take no gradient")
-            a.slopes, a.at_q, a.at_k, a.at_q_stride = slopes.data_ptr(), at_q.data_ptr(), at_k.data_ptr(), tq
-            a.at_k_stride = (tk, 0) if at_k.dim() == 2 else (kv * tk, tk)
-        a.batch, a.queries, a.keys, a.heads, a.kv_heads, a.d, a.type = b, tq, tk, h, kv, d, _TYPES[q.dtype]
-        a.scale, a.cap = d ** -0.5 if scale is None else scale, cap
-        _put(a, "q", q)
-        _put(a, "k", k)
-        _put(a, "v", v)
+            f, one = torch.float32, at_k.dim() == 2
+            bias = (_plain("slopes", slopes, f, (h,), q), _plain("at_q", at_q, f, (b, tq), q), tq,
+                    _plain("at_k", at_k, f, (b, tk) if one else (b, kv, tk), q), tk if one else kv * tk, 0 if one else tk)
+        else:
+            _need(at_q is None and at_k is None, "slopes, at_q and at_k go together")
+        self.masks = lrs + bias
+        self.tail = (b, tq, tk, h, kv, d, kind, d ** -0.5 if scale is None else scale, cap)
 
     def forward(self, q, k, v, want_lse, w_in, w_out, stream):
-        a, (b, tq, h, d, tk) = self.a, self.shape
-        out = torch.empty((b, tq, h, d), dtype=q.dtype, device=self.dev)
-        lse = torch.empty((b, h, tq), dtype=torch.float32, device=self.dev) if want_lse else None
-        _put(a, "out", out)
-        a.lse, a.w_in, a.w_out = _at(lse), _at(w_in), _at(w_out)
-        ws = _workspace(a, lib().frog_attend_workspace(C.byref(a), 0), self.dev)
-        _launch(lib().frog_attend, a, stream, self.dev, (q, k, v, *self.extra, out, lse, w_in, w_out, ws))
+        b, tq, h, d, tk, kv = self.shape
+        out = torch.empty((b, tq, h, d), dtype=q.dtype, device=self.device)
+        lse = torch.empty((b, h, tq), dtype=torch.float32, device=self.device) if want_lse else None
+        head = (*self.rows, out.data_ptr(), tq * h * d, h * d, d, *self.masks, 0 if lse is None else lse.data_ptr(),
+                0 if w_in is None else w_in.data_ptr(), 0 if w_out is None else w_out.data_ptr(), *_NO_GRADS)
+        args, ws, L = _pack_attend(*head, 0, 0, *self.tail), None, lib()
+        if _own_workspace(w_out is not None and q.numel() // d * tk > 2 ** 22):
+            ws, at = _workspace(lambda x: L.frog_attend_workspace(x, 0), args, self.device)
+            args = _pack_attend(*head, *at, *self.tail)
+        _launch(L.frog_attend, args, stream, self.device, (q, k, v, *self.extra, out, lse, w_in, w_out, ws))
         return out, lse
 
     def backward(self, q, k, v, out, lse, dout):
-        a = self.a
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=self.dev) for t in (q, k, v))
-        for name, t in (("q", q), ("k", k), ("v", v), ("out", out), ("dout", dout), ("dq", dq), ("dk", dk), ("dv", dv)):
-            _put(a, name, t)
-        a.lse, a.w_in, a.w_out, a.ws, a.ws_bytes = lse.data_ptr(), None, None, None, 0
-        ws = _workspace(a, lib().frog_attend_workspace(C.byref(a), 1), self.dev)
-        _launch(lib().frog_attend_backward, a, None, self.dev, (ws,))
+        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=self.device) for t in (q, k, v))
+        grads = (x for t in (dout, dq, dk, dv) for x in (t.data_ptr(), *t.stride()[:3]))
+        head = (*self.rows, out.data_ptr(), *out.stride()[:3], *self.masks, lse.data_ptr(), 0, 0, *grads)
+        args, ws, L = _pack_attend(*head, 0, 0, *self.tail), None, lib()
+        if _own_workspace(q.numel() > 2 ** 22 or k.numel() > 2 ** 22):
+            ws, at = _workspace(lambda x: L.frog_attend_workspace(x, 1), args, self.device)
+            args = _pack_attend(*head, *at, *self.tail)
+        _launch(L.frog_attend_backward, args, None, self.device, ())
         return dq, dk, dv
 
 
@@ -192,12 +211,13 @@ def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_
     queries] (return_lse) and the new weights (weights given).  q, k and v
     take gradients; lse and weights do not."""
     call = _Call(q, k, v, lr, scale, cap, slopes, at_q, at_k)
-    b, tq, h, d, tk = call.shape
     if weights is not None:
-        _tensor("weights", weights, torch.float32, (b, call.kv, tk), call.dev)
-        _tensor("weights_out", weights_out, torch.float32, (b, call.kv, tk), call.dev)
+        b, _, _, _, tk, kv = call.shape
+        _plain("weights", weights, torch.float32, (b, kv, tk), q)
         if weights_out is None:
             weights_out = torch.empty_like(weights)
+        else:
+            _plain("weights_out", weights_out, torch.float32, (b, kv, tk), q)
     else:
         _need(weights_out is None, "weights_out needs weights")
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
@@ -219,31 +239,28 @@ def attend_shared(q, k, v, k_pages, v_pages, pages, lengths, *, lr=None, scale=N
     (None: all).  slopes [heads]: scores fall with the distance of the query,
     which stands on the last row of its tail.  Returns out [batch, heads, d],
     and lse [batch, heads] with return_lse."""
-    _start(q)
-    dev = q.device
-    for name, t, dims in (("q", q, 3), ("k", k, 3), ("v", v, 3), ("k_pages", k_pages, 4), ("v_pages", v_pages, 4)):
-        _values(name, t, q.dtype, dims, dev)
+    kind = _values(("q", "k", "v", "k_pages", "v_pages"), (q, k, v, k_pages, v_pages), (3, 3, 3, 4, 4))
     b, h, d = q.shape
-    tk, kv = k.shape[:2]
-    _need(k.shape == (tk, kv, d) and v.shape == k.shape and k_pages.shape[2:] == (kv, d) and v_pages.shape == k_pages.shape,
+    tk, kv, _ = k.shape
+    num, page, _, _ = k_pages.shape
+    _need(k.shape == (tk, kv, d) and v.shape == k.shape and k_pages.shape == (num, page, kv, d) and v_pages.shape == k_pages.shape,
           f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, pages {tuple(k_pages.shape)}, {tuple(v_pages.shape)}: "
           "[batch, heads, d], twice [prefix, kv_heads, d], twice [num_pages, page, kv_heads, d] are wanted")
     _need(pages.dim() == 2, "pages: [batch, pages_per_request] is wanted")
-    _tensor("pages", pages, torch.int32, (b, pages.shape[1]), dev)
-    _tensor("lengths", lengths, torch.int32, (b,), dev)
-    _tensor("lr", lr, torch.int32, (b, 2), dev)
-    _tensor("slopes", slopes, torch.float32, (h,), dev)
-    out = torch.empty((b, h, d), dtype=q.dtype, device=dev)
-    lse = torch.empty((b, h), dtype=torch.float32, device=dev) if return_lse else None
-    a = SharedArgs()
-    for name, t in (("q", q), ("k", k), ("v", v), ("k_pages", k_pages), ("v_pages", v_pages), ("out", out)):
-        _put(a, name, t)
-    a.pages, a.lengths, a.lr, a.slopes, a.lse = pages.data_ptr(), lengths.data_ptr(), _at(lr), _at(slopes), _at(lse)
-    a.batch, a.prefix, a.num_pages, a.pages_per_request, a.page = b, tk, k_pages.shape[0], pages.shape[1], k_pages.shape[1]
-    a.heads, a.kv_heads, a.d, a.type = h, kv, d, _TYPES[q.dtype]
-    a.scale, a.cap = d ** -0.5 if scale is None else scale, cap
-    ws = _workspace(a, lib().frog_attend_shared_workspace(C.byref(a)), dev)
-    _launch(lib().frog_attend_shared, a, stream, dev, (q, k, v, k_pages, v_pages, pages, lengths, lr, slopes, out, lse, ws))
+    width, device = pages.shape[1], q.device
+    out = torch.empty((b, h, d), dtype=q.dtype, device=device)
+    lse = torch.empty((b, h), dtype=torch.float32, device=device) if return_lse else None
+    head = (q.data_ptr(), *q.stride()[:2], k.data_ptr(), *k.stride()[:2], v.data_ptr(), *v.stride()[:2], k_pages.data_ptr(),
+            *k_pages.stride()[:3], v_pages.data_ptr(), *v_pages.stride()[:3], _plain("pages", pages, torch.int32, (b, width), q),
+            _plain("lengths", lengths, torch.int32, (b,), q), 0 if lr is None else _plain("lr", lr, torch.int32, (b, 2), q),
+            0 if slopes is None else _plain("slopes", slopes, torch.float32, (h,), q), out.data_ptr(), h * d, d,
+            0 if lse is None else lse.data_ptr())
+    tail = (b, tk, num, width, page, h, kv, d, kind, d ** -0.5 if scale is None else scale, cap)
+    args, ws, L = _pack_shared(*head, 0, 0, *tail), None, lib()
+    if _own_workspace(q.numel() > 2 ** 22):
+        ws, at = _workspace(L.frog_attend_shared_workspace, args, device)
+        args = _pack_shared(*head, *at, *tail)
+    _launch(L.frog_attend_shared, args, stream, device, (q, k, v, k_pages, v_pages, pages, lengths, lr, slopes, out, lse, ws))
     return (out, lse) if return_lse else out
 
 
@@ -254,27 +271,23 @@ def evict(k, v, weights, positions, lengths, keep, *, recent=0, stream=None):
     the slots) [batch, heads, slots]; lengths int32 [batch].  Returns new
     (k, v, weights, positions, lengths) with ``keep`` slots; those past a
     length hold 0, 0, 0 and -1."""
-    _need(k.is_cuda and k.dtype in _TYPES, f"k is {k.dtype} on {k.device}: float32, float16 or bfloat16 on a GPU is wanted")
-    dev = k.device
-    _values("k", k, k.dtype, 4, dev)
-    _values("v", v, k.dtype, 4, dev)
+    kind = _values(("k", "v"), (k, v), (4, 4))
     _need(v.shape == k.shape, f"k {tuple(k.shape)}, v {tuple(v.shape)}: the same shape is wanted")
     b, t, h, d = k.shape
-    _tensor("weights", weights, torch.float32, (b, h, t), dev)
-    _tensor("positions", positions, torch.int32, (b, h, t), dev)
-    _tensor("lengths", lengths, torch.int32, (b,), dev)
     _need(0 <= recent <= keep <= t, f"recent {recent}, keep {keep}, slots {t}: 0 <= recent <= keep <= slots is wanted")
-    k_out, v_out = (torch.empty((b, keep, h, d), dtype=k.dtype, device=dev) for _ in range(2))
-    w_out = torch.empty((b, h, keep), dtype=torch.float32, device=dev)
-    p_out = torch.empty((b, h, keep), dtype=torch.int32, device=dev)
-    n_out = torch.empty((b,), dtype=torch.int32, device=dev)
-    a = EvictArgs()
-    _put(a, "k", k)
-    _put(a, "v", v)
-    a.weights, a.positions, a.lengths = weights.data_ptr(), _at(positions), lengths.data_ptr()
-    a.k_out, a.v_out, a.weights_out, a.positions_out = k_out.data_ptr(), v_out.data_ptr(), w_out.data_ptr(), p_out.data_ptr()
-    a.lengths_out = n_out.data_ptr()
-    a.batch, a.slots, a.keep, a.recent, a.heads, a.d, a.type = b, t, keep, recent, h, d, _TYPES[k.dtype]
-    ws = _workspace(a, lib().frog_evict_workspace(C.byref(a)), dev)
-    _launch(lib().frog_evict, a, stream, dev, (k, v, weights, positions, lengths, k_out, v_out, w_out, p_out, n_out, ws))
+    device = k.device
+    k_out, v_out = (torch.empty((b, keep, h, d), dtype=k.dtype, device=device) for _ in range(2))
+    w_out = torch.empty((b, h, keep), dtype=torch.float32, device=device)
+    p_out = torch.empty((b, h, keep), dtype=torch.int32, device=device)
+    n_out = torch.empty((b,), dtype=torch.int32, device=device)
+    head = (k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3], _plain("weights", weights, torch.float32, (b, h, t), k),
+            0 if positions is None else _plain("positions", positions, torch.int32, (b, h, t), k),
+            _plain("lengths", lengths, torch.int32, (b,), k), k_out.data_ptr(), v_out.data_ptr(), w_out.data_ptr(), p_out.data_ptr(),
+            n_out.data_ptr())
+    tail = (b, t, keep, recent, h, d, kind)
+    args, ws, L = _pack_evict(*head, 0, 0, *tail), None, lib()
+    if _own_workspace(b * h * keep > 2 ** 22):
+        ws, at = _workspace(L.frog_evict_workspace, args, device)
+        args = _pack_evict(*head, *at, *tail)
+    _launch(L.frog_evict, args, stream, device, (k, v, weights, positions, lengths, k_out, v_out, w_out, p_out, n_out, ws))
     return k_out, v_out, w_out, p_out, n_out
