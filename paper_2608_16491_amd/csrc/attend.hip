@@ -42,6 +42,13 @@ void clear(void* p, const int64_t (&st)[3], int64_t batch, int64_t tokens, int h
 
 }  // namespace
 
+// Up to so many keys a few-rows pass is not split: one launch, eight
+// wavefronts a workgroup, four steps each.  A CU takes in about 60 GB/s, so a
+// workgroup's step of 256 keys of 128 bf16 values costs 2.3 us; split over
+// CUs and joined by a second launch 1,001 keys take 12 us of device time
+// against 13, but 4 us more on the host; 2,048 keys 10 against 22.
+constexpr int64_t kWholeKeys = 1024;
+
 ForwardPlan forward_plan(const frog_attend_t& a) {
     ForwardPlan p{};
     const int64_t group = a.heads / a.kv_heads, pairs = a.batch * a.kv_heads;
@@ -54,6 +61,7 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     // (128 keys; 256 of the tiles', whose parts cost 4 D bytes a row)
     const int64_t blocks = pairs * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
     p.splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / std::max<int64_t>(blocks, 1), (a.keys + least - 1) / least));
+    if (p.few && p.groups == 1 && a.keys <= kWholeKeys) p.splits = 1;
     int64_t at = 0;
     if (p.splits > 1) {
         p.o = take(&at, p.splits * pairs * p.rows * a.d * 4);
@@ -143,6 +151,12 @@ SharedPlan shared_plan(const frog_attend_shared_t& a) {
     SharedPlan p{};
     const int64_t group = a.heads / a.kv_heads, rows = a.batch * group, all = a.batch * a.heads;
     const int64_t most = a.pages_per_request * a.page;
+    if (a.prefix + most <= kWholeKeys && a.batch * a.prefix <= 16 * kWholeKeys) {
+        p.whole = true;
+        p.groups = group <= 16 ? 1 : 2;
+        p.tail_blocks = a.batch * a.kv_heads * ((group + 16 * p.groups - 1) / (16 * p.groups));
+        return p;
+    }
     // parts as in forward_plan
     if (a.prefix > 0) {
         p.few = rows <= 32;
@@ -169,7 +183,7 @@ SharedPlan shared_plan(const frog_attend_shared_t& a) {
     return p;
 }
 
-int64_t attend_shared_ws(const frog_attend_shared_t& a) { return a.batch == 0 ? 0 : std::max<int64_t>(256, shared_plan(a).bytes); }
+int64_t attend_shared_ws(const frog_attend_shared_t& a) { return a.batch == 0 ? 0 : shared_plan(a).bytes; }
 
 int launch_attend_shared(const frog_attend_shared_t& a, void* ws, hipStream_t stream) {
     if (a.batch == 0) return FROG_OK;

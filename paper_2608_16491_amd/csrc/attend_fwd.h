@@ -236,6 +236,7 @@ struct FlatKeys {
     __device__ static inline Where of(Where x, int i, int j, int last) { return {min(j + i, last)}; }
     __device__ inline const T* key(Where x) const { return k + x.j * ks; }
     __device__ inline const T* value(Where x) const { return v + x.j * vs; }
+    static constexpr bool kPaged = false;
     __device__ static inline bool real(Where) { return true; }
 };
 
@@ -258,6 +259,7 @@ struct PagedKeys {
     __device__ static inline Where of(Where x, int i, int, int) { return {__shfl(x.page, i), __shfl(x.row, i)}; }
     __device__ inline const T* key(Where x) const { return x.page >= 0 ? k + x.page * ks[0] + x.row * ks[1] : spare; }
     __device__ inline const T* value(Where x) const { return x.page >= 0 ? v + x.page * vs[0] + x.row * vs[1] : spare; }
+    static constexpr bool kPaged = true;
     __device__ static inline bool real(Where x) { return x.page >= 0; }
 };
 
@@ -294,101 +296,100 @@ struct FewPass {
         }
     }
 
-    // at_key(j): attribute of key j (NULL functor result unused without bias);
-    // store(g, j, z): takes every score of key j <= last
-    template <typename Keys, typename At, typename Store>
+    // PLAIN: neither cap nor bias.  at_key(j): attribute of key j (with a bias);
+    // store(g, j, z, whole): takes four scores of the keys from j in log2 units
+    // (whole: all of them exist).
+    // The next step's keys are loaded once the scores have been taken from
+    // this one's registers, its values after the second product: two loads
+    // are in flight behind the arithmetic without registers for a second step.
+    template <bool PLAIN, typename Keys, typename At, typename Store>
     __device__ inline void run(const Keys& keys, const ScoreParams& sp, bool bias, At&& at_key, Store&& store, int first, int last, int w,
                                int W, int lane) {
         const int c = lane & 15, h = lane >> 4;
-        int fit_lo = 0, fit_hi = INT_MAX;   // keys every real row sees
+        int fit_lo = 0, fit_hi = last;   // keys every real row sees
 #pragma unroll
         for (int g = 0; g < RG; ++g) {
             const bool some = row.lo[g] <= row.hi[g];
             fit_lo = max(fit_lo, col_max(some ? row.lo[g] : 0));
             fit_hi = min(fit_hi, col_min(some ? row.hi[g] : INT_MAX));
         }
-        int64_t j0 = (int64_t)first + 32 * w;
-        if (j0 > last) return;
-        typename Keys::Where mine = keys.where(min((int)j0 + (lane & 31), last));
-        for (; j0 <= last; j0 += 32 * W) {
-            const int j = (int)j0;
-            // key rows c and 16 + c; value rows 4h .. 4h+3 and 16 + 4h ..
-            frag<T> kf[2][K];
-            vec<T, C> vv[8];
-            bool real[8];
+        frag<T> kf[2][K];   // key rows c and 16 + c
+        vec<T, C> vv[8];    // value rows 4h .. 4h+3 and 16 + 4h ..
+        uint32_t real = 255, coming = 255;   // bit e: value row e has a page
+        typename Keys::Where mine{};
+        auto row_of = [&](int e) { return 16 * (e >> 2) + 4 * h + (e & 3); };
+        auto load_keys = [&](int j) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const T* p = keys.key(Keys::of(mine, 16 * u + c, j, last)) + 8 * h;
 #pragma unroll
                 for (int s = 0; s < K; ++s) kf[u][s] = load_frag(p + 32 * s);
             }
+        };
+        auto load_values = [&](int j) {
+            if (Keys::kPaged) coming = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const auto x = Keys::of(mine, 16 * (e >> 2) + 4 * h + (e & 3), j, last);
-                vv[e] = load_piece(keys.value(x) + C * c);
-                real[e] = Keys::real(x);
+                const auto at = Keys::of(mine, row_of(e), j, last);
+                vv[e] = load_piece(keys.value(at) + C * c);
+                if (Keys::kPaged) coming |= (uint32_t)Keys::real(at) << e;
             }
-            const int64_t next = j0 + 32 * W;
-            if (next <= last) mine = keys.where((int)min(next + (lane & 31), (int64_t)last));
-            float ak[8];
-            if (bias) {
+        };
+        int64_t j64 = (int64_t)first + 32 * w;
+        if (j64 > last) return;
+        mine = keys.where((int)min(j64 + (lane & 31), (int64_t)last));
+        load_keys((int)j64);
+        load_values((int)j64);
+        real = coming;
+        auto step = [&](auto masked, int j, bool more, int next) {
+            constexpr bool MASKED = decltype(masked)::value;
+            if (more) mine = keys.where((int)min((int64_t)next + (lane & 31), (int64_t)last));
+            float z[RG][8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) ak[e] = at_key(min(j + 16 * (e >> 2) + 4 * h + (e & 3), last));
-            }
-            // keys that some row sees: the others' values, which may be anything,
-            // must not meet a weight of 0 in the second product
-            const bool whole = j >= fit_lo && j + 31 <= min(fit_hi, last);
-            if (!whole) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int at = j + 16 * (e >> 2) + 4 * h + (e & 3);
-                    bool in = false;
-#pragma unroll
-                    for (int g = 0; g < RG; ++g) in |= at >= row.lo[g] && at <= min(row.hi[g], last);
-                    real[e] = real[e] && ((__ballot(in) >> (16 * h)) & 0xffff) != 0;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (!real[e]) vv[e] = vec<T, C>{};
-            frag<T> p[RG];
-#pragma unroll
-            for (int g = 0; g < RG; ++g) {
-                float z[8];
+            for (int g = 0; g < RG; ++g)
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     acc4 s4 = acc4{};
 #pragma unroll
                     for (int s = 0; s < K; ++s) s4 = mma(kf[u][s], q[g][s], s4);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) z[4 * u + r] = s4[r];
+                    for (int r = 0; r < 4; ++r) z[g][4 * u + r] = s4[r];
                 }
-                if (sp.cap2 > 0.f) {
+            if (more) load_keys(next);
+            float ak[8];
+            if (!PLAIN && bias) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = score2<true>(sp, z[e]);
+                for (int e = 0; e < 8; ++e) ak[e] = at_key(min(j + row_of(e), last));
+            }
+            uint32_t met = 0;
+            frag<T> p[RG];
+#pragma unroll
+            for (int g = 0; g < RG; ++g) {
+                if (!PLAIN && sp.cap2 > 0.f) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[g][e] = score2<true>(sp, z[g][e]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] *= sp.mul;
+                    for (int e = 0; e < 8; ++e) z[g][e] *= sp.mul;
                 }
-                if (bias) {
+                if (!PLAIN && bias) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] -= row.slope[g] * fabsf(row.aq[g] - ak[e]);
+                    for (int e = 0; e < 8; ++e) z[g][e] -= row.slope[g] * fabsf(row.aq[g] - ak[e]);
                 }
 #pragma unroll
-                for (int e = 0; e < 8; ++e) store(g, j + 16 * (e >> 2) + 4 * h + (e & 3), z[e]);
-                if (!whole) {
+                for (int u = 0; u < 2; ++u) store(g, j + row_of(4 * u), &z[g][4 * u], !MASKED);
+                if constexpr (MASKED) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const int at = j + 16 * (e >> 2) + 4 * h + (e & 3);
-                        z[e] = at >= row.lo[g] && at <= min(row.hi[g], last) ? z[e] : -INFINITY;
+                        const int at = j + row_of(e);
+                        const bool in = at >= row.lo[g] && at <= min(row.hi[g], last) && ((real >> e) & 1);
+                        z[g][e] = in ? z[g][e] : -INFINITY;
+                        met |= (uint32_t)(((__ballot(in) >> (16 * h)) & 0xffff) != 0) << e;
                     }
                 }
-                float mx = -INFINITY;
+                float mx = z[g][0];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    z[e] = real[e] ? z[e] : -INFINITY;
-                    mx = fmaxf(mx, z[e]);
-                }
+                for (int e = 1; e < 8; ++e) mx = fmaxf(mx, z[g][e]);
                 mx = quarter_max(mx);
                 if (__any(mx > row.top[g] + 8.f)) {
                     const float up = fmaxf(row.top[g], mx), f = exp2_fast(row.top[g] - up);
@@ -400,11 +401,18 @@ struct FewPass {
                 vec<float, 8> y;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    y[e] = exp2_fast(z[e] - row.top[g]);
+                    y[e] = exp2_fast(z[g][e] - row.top[g]);
                     row.sum[g] += y[e];
                 }
                 if constexpr (sizeof(T) == 4) p[g] = y;
                 else p[g] = __builtin_convertvector(y, frag<T>);
+            }
+            if constexpr (MASKED) {
+                // values of keys that no row sees may be anything, and must not
+                // meet a weight of 0 in the second product
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (!((met >> e) & 1)) vv[e] = vec<T, C>{};
             }
 #pragma unroll
             for (int e = 0; e < C; ++e) {
@@ -412,9 +420,20 @@ struct FewPass {
 #pragma unroll
                 for (int g = 0; g < RG; ++g) o[g][e] = mma(vf, p[g], o[g][e]);
             }
+            if (more) {
+                load_values(next);
+                real = coming;
+            }
+        };
+        for (;;) {
+            const int j = (int)j64;
+            const int64_t next = j64 + 32 * W;
+            const bool more = next <= last;
+            if (j >= fit_lo && j + 31 <= fit_hi && (!Keys::kPaged || __all(real == 255))) step(std::false_type{}, j, more, (int)min(next, (int64_t)last));
+            else step(std::true_type{}, j, more, (int)min(next, (int64_t)last));
+            if (!more) break;
+            j64 = next;
         }
-#pragma unroll
-        for (int g = 0; g < RG; ++g) row.sum[g] = quarter_sum(row.sum[g]);
     }
 
     // D / 16 values from an address of that alignment (4, 8, 12, 16 or 32 bytes)
@@ -436,12 +455,16 @@ struct FewPass {
         return x;
     }
 
-    // Joins the wavefronts' results in lds (16 RG rows of D floats, and W times
-    // as many maxima and sums); then every wavefront holds the joint top and
-    // sum, and the rows in LDS are the unnormalised output
+    // Joins the W wavefronts' results: pairs of halves, through LDS in the
+    // registers' own layout, then the rows of the whole in lds (16 RG of D + 4
+    // floats, unnormalised) and their maxima and sums in tops, sums (W RG 16
+    // floats each).  Starts and ends with a barrier.
+    static constexpr int kJoin(int W) { return (W / 2) * 64 * RG * C * 4 > 16 * RG * (D + 4) ? (W / 2) * 64 * RG * C * 4 : 16 * RG * (D + 4); }
     template <int W>
     __device__ inline void join(float* lds, float* tops, float* sums, int w, int lane) {
         const int c = lane & 15, h = lane >> 4;
+#pragma unroll
+        for (int g = 0; g < RG; ++g) row.sum[g] = quarter_sum(row.sum[g]);
 #pragma unroll
         for (int g = 0; g < RG; ++g)
             if (h == 0) {
@@ -449,7 +472,6 @@ struct FewPass {
                 sums[(w * RG + g) * 16 + c] = row.sum[g];
             }
         __syncthreads();
-        float f[RG];
 #pragma unroll
         for (int g = 0; g < RG; ++g) {
             float top = kLow, sum = 0.f;
@@ -457,35 +479,53 @@ struct FewPass {
             for (int i = 0; i < W; ++i) top = fmaxf(top, tops[(i * RG + g) * 16 + c]);
 #pragma unroll
             for (int i = 0; i < W; ++i) sum += sums[(i * RG + g) * 16 + c] * exp2_fast(tops[(i * RG + g) * 16 + c] - top);
-            f[g] = exp2_fast(row.top[g] - top);
+            const float f = exp2_fast(row.top[g] - top);
+#pragma unroll
+            for (int e = 0; e < C; ++e) o[g][e] *= f;
             row.top[g] = top;
             row.sum[g] = sum;
         }
-        for (int i = 0; i < W; ++i) {
-            if (i == w) {
+        acc4* slots = (acc4*)lds;
+#pragma unroll
+        for (int half = W / 2; half >= 1; half /= 2) {
+            if (w >= half && w < 2 * half) {
 #pragma unroll
                 for (int g = 0; g < RG; ++g)
 #pragma unroll
-                    for (int e = 0; e < C; ++e)
+                    for (int e = 0; e < C; ++e) slots[((w - half) * RG * C + g * C + e) * 64 + lane] = o[g][e];
+            }
+            __syncthreads();
+            if (w < half) {
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            float* p = lds + (16 * g + c) * (D + 4) + (4 * h + r) * C + e;
-                            const float y = o[g][e][r] * f[g];
-                            *p = i ? *p + y : y;
-                        }
+                for (int g = 0; g < RG; ++g)
+#pragma unroll
+                    for (int e = 0; e < C; ++e) o[g][e] += slots[(w * RG * C + g * C + e) * 64 + lane];
             }
             __syncthreads();
         }
+        if (w == 0) {
+#pragma unroll
+            for (int g = 0; g < RG; ++g) {
+                if (h == 0) {
+                    tops[16 * g + c] = row.top[g];
+                    sums[16 * g + c] = row.lo[g] <= row.hi[g] ? row.sum[g] : 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < C; ++e)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) lds[(16 * g + c) * (D + 4) + (4 * h + r) * C + e] = o[g][e][r];
+            }
+        }
+        __syncthreads();
     }
 };
 
 // One workgroup per (sequence, kv head, part of the keys) for at most 16 RG
-// query rows; scores (optional) [batch][heads][queries][keys] receive every
-// score in log2 units for the key weights.
-template <typename T, int D, int RG>
-__global__ __launch_bounds__(256) void attend_few(frog_attend_t a, ScoreParams sp, int group, Parts parts, float* scores) {
-    constexpr int W = 4;
-    __shared__ float lds[16 * RG * (D + 4)], tops[W * RG * 16], sums[W * RG * 16];
+// query rows.  KEEP: scores [batch][heads][queries][keys] receive every score in
+// log2 units for the key weights.
+template <typename T, int D, int RG, int W, bool PLAIN, bool KEEP>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RG == 1 && sizeof(T) == 2 ? 2 : 1))) void attend_few(frog_attend_t a, ScoreParams sp, int group, Parts parts, float* scores) {
+    __shared__ __attribute__((aligned(16))) float lds[FewPass<T, D, RG>::kJoin(W)], tops[W * RG * 16], sums[W * RG * 16];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs;
     const int split = (int)(blockIdx.x / pairs);
@@ -508,7 +548,7 @@ __global__ __launch_bounds__(256) void attend_few(frog_attend_t a, ScoreParams s
         last = max(last, col_max(lo <= hi ? hi : -1));
         f.row.slope[g] = a.slopes ? a.slopes[q.head] * kLog2e : 0.f;
         f.row.aq[g] = a.slopes ? a.at_q[b * a.at_q_stride + q.token] : 0.f;
-        zp[g] = scores && r < rows ? scores + ((b * a.heads + q.head) * a.queries + q.token) * a.keys : nullptr;
+        zp[g] = KEEP && r < rows ? scores + ((b * a.heads + q.head) * a.queries + q.token) * a.keys : nullptr;
         const T* p = (const T*)a.q + b * a.q_stride[0] + q.token * a.q_stride[1] + q.head * a.q_stride[2] + (lane >> 4) * 8;
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) f.q[g][s] = load_frag(p + 32 * s);
@@ -523,21 +563,18 @@ __global__ __launch_bounds__(256) void attend_few(frog_attend_t a, ScoreParams s
                            a.k_stride[1], a.v_stride[1]};
     const float* akp = a.slopes ? a.at_k + b * a.at_k_stride[0] + hk * a.at_k_stride[1] : nullptr;
     if (first <= last)
-        f.run(keys, sp, akp != nullptr, [&](int j) { return akp[j]; },
-              [&](int g, int j, float z) {
-                  if (zp[g] && j <= last) zp[g][j] = z;
-              },
-              first, last, w, W, lane);
+        f.template run<PLAIN>(keys, sp, akp != nullptr, [&](int j) { return akp[j]; },
+                              [&](int g, int j, const float* z, bool all) {
+                                  if (!KEEP || !zp[g]) return;
+                                  using f4 = float __attribute__((ext_vector_type(4), aligned(4)));
+                                  if (all) *(f4*)(zp[g] + j) = f4{z[0], z[1], z[2], z[3]};
+                                  else
+                                      for (int e = 0; e < 4; ++e)
+                                          if (j + e <= last) zp[g][j + e] = z[e];
+                              },
+                              first, last, w, W, lane);
     f.template join<W>(lds, tops, sums, w, lane);
     // joint rows: out, or this part's
-    if (w == 0 && lane < 16) {
-#pragma unroll
-        for (int g = 0; g < RG; ++g) {
-            sums[16 * g + lane] = f.row.lo[g] <= f.row.hi[g] ? f.row.sum[g] : 0.f;
-            tops[16 * g + lane] = f.row.top[g];
-        }
-    }
-    __syncthreads();
     for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * W) {
         const int r = i / (D / 4), d = i % (D / 4) * 4;
         const float sum = sums[r], inv = sum > 0.f ? 1.f / sum : 0.f;
@@ -562,10 +599,10 @@ __global__ __launch_bounds__(256) void attend_few(frog_attend_t a, ScoreParams s
 // the rows of all requests (at most 16 RG per kv head; none when the prefix is
 // left to attend_tile), the others a part of one request's tail for 16 RG rows
 // of a kv head's group.
-template <typename T, int D, int RG>
-__global__ __launch_bounds__(256) void shared_few(frog_attend_shared_t a, ScoreParams sp, int group, int head, Parts prefix, Parts tail) {
+template <typename T, int D, int RG, bool PLAIN>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RG == 1 && sizeof(T) == 2 ? 2 : 1))) void shared_few(frog_attend_shared_t a, ScoreParams sp, int group, int head, Parts prefix, Parts tail) {
     constexpr int W = 4;
-    __shared__ float lds[16 * RG * (D + 4)], tops[W * RG * 16], sums[W * RG * 16];
+    __shared__ __attribute__((aligned(16))) float lds[FewPass<T, D, RG>::kJoin(W)], tops[W * RG * 16], sums[W * RG * 16];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     FewPass<T, D, RG> f;
     f.reset();
@@ -618,33 +655,87 @@ __global__ __launch_bounds__(256) void shared_few(frog_attend_shared_t a, ScoreP
         first = (int)min(from, (int64_t)last + 1);
     }
     auto at_key = [](int j) { return (float)j; };
-    auto none = [](int, int, float) {};
+    auto none = [](int, int, const float*, bool) {};
     if (first <= last) {
         if (own) {
             const PagedKeys<T> keys{(const T*)a.k_pages + hk * a.k_pages_stride[2], (const T*)a.v_pages + hk * a.v_pages_stride[2],
                                     {a.k_pages_stride[0], a.k_pages_stride[1]}, {a.v_pages_stride[0], a.v_pages_stride[1]},
                                     a.pages + b * a.pages_per_request, (uint32_t)a.page, a.num_pages,
                                     (const T*)a.q + b * a.q_stride[0] + hk * group * a.q_stride[1]};
-            f.run(keys, sp, a.slopes != nullptr, at_key, none, first, last, w, W, lane);
+            f.template run<PLAIN>(keys, sp, a.slopes != nullptr, at_key, none, first, last, w, W, lane);
         } else {
             const FlatKeys<T> keys{(const T*)a.k + hk * a.k_stride[1], (const T*)a.v + hk * a.v_stride[1], a.k_stride[0], a.v_stride[0]};
-            f.run(keys, sp, a.slopes != nullptr, at_key, none, first, last, w, W, lane);
+            f.template run<PLAIN>(keys, sp, a.slopes != nullptr, at_key, none, first, last, w, W, lane);
         }
     }
     f.template join<W>(lds, tops, sums, w, lane);
-    if (w == 0 && lane < 16) {
-#pragma unroll
-        for (int g = 0; g < RG; ++g) {
-            sums[16 * g + lane] = f.row.lo[g] <= f.row.hi[g] ? f.row.sum[g] : 0.f;
-            tops[16 * g + lane] = f.row.top[g];
-        }
-    }
-    __syncthreads();
     const int64_t base = split * parts.total + (own ? (b * a.kv_heads + hk) * group + row0 : (int64_t)hk * rows);
     for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * W) {
         const int r = i / (D / 4), d = i % (D / 4) * 4;
         if (sums[r] > 0.f) *(acc4*)(parts.o + (base + r) * D + d) = *(const acc4*)(lds + r * (D + 4) + d);
         if (d == 0) parts.ml[base + r] = make_float2(tops[r], sums[r]);
+    }
+}
+
+// The same where prefix and tails are short: one workgroup does both for 16 RG
+// rows of a (request, kv head) and nothing is left to join (the prefix comes
+// from L2 for all requests but the first).
+template <typename T, int D, int RG, int W, bool PLAIN>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RG == 1 && sizeof(T) == 2 ? 2 : 1))) void shared_whole(frog_attend_shared_t a, ScoreParams sp, int group) {
+    __shared__ __attribute__((aligned(16))) float lds[FewPass<T, D, RG>::kJoin(W)], tops[W * RG * 16], sums[W * RG * 16];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row_groups = (group + 16 * RG - 1) / (16 * RG);
+    uint32_t x = blockIdx.x;
+    const int hk = (int)(x % (uint32_t)a.kv_heads);
+    x /= (uint32_t)a.kv_heads;
+    const int row0 = (int)(x % (uint32_t)row_groups) * 16 * RG, rows = min(group - row0, 16 * RG);
+    const int64_t b = x / (uint32_t)row_groups;
+    const int len = a.pages_per_request > 0 ? (int)min((int64_t)max(a.lengths[b], 0), a.pages_per_request * a.page) : 0;
+    int lo = 0, hi = (int)a.prefix - 1;
+    if (a.lr) {
+        const int2 p = *(const int2*)(a.lr + 2 * b);
+        lo = max(lo, p.x);
+        hi = min(hi, p.y);
+    }
+    FewPass<T, D, RG> f;
+    f.reset();
+#pragma unroll
+    for (int g = 0; g < RG; ++g) {
+        const int h = hk * group + row0 + min(16 * g + (lane & 15), rows - 1);
+        f.row.slope[g] = a.slopes ? a.slopes[h] * kLog2e : 0.f;
+        const T* p = (const T*)a.q + b * a.q_stride[0] + h * a.q_stride[1] + (lane >> 4) * 8;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) f.q[g][s] = load_frag(p + 32 * s);
+    }
+    auto pass = [&](auto& keys, int first, int last, float at) {
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            f.row.lo[g] = first;
+            f.row.hi[g] = 16 * g + (lane & 15) < rows ? last : -1;
+            f.row.aq[g] = at;
+        }
+        if (first <= last)
+            f.template run<PLAIN>(keys, sp, a.slopes != nullptr, [](int j) { return (float)j; }, [](int, int, const float*, bool) {}, first, last, w, W, lane);
+    };
+    const FlatKeys<T> head{(const T*)a.k + hk * a.k_stride[1], (const T*)a.v + hk * a.v_stride[1], a.k_stride[0], a.v_stride[0]};
+    pass(head, lo, hi, (float)(a.prefix + len - 1));
+    const PagedKeys<T> tail{(const T*)a.k_pages + hk * a.k_pages_stride[2], (const T*)a.v_pages + hk * a.v_pages_stride[2],
+                            {a.k_pages_stride[0], a.k_pages_stride[1]}, {a.v_pages_stride[0], a.v_pages_stride[1]},
+                            a.pages + b * a.pages_per_request, (uint32_t)a.page, a.num_pages,
+                            (const T*)a.q + b * a.q_stride[0] + hk * group * a.q_stride[1]};
+    pass(tail, 0, len - 1, (float)(len - 1));
+#pragma unroll
+    for (int g = 0; g < RG; ++g) f.row.lo[g] = f.row.hi[g] = 0;   // (rows past the group have the sum 0)
+    f.template join<W>(lds, tops, sums, w, lane);
+    for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * W) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4, h = hk * group + row0 + r;
+        const float sum = sums[r], inv = sum > 0.f ? 1.f / sum : 0.f;
+        const acc4 y = *(const acc4*)(lds + r * (D + 4) + d);
+        vec<T, 4> t;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = (T)(y[e] * inv);
+        *(vec<T, 4>*)((T*)a.out + b * a.out_stride[0] + h * a.out_stride[1] + d) = t;
+        if (a.lse && d == 0) a.lse[b * a.heads + h] = sum > 0.f ? (tops[r] + __log2f(sum)) * kLn2 : -INFINITY;
     }
 }
 
@@ -709,9 +800,8 @@ struct Joined {
 };
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attend_join(frog_attend_t a, int group, Parts parts) {
-    const int lane = threadIdx.x & 63;
-    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), rows = a.queries * group;
+__device__ inline void join_row(const frog_attend_t& a, int group, const Parts& parts, int64_t i, int lane) {
+    const int64_t rows = a.queries * group;
     if (i >= parts.total) return;
     const int64_t x = i / rows, b = x / a.kv_heads;
     const QueryRow q(i % rows, group, (int)(x % a.kv_heads));
@@ -719,6 +809,62 @@ __global__ __launch_bounds__(256) void attend_join(frog_attend_t a, int group, P
     y.add(parts, i, lane);
     y.write((T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2], lane);
     if (a.lse && lane == 0) a.lse[(b * a.heads + q.head) * a.queries + q.token] = y.lse();
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attend_join(frog_attend_t a, int group, Parts parts) {
+    join_row<T, D>(a, group, parts, (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), threadIdx.x & 63);
+}
+
+// The end of a few-rows pass that wants key weights: the first `joins`
+// workgroups join its parts (none where it was not split), the others take
+// 256 keys of a (sequence, kv head) each, from the scores the pass kept and
+// the parts' maxima and sums.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void attend_few_end(frog_attend_t a, int group, Parts parts, const float* scores, int joins) {
+    __shared__ float lse2[32];
+    __shared__ int lo[32], hi[32];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if ((int)blockIdx.x < joins) {
+        join_row<T, D>(a, group, parts, (int64_t)blockIdx.x * 4 + w, lane);
+        return;
+    }
+    const uint32_t at = blockIdx.x - joins, pairs = (uint32_t)(a.batch * a.kv_heads), x = at % pairs;
+    const int64_t b = x / (uint32_t)a.kv_heads, j = (int64_t)(at / pairs) * 256 + threadIdx.x;
+    const int hk = (int)(x % (uint32_t)a.kv_heads), rows = (int)a.queries * group;
+    for (int r = w; r < rows; r += 4) {
+        const QueryRow q(r, group, hk);
+        float z;
+        if (joins) {
+            Joined<D> y;
+            for (int s = 0; s < parts.splits; s += 64) y.add_sums(parts, (int64_t)x * rows + r, s, lane);
+            z = y.sum > 0.f ? y.top + __log2f(y.sum) : INFINITY;
+        } else {
+            z = a.lse[(b * a.heads + q.head) * a.queries + q.token] * kLog2e;
+        }
+        if (lane == 0) {
+            lse2[r] = z;
+            interval(a, b, q.token, &lo[r], &hi[r]);
+        }
+    }
+    __syncthreads();
+    if (j >= a.keys) return;
+    float sum = 0.f;
+    for (int r0 = 0; r0 < rows; r0 += 4) {
+        float z[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const QueryRow q(min(r0 + u, rows - 1), group, hk);
+            z[u] = scores[((b * a.heads + q.head) * a.queries + q.token) * a.keys + j];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int r = min(r0 + u, rows - 1);
+            if (r0 + u < rows && j >= lo[r] && j <= hi[r]) sum += exp2_fast(z[u] - lse2[r]);
+        }
+    }
+    const int64_t i = (int64_t)x * a.keys + j;
+    a.w_out[i] = (a.w_in ? a.w_in[i] : 0.f) + sum;
 }
 
 template <typename T, int D>
@@ -743,24 +889,6 @@ static __global__ __launch_bounds__(256) void shared_places(frog_attend_shared_t
     if (i >= a.batch) return;
     const int64_t len = a.pages_per_request > 0 ? min((int64_t)max(a.lengths[i], 0), a.pages_per_request * a.page) : 0;
     at_q[i] = (float)(a.prefix + len - 1);
-}
-
-// The key weights of a few-rows pass, from the scores it kept: thread per key.
-static __global__ __launch_bounds__(256) void attend_weigh_few(frog_attend_t a, int group, const float* scores) {
-    const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs;
-    const int64_t b = x / (uint32_t)a.kv_heads, j = (int64_t)(blockIdx.x / pairs) * 256 + threadIdx.x;
-    const int hk = (int)(x % (uint32_t)a.kv_heads), rows = (int)a.queries * group;
-    if (j >= a.keys) return;
-    float sum = 0.f;
-    for (int r = 0; r < rows; ++r) {
-        const QueryRow q(r, group, hk);
-        int lo, hi;
-        interval(a, b, q.token, &lo, &hi);
-        const int64_t i = (b * a.heads + q.head) * a.queries + q.token;
-        if (j >= lo && j <= hi) sum += exp2_fast(scores[i * a.keys + j] - a.lse[i] * kLog2e);
-    }
-    const int64_t at = (int64_t)x * a.keys + j;
-    a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum;
 }
 
 }  // namespace frog

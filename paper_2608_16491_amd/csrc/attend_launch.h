@@ -23,6 +23,7 @@ ForwardPlan forward_plan(const frog_attend_t& a);
 
 // The same of a pass over a shared prefix.
 struct SharedPlan {
+    bool whole;               // one launch without parts
     bool few;                 // at most 32 query rows per kv head over the prefix
     int groups;               // groups of 16 rows of the few-rows passes
     int tiles;                // else: workgroups' row tiles over the prefix

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <algorithm>
+#include <type_traits>
 
 #include "attend_fwd.h"
 #include "attend_launch.h"
@@ -23,19 +24,26 @@ void launch_forward(const frog_attend_t& a, const ForwardPlan& p, char* ws, hipS
     const Parts parts{p.splits > 1 ? (float*)(ws + p.o) : nullptr, (float2*)(ws + p.ml), pairs * p.rows, p.splits};
     frog_attend_t b = a;
     if (a.w_out && !a.lse) b.lse = (float*)(ws + p.lse);
-    if (p.few) {
-        const dim3 grid((unsigned)(pairs * p.splits));
-        float* scores = a.w_out ? (float*)(ws + p.scores) : nullptr;
-        if (p.groups == 1) attend_few<T, D, 1><<<grid, 256, 0, s>>>(b, sp, group, parts, scores);
-        else attend_few<T, D, 2><<<grid, 256, 0, s>>>(b, sp, group, parts, scores);
-    } else {
+    if (!p.few) {
         launch_tiles<T, D>(b, sp, group, p.tiles, parts, s);
+        if (p.splits > 1) attend_join<T, D><<<dim3((unsigned)((parts.total + 3) / 4)), 256, 0, s>>>(b, group, parts);
+        if (a.w_out) AttendLaunch<T>::weigh(b, b.lse, ws + p.pack, s);
+        return;
     }
-    if (p.splits > 1) attend_join<T, D><<<dim3((unsigned)((parts.total + 3) / 4)), 256, 0, s>>>(b, group, parts);
-    if (a.w_out) {
-        if (p.few) attend_weigh_few<<<dim3((unsigned)((a.keys + 255) / 256 * pairs)), 256, 0, s>>>(b, group, (const float*)(ws + p.scores));
-        else AttendLaunch<T>::weigh(b, b.lse, ws + p.pack, s);
-    }
+    const dim3 grid((unsigned)(pairs * p.splits));
+    float* scores = a.w_out ? (float*)(ws + p.scores) : nullptr;
+    auto few = [&](auto plain, auto keep) {
+        constexpr bool P = decltype(plain)::value, S = decltype(keep)::value;
+        if (p.groups == 2) attend_few<T, D, 2, 4, P, S><<<grid, 256, 0, s>>>(b, sp, group, parts, scores);
+        else if (p.splits > 1 || sizeof(T) == 4) attend_few<T, D, 1, 4, P, S><<<grid, 256, 0, s>>>(b, sp, group, parts, scores);
+        else if constexpr (sizeof(T) == 2) attend_few<T, D, 1, 8, P, S><<<grid, 512, 0, s>>>(b, sp, group, parts, scores);
+    };
+    const bool plain = !(a.cap > 0.f) && !a.slopes;
+    if (plain) a.w_out ? few(std::true_type{}, std::true_type{}) : few(std::true_type{}, std::false_type{});
+    else a.w_out ? few(std::false_type{}, std::true_type{}) : few(std::false_type{}, std::false_type{});
+    const int64_t joins = p.splits > 1 ? (parts.total + 3) / 4 : 0;
+    if (a.w_out) attend_few_end<T, D><<<dim3((unsigned)(joins + (a.keys + 255) / 256 * pairs)), 256, 0, s>>>(b, group, parts, scores, (int)joins);
+    else if (joins) attend_join<T, D><<<dim3((unsigned)joins), 256, 0, s>>>(b, group, parts);
 }
 
 template <typename T>
@@ -51,6 +59,18 @@ void launch_shared(const frog_attend_shared_t& a, const SharedPlan& p, char* ws,
     const ScoreParams sp = score_params(a.scale, a.cap);
     const int group = a.heads / a.kv_heads;
     const int64_t rows = a.batch * a.heads;
+    const bool plain = !(a.cap > 0.f) && !a.slopes;
+    if (p.whole) {
+        const dim3 grid((unsigned)p.tail_blocks);
+        auto whole = [&](auto plain) {
+            constexpr bool P = decltype(plain)::value;
+            constexpr int W = sizeof(T) == 2 ? 8 : 4;
+            if (p.groups == 1) shared_whole<T, D, 1, W, P><<<grid, 64 * W, 0, s>>>(a, sp, group);
+            else shared_whole<T, D, 2, 4, P><<<grid, 256, 0, s>>>(a, sp, group);
+        };
+        plain ? whole(std::true_type{}) : whole(std::false_type{});
+        return;
+    }
     const Parts prefix{(float*)(ws + p.ho), (float2*)(ws + p.hml), rows, p.head_splits}, tail{(float*)(ws + p.to), (float2*)(ws + p.tml), rows, p.tail_splits};
     int64_t head = 0;
     if (p.few) {
@@ -71,8 +91,12 @@ void launch_shared(const frog_attend_shared_t& a, const SharedPlan& p, char* ws,
     }
     if (head + p.tail_blocks > 0) {
         const dim3 grid((unsigned)(head + p.tail_blocks));
-        if (p.groups == 1) shared_few<T, D, 1><<<grid, 256, 0, s>>>(a, sp, group, (int)head, prefix, tail);
-        else shared_few<T, D, 2><<<grid, 256, 0, s>>>(a, sp, group, (int)head, prefix, tail);
+        auto few = [&](auto plain) {
+            constexpr bool P = decltype(plain)::value;
+            if (p.groups == 1) shared_few<T, D, 1, P><<<grid, 256, 0, s>>>(a, sp, group, (int)head, prefix, tail);
+            else shared_few<T, D, 2, P><<<grid, 256, 0, s>>>(a, sp, group, (int)head, prefix, tail);
+        };
+        plain ? few(std::true_type{}) : few(std::false_type{});
     }
     shared_join<T, D><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(a, group, prefix, tail);
 }
