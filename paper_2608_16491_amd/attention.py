@@ -154,7 +154,7 @@ class _Call:
         head = (*self.rows, out.data_ptr(), tq * h * d, h * d, d, *self.masks, 0 if lse is None else lse.data_ptr(),
                 0 if w_in is None else w_in.data_ptr(), 0 if w_out is None else w_out.data_ptr(), *_NO_GRADS)
         args, ws, L = _pack_attend(*head, 0, 0, *self.tail), None, lib()
-        if _own_workspace(w_out is not None and q.numel() // d * tk > 2 ** 22):
+        if _own_workspace(w_out is not None and max(q.numel() // d, kv * 64) * tk > 2 ** 22):
             ws, at = _workspace(lambda x: L.frog_attend_workspace(x, 0), args, self.device)
             args = _pack_attend(*head, *at, *self.tail)
         _launch(L.frog_attend, args, stream, self.device, (q, k, v, *self.extra, out, lse, w_in, w_out, ws))

@@ -70,19 +70,26 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     if (a.w_out) {
         if (!a.lse) p.lse = take(&at, a.batch * a.heads * a.queries * 4);
         if (p.few) p.scores = take(&at, a.batch * a.heads * a.queries * a.keys * 4);
-        else p.pack = take(&at, pack_plan(a).bytes);
+        else p.pack = take(&at, pack_plan(a, false).bytes);
     }
     p.bytes = at;
     return p;
 }
 
-PackPlan pack_plan(const frog_attend_t& a) {
+PackPlan pack_plan(const frog_attend_t& a, bool grad) {
     PackPlan p{};
     p.tiles = (a.queries * (a.heads / a.kv_heads) + 31) / 32;
+    // Parts of the query rows until there are two workgroups for each of the
+    // 256 CUs, of 8 tiles at least: a workgroup's keys see anything from all
+    // rows to a few (causal: the first keys twice the mean), and one runs on a
+    // CU at a time.  Their fp32 sums cost 16 d bytes a key and part.
+    const int64_t blocks = a.batch * a.kv_heads * ((a.keys + kTileRows - 1) / kTileRows);
+    p.parts = (int)std::max<int64_t>(1, std::min((512 + blocks - 1) / std::max<int64_t>(blocks, 1), p.tiles / 8));
     int64_t at = 0;
     p.rows = take(&at, a.batch * a.kv_heads * p.tiles * 192 * 4);
     p.bounds = take(&at, a.batch * p.tiles * 16);
     p.zeros = take(&at, 512);
+    if (p.parts > 1) p.o = take(&at, p.parts * a.batch * a.kv_heads * a.keys * (grad ? 2 * a.d : 1) * 4);
     p.bytes = at;
     return p;
 }
@@ -130,7 +137,7 @@ int launch_attend(const frog_attend_t& a, void* ws, hipStream_t stream) {
     return launched("attention launch");
 }
 
-int64_t attend_bwd_ws(const frog_attend_t& a) { return empty(a) ? 0 : pack_plan(a).bytes; }
+int64_t attend_bwd_ws(const frog_attend_t& a) { return empty(a) ? 0 : pack_plan(a, true).bytes; }
 
 int launch_attend_bwd(const frog_attend_t& a, void* ws, hipStream_t stream) {
     const int size = a.type == FROG_STORAGE_F32 ? 4 : 2;
@@ -141,7 +148,8 @@ int launch_attend_bwd(const frog_attend_t& a, void* ws, hipStream_t stream) {
         return launched("attention gradient launch");
     }
     const int64_t pairs = a.batch * a.kv_heads;
-    int rc = check_grid(pairs * std::max(a.keys / kTileRows + 1, pack_plan(a).tiles));
+    const PackPlan p = pack_plan(a, true);
+    int rc = check_grid(pairs * std::max({(a.keys / kTileRows + 1) * p.parts, p.tiles, p.parts > 1 ? a.keys * a.d / 512 + 1 : 0}));
     if (rc != FROG_OK) return rc;
     by_type(a.type, [&](auto l) { l.backward(a, (char*)ws, stream); });
     return launched("attention gradient launch");

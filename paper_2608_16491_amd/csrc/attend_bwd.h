@@ -65,30 +65,51 @@ __global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, Row
     }
 }
 
-// The tiles of 32 query rows that see one of the keys first..last, in order;
-// 64 bounds are looked at together.  Every wavefront of a workgroup finds the
-// same ones.
+// The tiles of 32 query rows that see one of the keys first..last, in order,
+// every parts-th from the part-th on; 64 bounds are looked at together, and
+// the next 64 are on their way.  Every wavefront of a workgroup finds the same
+// ones.
 struct TileWalk {
     const int4* bounds;
-    int tiles, first, last, base = -64, lane;
+    int tiles, first, last, base = -64, lane, parts, skip;
+    int4 now, coming;
     uint64_t left = 0;
-    __device__ inline TileWalk(const int4* b, int n, int first_, int last_, int lane_) : bounds(b), tiles(n), first(first_), last(last_), lane(lane_) {}
-    // the next tile, -1 after the last
-    __device__ inline int next() {
-        while (!left) {
-            base += 64;
-            if (base >= tiles) return -1;
-            bool in = false;
-            if (base + lane < tiles) {
-                const int4 x = bounds[base + lane];
-                in = x.x <= last && x.y >= first;
-            }
-            left = __ballot(in);
-        }
-        const int t = base + __builtin_ctzll(left);
-        left &= left - 1;
-        return t;
+    __device__ inline TileWalk(const int4* b, int n, int first_, int last_, int part, int parts_, int lane_)
+        : bounds(b), tiles(n), first(first_), last(last_), lane(lane_), parts(parts_), skip(part) {
+        coming = bounds[min(lane, tiles - 1)];
     }
+    // the next tile and its bounds, -1 after the last
+    __device__ inline int next(int4* bd) {
+        for (;;) {
+            while (!left) {
+                base += 64;
+                if (base >= tiles) return -1;
+                now = coming;
+                if (base + 64 < tiles) coming = bounds[min(base + 64 + lane, tiles - 1)];
+                left = __ballot(base + lane < tiles && now.x <= last && now.y >= first);
+            }
+            const int t = __builtin_ctzll(left);
+            left &= left - 1;
+            if (skip) {
+                --skip;
+                continue;
+            }
+            skip = parts - 1;
+            *bd = make_int4(__builtin_amdgcn_readlane(now.x, t), __builtin_amdgcn_readlane(now.y, t), __builtin_amdgcn_readlane(now.z, t),
+                            __builtin_amdgcn_readlane(now.w, t));
+            return base + t;
+        }
+    }
+};
+
+// Sums of a pass that owns keys, cut into parts of the query rows (o null: one
+// part, which writes its results itself): part s of key i of all sequences' kv
+// heads, D floats for dk at o[(s * total + i) * D], for dv `total * parts * D`
+// further on; key weights: one float.
+struct KeyParts {
+    float* o;
+    int64_t total;
+    int parts;
 };
 
 // 4 r (1 - r), r = 1 / (1 + exp2(c1 dot)): the derivative of the cap; *z2 the
@@ -107,7 +128,7 @@ __device__ inline float cap_slope(const ScoreParams& sp, float dot, float* z2) {
 //   GRAD: dk = sum dx q, dv = sum p dout.  Else: w_out = w_in + sum p.
 template <typename T, int D, bool PLAIN, bool GRAD, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(1)))
-void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack) {
+void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack, KeyParts parts) {
     constexpr int K = D / 16, M = D / 32;
     using L = Tile<T, D>;
     __shared__ __attribute__((aligned(16))) T q0[32 * D], q1[32 * D];
@@ -115,7 +136,7 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
     __shared__ __attribute__((aligned(16))) float p0[RowPack::kFloats], p1[RowPack::kFloats];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs;
-    const int tile = (int)(blockIdx.x / pairs);
+    const int tile = (int)(blockIdx.x / pairs % (uint32_t)key_tiles), part = (int)(blockIdx.x / pairs / (uint32_t)key_tiles);
     const int64_t b = x / (uint32_t)a.kv_heads;
     const int hk = (int)(x % (uint32_t)a.kv_heads), rows = (int)(a.queries * group);
     const int first = tile * 32 * W, last = (int)min((int64_t)first + 32 * W, a.keys) - 1;
@@ -139,9 +160,8 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
 #pragma unroll
         for (int m = 0; m < M; ++m) dk[m] = dv[m] = acc16{};
     }
-    const int4* bounds = pack.bounds + b * pack.tiles;
     const float* blocks = pack.rows + (int64_t)x * pack.tiles * RowPack::kFloats;
-    TileWalk walk(bounds, pack.tiles, first, last, lane);
+    TileWalk walk(pack.bounds + b * pack.tiles, pack.tiles, first, last, part, parts.parts, lane);
 
     // returns whether every row of the tile sees some key (else rows of zeros
     // stand in)
@@ -171,99 +191,116 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
 #pragma unroll
             for (int s = 0; s < K; ++s) dp = mma(L::rows(gs, 0, s, lane), vf[s], dp);
         }
-        acc16 p, dx;
-        const bool whole = bd.z <= wfirst && bd.w >= wlast;
+        acc16 f;
+        if constexpr (!PLAIN) {
+            if (sp.cap2 > 0.f) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int at = 8 * i + 4 * h;
-            const vec<float, 4> lse = *(const vec<float, 4>*)(ps + RowPack::kLse + at);
-            vec<float, 4> sl = {}, aq = {};
-            if (!PLAIN && a.slopes) {
-                sl = *(const vec<float, 4>*)(ps + RowPack::kSlope + at);
-                aq = *(const vec<float, 4>*)(ps + RowPack::kAt + at);
-            }
-            vec<float, 4> f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float y;
-                if constexpr (PLAIN) {
-                    y = fmaf(z[4 * i + e], sp.mul, -lse[e]);
-                } else {
-                    f[e] = 1.f;
-                    if (sp.cap2 > 0.f) f[e] = cap_slope(sp, z[4 * i + e], &y);
-                    else y = z[4 * i + e] * sp.mul;
-                    if (a.slopes) y -= sl[e] * fabsf(aq[e] - ak);
-                    y -= lse[e];
+                for (int r = 0; r < 16; ++r) {
+                    float y;
+                    f[r] = cap_slope(sp, z[r], &y);
+                    z[r] = y;
                 }
-                p[4 * i + e] = exp2_fast(y);
-            }
-            if constexpr (GRAD) {
-                const vec<float, 4> delta = *(const vec<float, 4>*)(ps + RowPack::kDelta + at);
+            } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    dx[4 * i + e] = p[4 * i + e] * (dp[4 * i + e] - delta[e]);
-                    if constexpr (!PLAIN) dx[4 * i + e] *= f[e];
+                for (int r = 0; r < 16; ++r) {
+                    f[r] = 1.f;
+                    z[r] *= sp.mul;
+                }
+            }
+            if (a.slopes) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const vec<float, 4> sl = *(const vec<float, 4>*)(ps + RowPack::kSlope + 8 * i + 4 * h);
+                    const vec<float, 4> aq = *(const vec<float, 4>*)(ps + RowPack::kAt + 8 * i + 4 * h);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) z[4 * i + e] -= sl[e] * fabsf(aq[e] - ak);
                 }
             }
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const vec<float, 4> lse = *(const vec<float, 4>*)(ps + RowPack::kLse + 8 * i + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[4 * i + e] = exp2_fast(PLAIN ? fmaf(z[4 * i + e], sp.mul, -lse[e]) : z[4 * i + e] - lse[e]);
+        }
+        const bool whole = bd.z <= wfirst && bd.w >= wlast;
         if (!whole) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int at = 8 * i + 4 * h;
-                const vec<float, 4> lo = *(const vec<float, 4>*)(ps + RowPack::kLo + at), hi = *(const vec<float, 4>*)(ps + RowPack::kHi + at);
+                const vec<float, 4> lo = *(const vec<float, 4>*)(ps + RowPack::kLo + 8 * i + 4 * h);
+                const vec<float, 4> hi = *(const vec<float, 4>*)(ps + RowPack::kHi + 8 * i + 4 * h);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool in = j >= __float_as_int(lo[e]) && j <= __float_as_int(hi[e]);
-                    p[4 * i + e] = in ? p[4 * i + e] : 0.f;
-                    if constexpr (GRAD) dx[4 * i + e] = in ? dx[4 * i + e] : 0.f;
-                }
+                for (int e = 0; e < 4; ++e) z[4 * i + e] = j >= __float_as_int(lo[e]) && j <= __float_as_int(hi[e]) ? z[4 * i + e] : 0.f;
             }
         }
         if constexpr (GRAD) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const frag<T> pf = to_frag<T>(p, t), xf = to_frag<T>(dx, t);
+                const frag<T> pf = to_frag<T>(z, t);
 #pragma unroll
-                for (int m = 0; m < M; ++m) {
-                    dv[m] = mma(L::cols(gs, 16 * t, m, lane), pf, dv[m]);
-                    dk[m] = mma(L::cols(qs, 16 * t, m, lane), xf, dk[m]);
+                for (int m = 0; m < M; ++m) dv[m] = mma(L::cols(gs, 16 * t, m, lane), pf, dv[m]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const vec<float, 4> delta = *(const vec<float, 4>*)(ps + RowPack::kDelta + 8 * i + 4 * h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    dp[4 * i + e] -= delta[e];
+                    if constexpr (!PLAIN) dp[4 * i + e] *= f[4 * i + e];
                 }
+            }
+            // (a key without a query may hold anything: 0 times it is not 0)
+            if (!whole) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dp[r] = z[r] == 0.f ? 0.f : dp[r];
+            }
+            z *= dp;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const frag<T> xf = to_frag<T>(z, t);
+#pragma unroll
+                for (int m = 0; m < M; ++m) dk[m] = mma(L::cols(qs, 16 * t, m, lane), xf, dk[m]);
             }
         } else {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) sum += p[r];
+            for (int r = 0; r < 16; ++r) sum += z[r];
         }
     };
     auto ready = [&] {
         __builtin_amdgcn_s_waitcnt(0x0f70);
         __syncthreads();
     };
-    int t = walk.next();
+    int4 bd, bn;
+    int t = walk.next(&bd);
     if (t >= 0) {
-        int4 bd = bounds[t];
         fetch(q0, g0, p0, t, bd);
         for (;;) {
             ready();
-            t = walk.next();
-            int4 bn = bd;
-            if (t >= 0) {
-                bn = bounds[t];
-                fetch(q1, g1, p1, t, bn);
-            }
+            t = walk.next(&bn);
+            if (t >= 0) fetch(q1, g1, p1, t, bn);
             step(q0, g0, p0, bd);
             if (t < 0) break;
             ready();
-            t = walk.next();
-            if (t >= 0) {
-                bd = bounds[t];
-                fetch(q0, g0, p0, t, bd);
-            }
+            t = walk.next(&bd);
+            if (t >= 0) fetch(q0, g0, p0, t, bd);
             step(q1, g1, p1, bn);
             if (t < 0) break;
         }
     }
     if constexpr (GRAD) {
         if (j > last) return;
+        if (parts.o) {
+            float* po = parts.o + (part * parts.total + (int64_t)x * a.keys + j) * D + 4 * h;
+            const int64_t to_dv = parts.total * parts.parts * D;
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    *(vec<float, 4>*)(po + 32 * m + 8 * i) = vec<float, 4>{dk[m][4 * i], dk[m][4 * i + 1], dk[m][4 * i + 2], dk[m][4 * i + 3]};
+                    *(vec<float, 4>*)(po + to_dv + 32 * m + 8 * i) = vec<float, 4>{dv[m][4 * i], dv[m][4 * i + 1], dv[m][4 * i + 2], dv[m][4 * i + 3]};
+                }
+            return;
+        }
         T* pk = (T*)a.dk + b * a.dk_stride[0] + hk * a.dk_stride[2] + j * a.dk_stride[1];
         T* pv = (T*)a.dv + b * a.dv_stride[0] + hk * a.dv_stride[2] + j * a.dv_stride[1];
 #pragma unroll
@@ -283,8 +320,41 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
         sum = half_sum(sum);
         if (j > last || lane >= 32) return;
         const int64_t at = (int64_t)x * a.keys + j;
-        a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum;
+        if (parts.o) parts.o[part * parts.total + at] = sum;
+        else a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum;
     }
+}
+
+// The parts of dk and dv summed, four values a thread.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void keys_join(frog_attend_t a, ScoreParams sp, KeyParts parts) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, each = parts.total * (D / 4);
+    if (i >= 2 * each) return;
+    const bool second = i >= each;
+    const int64_t at = second ? i - each : i;
+    const float* p = parts.o + (second ? parts.total * parts.parts * D : 0) + at * 4;
+    vec<float, 4> y{};
+#pragma unroll 4
+    for (int s = 0; s < parts.parts; ++s) y += *(const vec<float, 4>*)(p + s * parts.total * D);
+    const int64_t key = at / (D / 4), j = key % a.keys, x = key / a.keys, b = x / a.kv_heads, hk = x % a.kv_heads;
+    const int d = (int)(at % (D / 4)) * 4;
+    if (!second) y *= sp.scale;
+    vec<T, 4> t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = (T)y[e];
+    T* out = second ? (T*)a.dv + b * a.dv_stride[0] + j * a.dv_stride[1] + hk * a.dv_stride[2]
+                    : (T*)a.dk + b * a.dk_stride[0] + j * a.dk_stride[1] + hk * a.dk_stride[2];
+    *(vec<T, 4>*)(out + d) = t;
+}
+
+// The parts of the key weights.
+static __global__ __launch_bounds__(256) void weights_join(frog_attend_t a, KeyParts parts) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= parts.total) return;
+    float y = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < parts.parts; ++s) y += parts.o[s * parts.total + i];
+    a.w_out[i] = (a.w_in ? a.w_in[i] : 0.f) + y;
 }
 
 // dq: one workgroup of W wavefronts, 32 query rows each (a lane owns a query),

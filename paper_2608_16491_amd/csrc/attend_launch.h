@@ -35,10 +35,12 @@ struct SharedPlan {
 SharedPlan shared_plan(const frog_attend_shared_t& a);
 
 // What pack_rows prepares: offsets from the start of the region
+// and how the passes that own keys are cut
 struct PackPlan {
-    int64_t tiles, rows, bounds, zeros, bytes;
+    int64_t tiles, rows, bounds, zeros, o, bytes;
+    int parts;                // of the query rows; 1: no partial sums at o
 };
-PackPlan pack_plan(const frog_attend_t& a);
+PackPlan pack_plan(const frog_attend_t& a, bool grad);
 
 template <typename T>
 struct AttendLaunch {

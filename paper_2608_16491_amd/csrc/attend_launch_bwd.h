@@ -7,37 +7,43 @@
 namespace frog {
 
 template <typename T, int D, bool GRAD>
-RowPack launch_pack(const frog_attend_t& a, const float* lse, char* pack, hipStream_t s) {
-    const PackPlan p = pack_plan(a);
+RowPack launch_pack(const frog_attend_t& a, const PackPlan& p, const float* lse, char* pack, hipStream_t s) {
     const RowPack r{(float*)(pack + p.rows), (int4*)(pack + p.bounds), pack + p.zeros, (int)p.tiles};
     const int64_t waves = a.batch * a.kv_heads * p.tiles;
     pack_rows<T, D, GRAD><<<dim3((unsigned)((waves + 3) / 4)), 256, 0, s>>>(a, a.heads / a.kv_heads, r, lse);
     return r;
 }
 
+template <typename T, int D, bool GRAD>
+void launch_keys(const frog_attend_t& a, const ScoreParams& sp, const PackPlan& p, const RowPack& r, char* pack, hipStream_t s) {
+    const int group = a.heads / a.kv_heads, tiles = (int)((a.keys + kTileRows - 1) / kTileRows);
+    const KeyParts parts{p.parts > 1 ? (float*)(pack + p.o) : nullptr, a.batch * a.kv_heads * a.keys, p.parts};
+    const dim3 grid((unsigned)(a.batch * a.kv_heads * tiles * p.parts));
+    if (a.cap > 0.f || a.slopes) attend_keys<T, D, false, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts);
+    else attend_keys<T, D, true, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts);
+    if (p.parts == 1) return;
+    if constexpr (GRAD) keys_join<T, D><<<dim3((unsigned)((parts.total * (D / 2) + 255) / 256)), 256, 0, s>>>(a, sp, parts);
+    else weights_join<<<dim3((unsigned)((parts.total + 255) / 256)), 256, 0, s>>>(a, parts);
+}
+
 template <typename T, int D>
 void launch_weigh(const frog_attend_t& a, const float* lse, char* pack, hipStream_t s) {
-    const RowPack r = launch_pack<T, D, false>(a, lse, pack, s);
-    const ScoreParams sp = score_params(a.scale, a.cap);
-    const int tiles = (int)((a.keys + kTileRows - 1) / kTileRows);
-    attend_keys<T, D, false, false, 4><<<dim3((unsigned)(a.batch * a.kv_heads * tiles)), 256, 0, s>>>(a, sp, a.heads / a.kv_heads, tiles, r);
+    const PackPlan p = pack_plan(a, false);
+    const RowPack r = launch_pack<T, D, false>(a, p, lse, pack, s);
+    launch_keys<T, D, false>(a, score_params(a.scale, a.cap), p, r, pack, s);
 }
 
 template <typename T, int D>
 void launch_backward(const frog_attend_t& a, char* pack, hipStream_t s) {
-    const RowPack r = launch_pack<T, D, true>(a, a.lse, pack, s);
+    const PackPlan p = pack_plan(a, true);
+    const RowPack r = launch_pack<T, D, true>(a, p, a.lse, pack, s);
     const ScoreParams sp = score_params(a.scale, a.cap);
     const int group = a.heads / a.kv_heads;
-    const int64_t rows = a.queries * group, pairs = a.batch * a.kv_heads;
-    const int kt = (int)((a.keys + kTileRows - 1) / kTileRows), qt = (int)((rows + kTileRows - 1) / kTileRows);
-    const dim3 kg((unsigned)(pairs * kt)), qg((unsigned)(pairs * qt));
-    if (a.cap > 0.f || a.slopes) {
-        if (kt) attend_keys<T, D, false, true, 4><<<kg, 256, 0, s>>>(a, sp, group, kt, r);
-        attend_dq<T, D, false, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r);
-    } else {
-        if (kt) attend_keys<T, D, true, true, 4><<<kg, 256, 0, s>>>(a, sp, group, kt, r);
-        attend_dq<T, D, true, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r);
-    }
+    const int qt = (int)((a.queries * group + kTileRows - 1) / kTileRows);
+    const dim3 qg((unsigned)(a.batch * a.kv_heads * qt));
+    launch_keys<T, D, true>(a, sp, p, r, pack, s);
+    if (a.cap > 0.f || a.slopes) attend_dq<T, D, false, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r);
+    else attend_dq<T, D, true, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r);
 }
 
 template <typename T>
