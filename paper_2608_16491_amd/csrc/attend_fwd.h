@@ -107,7 +107,7 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(akp + min(j + lane, last)),
                                              (__attribute__((address_space(3))) void*)as, 4, 0, 0);
     };
-    auto step = [&](const T* ks, const T* vs, const float* as, int j) {
+    auto step = [&](const T* ks, const T* vs, const float* as, int j) __attribute__((always_inline)) {
         if (j > whi || j + N <= wlo) return;
         acc16 z[S];
 #pragma unroll
@@ -341,7 +341,7 @@ struct FewPass {
         load_keys((int)j64);
         load_values((int)j64);
         real = coming;
-        auto step = [&](auto masked, int j, bool more, int next) {
+        auto step = [&](auto masked, int j, bool more, int next) __attribute__((always_inline)) {
             constexpr bool MASKED = decltype(masked)::value;
             if (more) mine = keys.where((int)min((int64_t)next + (lane & 31), (int64_t)last));
             float z[RG][8];

@@ -73,15 +73,23 @@ __device__ inline int col_max(int x) {
 }
 
 // A tile of rows of D values in LDS, packed, the 16-byte pieces of a row
-// permuted by an XOR with bits of the row's number so that 16 rows read at the
-// same piece (row fragments) spread over all banks.
+// permuted by an XOR with bits of the row's number so that the reads spread
+// over all banks.
 template <typename T, int D>
 struct Tile {
     static constexpr int kPer = 16 / sizeof(T);   // values of a piece
     static constexpr int kPieces = D / kPer;      // pieces of a row: 4, 8, 12, 16, 24 or 32
 
+    // Bits of the row's number for the XOR: 16 rows at one piece (row
+    // fragments) and four rows at the four pieces of 64 bytes (the two reads
+    // of 32 lanes of a transposed fragment) each cover 256 bytes of banks; of
+    // 4-byte values rows r and r + 4 at eight pieces.  (With row % 16 alone a
+    // transposed read of d = 128, bf16, took 10 cycles instead of 4, 60 % of
+    // the cycles LDS was busy.)
     __device__ static inline int turn(int row) {
-        if constexpr (kPieces % 16 == 0) return row & 15;
+        if constexpr (kPieces % 16 == 0 && sizeof(T) == 4) return (row & 3) | ((row >> 1) & 4) | ((row << 1) & 8);
+        else if constexpr (kPieces == 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+        else if constexpr (kPieces % 8 == 0 && sizeof(T) == 2) return ((row << 1) & 4) | ((row >> 2) & 3);
         else if constexpr (kPieces % 8 == 0) return (row >> 1) & 7;
         else return (row >> 2) & 3;
     }
@@ -249,6 +257,33 @@ struct QueryRow {
     __device__ inline QueryRow(int64_t row, int group, int kv_head) {
         token = (uint32_t)row / (uint32_t)group;
         head = kv_head * group + (int)((uint32_t)row % (uint32_t)group);
+    }
+};
+
+// Addresses of the query rows of a tile: the first row's token once for all
+// lanes, the others' from it by a product with 1 / group (exact: the half keeps
+// the quotient of numbers below 2^17 away from a whole one), and 32-bit
+// distances between tokens (kMaxTokenStride).
+struct RowTile {
+    int first;        // head of the first row within its group
+    const char* base; // its token, the group's first head
+    uint32_t token_bytes;
+    int64_t head_bytes;
+    int group;
+    float inv;
+    __device__ inline RowTile(const void* p, int64_t sequence, const int64_t (&stride)[3], int size, int row0, int group_, int kv_head) {
+        const uint32_t token = (uint32_t)row0 / (uint32_t)group_;
+        first = row0 - (int)token * group_;
+        group = group_;
+        inv = 1.f / (float)group_;
+        base = (const char*)p + (sequence * stride[0] + token * stride[1] + (int64_t)kv_head * group_ * stride[2]) * size;
+        token_bytes = (uint32_t)stride[1] * size;
+        head_bytes = stride[2] * size;
+    }
+    // row i of the tile
+    __device__ inline const char* row(int i) const {
+        const int r = first + i, t = (int)(((float)r + 0.5f) * inv);
+        return base + (uint32_t)t * token_bytes + (uint32_t)(r - t * group) * head_bytes;
     }
 };
 
