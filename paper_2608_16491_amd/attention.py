@@ -121,7 +121,7 @@ _NO_GRADS = _NONE4 * 4
 class _Call:
     """The checked arguments of one attention call, apart from its outputs."""
 
-    __slots__ = ("device", "shape", "extra", "rows", "masks", "tail")
+    __slots__ = ("device", "shape", "extra", "rows", "masks", "tail", "lse")
 
     def __init__(self, q, k, v, lr, scale, cap, slopes, at_q, at_k):
         kind = _values(("q", "k", "v"), (q, k, v), (4, 4, 4))
@@ -175,15 +175,14 @@ class _Call:
 class _Attend(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, call, w_in, w_out, stream):
-        out, lse = call.forward(q, k, v, True, w_in, w_out, stream)
+        out, call.lse = call.forward(q, k, v, True, w_in, w_out, stream)
         ctx.call = call
-        ctx.save_for_backward(q, k, v, out, lse, *(t for t in call.extra if t is not None))
-        ctx.mark_non_differentiable(lse)
-        return out, lse
+        ctx.save_for_backward(q, k, v, out, call.lse, *(t for t in call.extra if t is not None))
+        return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
-    def backward(ctx, dout, _):
+    def backward(ctx, dout):
         q, k, v, out, lse = ctx.saved_tensors[:5]
         size = 16 // dout.element_size()
         if dout.stride(-1) != 1 or dout.data_ptr() % 16 or any(s % size for s in dout.stride()[:-1]):
@@ -221,7 +220,8 @@ def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_
     else:
         _need(weights_out is None, "weights_out needs weights")
     if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
-        out, lse = _Attend.apply(q, k, v, call, weights, weights_out, stream)
+        out = _Attend.apply(q, k, v, call, weights, weights_out, stream)
+        lse = call.lse
     else:
         out, lse = call.forward(q, k, v, return_lse, weights, weights_out, stream)
     if not return_lse and weights is None:

@@ -45,6 +45,27 @@ inline ScoreParams score_params(float scale, float cap) {
     return s;
 }
 
+// What a kernel is built for: no cap and no bias (the scale is then part of the
+// exponent's multiply-add), one of them, or whatever the arguments say.  A
+// test of the arguments between two products keeps the one's arithmetic from
+// running beside the other: with it the forward pass of a long biased prompt
+// took 1.37 ms instead of 1.28.
+enum Scores { kPlain, kCapped, kBiased, kAny };
+
+inline Scores scores_of(bool cap, bool bias, bool positive) {
+    if (cap) return bias ? kAny : kCapped;
+    return bias ? kBiased : positive ? kPlain : kAny;
+}
+
+template <Scores S>
+__device__ inline bool capped(const ScoreParams& s) {
+    return S == kCapped || (S == kAny && s.cap2 > 0.f);
+}
+template <Scores S>
+__device__ inline bool biased(const void* slopes) {
+    return S == kBiased || (S == kAny && slopes);
+}
+
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
 
@@ -52,7 +73,7 @@ __device__ inline float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
 template <bool CAP>
 __device__ inline float score2(const ScoreParams& s, float dot) {
     if constexpr (!CAP) return dot * s.mul;
-    return s.cap2 - 2.f * s.cap2 * rcp_fast(1.f + exp2_fast(dot * s.mul));
+    return fmaf(-2.f * s.cap2, rcp_fast(1.f + exp2_fast(dot * s.mul)), s.cap2);
 }
 
 // launchers (attend.hip, evict.hip).  The

@@ -38,18 +38,28 @@ __global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, Row
     float* out = pack.rows + at * RowPack::kFloats;
     const int64_t stat = (b * a.heads + q.head) * a.queries + q.token;
     if constexpr (GRAD) {
-        // half a row a lane
-        const T* g = (const T*)a.dout + b * a.dout_stride[0] + q.token * a.dout_stride[1] + q.head * a.dout_stride[2] + h * (D / 2);
-        const T* o = (const T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2] + h * (D / 2);
-        float delta = 0.f;
+        // a piece of 16 bytes a lane, LANES lanes a row (a power of two; D = 96
+        // leaves some without one), as many rows at once as fit
+        constexpr int PER = 16 / sizeof(T), PIECES = D / PER, LANES = PIECES <= 4 ? 4 : PIECES <= 8 ? 8 : PIECES <= 16 ? 16 : 32, AT = 64 / LANES;
+        const int piece = lane % LANES;
 #pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            const frag<T> u = load_frag(g + 8 * s), v = load_frag(o + 8 * s);
+        for (int r0 = 0; r0 < 32; r0 += AT) {
+            const int r = r0 + lane / LANES;
+            const QueryRow qr(min((int64_t)tile * 32 + r, rows - 1), group, hk);
+            float delta = 0.f;
+            if (piece < PIECES) {
+                const vec<T, PER> u = *(const vec<T, PER>*)((const T*)a.dout + b * a.dout_stride[0] + qr.token * a.dout_stride[1] +
+                                                            qr.head * a.dout_stride[2] + piece * PER);
+                const vec<T, PER> v = *(const vec<T, PER>*)((const T*)a.out + b * a.out_stride[0] + qr.token * a.out_stride[1] +
+                                                            qr.head * a.out_stride[2] + piece * PER);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) delta = fmaf((float)u[e], (float)v[e], delta);
+                for (int e = 0; e < PER; ++e) delta = fmaf((float)u[e], (float)v[e], delta);
+            }
+#pragma unroll
+            for (int o = LANES / 2; o; o >>= 1) delta += __shfl_xor(delta, o);
+            const int seen = __shfl(some, r);   // row r's lane
+            if (piece == 0) out[RowPack::kDelta + r] = seen ? delta : 0.f;
         }
-        delta = half_sum(delta);
-        if (h == 0) out[RowPack::kDelta + i] = some ? delta : 0.f;
     }
     if (h == 0) {
         out[RowPack::kLse + i] = some ? lse[stat] * kLog2e : INFINITY;
@@ -116,8 +126,9 @@ struct KeyParts {
 // capped score
 __device__ inline float cap_slope(const ScoreParams& sp, float dot, float* z2) {
     const float r = rcp_fast(1.f + exp2_fast(dot * sp.mul));
-    *z2 = sp.cap2 - 2.f * sp.cap2 * r;
-    return 4.f * r * (1.f - r);
+    const float r4 = 4.f * r;
+    *z2 = fmaf(-2.f * sp.cap2, r, sp.cap2);
+    return fmaf(-r4, r, r4);
 }
 
 // One workgroup of W wavefronts, 32 keys each (a lane owns a key), over the
@@ -126,9 +137,10 @@ __device__ inline float cap_slope(const ScoreParams& sp, float dot, float* z2) {
 // Query and dout rows are double buffered in LDS, keys and values stay in
 // registers.
 //   GRAD: dk = sum dx q, dv = sum p dout.  Else: w_out = w_in + sum p.
-template <typename T, int D, bool PLAIN, bool GRAD, int W>
+template <typename T, int D, Scores KIND, bool GRAD, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(1)))
 void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack, KeyParts parts) {
+    constexpr bool PLAIN = KIND == kPlain;
     constexpr int K = D / 16, M = D / 32;
     using L = Tile<T, D>;
     __shared__ __attribute__((aligned(16))) T q0[32 * D], q1[32 * D];
@@ -153,7 +165,7 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
             for (int s = 0; s < K; ++s) vf[s] = load_frag(p + 16 * s);
         }
     }
-    const float ak = !PLAIN && a.slopes ? a.at_k[b * a.at_k_stride[0] + hk * a.at_k_stride[1] + jc] : 0.f;
+    const float ak = biased<KIND>(a.slopes) ? a.at_k[b * a.at_k_stride[0] + hk * a.at_k_stride[1] + jc] : 0.f;
     acc16 dk[GRAD ? M : 1], dv[GRAD ? M : 1];
     float sum = 0.f;
     if constexpr (GRAD) {
@@ -193,7 +205,7 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
         }
         acc16 f;
         if constexpr (!PLAIN) {
-            if (sp.cap2 > 0.f) {
+            if (capped<KIND>(sp)) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     float y;
@@ -203,17 +215,17 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
             } else {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    f[r] = 1.f;
+                    if (KIND == kAny) f[r] = 1.f;
                     z[r] *= sp.mul;
                 }
             }
-            if (a.slopes) {
+            if (biased<KIND>(a.slopes)) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const vec<float, 4> sl = *(const vec<float, 4>*)(ps + RowPack::kSlope + 8 * i + 4 * h);
                     const vec<float, 4> aq = *(const vec<float, 4>*)(ps + RowPack::kAt + 8 * i + 4 * h);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) z[4 * i + e] -= sl[e] * fabsf(aq[e] - ak);
+                    for (int e = 0; e < 4; ++e) z[4 * i + e] = fmaf(-sl[e], fabsf(aq[e] - ak), z[4 * i + e]);
                 }
             }
         }
@@ -246,7 +258,7 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     dp[4 * i + e] -= delta[e];
-                    if constexpr (!PLAIN) dp[4 * i + e] *= f[4 * i + e];
+                    if constexpr (KIND == kCapped || KIND == kAny) dp[4 * i + e] *= f[4 * i + e];
                 }
             }
             // (a key without a query may hold anything: 0 times it is not 0)
@@ -359,14 +371,15 @@ static __global__ __launch_bounds__(256) void weights_join(frog_attend_t a, KeyP
 
 // dq: one workgroup of W wavefronts, 32 query rows each (a lane owns a query),
 // over the keys of their intervals in tiles of N, double buffered.
-template <typename T, int D, bool PLAIN, int W>
+template <typename T, int D, Scores KIND, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
 void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pack) {
+    constexpr bool PLAIN = KIND == kPlain;
     constexpr int N = sizeof(T) == 2 ? 64 : 32, S = N / 32, K = D / 16, M = D / 32;
     // (buffers by name: the compiler then knows that reads of one need not wait
     // for the direct loads into the other)
     __shared__ __attribute__((aligned(16))) T k0[N * D], k1[N * D], v0[N * D], v1[N * D];
-    __shared__ float a0[64], a1[64];
+    __shared__ __attribute__((aligned(16))) float a0[64], a1[64];
     __shared__ int ends[4 * W];
     __shared__ Gaps<32 * W> rows_of;
     using L = Tile<T, D>;
@@ -409,7 +422,7 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
     const T* vp = (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2];
     const float* akp = nullptr;
     float slope = 0.f, aq = 0.f;
-    if (!PLAIN && a.slopes) {
+    if (biased<KIND>(a.slopes)) {
         akp = a.at_k + b * a.at_k_stride[0] + hk * a.at_k_stride[1];
         slope = a.slopes[q.head] * kLog2e;
         aq = a.at_q[b * a.at_q_stride + q.token];
@@ -434,7 +447,7 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
     auto fetch = [&](T* ks, T* vs, float* as, int j) {
         L::template load<N, W>(ks, kp, a.k_stride[1], j, last, w, lane);
         L::template load<N, W>(vs, vp, a.v_stride[1], j, last, w, lane);
-        if (!PLAIN && akp && w == 0)
+        if (biased<KIND>(akp) && w == 0)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(akp + min(j + lane, last)),
                                              (__attribute__((address_space(3))) void*)as, 4, 0, 0);
     };
@@ -448,25 +461,36 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
 #pragma unroll
             for (int s = 0; s < K; ++s) z[0] = mma(L::rows(ks, 32 * n, s, lane), qf[s], z[0]);
             // p (times the cap's slope), before the other product needs registers
-            if (j < flo || j + 31 > fhi) mask_scores<1>(z, lo - j, hi - j, lane);
+            acc16 f{};
+            if constexpr (!PLAIN) {
+                if (capped<KIND>(sp)) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                if constexpr (PLAIN) {
-                    z[0][r] = exp2_fast(fmaf(z[0][r], sp.mul, -lse));
+                    for (int r = 0; r < 16; ++r) {
+                        float y;
+                        f[r] = cap_slope(sp, z[0][r], &y);
+                        z[0][r] = y;
+                    }
                 } else {
-                    float y, f = 1.f;
-                    if (sp.cap2 > 0.f) f = cap_slope(sp, z[0][r], &y);
-                    else y = z[0][r] * sp.mul;
-                    if (akp) y -= slope * fabsf(aq - as[32 * n + acc_row(r, lane)]);
-                    z[0][r] = exp2_fast(z[0][r] > -INFINITY ? y - lse : -INFINITY) * f;
+                    z[0] *= sp.mul;
+                }
+                if (biased<KIND>(akp)) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const vec<float, 4> ak = *(const vec<float, 4>*)(as + 32 * n + 8 * i + 4 * (lane >> 5));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z[0][4 * i + e] = fmaf(-slope, fabsf(aq - ak[e]), z[0][4 * i + e]);
+                    }
                 }
             }
-            acc16 dp = acc16{};
+            // (all rows here are finite: what no interval meets was cleared)
+            if (j < flo || j + 31 > fhi) mask_scores<1>(z, lo - j, hi - j, lane);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) z[0][r] = exp2_fast(PLAIN ? fmaf(z[0][r], sp.mul, -lse) : z[0][r] - lse);
+            if (capped<KIND>(sp)) z[0] *= f;
+            acc16 dp = acc16{} - delta;
 #pragma unroll
             for (int s = 0; s < K; ++s) dp = mma(L::rows(vs, 32 * n, s, lane), gf[s], dp);
-            // (a masked key's value row may hold anything: 0 times it is not 0)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) dp[r] = z[0][r] == 0.f ? 0.f : z[0][r] * (dp[r] - delta);
+            dp *= z[0];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const frag<T> xf = to_frag<T>(dp, t);
@@ -484,6 +508,7 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
         if (j + N <= last) fetch(kn, vn, an, j + N);
         if (gaps) {
             rows_of.template clear<N, D, W>(ks, j, w, lane);
+            rows_of.template clear<N, D, W>(vs, j, w, lane);
             __syncthreads();
         }
         step(ks, vs, as, j);

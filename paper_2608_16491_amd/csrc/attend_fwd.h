@@ -22,16 +22,15 @@ constexpr float kLow = -FLT_MAX;   // running maximum of a row that has seen no 
 // intervals in tiles of N: scores transposed (keys x queries) so that a lane
 // owns a query, one pass with the running maximum and sum, keys and values
 // double buffered in LDS by direct loads.
-//   PLAIN: neither cap nor bias and a positive scale; the scale is then part
-//   of the exponent's multiply-add.
-template <typename T, int D, bool PLAIN, int W>
+template <typename T, int D, Scores KIND, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
 void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts parts) {
+    constexpr bool PLAIN = KIND == kPlain;
     constexpr int N = sizeof(T) == 2 ? 64 : 32, S = N / 32, K = D / 16, M = D / 32;
     // (buffers by name: the compiler then knows that reads of one need not wait
     // for the direct loads into the other)
     __shared__ __attribute__((aligned(16))) T k0[N * D], k1[N * D], v0[N * D], v1[N * D];
-    __shared__ float a0[64], a1[64];
+    __shared__ __attribute__((aligned(16))) float a0[64], a1[64];
     __shared__ int ends[4 * W];
     __shared__ Gaps<32 * W> rows_of;
     using L = Tile<T, D>;
@@ -84,7 +83,7 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
     const T* vp = (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2];
     const float* akp = nullptr;
     float slope = 0.f, aq = 0.f;
-    if (!PLAIN && a.slopes) {
+    if (biased<KIND>(a.slopes)) {
         akp = a.at_k + b * a.at_k_stride[0] + hk * a.at_k_stride[1];
         slope = a.slopes[q.head] * kLog2e;
         aq = a.at_q[b * a.at_q_stride + q.token];
@@ -103,7 +102,7 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
     auto fetch = [&](T* ks, T* vs, float* as, int j) {
         L::template load<N, W>(ks, kp, a.k_stride[1], j, last, w, lane);
         L::template load<N, W>(vs, vp, a.v_stride[1], j, last, w, lane);
-        if (!PLAIN && akp && w == 0)
+        if (biased<KIND>(akp) && w == 0)
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(akp + min(j + lane, last)),
                                              (__attribute__((address_space(3))) void*)as, 4, 0, 0);
     };
@@ -117,7 +116,7 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
             for (int s = 0; s < K; ++s) z[n] = mma(L::rows(ks, 32 * n, s, lane), qf[s], z[n]);
         }
         if constexpr (!PLAIN) {
-            if (sp.cap2 > 0.f) {
+            if (capped<KIND>(sp)) {
 #pragma unroll
                 for (int n = 0; n < S; ++n)
 #pragma unroll
@@ -126,16 +125,17 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
 #pragma unroll
                 for (int n = 0; n < S; ++n) z[n] *= sp.mul;
             }
-            if (akp) {
+            if (biased<KIND>(akp)) {
 #pragma unroll
                 for (int n = 0; n < S; ++n)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) z[n][r] -= slope * fabsf(aq - as[32 * n + acc_row(r, lane)]);
+                    for (int i = 0; i < 4; ++i) {
+                        const vec<float, 4> ak = *(const vec<float, 4>*)(as + 32 * n + 8 * i + 4 * (lane >> 5));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) z[n][4 * i + e] = fmaf(-slope, fabsf(aq - ak[e]), z[n][4 * i + e]);
+                    }
             }
         }
-        // bit 16 n + r: some row of the wavefront sees the key of register r.
-        // The others' values, which may be anything, must not meet a weight
-        // of 0 in the second product.
         if (j < flo || j + N - 1 > fhi) mask_scores<S>(z, lo - j, hi - j, lane);
         float mx = z[0][0];
 #pragma unroll
@@ -374,7 +374,7 @@ struct FewPass {
                 }
                 if (!PLAIN && bias) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[g][e] -= row.slope[g] * fabsf(row.aq[g] - ak[e]);
+                    for (int e = 0; e < 8; ++e) z[g][e] = fmaf(-row.slope[g], fabsf(row.aq[g] - ak[e]), z[g][e]);
                 }
 #pragma unroll
                 for (int u = 0; u < 2; ++u) store(g, j + row_of(4 * u), &z[g][4 * u], !MASKED);

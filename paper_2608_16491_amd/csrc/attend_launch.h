@@ -3,6 +3,8 @@
 // with the workspace query.
 #pragma once
 
+#include <type_traits>
+
 #include "attend.h"
 
 namespace frog {
@@ -41,6 +43,15 @@ struct PackPlan {
     int parts;                // of the query rows; 1: no partial sums at o
 };
 PackPlan pack_plan(const frog_attend_t& a, bool grad);
+
+// f(a constant of this kind)
+template <typename F>
+void by_scores(Scores kind, F&& f) {
+    if (kind == kPlain) f(std::integral_constant<Scores, kPlain>{});
+    else if (kind == kCapped) f(std::integral_constant<Scores, kCapped>{});
+    else if (kind == kBiased) f(std::integral_constant<Scores, kBiased>{});
+    else f(std::integral_constant<Scores, kAny>{});
+}
 
 template <typename T>
 struct AttendLaunch {

@@ -19,8 +19,9 @@ void launch_keys(const frog_attend_t& a, const ScoreParams& sp, const PackPlan& 
     const int group = a.heads / a.kv_heads, tiles = (int)((a.keys + kTileRows - 1) / kTileRows);
     const KeyParts parts{p.parts > 1 ? (float*)(pack + p.o) : nullptr, a.batch * a.kv_heads * a.keys, p.parts};
     const dim3 grid((unsigned)(a.batch * a.kv_heads * tiles * p.parts));
-    if (a.cap > 0.f || a.slopes) attend_keys<T, D, false, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts);
-    else attend_keys<T, D, true, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts);
+    by_scores(scores_of(a.cap > 0.f, a.slopes, true), [&](auto kind) {
+        attend_keys<T, D, decltype(kind)::value, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts);
+    });
     if (p.parts == 1) return;
     if constexpr (GRAD) keys_join<T, D><<<dim3((unsigned)((parts.total * (D / 2) + 255) / 256)), 256, 0, s>>>(a, sp, parts);
     else weights_join<<<dim3((unsigned)((parts.total + 255) / 256)), 256, 0, s>>>(a, parts);
@@ -42,8 +43,7 @@ void launch_backward(const frog_attend_t& a, char* pack, hipStream_t s) {
     const int qt = (int)((a.queries * group + kTileRows - 1) / kTileRows);
     const dim3 qg((unsigned)(a.batch * a.kv_heads * qt));
     launch_keys<T, D, true>(a, sp, p, r, pack, s);
-    if (a.cap > 0.f || a.slopes) attend_dq<T, D, false, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r);
-    else attend_dq<T, D, true, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r);
+    by_scores(scores_of(a.cap > 0.f, a.slopes, true), [&](auto kind) { attend_dq<T, D, decltype(kind)::value, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r); });
 }
 
 template <typename T>

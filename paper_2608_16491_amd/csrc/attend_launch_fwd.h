@@ -12,8 +12,9 @@ namespace frog {
 template <typename T, int D>
 void launch_tiles(const frog_attend_t& a, const ScoreParams& sp, int group, int tiles, const Parts& parts, hipStream_t s) {
     const dim3 grid((unsigned)(a.batch * a.kv_heads * parts.splits * tiles));
-    if (a.cap > 0.f || a.slopes || !(a.scale > 0.f)) attend_tile<T, D, false, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, parts);
-    else attend_tile<T, D, true, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, parts);
+    by_scores(scores_of(a.cap > 0.f, a.slopes, a.scale > 0.f), [&](auto kind) {
+        attend_tile<T, D, decltype(kind)::value, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, parts);
+    });
 }
 
 template <typename T, int D>
