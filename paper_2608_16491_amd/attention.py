@@ -80,24 +80,44 @@ def _values(names, tensors, dims):
     return _TYPES[dtype]
 
 
-def _launch(fn, args, stream, device, tensors):
-    """Enqueue on `stream` (default: the current one of the device); memory that another stream's allocator pool holds is kept
-    until `stream` is done with it."""
+def _launch(fn, args, device):
+    """Enqueue on the device's current stream."""
     index = device.index
-    here = _current(index)
-    handle = here if stream is None else stream.cuda_stream
-    _need(stream is None or stream.device == device, f"the stream is not on {device}")
     if torch.cuda.current_device() == index:
-        rc = fn(args, handle)
+        rc = fn(args, _current(index))
     else:
         with torch.cuda.device(index):
-            rc = fn(args, handle)
+            rc = fn(args, _current(index))
     if rc:
         _check(rc)
-    if handle != here:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+
+
+def _on(stream, call, inputs):
+    """The tensors `call()` returns, with its work enqueued on `stream` (None: the current one of the inputs' device).  On
+    another stream than the current one the call allocates from that stream's memory, which no earlier work of the current
+    stream may still use; and inputs and outputs are kept until both streams are done with them."""
+    if stream is None:
+        return call()
+    device = inputs[0].device
+    _need(stream.device == device, f"the stream is not on {device}")
+    here = torch.cuda.current_stream(device)
+    if stream == here:
+        return call()
+    with torch.cuda.stream(stream):
+        outs = call()
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    for t in outs:
+        if t is not None:
+            t.record_stream(here)
+    return outs
+
+
+def _no_gradient(names, tensors):
+    if torch.is_grad_enabled():
+        for name, t in zip(names, tensors):
+            _need(t is None or not t.requires_grad, f"{name} takes no gradient: detach it, or call under torch.no_grad()")
 
 
 def _own_workspace(large):
@@ -121,15 +141,16 @@ _NO_GRADS = _NONE4 * 4
 class _Call:
     """The checked arguments of one attention call, apart from its outputs."""
 
-    __slots__ = ("device", "shape", "extra", "rows", "masks", "tail", "lse")
+    __slots__ = ("device", "shape", "rows", "masks", "tail")
 
     def __init__(self, q, k, v, lr, scale, cap, slopes, at_q, at_k):
         kind = _values(("q", "k", "v"), (q, k, v), (4, 4, 4))
+        _no_gradient(("slopes", "at_q", "at_k"), (slopes, at_q, at_k))
         b, tq, h, d = q.shape
         _, tk, kv, _ = ks = k.shape
         _need(ks == (b, tk, kv, d) and v.shape == ks, f"q {tuple(q.shape)}, k {tuple(ks)}, v {tuple(v.shape)}: "
               "[batch, queries, heads, d] and twice [batch, keys, kv_heads, d] are wanted")
-        self.device, self.shape, self.extra = q.device, (b, tq, h, d, tk, kv), (lr, slopes, at_q, at_k)
+        self.device, self.shape = q.device, (b, tq, h, d, tk, kv)
         self.rows = (q.data_ptr(), *q.stride()[:3], k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3])
         lrs = (0, 0)
         if lr is not None:
@@ -138,7 +159,6 @@ class _Call:
         bias = (0, 0, 0, 0, 0, 0)
         if slopes is not None:
             _need(at_q is not None and at_k is not None, "slopes, at_q and at_k go together")
-            _need(not slopes.requires_grad, "slopes take no gradient")
             f, one = torch.float32, at_k.dim() == 2
             bias = (_plain("slopes", slopes, f, (h,), q), _plain("at_q", at_q, f, (b, tq), q), tq,
                     _plain("at_k", at_k, f, (b, tk) if one else (b, kv, tk), q), tk if one else kv * tk, 0 if one else tk)
@@ -147,7 +167,7 @@ class _Call:
         self.masks = lrs + bias
         self.tail = (b, tq, tk, h, kv, d, kind, d ** -0.5 if scale is None else scale, cap)
 
-    def forward(self, q, k, v, want_lse, w_in, w_out, stream):
+    def forward(self, q, want_lse, w_in, w_out):
         b, tq, h, d, tk, kv = self.shape
         out = torch.empty((b, tq, h, d), dtype=q.dtype, device=self.device)
         lse = torch.empty((b, h, tq), dtype=torch.float32, device=self.device) if want_lse else None
@@ -157,7 +177,7 @@ class _Call:
         if _own_workspace(w_out is not None and max(q.numel() // d, kv * 64) * tk > 2 ** 22):
             ws, at = _workspace(lambda x: L.frog_attend_workspace(x, 0), args, self.device)
             args = _pack_attend(*head, *at, *self.tail)
-        _launch(L.frog_attend, args, stream, self.device, (q, k, v, *self.extra, out, lse, w_in, w_out, ws))
+        _launch(L.frog_attend, args, self.device)
         return out, lse
 
     def backward(self, q, k, v, out, lse, dout):
@@ -168,26 +188,29 @@ class _Call:
         if _own_workspace(q.numel() > 2 ** 22 or k.numel() > 2 ** 22):
             ws, at = _workspace(lambda x: L.frog_attend_workspace(x, 1), args, self.device)
             args = _pack_attend(*head, *at, *self.tail)
-        _launch(L.frog_attend_backward, args, None, self.device, ())
+        _launch(L.frog_attend_backward, args, self.device)
         return dq, dk, dv
 
 
 class _Attend(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, call, w_in, w_out, stream):
-        out, call.lse = call.forward(q, k, v, True, w_in, w_out, stream)
-        ctx.call = call
-        ctx.save_for_backward(q, k, v, out, call.lse, *(t for t in call.extra if t is not None))
+    def forward(ctx, q, k, v, call, mask, w_in, w_out, kept):
+        out, lse = call.forward(q, True, w_in, w_out)
+        kept.append(lse)
+        lr, ctx.scale, ctx.cap, *bias = mask
+        ctx.save_for_backward(q, k, v, out, lse, lr, *bias)
         return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
-        q, k, v, out, lse = ctx.saved_tensors[:5]
+        # (the tensors may have moved since: hooks on saved tensors, recomputation)
+        q, k, v, out, lse, lr, *bias = ctx.saved_tensors
         size = 16 // dout.element_size()
         if dout.stride(-1) != 1 or dout.data_ptr() % 16 or any(s % size for s in dout.stride()[:-1]):
             dout = dout.contiguous()
-        return (*ctx.call.backward(q, k, v, out, lse, dout), None, None, None, None)
+        call = _Call(q, k, v, lr, ctx.scale, ctx.cap, *bias)
+        return (*call.backward(q, k, v, out, lse, dout), None, None, None, None, None)
 
 
 def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_k=None, weights=None, weights_out=None,
@@ -209,24 +232,29 @@ def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_
     Returns out [batch, queries, heads, d], followed by lse [batch, heads,
     queries] (return_lse) and the new weights (weights given).  q, k and v
     take gradients; lse and weights do not."""
-    call = _Call(q, k, v, lr, scale, cap, slopes, at_q, at_k)
+    mask = (lr, scale, cap, slopes, at_q, at_k)
+    call = _Call(q, k, v, *mask)
     if weights is not None:
         b, _, _, _, tk, kv = call.shape
         _plain("weights", weights, torch.float32, (b, kv, tk), q)
-        if weights_out is None:
-            weights_out = torch.empty_like(weights)
-        else:
+        _no_gradient(("weights", "weights_out"), (weights, weights_out))
+        if weights_out is not None:
             _plain("weights_out", weights_out, torch.float32, (b, kv, tk), q)
     else:
         _need(weights_out is None, "weights_out needs weights")
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
-        out = _Attend.apply(q, k, v, call, weights, weights_out, stream)
-        lse = call.lse
-    else:
-        out, lse = call.forward(q, k, v, return_lse, weights, weights_out, stream)
+    grad = torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad)
+
+    def run():
+        new = torch.empty_like(weights) if weights is not None and weights_out is None else weights_out
+        if not grad:
+            return (*call.forward(q, return_lse, weights, new), new)
+        kept = []
+        return _Attend.apply(q, k, v, call, mask, weights, new, kept), kept[0], new
+
+    out, lse, new = _on(stream, run, (q, k, v, lr, slopes, at_q, at_k, weights, weights_out))
     if not return_lse and weights is None:
         return out
-    return (out,) + ((lse,) if return_lse else ()) + ((weights_out,) if weights is not None else ())
+    return (out,) + ((lse,) if return_lse else ()) + ((new,) if weights is not None else ())
 
 
 def attend_shared(q, k, v, k_pages, v_pages, pages, lengths, *, lr=None, scale=None, cap=0.0, slopes=None, return_lse=False,
@@ -247,6 +275,16 @@ def attend_shared(q, k, v, k_pages, v_pages, pages, lengths, *, lr=None, scale=N
           f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, pages {tuple(k_pages.shape)}, {tuple(v_pages.shape)}: "
           "[batch, heads, d], twice [prefix, kv_heads, d], twice [num_pages, page, kv_heads, d] are wanted")
     _need(pages.dim() == 2, "pages: [batch, pages_per_request] is wanted")
+    _no_gradient(("q", "k", "v", "k_pages", "v_pages", "slopes"), (q, k, v, k_pages, v_pages, slopes))
+    outs = _on(stream, lambda: _attend_shared(kind, q, k, v, k_pages, v_pages, pages, lengths, lr, scale, cap, slopes, return_lse),
+               (q, k, v, k_pages, v_pages, pages, lengths, lr, slopes))
+    return outs if return_lse else outs[0]
+
+
+def _attend_shared(kind, q, k, v, k_pages, v_pages, pages, lengths, lr, scale, cap, slopes, return_lse):
+    b, h, d = q.shape
+    tk, kv, _ = k.shape
+    num, page, _, _ = k_pages.shape
     width, device = pages.shape[1], q.device
     out = torch.empty((b, h, d), dtype=q.dtype, device=device)
     lse = torch.empty((b, h), dtype=torch.float32, device=device) if return_lse else None
@@ -260,8 +298,8 @@ def attend_shared(q, k, v, k_pages, v_pages, pages, lengths, *, lr=None, scale=N
     if _own_workspace(q.numel() > 2 ** 22):
         ws, at = _workspace(L.frog_attend_shared_workspace, args, device)
         args = _pack_shared(*head, *at, *tail)
-    _launch(L.frog_attend_shared, args, stream, device, (q, k, v, k_pages, v_pages, pages, lengths, lr, slopes, out, lse, ws))
-    return (out, lse) if return_lse else out
+    _launch(L.frog_attend_shared, args, device)
+    return out, lse
 
 
 def evict(k, v, weights, positions, lengths, keep, *, recent=0, stream=None):
@@ -275,6 +313,12 @@ def evict(k, v, weights, positions, lengths, keep, *, recent=0, stream=None):
     _need(v.shape == k.shape, f"k {tuple(k.shape)}, v {tuple(v.shape)}: the same shape is wanted")
     b, t, h, d = k.shape
     _need(0 <= recent <= keep <= t, f"recent {recent}, keep {keep}, slots {t}: 0 <= recent <= keep <= slots is wanted")
+    _no_gradient(("k", "v", "weights"), (k, v, weights))
+    return _on(stream, lambda: _evict(kind, k, v, weights, positions, lengths, keep, recent), (k, v, weights, positions, lengths))
+
+
+def _evict(kind, k, v, weights, positions, lengths, keep, recent):
+    b, t, h, d = k.shape
     device = k.device
     k_out, v_out = (torch.empty((b, keep, h, d), dtype=k.dtype, device=device) for _ in range(2))
     w_out = torch.empty((b, h, keep), dtype=torch.float32, device=device)
@@ -289,5 +333,5 @@ def evict(k, v, weights, positions, lengths, keep, *, recent=0, stream=None):
     if _own_workspace(b * h * keep > 2 ** 22):
         ws, at = _workspace(L.frog_evict_workspace, args, device)
         args = _pack_evict(*head, *at, *tail)
-    _launch(L.frog_evict, args, stream, device, (k, v, weights, positions, lengths, k_out, v_out, w_out, p_out, n_out, ws))
+    _launch(L.frog_evict, args, device)
     return k_out, v_out, w_out, p_out, n_out
