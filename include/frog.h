@@ -309,9 +309,10 @@ int frog_bruteforce_filtered(const frog_index_t* idx, const float* d_queries, in
  *   lse = log sum exp z,  p = exp(z - lse),  out = sum p v
  * over the keys of the interval; out = 0 and lse = -inf for an empty one.
  * Values are fp32, fp16 or bf16 (FROG_STORAGE_*); products, softmax
- * statistics and sums are fp32.  With 16-bit values p (and in the gradient
- * p's share of the score's) is rounded to the type as a factor of the second
- * product, and each output once.
+ * statistics and sums are fp32.  With 16-bit values p and the gradient of x
+ * are rounded to the type as factors of the second products, and each output
+ * once; an fp16 gradient of x below 6e-8 is lost, so scale the loss where
+ * training in fp16.
  *
  * Rows no interval meets are not read into any result: a cache's unused tail
  * may hold anything.  Rows some interval meets must be finite (a NaN or
@@ -373,10 +374,11 @@ int frog_attend_backward(const frog_attend_t* a, void* stream);
  * t % page of page pages[b][t / page] of k_pages / v_pages.  Keys count 0 ..
  * prefix - 1 for the prefix, prefix + t for the tail; the query stands at
  * prefix + lengths[b] - 1 (its distance to a key is the difference of these
- * numbers).  lr (optional) limits what a request sees of the prefix.  The
- * prefix is read once for all requests.  Page entries past a tail's length
- * are not read; a length is clipped to pages_per_request * page, and an entry
- * outside [0, num_pages) counts as no rows. */
+ * numbers as floats: exact up to 2^24).  lr (optional) limits what a request
+ * sees of the prefix.  The prefix is read once for all requests.  Page entries
+ * past a tail's length are not read; a length is clipped to
+ * pages_per_request * page, and an entry outside [0, num_pages) counts as no
+ * rows. */
 typedef struct {
     const void* q; int64_t q_stride[2];        /* [batch, heads, d]: request, head */
     const void* k; int64_t k_stride[2];        /* prefix: token, head */

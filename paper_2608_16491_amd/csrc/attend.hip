@@ -106,9 +106,11 @@ void by_type(int type, F&& f) {
     else f(AttendLaunch<bf16_t>{});
 }
 
-// grids are one number of workgroups
+// grids are one number of workgroups, of 512 threads at most; a launch takes
+// fewer than 2^32 threads
+constexpr int64_t kMaxBlocks = 0xffffffffll / 512;
 int check_grid(int64_t blocks) {
-    return blocks > 0x7fffffff ? fail(FROG_EUNSUPPORTED, "%lld workgroups: more than one launch takes", (long long)blocks) : FROG_OK;
+    return blocks > kMaxBlocks ? fail(FROG_EUNSUPPORTED, "%lld workgroups: more than one launch takes", (long long)blocks) : FROG_OK;
 }
 
 __global__ void fill_lse(float* lse, int64_t n) {

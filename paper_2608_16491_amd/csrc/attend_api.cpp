@@ -37,6 +37,7 @@ int check_heads(int heads, int kv_heads, int d, float scale, float cap) {
     if (d != 32 && d != 64 && d != 96 && d != 128) return fail(FROG_EUNSUPPORTED, "d %d: 32, 64, 96 or 128", d);
     if (!std::isfinite(scale)) return fail(FROG_EINVAL, "scale is not finite");
     if (!std::isfinite(cap) || cap < 0.f) return fail(FROG_EINVAL, "cap must be finite and >= 0");
+    if (cap > 0.f && !(std::isfinite(4.f * scale / cap) && std::isfinite(4.f * cap))) return fail(FROG_EINVAL, "cap %g: scale / cap or cap overflows", (double)cap);
     return FROG_OK;
 }
 

@@ -62,7 +62,9 @@ __global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, Row
         }
     }
     if (h == 0) {
-        out[RowPack::kLse + i] = some ? lse[stat] * kLog2e : INFINITY;
+        // (-inf: no key, or a bias that leaves none a weight)
+        const float z = some ? lse[stat] : -INFINITY;
+        out[RowPack::kLse + i] = z > -INFINITY ? z * kLog2e : INFINITY;
         out[RowPack::kLo + i] = __int_as_float(lo);
         out[RowPack::kHi + i] = __int_as_float(hi);
         out[RowPack::kSlope + i] = a.slopes ? a.slopes[q.head] * kLog2e : 0.f;
@@ -122,13 +124,21 @@ struct KeyParts {
     int parts;
 };
 
-// 4 r (1 - r), r = 1 / (1 + exp2(c1 dot)): the derivative of the cap; *z2 the
-// capped score
-__device__ inline float cap_slope(const ScoreParams& sp, float dot, float* z2) {
-    const float r = rcp_fast(1.f + exp2_fast(dot * sp.mul));
-    const float r4 = 4.f * r;
-    *z2 = fmaf(-2.f * sp.cap2, r, sp.cap2);
-    return fmaf(-r4, r, r4);
+// f = 4 r (1 - r), r = 1 / (1 + exp2(c1 dot)): the derivative of the cap, of 16
+// products z, which become the capped scores
+template <Scores S>
+__device__ inline void cap_slopes(const ScoreParams& sp, acc16& z, acc16& f) {
+    auto each = [&](auto fine) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float y = z[i] * sp.mul, r = rcp_fast(1.f + exp2_fast(y)), r4 = 4.f * r;
+            if constexpr (decltype(fine)::value) z[i] = fine_tanh(sp, y, r);
+            else z[i] = fmaf(-2.f * sp.cap2, r, sp.cap2);
+            f[i] = fmaf(-r4, r, r4);
+        }
+    };
+    if (S == kAny && sp.fine) each(std::true_type{});
+    else each(std::false_type{});
 }
 
 // One workgroup of W wavefronts, 32 keys each (a lane owns a key), over the
@@ -206,12 +216,7 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
         acc16 f;
         if constexpr (!PLAIN) {
             if (capped<KIND>(sp)) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float y;
-                    f[r] = cap_slope(sp, z[r], &y);
-                    z[r] = y;
-                }
+                cap_slopes<KIND>(sp, z, f);
             } else {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
@@ -233,7 +238,7 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
         for (int i = 0; i < 4; ++i) {
             const vec<float, 4> lse = *(const vec<float, 4>*)(ps + RowPack::kLse + 8 * i + 4 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[4 * i + e] = exp2_fast(PLAIN ? fmaf(z[4 * i + e], sp.mul, -lse[e]) : z[4 * i + e] - lse[e]);
+            for (int e = 0; e < 4; ++e) z[4 * i + e] = weight2(PLAIN ? fmaf(z[4 * i + e], sp.mul, -lse[e]) : z[4 * i + e] - lse[e]);
         }
         const bool whole = bd.z <= wfirst && bd.w >= wlast;
         if (!whole) {
@@ -464,12 +469,7 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
             acc16 f{};
             if constexpr (!PLAIN) {
                 if (capped<KIND>(sp)) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        float y;
-                        f[r] = cap_slope(sp, z[0][r], &y);
-                        z[0][r] = y;
-                    }
+                    cap_slopes<KIND>(sp, z[0], f);
                 } else {
                     z[0] *= sp.mul;
                 }
@@ -485,7 +485,7 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
             // (all rows here are finite: what no interval meets was cleared)
             if (j < flo || j + 31 > fhi) mask_scores<1>(z, lo - j, hi - j, lane);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) z[0][r] = exp2_fast(PLAIN ? fmaf(z[0][r], sp.mul, -lse) : z[0][r] - lse);
+            for (int r = 0; r < 16; ++r) z[0][r] = weight2(PLAIN ? fmaf(z[0][r], sp.mul, -lse) : z[0][r] - lse);
             if (capped<KIND>(sp)) z[0] *= f;
             acc16 dp = acc16{} - delta;
 #pragma unroll

@@ -118,9 +118,7 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
         if constexpr (!PLAIN) {
             if (capped<KIND>(sp)) {
 #pragma unroll
-                for (int n = 0; n < S; ++n)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) z[n][r] = score2<true>(sp, z[n][r]);
+                for (int n = 0; n < S; ++n) cap_scores<KIND, 16>(sp, z[n]);
             } else {
 #pragma unroll
                 for (int n = 0; n < S; ++n) z[n] *= sp.mul;
@@ -366,8 +364,7 @@ struct FewPass {
 #pragma unroll
             for (int g = 0; g < RG; ++g) {
                 if (!PLAIN && sp.cap2 > 0.f) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) z[g][e] = score2<true>(sp, z[g][e]);
+                    cap_scores<kAny, 8>(sp, z[g]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) z[g][e] *= sp.mul;
@@ -841,6 +838,7 @@ __global__ __launch_bounds__(256) void attend_few_end(frog_attend_t a, int group
             z = y.sum > 0.f ? y.top + __log2f(y.sum) : INFINITY;
         } else {
             z = a.lse[(b * a.heads + q.head) * a.queries + q.token] * kLog2e;
+            if (z == -INFINITY) z = INFINITY;
         }
         if (lane == 0) {
             lse2[r] = z;
@@ -860,7 +858,7 @@ __global__ __launch_bounds__(256) void attend_few_end(frog_attend_t a, int group
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int r = min(r0 + u, rows - 1);
-            if (r0 + u < rows && j >= lo[r] && j <= hi[r]) sum += exp2_fast(z[u] - lse2[r]);
+            if (r0 + u < rows && j >= lo[r] && j <= hi[r]) sum += weight2(z[u] - lse2[r]);
         }
     }
     const int64_t i = (int64_t)x * a.keys + j;

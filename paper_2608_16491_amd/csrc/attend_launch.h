@@ -44,12 +44,13 @@ struct PackPlan {
 };
 PackPlan pack_plan(const frog_attend_t& a, bool grad);
 
-// f(a constant of this kind)
-template <typename F>
+// f(a constant of this kind), for rows of type T (fp32 rows are never kCapped)
+template <typename T, typename F>
 void by_scores(Scores kind, F&& f) {
     if (kind == kPlain) f(std::integral_constant<Scores, kPlain>{});
-    else if (kind == kCapped) f(std::integral_constant<Scores, kCapped>{});
-    else if (kind == kBiased) f(std::integral_constant<Scores, kBiased>{});
+    else if (kind == kCapped) {
+        if constexpr (sizeof(T) == 2) f(std::integral_constant<Scores, kCapped>{});
+    } else if (kind == kBiased) f(std::integral_constant<Scores, kBiased>{});
     else f(std::integral_constant<Scores, kAny>{});
 }
 

@@ -19,7 +19,7 @@ void launch_keys(const frog_attend_t& a, const ScoreParams& sp, const PackPlan& 
     const int group = a.heads / a.kv_heads, tiles = (int)((a.keys + kTileRows - 1) / kTileRows);
     const KeyParts parts{p.parts > 1 ? (float*)(pack + p.o) : nullptr, a.batch * a.kv_heads * a.keys, p.parts};
     const dim3 grid((unsigned)(a.batch * a.kv_heads * tiles * p.parts));
-    by_scores(scores_of(a.cap > 0.f, a.slopes, true), [&](auto kind) {
+    by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) {
         attend_keys<T, D, decltype(kind)::value, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts);
     });
     if (p.parts == 1) return;
@@ -31,19 +31,19 @@ template <typename T, int D>
 void launch_weigh(const frog_attend_t& a, const float* lse, char* pack, hipStream_t s) {
     const PackPlan p = pack_plan(a, false);
     const RowPack r = launch_pack<T, D, false>(a, p, lse, pack, s);
-    launch_keys<T, D, false>(a, score_params(a.scale, a.cap), p, r, pack, s);
+    launch_keys<T, D, false>(a, score_params(a.scale, a.cap, a.type), p, r, pack, s);
 }
 
 template <typename T, int D>
 void launch_backward(const frog_attend_t& a, char* pack, hipStream_t s) {
     const PackPlan p = pack_plan(a, true);
     const RowPack r = launch_pack<T, D, true>(a, p, a.lse, pack, s);
-    const ScoreParams sp = score_params(a.scale, a.cap);
+    const ScoreParams sp = score_params(a.scale, a.cap, a.type);
     const int group = a.heads / a.kv_heads;
     const int qt = (int)((a.queries * group + kTileRows - 1) / kTileRows);
     const dim3 qg((unsigned)(a.batch * a.kv_heads * qt));
     launch_keys<T, D, true>(a, sp, p, r, pack, s);
-    by_scores(scores_of(a.cap > 0.f, a.slopes, true), [&](auto kind) { attend_dq<T, D, decltype(kind)::value, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r); });
+    by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) { attend_dq<T, D, decltype(kind)::value, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r); });
 }
 
 template <typename T>

@@ -12,14 +12,14 @@ namespace frog {
 template <typename T, int D>
 void launch_tiles(const frog_attend_t& a, const ScoreParams& sp, int group, int tiles, const Parts& parts, hipStream_t s) {
     const dim3 grid((unsigned)(a.batch * a.kv_heads * parts.splits * tiles));
-    by_scores(scores_of(a.cap > 0.f, a.slopes, a.scale > 0.f), [&](auto kind) {
+    by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) {
         attend_tile<T, D, decltype(kind)::value, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, parts);
     });
 }
 
 template <typename T, int D>
 void launch_forward(const frog_attend_t& a, const ForwardPlan& p, char* ws, hipStream_t s) {
-    const ScoreParams sp = score_params(a.scale, a.cap);
+    const ScoreParams sp = score_params(a.scale, a.cap, a.type);
     const int group = a.heads / a.kv_heads;
     const int64_t pairs = a.batch * a.kv_heads;
     const Parts parts{p.splits > 1 ? (float*)(ws + p.o) : nullptr, (float2*)(ws + p.ml), pairs * p.rows, p.splits};
@@ -57,7 +57,7 @@ void AttendLaunch<T>::forward(const frog_attend_t& a, const ForwardPlan& p, char
 
 template <typename T, int D>
 void launch_shared(const frog_attend_shared_t& a, const SharedPlan& p, char* ws, hipStream_t s) {
-    const ScoreParams sp = score_params(a.scale, a.cap);
+    const ScoreParams sp = score_params(a.scale, a.cap, a.type);
     const int group = a.heads / a.kv_heads;
     const int64_t rows = a.batch * a.heads;
     const bool plain = !(a.cap > 0.f) && !a.slopes;

@@ -260,33 +260,6 @@ struct QueryRow {
     }
 };
 
-// Addresses of the query rows of a tile: the first row's token once for all
-// lanes, the others' from it by a product with 1 / group (exact: the half keeps
-// the quotient of numbers below 2^17 away from a whole one), and 32-bit
-// distances between tokens (kMaxTokenStride).
-struct RowTile {
-    int first;        // head of the first row within its group
-    const char* base; // its token, the group's first head
-    uint32_t token_bytes;
-    int64_t head_bytes;
-    int group;
-    float inv;
-    __device__ inline RowTile(const void* p, int64_t sequence, const int64_t (&stride)[3], int size, int row0, int group_, int kv_head) {
-        const uint32_t token = (uint32_t)row0 / (uint32_t)group_;
-        first = row0 - (int)token * group_;
-        group = group_;
-        inv = 1.f / (float)group_;
-        base = (const char*)p + (sequence * stride[0] + token * stride[1] + (int64_t)kv_head * group_ * stride[2]) * size;
-        token_bytes = (uint32_t)stride[1] * size;
-        head_bytes = stride[2] * size;
-    }
-    // row i of the tile
-    __device__ inline const char* row(int i) const {
-        const int r = first + i, t = (int)(((float)r + 0.5f) * inv);
-        return base + (uint32_t)t * token_bytes + (uint32_t)(r - t * group) * head_bytes;
-    }
-};
-
 // the interval of a query clipped to the keys; empty: lo > hi
 __device__ inline void interval(const frog_attend_t& a, int64_t b, int64_t token, int* lo, int* hi) {
     *lo = 0;

@@ -131,3 +131,9 @@ def test_names_are_reached_from_the_package():
     assert all(callable(getattr(F, n)) for n in ("attend", "attend_shared", "evict"))
     with pytest.raises(AttributeError):
         F.no_such_name
+
+
+@pytest.mark.parametrize("cap", [1e-39, 3e38])
+def test_caps_whose_quotient_or_multiple_overflows_are_refused(cap):
+    assert F.lib().frog_attend(C.byref(attend_args(cap=cap)), None) == -1
+    assert F.lib().frog_attend_shared(C.byref(shared_args(cap=cap)), None) == -1

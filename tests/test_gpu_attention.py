@@ -256,3 +256,93 @@ def test_refusals():
         with pytest.raises(F.FrogError) as e:
             bad()
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("tq", [2, 90])
+@pytest.mark.parametrize("scale", [-0.3, 0.0])
+def test_scales_that_are_not_positive(scale, tq):
+    # both kinds of pass, with keys outside the intervals next to keys inside
+    s, _, dout = make("bf16", 2, tq, 100, 4, 2, 64, "documents", seed=8)
+    x = [s[n].detach().requires_grad_() for n in ("q", "k", "v")]
+    ref = Attention(*(s[n] for n in ("q", "k", "v", "lr")), scale=scale, dout=dout)
+    o = F.attend(*x, s["lr"], scale=scale)
+    near(o, ref.out, ref.out_err, "out")
+    for n, got in zip(("dq", "dk", "dv"), torch.autograd.grad(o, x, dout)):
+        near(got, getattr(ref, n), getattr(ref, n + "_err"), n)
+
+
+@pytest.mark.parametrize("tq", [1, 60])
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+def test_a_cap_far_above_the_scores_changes_nothing(kind, tq):
+    # scores below 30 capped at 10^6: x - x^3 / (3 cap^2) is x within 3e-10 of it,
+    # far inside the bounds of the call without a cap
+    s, _, dout = make(kind, 2, tq, 90, 4, 2, 64, "causal", seed=12)
+    x = [s[n].detach().requires_grad_() for n in ("q", "k", "v")]
+    ref = Attention(*(s[n] for n in ("q", "k", "v", "lr")), dout=dout)
+    # twice the uncapped bound of a score: the series rounds a few times
+    o, lse = F.attend(*x, s["lr"], cap=1e6, return_lse=True)
+    near(o, ref.out, 2 * ref.out_err, "out")
+    near(lse, ref.lse, 2 * ref.lse_err, "lse")
+    for n, got in zip(("dq", "dk", "dv"), torch.autograd.grad(o, x, dout)):
+        near(got, getattr(ref, n), 2 * getattr(ref, n + "_err"), n)
+
+
+def test_saved_tensors_that_move():
+    # the gradient of a call whose tensors were kept on the host, and of one that is computed again
+    from torch.utils.checkpoint import checkpoint
+    s, opt, dout = make("bf16", 2, 70, 90, 4, 2, 64, "causal", bias=True, seed=13)
+
+    def grads(wrap):
+        x = [s[n].detach().clone().requires_grad_() for n in ("q", "k", "v")]
+        with torch.autograd.graph.save_on_cpu() if wrap == "host" else torch.enable_grad():
+            y = [t * 1.0 for t in x]         # the call's own inputs end with this block
+            o = checkpoint(lambda *a: F.attend(*a, s["lr"], **opt), *y, use_reentrant=False) if wrap == "again" else F.attend(*y, s["lr"], **opt)
+        del y
+        other = [torch.full_like(t, math.nan) for t in x]       # takes the memory they had
+        out = torch.autograd.grad(o, x, dout)
+        del other
+        return out
+
+    want = grads(None)
+    for wrap in ("host", "again"):
+        for a, b in zip(want, grads(wrap)):
+            assert torch.equal(a, b), wrap
+
+
+def test_gradients_of_a_call_on_another_stream():
+    s, opt, dout = make("bf16", 1, 600, 600, 8, 2, 128, "causal", seed=14)
+    x = [s[n].detach().requires_grad_() for n in ("q", "k", "v")]
+    want = torch.autograd.grad(F.attend(*x, s["lr"]), x, dout)
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        side.wait_stream(torch.cuda.current_stream())
+        o = F.attend(*x, s["lr"], stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        got = torch.autograd.grad(o, x, dout)
+        for a, b in zip(want, got):
+            assert torch.equal(a, b)
+
+
+def test_a_bias_that_leaves_a_row_no_weight():
+    # slope times distance overflows to infinity: every weight of the row is 0, as for an empty interval
+    s, _, dout = make("fp32", 1, 70, 90, 2, 1, 32, "causal", seed=15)
+    opt = dict(slopes=torch.tensor([1e30, 0.5], device="cuda"), at_q=torch.zeros((1, 70), device="cuda"), at_k=torch.full((1, 90), 1e30, device="cuda"))
+    opt["at_k"][:, 20:] = 0.0                    # rows whose interval ends before key 20 see none
+    s["lr"][:, :10, 1] = 15
+    for tq in (2, 70):
+        x = [s[n][:, :tq if n == "q" else None].contiguous().requires_grad_() for n in ("q", "k", "v")]
+        o = dict(opt, at_q=opt["at_q"][:, :tq].contiguous())
+        out, lse, w = F.attend(*x, s["lr"][:, :tq].contiguous(), return_lse=True, weights=torch.zeros((1, 1, 90), device="cuda"), **o)
+        assert not out[:, :2, 0].any() and bool((lse[:, 0, :2] == -math.inf).all())
+        assert all(bool(torch.isfinite(t).all()) for t in (out, w, *torch.autograd.grad(out, x, dout[:, :tq].contiguous())))
+
+
+def test_gradients_that_do_not_exist_are_refused():
+    s, opt, _ = make("bf16", 1, 2, 20, 4, 2, 64, "causal", bias=True)
+    w = torch.zeros((1, 2, 20), device="cuda")
+    for bad in (dict(opt, slopes=opt["slopes"].requires_grad_()), dict(opt, at_k=opt["at_k"].clone().requires_grad_()),
+                dict(weights=w.requires_grad_())):
+        with pytest.raises(ValueError):
+            F.attend(s["q"], s["k"], s["v"], **bad)
+        with torch.no_grad():
+            F.attend(s["q"], s["k"], s["v"], **bad)
