@@ -4,6 +4,7 @@
 #include <algorithm>
 
 #include "attend_launch.h"
+#include "attend_tile.h"
 
 namespace frog {
 namespace {
@@ -49,6 +50,14 @@ void clear(void* p, const int64_t (&st)[3], int64_t batch, int64_t tokens, int h
 // against 13, but 4 us more on the host; 2,048 keys 10 against 22.
 constexpr int64_t kWholeKeys = 1024;
 
+// Whether the workgroups of so many tiles a sequence, in `parts` each, start in
+// the order of their lengths.
+constexpr int64_t kSortedKeys = 2048, kSortedTiles = 65536;
+
+bool sort_tiles(const frog_attend_t& a, int64_t tiles, int64_t parts) {
+    return a.lr && std::max(a.keys, a.queries) >= kSortedKeys && a.batch * tiles * parts * a.kv_heads > 256 && a.batch * tiles <= kSortedTiles;
+}
+
 ForwardPlan forward_plan(const frog_attend_t& a) {
     ForwardPlan p{};
     const int64_t group = a.heads / a.kv_heads, pairs = a.batch * a.kv_heads;
@@ -62,7 +71,9 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     const int64_t blocks = pairs * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
     p.splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / std::max<int64_t>(blocks, 1), (a.keys + least - 1) / least));
     if (p.few && p.groups == 1 && a.keys <= kWholeKeys) p.splits = 1;
+    p.sorted = !p.few && sort_tiles(a, p.tiles, p.splits);
     int64_t at = 0;
+    if (p.sorted) p.order = take(&at, a.batch * p.tiles * 8);
     if (p.splits > 1) {
         p.o = take(&at, p.splits * pairs * p.rows * a.d * 4);
         p.ml = take(&at, p.splits * pairs * p.rows * 8);
@@ -85,7 +96,12 @@ PackPlan pack_plan(const frog_attend_t& a, bool grad) {
     // CU at a time.  Their fp32 sums cost 16 d bytes a key and part.
     const int64_t blocks = a.batch * a.kv_heads * ((a.keys + kTileRows - 1) / kTileRows);
     p.parts = (int)std::max<int64_t>(1, std::min((512 + blocks - 1) / std::max<int64_t>(blocks, 1), p.tiles / 8));
+    const int64_t key_tiles = (a.keys + kTileRows - 1) / kTileRows, row_tiles = (p.tiles + 3) / 4;
+    p.keys_sorted = sort_tiles(a, key_tiles, p.parts);
+    p.rows_sorted = grad && sort_tiles(a, row_tiles, 1);
     int64_t at = 0;
+    if (p.keys_sorted) p.key_order = take(&at, a.batch * key_tiles * 8);
+    if (p.rows_sorted) p.row_order = take(&at, a.batch * row_tiles * 8);
     p.rows = take(&at, a.batch * a.kv_heads * p.tiles * 192 * 4);
     p.bounds = take(&at, a.batch * p.tiles * 16);
     p.zeros = take(&at, 512);
@@ -119,6 +135,99 @@ __global__ void fill_lse(float* lse, int64_t n) {
 }
 
 }  // namespace
+
+namespace {
+
+// Longest first by counting: one workgroup, lengths in 1,024 classes of equal
+// width up to the greatest that occurs, tiles of a class in any order (no
+// result depends on it).  order: 2 x items, the second half for the lengths.
+// length(item) is called by whole wavefronts (WAVE) or by single threads.
+constexpr int kSortBlock = 1024;
+template <bool WAVE, typename F>
+__device__ inline void sort_longest(int items, int* order, F&& length) {
+    __shared__ int hist[kSortBlock], part[kSortBlock / 64], most;
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    const int first = WAVE ? w : t, step = WAVE ? kSortBlock / 64 : kSortBlock;
+    const bool writes = !WAVE || lane == 0;
+    int* lengths = order + items;
+    hist[t] = 0;
+    if (t == 0) most = 1;
+    __syncthreads();
+    int top = 0;
+    for (int i = first; i < items; i += step) {
+        const int n = length(i);
+        if (writes) lengths[i] = n;       // read by the same thread
+        top = max(top, n);
+    }
+    if (writes) atomicMax(&most, top);
+    __syncthreads();
+    const float scale = (float)(kSortBlock - 1) / (float)most;
+    auto bin = [&](int n) { return kSortBlock - 1 - min((int)((float)n * scale), kSortBlock - 1); };
+    if (writes)
+        for (int i = first; i < items; i += step) atomicAdd(&hist[bin(lengths[i])], 1);
+    __syncthreads();
+    const int own = hist[t];
+    int x = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    if (lane == 63) part[w] = x;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) x += part[i];
+    hist[t] = x - own;
+    __syncthreads();
+    if (writes)
+        for (int i = first; i < items; i += step) order[atomicAdd(&hist[bin(lengths[i])], 1)] = i;
+}
+
+// Lengths of row tiles: the keys from the first to the last that the first,
+// middle and last token of a tile see.
+__global__ __launch_bounds__(kSortBlock) void sort_rows(frog_attend_t a, int group, int tiles, int* order) {
+    sort_longest<false>((int)a.batch * tiles, order, [&](int item) {
+        const int64_t b = item / tiles, rows = a.queries * group, r0 = (int64_t)(item % tiles) * kTileRows, r1 = min(rows, r0 + kTileRows) - 1;
+        const int64_t t0 = r0 / group, t1 = r1 / group, tokens[3] = {t0, (t0 + t1) / 2, t1};
+        int first = INT_MAX, last = -1;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            int lo, hi;
+            interval(a, b, tokens[i], &lo, &hi);
+            if (lo > hi) continue;
+            first = min(first, lo);
+            last = max(last, hi);
+        }
+        return last < 0 ? 0 : last - first + 1;
+    });
+}
+
+// Lengths of key tiles: how many of at most 256 of the sequence's row tiles
+// (evenly spread) see one of its keys.
+__global__ __launch_bounds__(kSortBlock) void sort_keys(frog_attend_t a, int tiles, const int4* bounds, int row_tiles, int* order) {
+    const int lane = threadIdx.x & 63, stride = (row_tiles + 255) / 256;
+    sort_longest<true>((int)a.batch * tiles, order, [&](int item) {
+        const int4* of = bounds + (int64_t)(item / tiles) * row_tiles;
+        const int first = item % tiles * kTileRows, last = (int)min((int64_t)first + kTileRows, a.keys) - 1;
+        int n = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t t = (int64_t)(u * 64 + lane) * stride;
+            const int4 bd = of[min(t, (int64_t)row_tiles - 1)];
+            n += __popcll(__ballot(t < row_tiles && bd.x <= last && bd.y >= first));
+        }
+        return n;
+    });
+}
+
+}  // namespace
+
+void order_rows(const frog_attend_t& a, int tiles, int* order, hipStream_t s) {
+    sort_rows<<<dim3(1), kSortBlock, 0, s>>>(a, a.heads / a.kv_heads, tiles, order);
+}
+
+void order_keys(const frog_attend_t& a, int tiles, const int4* bounds, int row_tiles, int* order, hipStream_t s) {
+    sort_keys<<<dim3(1), kSortBlock, 0, s>>>(a, tiles, bounds, row_tiles, order);
+}
 
 int64_t attend_ws(const frog_attend_t& a) { return empty(a) ? 0 : forward_plan(a).bytes; }
 

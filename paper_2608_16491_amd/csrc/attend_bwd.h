@@ -149,7 +149,7 @@ __device__ inline void cap_slopes(const ScoreParams& sp, acc16& z, acc16& f) {
 //   GRAD: dk = sum dx q, dv = sum p dout.  Else: w_out = w_in + sum p.
 template <typename T, int D, Scores KIND, bool GRAD, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(1)))
-void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack, KeyParts parts) {
+void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack, KeyParts parts, const int* order) {
     constexpr bool PLAIN = KIND == kPlain;
     constexpr int K = D / 16, M = D / 32;
     using L = Tile<T, D>;
@@ -157,10 +157,13 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
     __shared__ __attribute__((aligned(16))) T g0[GRAD ? 32 * D : 8], g1[GRAD ? 32 * D : 8];
     __shared__ __attribute__((aligned(16))) float p0[RowPack::kFloats], p1[RowPack::kFloats];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs;
-    const int tile = (int)(blockIdx.x / pairs % (uint32_t)key_tiles), part = (int)(blockIdx.x / pairs / (uint32_t)key_tiles);
-    const int64_t b = x / (uint32_t)a.kv_heads;
-    const int hk = (int)(x % (uint32_t)a.kv_heads), rows = (int)(a.queries * group);
+    const int hk = (int)(blockIdx.x % (uint32_t)a.kv_heads), rows = (int)(a.queries * group);
+    const uint32_t rest = blockIdx.x / (uint32_t)a.kv_heads;
+    const int part = (int)(rest % (uint32_t)parts.parts);
+    TileOf at(order, rest / (uint32_t)parts.parts, a.batch, key_tiles);
+    // (without an order: earlier keys, which more queries see, first)
+    const int tile = order ? at.tile : key_tiles - 1 - at.tile;
+    const int64_t b = at.b, x = b * a.kv_heads + hk;
     const int first = tile * 32 * W, last = (int)min((int64_t)first + 32 * W, a.keys) - 1;
     const int j = first + w * 32 + (lane & 31), jc = min(j, last);
     const int wfirst = first + w * 32, wlast = wfirst + 31;
@@ -378,7 +381,7 @@ static __global__ __launch_bounds__(256) void weights_join(frog_attend_t a, KeyP
 // over the keys of their intervals in tiles of N, double buffered.
 template <typename T, int D, Scores KIND, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
-void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pack) {
+void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pack, const int* order) {
     constexpr bool PLAIN = KIND == kPlain;
     constexpr int N = sizeof(T) == 2 ? 64 : 32, S = N / 32, K = D / 16, M = D / 32;
     // (buffers by name: the compiler then knows that reads of one need not wait
@@ -389,10 +392,10 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
     __shared__ Gaps<32 * W> rows_of;
     using L = Tile<T, D>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs;
-    const int tile = tiles - 1 - (int)(blockIdx.x / pairs);
-    const int64_t b = x / (uint32_t)a.kv_heads;
-    const int hk = (int)(x % (uint32_t)a.kv_heads);
+    const int hk = (int)(blockIdx.x % (uint32_t)a.kv_heads);
+    const TileOf at(order, blockIdx.x / (uint32_t)a.kv_heads, a.batch, tiles);
+    const int tile = at.tile;
+    const int64_t b = at.b, x = b * a.kv_heads + hk;
     const int64_t rows = a.queries * group, row = ((int64_t)tile * W + w) * 32 + (lane & 31);
     const QueryRow q(min(row, rows - 1), group, hk);
     int lo, hi;

@@ -24,7 +24,7 @@ constexpr float kLow = -FLT_MAX;   // running maximum of a row that has seen no 
 // double buffered in LDS by direct loads.
 template <typename T, int D, Scores KIND, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
-void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts parts) {
+void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts parts, const int* order) {
     constexpr bool PLAIN = KIND == kPlain;
     constexpr int N = sizeof(T) == 2 ? 64 : 32, S = N / 32, K = D / 16, M = D / 32;
     // (buffers by name: the compiler then knows that reads of one need not wait
@@ -36,12 +36,13 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
     using L = Tile<T, D>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // heads fastest (XCDs take workgroups in turn: with 8 heads or a multiple
-    // each XCD's L2 holds its own), later rows, which see more under a causal
-    // mask, first
-    const uint32_t pairs = (uint32_t)(a.batch * a.kv_heads), x = blockIdx.x % pairs, rest = blockIdx.x / pairs;
-    const int split = (int)(rest % (uint32_t)parts.splits), tile = tiles - 1 - (int)(rest / (uint32_t)parts.splits);
-    const int64_t b = x / (uint32_t)a.kv_heads;
-    const int hk = (int)(x % (uint32_t)a.kv_heads);
+    // each XCD's L2 holds its own)
+    const int hk = (int)(blockIdx.x % (uint32_t)a.kv_heads);
+    const uint32_t rest = blockIdx.x / (uint32_t)a.kv_heads;
+    const int split = (int)(rest % (uint32_t)parts.splits);
+    const TileOf at(order, rest / (uint32_t)parts.splits, a.batch, tiles);
+    const int tile = at.tile;
+    const int64_t b = at.b, x = b * a.kv_heads + hk;
     const int64_t rows = a.queries * group, row = ((int64_t)tile * W + w) * 32 + (lane & 31);
     const QueryRow q(min(row, rows - 1), group, hk);
     int lo, hi;

@@ -17,7 +17,8 @@ struct ForwardPlan {
     int tiles;         // else: workgroups' row tiles
     int splits;        // parts of the keys
     int64_t rows;      // query rows per (sequence, kv head)
-    int64_t lse, o, ml, scores, pack;   // workspace
+    bool sorted;       // the row tiles are put in the order of their lengths
+    int64_t lse, o, ml, scores, pack, order;   // workspace
     int64_t bytes;
 };
 constexpr int kTileRows = 128;    // query rows (keys, in the passes that own keys) of a workgroup
@@ -39,10 +40,16 @@ SharedPlan shared_plan(const frog_attend_shared_t& a);
 // What pack_rows prepares: offsets from the start of the region
 // and how the passes that own keys are cut
 struct PackPlan {
-    int64_t tiles, rows, bounds, zeros, o, bytes;
+    int64_t tiles, rows, bounds, zeros, o, key_order, row_order, bytes;
     int parts;                // of the query rows; 1: no partial sums at o
+    bool keys_sorted, rows_sorted;
 };
 PackPlan pack_plan(const frog_attend_t& a, bool grad);
+
+// order: the tiles (sequence * tiles + tile) of kTileRows query rows, and of as
+// many keys (bounds, row_tiles: RowPack), longest first
+void order_rows(const frog_attend_t& a, int tiles, int* order, hipStream_t s);
+void order_keys(const frog_attend_t& a, int tiles, const int4* bounds, int row_tiles, int* order, hipStream_t s);
 
 // f(a constant of this kind), for rows of type T (fp32 rows are never kCapped)
 template <typename T, typename F>

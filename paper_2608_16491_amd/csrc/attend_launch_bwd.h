@@ -19,8 +19,10 @@ void launch_keys(const frog_attend_t& a, const ScoreParams& sp, const PackPlan& 
     const int group = a.heads / a.kv_heads, tiles = (int)((a.keys + kTileRows - 1) / kTileRows);
     const KeyParts parts{p.parts > 1 ? (float*)(pack + p.o) : nullptr, a.batch * a.kv_heads * a.keys, p.parts};
     const dim3 grid((unsigned)(a.batch * a.kv_heads * tiles * p.parts));
+    int* order = p.keys_sorted ? (int*)(pack + p.key_order) : nullptr;
+    if (order) order_keys(a, tiles, r.bounds, r.tiles, order, s);
     by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) {
-        attend_keys<T, D, decltype(kind)::value, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts);
+        attend_keys<T, D, decltype(kind)::value, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts, order);
     });
     if (p.parts == 1) return;
     if constexpr (GRAD) keys_join<T, D><<<dim3((unsigned)((parts.total * (D / 2) + 255) / 256)), 256, 0, s>>>(a, sp, parts);
@@ -43,7 +45,9 @@ void launch_backward(const frog_attend_t& a, char* pack, hipStream_t s) {
     const int qt = (int)((a.queries * group + kTileRows - 1) / kTileRows);
     const dim3 qg((unsigned)(a.batch * a.kv_heads * qt));
     launch_keys<T, D, true>(a, sp, p, r, pack, s);
-    by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) { attend_dq<T, D, decltype(kind)::value, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r); });
+    int* order = p.rows_sorted ? (int*)(pack + p.row_order) : nullptr;
+    if (order) order_rows(a, qt, order, s);
+    by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) { attend_dq<T, D, decltype(kind)::value, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r, order); });
 }
 
 template <typename T>

@@ -260,6 +260,24 @@ struct QueryRow {
     }
 };
 
+// Tiles of all sequences in the order their workgroups start, the longest
+// first (order: sequence * tiles + tile; null: later tiles first, which is that
+// order under a causal mask).
+struct TileOf {
+    int64_t b;
+    int tile;
+    __device__ inline TileOf(const int* order, uint32_t i, int64_t batch, int tiles) {
+        if (order) {
+            const uint32_t item = (uint32_t)__builtin_amdgcn_readfirstlane(order[i]);
+            b = item / (uint32_t)tiles;
+            tile = (int)(item % (uint32_t)tiles);
+        } else {
+            b = i % (uint32_t)batch;
+            tile = tiles - 1 - (int)(i / (uint32_t)batch);
+        }
+    }
+};
+
 // the interval of a query clipped to the keys; empty: lo > hi
 __device__ inline void interval(const frog_attend_t& a, int64_t b, int64_t token, int* lo, int* hi) {
     *lo = 0;
