@@ -114,14 +114,14 @@ struct TileWalk {
     }
 };
 
-// Sums of a pass that owns keys, cut into parts of the query rows (o null: one
-// part, which writes its results itself): part s of key i of all sequences' kv
-// heads, D floats for dk at o[(s * total + i) * D], for dv `total * parts * D`
-// further on; key weights: one float.
+// Sums of tiles of keys cut into parts of the query rows (a tile of one part
+// writes its results itself): part s of key i of the tile with slot y, kv head h
+// at index z = ((y + s) * kv_heads + h) * kTileRows + i, D floats for dk at
+// o[2 z D], as many for dv behind them; key weights: one float at o[z].
 struct KeyParts {
     float* o;
-    int64_t total;
-    int parts;
+    int parts;      // without a schedule: of every tile
+    __device__ static inline int64_t at(int slot, int kv_heads, int hk, int i) { return ((int64_t)slot * kv_heads + hk) * kTileRows + i; }
 };
 
 // f = 4 r (1 - r), r = 1 / (1 + exp2(c1 dot)): the derivative of the cap, of 16
@@ -149,7 +149,7 @@ __device__ inline void cap_slopes(const ScoreParams& sp, acc16& z, acc16& f) {
 //   GRAD: dk = sum dx q, dv = sum p dout.  Else: w_out = w_in + sum p.
 template <typename T, int D, Scores KIND, bool GRAD, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(1)))
-void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack, KeyParts parts, const int* order) {
+void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack, KeyParts parts, Schedule plan) {
     constexpr bool PLAIN = KIND == kPlain;
     constexpr int K = D / 16, M = D / 32;
     using L = Tile<T, D>;
@@ -159,11 +159,15 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int hk = (int)(blockIdx.x % (uint32_t)a.kv_heads), rows = (int)(a.queries * group);
     const uint32_t rest = blockIdx.x / (uint32_t)a.kv_heads;
-    const int part = (int)(rest % (uint32_t)parts.parts);
-    TileOf at(order, rest / (uint32_t)parts.parts, a.batch, key_tiles);
-    // (without an order: earlier keys, which more queries see, first)
-    const int tile = order ? at.tile : key_tiles - 1 - at.tile;
-    const int64_t b = at.b, x = b * a.kv_heads + hk;
+    Work work(plan.items, rest, a.batch, key_tiles, parts.parts);
+    if (work.tile < 0) return;
+    if (!plan.items) {
+        // earlier keys, which more queries see, first
+        work.tile = key_tiles - 1 - work.tile;
+        work.slot = ((int)work.b * key_tiles + work.tile) * parts.parts;
+    }
+    const int tile = work.tile, part = work.part;
+    const int64_t b = work.b, x = b * a.kv_heads + hk;
     const int first = tile * 32 * W, last = (int)min((int64_t)first + 32 * W, a.keys) - 1;
     const int j = first + w * 32 + (lane & 31), jc = min(j, last);
     const int wfirst = first + w * 32, wlast = wfirst + 31;
@@ -186,7 +190,7 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
         for (int m = 0; m < M; ++m) dk[m] = dv[m] = acc16{};
     }
     const float* blocks = pack.rows + (int64_t)x * pack.tiles * RowPack::kFloats;
-    TileWalk walk(pack.bounds + b * pack.tiles, pack.tiles, first, last, part, parts.parts, lane);
+    TileWalk walk(pack.bounds + b * pack.tiles, pack.tiles, first, last, part, work.parts, lane);
 
     // returns whether every row of the tile sees some key (else rows of zeros
     // stand in)
@@ -309,9 +313,9 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
     }
     if constexpr (GRAD) {
         if (j > last) return;
-        if (parts.o) {
-            float* po = parts.o + (part * parts.total + (int64_t)x * a.keys + j) * D + 4 * h;
-            const int64_t to_dv = parts.total * parts.parts * D;
+        if (work.parts > 1) {
+            float* po = parts.o + KeyParts::at(work.slot + part, a.kv_heads, hk, j - first) * 2 * D + 4 * h;
+            constexpr int to_dv = D;
 #pragma unroll
             for (int m = 0; m < M; ++m)
 #pragma unroll
@@ -340,48 +344,49 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
         sum = half_sum(sum);
         if (j > last || lane >= 32) return;
         const int64_t at = (int64_t)x * a.keys + j;
-        if (parts.o) parts.o[part * parts.total + at] = sum;
+        if (work.parts > 1) parts.o[KeyParts::at(work.slot + part, a.kv_heads, hk, j - first)] = sum;
         else a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum;
     }
 }
 
-// The parts of dk and dv summed, four values a thread.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void keys_join(frog_attend_t a, ScoreParams sp, KeyParts parts) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, each = parts.total * (D / 4);
-    if (i >= 2 * each) return;
-    const bool second = i >= each;
-    const int64_t at = second ? i - each : i;
-    const float* p = parts.o + (second ? parts.total * parts.parts * D : 0) + at * 4;
-    vec<float, 4> y{};
+// The parts of dk and dv summed, four values a thread; of the key weights, one.
+template <typename T, int D, bool GRAD>
+__global__ __launch_bounds__(256) void keys_join(frog_attend_t a, ScoreParams sp, int tiles, KeyParts parts, const int2* slots) {
+    constexpr int EACH = GRAD ? D / 2 : 1;      // threads a key
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, key = t / EACH;
+    const int c = (int)(t % EACH), i = (int)(key % kTileRows), hk = (int)(key / kTileRows % a.kv_heads);
+    const int64_t item = key / kTileRows / a.kv_heads, b = item / tiles, j = item % tiles * kTileRows + i;
+    if (b >= a.batch || j >= a.keys) return;
+    const int2 of = slots ? slots[item] : make_int2((int)item * parts.parts, parts.parts);
+    if (of.y < 2) return;
+    const float* p = parts.o + KeyParts::at(of.x, a.kv_heads, hk, i) * (GRAD ? 2 * D : 1);
+    const int64_t step = (int64_t)a.kv_heads * kTileRows * (GRAD ? 2 * D : 1);
+    if constexpr (GRAD) {
+        vec<float, 4> y{};
 #pragma unroll 4
-    for (int s = 0; s < parts.parts; ++s) y += *(const vec<float, 4>*)(p + s * parts.total * D);
-    const int64_t key = at / (D / 4), j = key % a.keys, x = key / a.keys, b = x / a.kv_heads, hk = x % a.kv_heads;
-    const int d = (int)(at % (D / 4)) * 4;
-    if (!second) y *= sp.scale;
-    vec<T, 4> t;
+        for (int s = 0; s < of.y; ++s) y += *(const vec<float, 4>*)(p + s * step + 4 * c);
+        const bool second = c >= D / 4;
+        if (!second) y *= sp.scale;
+        vec<T, 4> x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t[e] = (T)y[e];
-    T* out = second ? (T*)a.dv + b * a.dv_stride[0] + j * a.dv_stride[1] + hk * a.dv_stride[2]
-                    : (T*)a.dk + b * a.dk_stride[0] + j * a.dk_stride[1] + hk * a.dk_stride[2];
-    *(vec<T, 4>*)(out + d) = t;
-}
-
-// The parts of the key weights.
-static __global__ __launch_bounds__(256) void weights_join(frog_attend_t a, KeyParts parts) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= parts.total) return;
-    float y = 0.f;
+        for (int e = 0; e < 4; ++e) x[e] = (T)y[e];
+        T* out = second ? (T*)a.dv + b * a.dv_stride[0] + j * a.dv_stride[1] + hk * a.dv_stride[2]
+                        : (T*)a.dk + b * a.dk_stride[0] + j * a.dk_stride[1] + hk * a.dk_stride[2];
+        *(vec<T, 4>*)(out + 4 * (second ? c - D / 4 : c)) = x;
+    } else {
+        float y = 0.f;
 #pragma unroll 4
-    for (int s = 0; s < parts.parts; ++s) y += parts.o[s * parts.total + i];
-    a.w_out[i] = (a.w_in ? a.w_in[i] : 0.f) + y;
+        for (int s = 0; s < of.y; ++s) y += p[s * step];
+        const int64_t at = (b * a.kv_heads + hk) * a.keys + j;
+        a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + y;
+    }
 }
 
 // dq: one workgroup of W wavefronts, 32 query rows each (a lane owns a query),
 // over the keys of their intervals in tiles of N, double buffered.
 template <typename T, int D, Scores KIND, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
-void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pack, const int* order) {
+void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pack, Schedule plan) {
     constexpr bool PLAIN = KIND == kPlain;
     constexpr int N = sizeof(T) == 2 ? 64 : 32, S = N / 32, K = D / 16, M = D / 32;
     // (buffers by name: the compiler then knows that reads of one need not wait
@@ -393,9 +398,10 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
     using L = Tile<T, D>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hk = (int)(blockIdx.x % (uint32_t)a.kv_heads);
-    const TileOf at(order, blockIdx.x / (uint32_t)a.kv_heads, a.batch, tiles);
-    const int tile = at.tile;
-    const int64_t b = at.b, x = b * a.kv_heads + hk;
+    const Work work(plan.items, blockIdx.x / (uint32_t)a.kv_heads, a.batch, tiles, 1);
+    if (work.tile < 0) return;
+    const int tile = work.tile;
+    const int64_t b = work.b, x = b * a.kv_heads + hk;
     const int64_t rows = a.queries * group, row = ((int64_t)tile * W + w) * 32 + (lane & 31);
     const QueryRow q(min(row, rows - 1), group, hk);
     int lo, hi;

@@ -5,9 +5,22 @@
 
 #include <type_traits>
 
-#include "attend.h"
+#include "attend_tile.h"
 
 namespace frog {
+
+// A schedule (attend_tile.h) of the tiles of a pass over a kv head: how many
+// items and slots it may have, and where it lies.
+struct SchedulePlan {
+    int64_t tiles;     // of a sequence; 0: no schedule
+    int64_t items, slots;
+    int parts;         // of every tile, where none is cut by its length
+    int64_t at, bytes;
+    Schedule schedule(char* ws) const {
+        if (!tiles) return Schedule{nullptr, nullptr};
+        return Schedule{(const int4*)(ws + at), (const int2*)(ws + at + items * 16)};
+    }
+};
 
 // How a forward pass is cut, by sizes alone, and where its workspace lies
 // (byte offsets).
@@ -17,11 +30,10 @@ struct ForwardPlan {
     int tiles;         // else: workgroups' row tiles
     int splits;        // parts of the keys
     int64_t rows;      // query rows per (sequence, kv head)
-    bool sorted;       // the row tiles are put in the order of their lengths
-    int64_t lse, o, ml, scores, pack, order;   // workspace
+    int64_t lse, o, ml, scores, pack;   // workspace
+    SchedulePlan plan;
     int64_t bytes;
 };
-constexpr int kTileRows = 128;    // query rows (keys, in the passes that own keys) of a workgroup
 ForwardPlan forward_plan(const frog_attend_t& a);
 
 // The same of a pass over a shared prefix.
@@ -40,16 +52,16 @@ SharedPlan shared_plan(const frog_attend_shared_t& a);
 // What pack_rows prepares: offsets from the start of the region
 // and how the passes that own keys are cut
 struct PackPlan {
-    int64_t tiles, rows, bounds, zeros, o, key_order, row_order, bytes;
-    int parts;                // of the query rows; 1: no partial sums at o
-    bool keys_sorted, rows_sorted;
+    int64_t tiles, rows, bounds, zeros, o, bytes;
+    int parts;                // of the query rows, without a schedule
+    SchedulePlan keys_plan, rows_plan;
 };
 PackPlan pack_plan(const frog_attend_t& a, bool grad);
 
-// order: the tiles (sequence * tiles + tile) of kTileRows query rows, and of as
-// many keys (bounds, row_tiles: RowPack), longest first
-void order_rows(const frog_attend_t& a, int tiles, int* order, hipStream_t s);
-void order_keys(const frog_attend_t& a, int tiles, const int4* bounds, int row_tiles, int* order, hipStream_t s);
+// Write the schedule of tiles of kTileRows query rows, or of as many keys
+// (bounds, row_tiles: RowPack).
+void schedule_rows(const frog_attend_t& a, const SchedulePlan& p, char* ws, hipStream_t s);
+void schedule_keys(const frog_attend_t& a, const SchedulePlan& p, const int4* bounds, int row_tiles, char* ws, hipStream_t s);
 
 // f(a constant of this kind), for rows of type T (fp32 rows are never kCapped)
 template <typename T, typename F>

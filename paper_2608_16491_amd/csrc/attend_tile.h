@@ -20,6 +20,8 @@
 
 namespace frog {
 
+constexpr int kTileRows = 128;    // query rows (keys, in the passes that own keys) of a workgroup
+
 using acc16 = vec<float, 16>;
 template <typename T>
 using frag = vec<T, 8>;
@@ -260,20 +262,35 @@ struct QueryRow {
     }
 };
 
-// Tiles of all sequences in the order their workgroups start, the longest
-// first (order: sequence * tiles + tile; null: later tiles first, which is that
-// order under a causal mask).
-struct TileOf {
+// What the workgroups of a pass over tiles (of query rows or of keys) do: part
+// `part` of `parts` of tile `tile` of sequence b; the parts of a key tile lie at
+// slot `slot` + part.  With a schedule (Schedule::items: sequence * tiles + tile,
+// part, parts, slot; an item below 0 is none) tiles come longest first, and
+// those of keys may differ in their number of parts; without one later tiles
+// come first, which is the order of their lengths under a causal mask.
+struct Schedule {
+    const int4* items;    // null: none
+    const int2* slots;    // of every sequence * tiles + tile: its first slot, its parts
+};
+struct Work {
     int64_t b;
-    int tile;
-    __device__ inline TileOf(const int* order, uint32_t i, int64_t batch, int tiles) {
-        if (order) {
-            const uint32_t item = (uint32_t)__builtin_amdgcn_readfirstlane(order[i]);
-            b = item / (uint32_t)tiles;
-            tile = (int)(item % (uint32_t)tiles);
+    int tile, part, parts, slot;
+    __device__ inline Work(const int4* items, uint32_t i, int64_t batch, int tiles, int parts_) {
+        if (items) {
+            const int4 it = items[i];
+            const int item = __builtin_amdgcn_readfirstlane(it.x);
+            b = max(item, 0) / tiles;
+            tile = item < 0 ? -1 : item % tiles;
+            part = __builtin_amdgcn_readfirstlane(it.y);
+            parts = __builtin_amdgcn_readfirstlane(it.z);
+            slot = __builtin_amdgcn_readfirstlane(it.w);
         } else {
-            b = i % (uint32_t)batch;
-            tile = tiles - 1 - (int)(i / (uint32_t)batch);
+            parts = parts_;
+            part = (int)(i % (uint32_t)parts_);
+            const uint32_t rest = i / (uint32_t)parts_;
+            b = rest % (uint32_t)batch;
+            tile = tiles - 1 - (int)(rest / (uint32_t)batch);
+            slot = ((int)b * tiles + tile) * parts_;
         }
     }
 };

@@ -346,3 +346,16 @@ def test_gradients_that_do_not_exist_are_refused():
             F.attend(s["q"], s["k"], s["v"], **bad)
         with torch.no_grad():
             F.attend(s["q"], s["k"], s["v"], **bad)
+
+
+@pytest.mark.parametrize("mask,kind,shape", [("documents", "fp16", (1, 2300, 2300, 4, 2, 64)), ("wild", "bf16", (2, 2049, 2500, 3, 1, 96)),
+                                             ("lengths", "bf16", (2, 2100, 2100, 2, 2, 128)), ("causal", "fp32", (1, 2100, 2200, 2, 1, 32)),
+                                             ("one", "bf16", (1, 2200, 2200, 2, 2, 64)), ("empty", "bf16", (1, 2100, 2100, 2, 2, 64))], ids=str)
+def test_long_sequences_of_unequal_rows(mask, kind, shape):
+    # lengths from which tiles start longest first and long ones are cut
+    s, opt, dout = make(kind, *shape, "causal" if mask == "one" else mask, seed=31)
+    if mask == "one":
+        # a few rows see every key, the others one
+        s["lr"][:, :, 0] = s["lr"][:, :, 1]
+        s["lr"][:, 700:704, 0], s["lr"][:, 700:704, 1] = 0, 2199
+    check(s, opt, dout, 5.0 if mask == "documents" else 0.0, mask)
