@@ -56,6 +56,7 @@ _current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index
 
 
 def _need(ok, text):
+    """(where the text is put together from values, the test stands at the call: it costs microseconds)"""
     if not ok:
         raise ValueError(text)
 
@@ -71,13 +72,15 @@ def _values(names, tensors, dims):
     """Tensors of rows: of one supported type, on one GPU, their last axes without gaps."""
     first = tensors[0]
     dtype, device = first.dtype, first.get_device()
-    _need(device >= 0, f"{names[0]} is on {first.device}: a GPU tensor is wanted")
-    _need(dtype in _TYPES, f"{names[0]} is {dtype}: float32, float16 or bfloat16")
+    kind = _TYPES.get(dtype)
+    if device < 0 or kind is None:
+        raise ValueError(f"{names[0]} is {dtype} on {first.device}: float32, float16 or bfloat16 on a GPU is wanted")
     for name, t, n in zip(names, tensors, dims):
-        _need(t.dtype == dtype and t.get_device() == device and t.dim() == n, f"{name}: {n} axes of {dtype} on {first.device} are wanted, "
-              f"not {t.dim()} of {t.dtype} on {t.device}")
-        _need(t.stride(-1) == 1 or t.shape[-1] < 2, f"{name}: the last axis must have stride 1")
-    return _TYPES[dtype]
+        if t.dtype != dtype or t.get_device() != device or t.dim() != n:
+            raise ValueError(f"{name}: {n} axes of {dtype} on {first.device} are wanted, not {t.dim()} of {t.dtype} on {t.device}")
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            raise ValueError(f"{name}: the last axis must have stride 1")
+    return kind
 
 
 def _launch(fn, args, device):
@@ -117,7 +120,8 @@ def _on(stream, call, inputs):
 def _no_gradient(names, tensors):
     if torch.is_grad_enabled():
         for name, t in zip(names, tensors):
-            _need(t is None or not t.requires_grad, f"{name} takes no gradient: detach it, or call under torch.no_grad()")
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{name} takes no gradient: detach it, or call under torch.no_grad()")
 
 
 def _own_workspace(large):
@@ -148,8 +152,9 @@ class _Call:
         _no_gradient(("slopes", "at_q", "at_k"), (slopes, at_q, at_k))
         b, tq, h, d = q.shape
         _, tk, kv, _ = ks = k.shape
-        _need(ks == (b, tk, kv, d) and v.shape == ks, f"q {tuple(q.shape)}, k {tuple(ks)}, v {tuple(v.shape)}: "
-              "[batch, queries, heads, d] and twice [batch, keys, kv_heads, d] are wanted")
+        if ks != (b, tk, kv, d) or v.shape != ks:
+            raise ValueError(f"q {tuple(q.shape)}, k {tuple(ks)}, v {tuple(v.shape)}: [batch, queries, heads, d] and twice "
+                             "[batch, keys, kv_heads, d] are wanted")
         self.device, self.shape = q.device, (b, tq, h, d, tk, kv)
         self.rows = (q.data_ptr(), *q.stride()[:3], k.data_ptr(), *k.stride()[:3], v.data_ptr(), *v.stride()[:3])
         lrs = (0, 0)
@@ -271,9 +276,9 @@ def attend_shared(q, k, v, k_pages, v_pages, pages, lengths, *, lr=None, scale=N
     b, h, d = q.shape
     tk, kv, _ = k.shape
     num, page, _, _ = k_pages.shape
-    _need(k.shape == (tk, kv, d) and v.shape == k.shape and k_pages.shape == (num, page, kv, d) and v_pages.shape == k_pages.shape,
-          f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, pages {tuple(k_pages.shape)}, {tuple(v_pages.shape)}: "
-          "[batch, heads, d], twice [prefix, kv_heads, d], twice [num_pages, page, kv_heads, d] are wanted")
+    if k.shape != (tk, kv, d) or v.shape != k.shape or k_pages.shape != (num, page, kv, d) or v_pages.shape != k_pages.shape:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, pages {tuple(k_pages.shape)}, {tuple(v_pages.shape)}: "
+                         "[batch, heads, d], twice [prefix, kv_heads, d], twice [num_pages, page, kv_heads, d] are wanted")
     _need(pages.dim() == 2, "pages: [batch, pages_per_request] is wanted")
     _no_gradient(("q", "k", "v", "k_pages", "v_pages", "slopes"), (q, k, v, k_pages, v_pages, slopes))
     outs = _on(stream, lambda: _attend_shared(kind, q, k, v, k_pages, v_pages, pages, lengths, lr, scale, cap, slopes, return_lse),
@@ -310,9 +315,10 @@ def evict(k, v, weights, positions, lengths, keep, *, recent=0, stream=None):
     (k, v, weights, positions, lengths) with ``keep`` slots; those past a
     length hold 0, 0, 0 and -1."""
     kind = _values(("k", "v"), (k, v), (4, 4))
-    _need(v.shape == k.shape, f"k {tuple(k.shape)}, v {tuple(v.shape)}: the same shape is wanted")
     b, t, h, d = k.shape
-    _need(0 <= recent <= keep <= t, f"recent {recent}, keep {keep}, slots {t}: 0 <= recent <= keep <= slots is wanted")
+    if v.shape != k.shape or not 0 <= recent <= keep <= t:
+        raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}, recent {recent}, keep {keep}: the same shape and "
+                         "0 <= recent <= keep <= slots are wanted")
     _no_gradient(("k", "v", "weights"), (k, v, weights))
     return _on(stream, lambda: _evict(kind, k, v, weights, positions, lengths, keep, recent), (k, v, weights, positions, lengths))
 
