@@ -52,29 +52,16 @@ constexpr int64_t kWholeKeys = 1024;
 
 // Schedules are made where intervals may differ (lr) and both axes are long: a
 // workgroup's work is then anything from one step to hundreds, and the longest
-// one decides (documents of 182 to 1,638 tokens, 12 heads: in order of the rows
-// 2.3 times the time that equal workgroups would take).  A schedule costs a
-// launch of 6 to 9 us.
+// one decides.  Documents of 546 to 2,730 tokens, 16 heads, d = 128: forward 142
+// -> 121 us, dq 228 -> 212, dk and dv 503 -> 367, for launches of 6 to 9 us.
+// (Cutting long tiles into more parts than short ones made dk and dv 319 us
+// there, but their parts' traffic and that of the forward pass took it back.)
 constexpr int64_t kScheduleLength = 2048, kScheduleTiles = 65536;
-// Key tiles (one workgroup on a CU at a time) are cut by their lengths where
-// equal parts would leave the longest workgroup above 1.2 times the work of a
-// CU: then every tile longer than 1 / kKeyShare of the work of all kv heads.
-// Documents of 546 to 2,730 tokens, 16 heads: dk and dv 367 -> 319 us; causal,
-// where equal parts are as good and read query rows closer together, 3 % slower.
-// (Row tiles: the parts' traffic, 20 us, outweighs what it evens out, 5 of 83.)
-constexpr int64_t kKeyShare = 384;
-
-SchedulePlan schedule_plan(const frog_attend_t& a, int64_t tiles, int parts, int64_t share) {
+SchedulePlan schedule_plan(const frog_attend_t& a, int64_t tiles) {
     SchedulePlan p{};
     if (!a.lr || std::min(a.keys, a.queries) < kScheduleLength || a.batch * tiles > kScheduleTiles) return p;
-    // with L = ceil(total / each): the sum of ceil(length / L) over the tiles is
-    // at most tiles + each, over the cut ones (length > L) less than 2 each
-    const int64_t each = (share + a.kv_heads - 1) / a.kv_heads;
     p.tiles = tiles;
-    p.parts = parts;
-    p.items = std::max(a.batch * tiles * parts, a.batch * tiles + each);
-    p.slots = std::max(parts > 1 ? a.batch * tiles * parts : 0, 2 * each);
-    p.bytes = p.items * 16 + a.batch * tiles * 8;
+    p.bytes = a.batch * tiles * 8;
     return p;
 }
 
@@ -91,7 +78,7 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     const int64_t blocks = pairs * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
     p.splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / std::max<int64_t>(blocks, 1), (a.keys + least - 1) / least));
     if (p.few && p.groups == 1 && a.keys <= kWholeKeys) p.splits = 1;
-    if (!p.few) p.plan = schedule_plan(a, p.tiles, p.splits, 0);
+    if (!p.few) p.plan = schedule_plan(a, p.tiles);
     int64_t at = 0;
     p.plan.at = take(&at, p.plan.bytes);
     if (p.splits > 1) {
@@ -110,23 +97,23 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
 PackPlan pack_plan(const frog_attend_t& a, bool grad) {
     PackPlan p{};
     p.tiles = (a.queries * (a.heads / a.kv_heads) + 31) / 32;
-    // Parts of the query rows until there are two workgroups for each of the
-    // 256 CUs, of 8 tiles at least: a workgroup's keys see anything from all
-    // rows to a few (causal: the first keys twice the mean), and one runs on a
-    // CU at a time.  Their fp32 sums cost 16 d bytes a key and part.
+    // Parts of the query rows until there are four workgroups for each of the
+    // 256 CUs, which hold two at a time, of 8 tiles at least: a workgroup's keys
+    // see anything from all rows to a few (causal: the first keys twice the
+    // mean).  Their fp32 sums cost 16 d bytes a key and part.  (Two instead of
+    // four: a causal step of 8,192 tokens 1.78 -> 1.48 ms; three: 1.57.)
     const int64_t blocks = a.batch * a.kv_heads * ((a.keys + kTileRows - 1) / kTileRows);
-    p.parts = (int)std::max<int64_t>(1, std::min((512 + blocks - 1) / std::max<int64_t>(blocks, 1), p.tiles / 8));
+    p.parts = (int)std::max<int64_t>(1, std::min((1024 + blocks - 1) / std::max<int64_t>(blocks, 1), p.tiles / 8));
     const int64_t key_tiles = (a.keys + kTileRows - 1) / kTileRows, row_tiles = (p.tiles + 3) / 4;
-    p.keys_plan = schedule_plan(a, key_tiles, p.parts, kKeyShare);
-    if (grad) p.rows_plan = schedule_plan(a, row_tiles, 1, 0);
+    p.keys_plan = schedule_plan(a, key_tiles);
+    if (grad) p.rows_plan = schedule_plan(a, row_tiles);
     int64_t at = 0;
     p.keys_plan.at = take(&at, p.keys_plan.bytes);
     p.rows_plan.at = take(&at, p.rows_plan.bytes);
     p.rows = take(&at, a.batch * a.kv_heads * p.tiles * 192 * 4);
     p.bounds = take(&at, a.batch * p.tiles * 16);
     p.zeros = take(&at, 512);
-    const int64_t slots = p.keys_plan.tiles ? p.keys_plan.slots : p.parts > 1 ? p.parts * a.batch * key_tiles : 0;
-    p.o = take(&at, slots * a.kv_heads * kTileRows * (grad ? 2 * a.d : 1) * 4);
+    if (p.parts > 1) p.o = take(&at, p.parts * a.batch * key_tiles * a.kv_heads * kTileRows * (grad ? 2 * a.d : 1) * 4);
     p.bytes = at;
     return p;
 }
@@ -159,54 +146,37 @@ __global__ void fill_lse(float* lse, int64_t n) {
 
 namespace {
 
-// A schedule by one workgroup.  Tiles have `equal` parts each, or, where
-// that leaves the longest above 1.2 times the mean of a CU (kv_heads times the
-// total over 256), ceil(length / L) with L = ceil(total / each), at least
-// `least` (each 0: never).  Items then come longest first by counting in 1,024
-// classes of equal width (of a class in any order: neither that nor the slots'
-// order changes a result).  length(tile) is called by whole wavefronts (WAVE) or
-// by single threads.
+// Tiles longest first, by one workgroup counting in 1,024 classes of equal width
+// (of a class in any order: it changes no result).  order: the tiles, and as
+// many lengths.  length(tile) is called by whole wavefronts (WAVE) or by single
+// threads.
 constexpr int kSortBlock = 1024;
 template <bool WAVE, typename F>
-__device__ inline void schedule(int tiles, int equal, int kv_heads, int64_t each, int least, int64_t items, int4* out, int2* slots, F&& length) {
-    constexpr int HELD = 4 * kSortBlock;          // lengths kept in LDS, the others' in slots[].y
-    __shared__ int held[HELD], hist[kSortBlock], wave_sum[kSortBlock / 64], most, taken;
-    __shared__ unsigned long long total;
+__device__ inline void longest_first(int tiles, int* order, F&& length) {
+    constexpr int HELD = 4 * kSortBlock;          // lengths kept in LDS, the others' behind the tiles
+    __shared__ int held[HELD], hist[kSortBlock], wave_sum[kSortBlock / 64], most;
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
     const int first = WAVE ? w : t, step = WAVE ? kSortBlock / 64 : kSortBlock;
     const bool writes = !WAVE || lane == 0;
     hist[t] = 0;
-    if (t == 0) {
-        most = 1;
-        taken = 0;
-        total = 0;
-    }
-    for (int64_t i = tiles + t; i < items; i += kSortBlock) out[i] = make_int4(-1, 0, 1, 0);
+    if (t == 0) most = 1;
     __syncthreads();
     int top = 0;
-    unsigned long long sum = 0;
     for (int i = first; i < tiles; i += step) {
         const int n = length(i);
         if (writes && i < HELD) held[i] = n;          // read back by the same thread
-        else if (writes) slots[i].y = n;
+        else if (writes) order[tiles + i] = n;
         top = max(top, n);
-        sum += n;
     }
-    if (writes) {
-        atomicMax(&most, top);
-        atomicAdd(&total, sum);
-    }
+    if (writes) atomicMax(&most, top);
     __syncthreads();
-    const bool cut = each && (int64_t)most * 256 * 5 > (int64_t)total * kv_heads * equal * 6;
-    const int64_t limit = cut ? max((int64_t)((total + each - 1) / each), (int64_t)least) : 1;
     const float scale = (float)(kSortBlock - 1) / (float)most;
-    auto parts_of = [&](int n) { return cut ? (int)max((int64_t)1, (n + limit - 1) / limit) : equal; };
-    auto bin = [&](int n, int parts) { return kSortBlock - 1 - min((int)((float)(n / parts) * scale), kSortBlock - 1); };
+    auto bin = [&](int i) {
+        const int n = i < HELD ? held[i] : order[tiles + i];
+        return kSortBlock - 1 - min((int)((float)n * scale), kSortBlock - 1);
+    };
     if (writes)
-        for (int i = first; i < tiles; i += step) {
-            const int n = i < HELD ? held[i] : slots[i].y, parts = parts_of(n);
-            atomicAdd(&hist[bin(n, parts)], parts);
-        }
+        for (int i = first; i < tiles; i += step) atomicAdd(&hist[bin(i)], 1);
     __syncthreads();
     const int own = hist[t];
     int x = own;
@@ -221,18 +191,13 @@ __device__ inline void schedule(int tiles, int equal, int kv_heads, int64_t each
     hist[t] = x - own;
     __syncthreads();
     if (writes)
-        for (int i = first; i < tiles; i += step) {
-            const int n = i < HELD ? held[i] : slots[i].y, parts = parts_of(n);
-            const int slot = parts > 1 ? atomicAdd(&taken, parts) : 0, at = atomicAdd(&hist[bin(n, parts)], parts);
-            for (int s = 0; s < parts; ++s) out[at + s] = make_int4(i, s, parts, slot);
-            slots[i] = make_int2(slot, parts);
-        }
+        for (int i = first; i < tiles; i += step) order[atomicAdd(&hist[bin(i)], 1)] = i;
 }
 
 // Lengths of row tiles: the keys from the first to the last that the first,
 // middle and last token of a tile see.
-__global__ __launch_bounds__(kSortBlock) void schedule_row_tiles(frog_attend_t a, int group, int tiles, int equal, int64_t items, int4* out, int2* slots) {
-    schedule<false>((int)a.batch * tiles, equal, a.kv_heads, 0, 1, items, out, slots, [&](int item) {
+__global__ __launch_bounds__(kSortBlock) void schedule_row_tiles(frog_attend_t a, int group, int tiles, int* order) {
+    longest_first<false>((int)a.batch * tiles, order, [&](int item) {
         const int64_t b = item / tiles, rows = a.queries * group, r0 = (int64_t)(item % tiles) * kTileRows, r1 = min(rows, r0 + kTileRows) - 1;
         const int64_t t0 = r0 / group, t1 = r1 / group, tokens[3] = {t0, (t0 + t1) / 2, t1};
         int first = INT_MAX, last = -1;
@@ -250,10 +215,9 @@ __global__ __launch_bounds__(kSortBlock) void schedule_row_tiles(frog_attend_t a
 
 // Lengths of key tiles: how many of at most 256 of the sequence's row tiles
 // (evenly spread) see one of its keys.
-__global__ __launch_bounds__(kSortBlock) void schedule_key_tiles(frog_attend_t a, int tiles, const int4* bounds, int row_tiles, int equal, int64_t each,
-                                                                 int64_t items, int4* out, int2* slots) {
+__global__ __launch_bounds__(kSortBlock) void schedule_key_tiles(frog_attend_t a, int tiles, const int4* bounds, int row_tiles, int* order) {
     const int lane = threadIdx.x & 63, stride = (row_tiles + 255) / 256;
-    schedule<true>((int)a.batch * tiles, equal, a.kv_heads, each, (8 + stride - 1) / stride, items, out, slots, [&](int item) {
+    longest_first<true>((int)a.batch * tiles, order, [&](int item) {
         const int4* of = bounds + (int64_t)(item / tiles) * row_tiles;
         const int first = item % tiles * kTileRows, last = (int)min((int64_t)first + kTileRows, a.keys) - 1;
         int n = 0;
@@ -270,13 +234,11 @@ __global__ __launch_bounds__(kSortBlock) void schedule_key_tiles(frog_attend_t a
 }  // namespace
 
 void schedule_rows(const frog_attend_t& a, const SchedulePlan& p, char* ws, hipStream_t s) {
-    schedule_row_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, a.heads / a.kv_heads, (int)p.tiles, p.parts, p.items, (int4*)(ws + p.at),
-                                                      (int2*)(ws + p.at + p.items * 16));
+    schedule_row_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, a.heads / a.kv_heads, (int)p.tiles, (int*)(ws + p.at));
 }
 
 void schedule_keys(const frog_attend_t& a, const SchedulePlan& p, const int4* bounds, int row_tiles, char* ws, hipStream_t s) {
-    schedule_key_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, (int)p.tiles, bounds, row_tiles, p.parts, (kKeyShare + a.kv_heads - 1) / a.kv_heads, p.items,
-                                                      (int4*)(ws + p.at), (int2*)(ws + p.at + p.items * 16));
+    schedule_key_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, (int)p.tiles, bounds, row_tiles, (int*)(ws + p.at));
 }
 
 int64_t attend_ws(const frog_attend_t& a) { return empty(a) ? 0 : forward_plan(a).bytes; }
@@ -311,7 +273,7 @@ int launch_attend_bwd(const frog_attend_t& a, void* ws, hipStream_t stream) {
     const int64_t pairs = a.batch * a.kv_heads;
     const PackPlan p = pack_plan(a, true);
     const int64_t key_tiles = a.keys / kTileRows + 1;
-    int rc = check_grid(std::max(pairs * std::max({key_tiles * p.parts, p.tiles, key_tiles * a.d / 4}), a.kv_heads * p.keys_plan.items));
+    int rc = check_grid(pairs * std::max({key_tiles * p.parts, p.tiles, key_tiles * a.d / 4}));
     if (rc != FROG_OK) return rc;
     by_type(a.type, [&](auto l) { l.backward(a, (char*)ws, stream); });
     return launched("attention gradient launch");

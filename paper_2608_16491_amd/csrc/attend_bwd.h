@@ -114,14 +114,14 @@ struct TileWalk {
     }
 };
 
-// Sums of tiles of keys cut into parts of the query rows (a tile of one part
-// writes its results itself): part s of key i of the tile with slot y, kv head h
-// at index z = ((y + s) * kv_heads + h) * kTileRows + i, D floats for dk at
-// o[2 z D], as many for dv behind them; key weights: one float at o[z].
+// Sums of tiles of keys cut into parts of the query rows (parts 1: the pass
+// writes its results itself): part s of key i of tile y (of all sequences), kv
+// head h at index z = ((y * parts + s) * kv_heads + h) * kTileRows + i, D floats
+// for dk at o[2 z D], as many for dv behind them; key weights: one float at o[z].
 struct KeyParts {
     float* o;
-    int parts;      // without a schedule: of every tile
-    __device__ static inline int64_t at(int slot, int kv_heads, int hk, int i) { return ((int64_t)slot * kv_heads + hk) * kTileRows + i; }
+    int parts;
+    __device__ inline int64_t at(int64_t tile, int s, int kv_heads, int hk, int i) const { return ((tile * parts + s) * kv_heads + hk) * kTileRows + i; }
 };
 
 // f = 4 r (1 - r), r = 1 / (1 + exp2(c1 dot)): the derivative of the cap, of 16
@@ -144,43 +144,44 @@ __device__ inline void cap_slopes(const ScoreParams& sp, acc16& z, acc16& f) {
 // One workgroup of W wavefronts, 32 keys each (a lane owns a key), over the
 // tiles of 32 query rows that see them, all heads of the group: the sums over
 // the group need no further pass, and no addition's order is left to chance.
-// Query and dout rows are double buffered in LDS, keys and values stay in
-// registers.
+// Query and dout rows are double buffered in LDS, keys stay in registers, values
+// in LDS: with them there, addresses computed anew (fresh) and one product's
+// registers given up before the next, two wavefronts a SIMD of 16-bit rows run
+// without spilling (d = 128: 242 to 256 registers), one's products beside the
+// other's exponentials.  Documents of 546 to 2,730 tokens, 16 heads, capped: 320
+// us with one, 287 with two (one waited 38 % of its cycles, its vector
+// instructions took 36 %, its products 21 %); every key of 8,192 seen, no cap:
+// a step 2.79 -> 2.66 ms.
 //   GRAD: dk = sum dx q, dv = sum p dout.  Else: w_out = w_in + sum p.
 template <typename T, int D, Scores KIND, bool GRAD, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(1)))
-void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack, KeyParts parts, Schedule plan) {
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
+void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowPack pack, KeyParts parts, const int* order) {
     constexpr bool PLAIN = KIND == kPlain;
     constexpr int K = D / 16, M = D / 32;
     using L = Tile<T, D>;
     __shared__ __attribute__((aligned(16))) T q0[32 * D], q1[32 * D];
     __shared__ __attribute__((aligned(16))) T g0[GRAD ? 32 * D : 8], g1[GRAD ? 32 * D : 8];
     __shared__ __attribute__((aligned(16))) float p0[RowPack::kFloats], p1[RowPack::kFloats];
+    __shared__ __attribute__((aligned(16))) T vl[GRAD ? 32 * W * D : 8];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int hk = (int)(blockIdx.x % (uint32_t)a.kv_heads), rows = (int)(a.queries * group);
     const uint32_t rest = blockIdx.x / (uint32_t)a.kv_heads;
-    Work work(plan.items, rest, a.batch, key_tiles, parts.parts);
-    if (work.tile < 0) return;
-    if (!plan.items) {
-        // earlier keys, which more queries see, first
-        work.tile = key_tiles - 1 - work.tile;
-        work.slot = ((int)work.b * key_tiles + work.tile) * parts.parts;
-    }
-    const int tile = work.tile, part = work.part;
+    const Work work(order, rest, a.batch, key_tiles, parts.parts);
+    // (without an order: earlier keys, which more queries see, first)
+    const int tile = order ? work.tile : key_tiles - 1 - work.tile, part = work.part;
     const int64_t b = work.b, x = b * a.kv_heads + hk;
     const int first = tile * 32 * W, last = (int)min((int64_t)first + 32 * W, a.keys) - 1;
     const int j = first + w * 32 + (lane & 31), jc = min(j, last);
     const int wfirst = first + w * 32, wlast = wfirst + 31;
-    frag<T> kf[K], vf[GRAD ? K : 1];
+    frag<T> kf[K];
     {
         const T* p = (const T*)a.k + b * a.k_stride[0] + hk * a.k_stride[2] + jc * a.k_stride[1] + 8 * h;
 #pragma unroll
         for (int s = 0; s < K; ++s) kf[s] = load_frag(p + 16 * s);
-        if constexpr (GRAD) {
-            const T* p = (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2] + jc * a.v_stride[1] + 8 * h;
-#pragma unroll
-            for (int s = 0; s < K; ++s) vf[s] = load_frag(p + 16 * s);
-        }
+        if constexpr (GRAD)
+            L::template load_rows<32 * W, W>(vl, w, lane, [&](int i) {
+                return (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2] + min(first + i, last) * a.v_stride[1];
+            });
     }
     const float ak = biased<KIND>(a.slopes) ? a.at_k[b * a.at_k_stride[0] + hk * a.at_k_stride[1] + jc] : 0.f;
     acc16 dk[GRAD ? M : 1], dv[GRAD ? M : 1];
@@ -190,7 +191,7 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
         for (int m = 0; m < M; ++m) dk[m] = dv[m] = acc16{};
     }
     const float* blocks = pack.rows + (int64_t)x * pack.tiles * RowPack::kFloats;
-    TileWalk walk(pack.bounds + b * pack.tiles, pack.tiles, first, last, part, work.parts, lane);
+    TileWalk walk(pack.bounds + b * pack.tiles, pack.tiles, first, last, part, parts.parts, lane);
 
     // returns whether every row of the tile sees some key (else rows of zeros
     // stand in)
@@ -212,14 +213,10 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
     };
     auto step = [&](const T* qs, const T* gs, const float* ps, const int4& bd) {
         if (bd.x > wlast || bd.y < wfirst) return;
+        const int from = fresh(lane);
         acc16 z = acc16{};
 #pragma unroll
-        for (int s = 0; s < K; ++s) z = mma(L::rows(qs, 0, s, lane), kf[s], z);
-        acc16 dp = acc16{};
-        if constexpr (GRAD) {
-#pragma unroll
-            for (int s = 0; s < K; ++s) dp = mma(L::rows(gs, 0, s, lane), vf[s], dp);
-        }
+        for (int s = 0; s < K; ++s) z = mma(L::rows(qs, 0, s, from), kf[s], z);
         acc16 f;
         if constexpr (!PLAIN) {
             if (capped<KIND>(sp)) {
@@ -258,20 +255,30 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
             }
         }
         if constexpr (GRAD) {
+            // (the barriers keep the registers of one product from those of the
+            // next: two wavefronts a SIMD overlap instead)
+            __builtin_amdgcn_sched_barrier(0);
+            int at = fresh(lane);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const frag<T> pf = to_frag<T>(z, t);
 #pragma unroll
-                for (int m = 0; m < M; ++m) dv[m] = mma(L::cols(gs, 16 * t, m, lane), pf, dv[m]);
+                for (int m = 0; m < M; ++m) dv[m] = mma(L::cols(gs, 16 * t, m, at), pf, dv[m]);
             }
+            if constexpr (KIND == kCapped || KIND == kAny) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) z[r] = z[r] == 0.f ? 0.f : z[r] * f[r];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            acc16 dp = acc16{};
+            at = fresh(lane);
+#pragma unroll
+            for (int s = 0; s < K; ++s) dp = mma(L::rows(gs, 0, s, at), L::rows(vl, 32 * w, s, at), dp);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const vec<float, 4> delta = *(const vec<float, 4>*)(ps + RowPack::kDelta + 8 * i + 4 * h);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    dp[4 * i + e] -= delta[e];
-                    if constexpr (KIND == kCapped || KIND == kAny) dp[4 * i + e] *= f[4 * i + e];
-                }
+                for (int e = 0; e < 4; ++e) dp[4 * i + e] -= delta[e];
             }
             // (a key without a query may hold anything: 0 times it is not 0)
             if (!whole) {
@@ -279,11 +286,13 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
                 for (int r = 0; r < 16; ++r) dp[r] = z[r] == 0.f ? 0.f : dp[r];
             }
             z *= dp;
+            __builtin_amdgcn_sched_barrier(0);
+            at = fresh(lane);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const frag<T> xf = to_frag<T>(z, t);
 #pragma unroll
-                for (int m = 0; m < M; ++m) dk[m] = mma(L::cols(qs, 16 * t, m, lane), xf, dk[m]);
+                for (int m = 0; m < M; ++m) dk[m] = mma(L::cols(qs, 16 * t, m, at), xf, dk[m]);
             }
         } else {
 #pragma unroll
@@ -313,8 +322,8 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
     }
     if constexpr (GRAD) {
         if (j > last) return;
-        if (work.parts > 1) {
-            float* po = parts.o + KeyParts::at(work.slot + part, a.kv_heads, hk, j - first) * 2 * D + 4 * h;
+        if (parts.parts > 1) {
+            float* po = parts.o + parts.at(b * key_tiles + tile, part, a.kv_heads, hk, j - first) * 2 * D + 4 * h;
             constexpr int to_dv = D;
 #pragma unroll
             for (int m = 0; m < M; ++m)
@@ -344,27 +353,25 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
         sum = half_sum(sum);
         if (j > last || lane >= 32) return;
         const int64_t at = (int64_t)x * a.keys + j;
-        if (work.parts > 1) parts.o[KeyParts::at(work.slot + part, a.kv_heads, hk, j - first)] = sum;
+        if (parts.parts > 1) parts.o[parts.at(b * key_tiles + tile, part, a.kv_heads, hk, j - first)] = sum;
         else a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + sum;
     }
 }
 
 // The parts of dk and dv summed, four values a thread; of the key weights, one.
 template <typename T, int D, bool GRAD>
-__global__ __launch_bounds__(256) void keys_join(frog_attend_t a, ScoreParams sp, int tiles, KeyParts parts, const int2* slots) {
+__global__ __launch_bounds__(256) void keys_join(frog_attend_t a, ScoreParams sp, int tiles, KeyParts parts) {
     constexpr int EACH = GRAD ? D / 2 : 1;      // threads a key
     const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, key = t / EACH;
     const int c = (int)(t % EACH), i = (int)(key % kTileRows), hk = (int)(key / kTileRows % a.kv_heads);
     const int64_t item = key / kTileRows / a.kv_heads, b = item / tiles, j = item % tiles * kTileRows + i;
     if (b >= a.batch || j >= a.keys) return;
-    const int2 of = slots ? slots[item] : make_int2((int)item * parts.parts, parts.parts);
-    if (of.y < 2) return;
-    const float* p = parts.o + KeyParts::at(of.x, a.kv_heads, hk, i) * (GRAD ? 2 * D : 1);
+    const float* p = parts.o + parts.at(item, 0, a.kv_heads, hk, i) * (GRAD ? 2 * D : 1);
     const int64_t step = (int64_t)a.kv_heads * kTileRows * (GRAD ? 2 * D : 1);
     if constexpr (GRAD) {
         vec<float, 4> y{};
 #pragma unroll 4
-        for (int s = 0; s < of.y; ++s) y += *(const vec<float, 4>*)(p + s * step + 4 * c);
+        for (int s = 0; s < parts.parts; ++s) y += *(const vec<float, 4>*)(p + s * step + 4 * c);
         const bool second = c >= D / 4;
         if (!second) y *= sp.scale;
         vec<T, 4> x;
@@ -376,7 +383,7 @@ __global__ __launch_bounds__(256) void keys_join(frog_attend_t a, ScoreParams sp
     } else {
         float y = 0.f;
 #pragma unroll 4
-        for (int s = 0; s < of.y; ++s) y += p[s * step];
+        for (int s = 0; s < parts.parts; ++s) y += p[s * step];
         const int64_t at = (b * a.kv_heads + hk) * a.keys + j;
         a.w_out[at] = (a.w_in ? a.w_in[at] : 0.f) + y;
     }
@@ -386,7 +393,7 @@ __global__ __launch_bounds__(256) void keys_join(frog_attend_t a, ScoreParams sp
 // over the keys of their intervals in tiles of N, double buffered.
 template <typename T, int D, Scores KIND, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
-void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pack, Schedule plan) {
+void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pack, const int* order) {
     constexpr bool PLAIN = KIND == kPlain;
     constexpr int N = sizeof(T) == 2 ? 64 : 32, S = N / 32, K = D / 16, M = D / 32;
     // (buffers by name: the compiler then knows that reads of one need not wait
@@ -398,8 +405,7 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
     using L = Tile<T, D>;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int hk = (int)(blockIdx.x % (uint32_t)a.kv_heads);
-    const Work work(plan.items, blockIdx.x / (uint32_t)a.kv_heads, a.batch, tiles, 1);
-    if (work.tile < 0) return;
+    const Work work(order, blockIdx.x / (uint32_t)a.kv_heads, a.batch, tiles, 1);
     const int tile = work.tile;
     const int64_t b = work.b, x = b * a.kv_heads + hk;
     const int64_t rows = a.queries * group, row = ((int64_t)tile * W + w) * 32 + (lane & 31);
@@ -472,8 +478,9 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
             const int j = j0 + 32 * n;
             if (j > whi || j + 32 <= wlo) continue;
             acc16 z[1] = {acc16{}};
+            int at = fresh(lane);
 #pragma unroll
-            for (int s = 0; s < K; ++s) z[0] = mma(L::rows(ks, 32 * n, s, lane), qf[s], z[0]);
+            for (int s = 0; s < K; ++s) z[0] = mma(L::rows(ks, 32 * n, s, at), qf[s], z[0]);
             // p (times the cap's slope), before the other product needs registers
             acc16 f{};
             if constexpr (!PLAIN) {
@@ -498,13 +505,14 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
             if (capped<KIND>(sp)) z[0] *= f;
             acc16 dp = acc16{} - delta;
 #pragma unroll
-            for (int s = 0; s < K; ++s) dp = mma(L::rows(vs, 32 * n, s, lane), gf[s], dp);
+            for (int s = 0; s < K; ++s) dp = mma(L::rows(vs, 32 * n, s, at), gf[s], dp);
             dp *= z[0];
+            at = fresh(lane);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const frag<T> xf = to_frag<T>(dp, t);
 #pragma unroll
-                for (int m = 0; m < M; ++m) dq[m] = mma(L::cols(ks, 32 * n + 16 * t, m, lane), xf, dq[m]);
+                for (int m = 0; m < M; ++m) dq[m] = mma(L::cols(ks, 32 * n + 16 * t, m, at), xf, dq[m]);
             }
         }
     };

@@ -24,7 +24,7 @@ constexpr float kLow = -FLT_MAX;   // running maximum of a row that has seen no 
 // double buffered in LDS by direct loads.
 template <typename T, int D, Scores KIND, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
-void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts parts, Schedule plan) {
+void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts parts, const int* order) {
     constexpr bool PLAIN = KIND == kPlain;
     constexpr int N = sizeof(T) == 2 ? 64 : 32, S = N / 32, K = D / 16, M = D / 32;
     // (buffers by name: the compiler then knows that reads of one need not wait
@@ -39,8 +39,7 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
     // each XCD's L2 holds its own)
     const int hk = (int)(blockIdx.x % (uint32_t)a.kv_heads);
     const uint32_t rest = blockIdx.x / (uint32_t)a.kv_heads;
-    const Work work(plan.items, rest, a.batch, tiles, parts.splits);
-    if (work.tile < 0) return;
+    const Work work(order, rest, a.batch, tiles, parts.splits);
     const int tile = work.tile, split = work.part;
     const int64_t b = work.b, x = b * a.kv_heads + hk;
     const int64_t rows = a.queries * group, row = ((int64_t)tile * W + w) * 32 + (lane & 31);
@@ -74,8 +73,8 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
     const bool gaps = inner_lo > inner_hi && rows_of.any(last, lane);
     first = __builtin_amdgcn_readfirstlane(first);
     last = __builtin_amdgcn_readfirstlane(last);
-    if (work.parts > 1 && last >= 0) {
-        const int each = ((last - first) / work.parts / N + 1) * N;
+    if (parts.splits > 1 && last >= 0) {
+        const int each = ((last - first) / parts.splits / N + 1) * N;
         const int64_t from = first + (int64_t)split * each;
         last = (int)min((int64_t)last, from + each - 1);
         first = (int)min(from, (int64_t)last + 1);

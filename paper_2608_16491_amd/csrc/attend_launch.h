@@ -9,17 +9,11 @@
 
 namespace frog {
 
-// A schedule (attend_tile.h) of the tiles of a pass over a kv head: how many
-// items and slots it may have, and where it lies.
+// The order in which a pass starts the tiles of a kv head (attend_tile.h: Work).
 struct SchedulePlan {
-    int64_t tiles;     // of a sequence; 0: no schedule
-    int64_t items, slots;
-    int parts;         // of every tile, where none is cut by its length
+    int64_t tiles;     // of a sequence; 0: none
     int64_t at, bytes;
-    Schedule schedule(char* ws) const {
-        if (!tiles) return Schedule{nullptr, nullptr};
-        return Schedule{(const int4*)(ws + at), (const int2*)(ws + at + items * 16)};
-    }
+    int* order(char* ws) const { return tiles ? (int*)(ws + at) : nullptr; }
 };
 
 // How a forward pass is cut, by sizes alone, and where its workspace lies

@@ -18,15 +18,15 @@ template <typename T, int D, bool GRAD>
 void launch_keys(const frog_attend_t& a, const ScoreParams& sp, const PackPlan& p, const RowPack& r, char* pack, hipStream_t s) {
     const int group = a.heads / a.kv_heads, tiles = (int)((a.keys + kTileRows - 1) / kTileRows);
     const KeyParts parts{(float*)(pack + p.o), p.parts};
-    const Schedule plan = p.keys_plan.schedule(pack);
-    if (plan.items) schedule_keys(a, p.keys_plan, r.bounds, r.tiles, pack, s);
-    const dim3 grid((unsigned)(a.kv_heads * (plan.items ? p.keys_plan.items : a.batch * tiles * p.parts)));
+    const int* order = p.keys_plan.order(pack);
+    if (order) schedule_keys(a, p.keys_plan, r.bounds, r.tiles, pack, s);
+    const dim3 grid((unsigned)(a.batch * a.kv_heads * tiles * p.parts));
     by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) {
-        attend_keys<T, D, decltype(kind)::value, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts, plan);
+        attend_keys<T, D, decltype(kind)::value, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts, order);
     });
-    if (p.parts == 1 && !plan.items) return;
+    if (p.parts == 1) return;
     const int64_t threads = a.batch * a.kv_heads * tiles * kTileRows * (GRAD ? D / 2 : 1);
-    keys_join<T, D, GRAD><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, s>>>(a, sp, tiles, parts, plan.slots);
+    keys_join<T, D, GRAD><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, s>>>(a, sp, tiles, parts);
 }
 
 template <typename T, int D>
@@ -44,10 +44,10 @@ void launch_backward(const frog_attend_t& a, char* pack, hipStream_t s) {
     const int group = a.heads / a.kv_heads;
     const int qt = (int)((a.queries * group + kTileRows - 1) / kTileRows);
     launch_keys<T, D, true>(a, sp, p, r, pack, s);
-    const Schedule plan = p.rows_plan.schedule(pack);
-    if (plan.items) schedule_rows(a, p.rows_plan, pack, s);
-    const dim3 qg((unsigned)(a.kv_heads * (plan.items ? p.rows_plan.items : a.batch * qt)));
-    by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) { attend_dq<T, D, decltype(kind)::value, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r, plan); });
+    const int* order = p.rows_plan.order(pack);
+    if (order) schedule_rows(a, p.rows_plan, pack, s);
+    const dim3 qg((unsigned)(a.batch * a.kv_heads * qt));
+    by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) { attend_dq<T, D, decltype(kind)::value, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r, order); });
 }
 
 template <typename T>

@@ -10,11 +10,10 @@
 namespace frog {
 
 template <typename T, int D>
-void launch_tiles(const frog_attend_t& a, const ScoreParams& sp, int group, int tiles, const Parts& parts, const Schedule& plan, int64_t items,
-                  hipStream_t s) {
-    const dim3 grid((unsigned)(a.kv_heads * (plan.items ? items : a.batch * parts.splits * tiles)));
+void launch_tiles(const frog_attend_t& a, const ScoreParams& sp, int group, int tiles, const Parts& parts, const int* order, hipStream_t s) {
+    const dim3 grid((unsigned)(a.batch * a.kv_heads * parts.splits * tiles));
     by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) {
-        attend_tile<T, D, decltype(kind)::value, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, parts, plan);
+        attend_tile<T, D, decltype(kind)::value, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, parts, order);
     });
 }
 
@@ -27,9 +26,9 @@ void launch_forward(const frog_attend_t& a, const ForwardPlan& p, char* ws, hipS
     frog_attend_t b = a;
     if (a.w_out && !a.lse) b.lse = (float*)(ws + p.lse);
     if (!p.few) {
-        const Schedule plan = p.plan.schedule(ws);
-        if (plan.items) schedule_rows(a, p.plan, ws, s);
-        launch_tiles<T, D>(b, sp, group, p.tiles, parts, plan, p.plan.items, s);
+        const int* order = p.plan.order(ws);
+        if (order) schedule_rows(a, p.plan, ws, s);
+        launch_tiles<T, D>(b, sp, group, p.tiles, parts, order, s);
         if (p.splits > 1) attend_join<T, D><<<dim3((unsigned)((parts.total + 3) / 4)), 256, 0, s>>>(b, group, parts);
         if (a.w_out) AttendLaunch<T>::weigh(b, b.lse, ws + p.pack, s);
         return;
@@ -91,7 +90,7 @@ void launch_shared(const frog_attend_shared_t& a, const SharedPlan& p, char* ws,
             q.slopes = a.slopes, q.at_q = (const float*)(ws + p.at_q), q.at_k = (const float*)(ws + p.at_k);
             shared_places<<<dim3((unsigned)((std::max(a.prefix, a.batch) + 255) / 256)), 256, 0, s>>>(a, (float*)(ws + p.at_q), (float*)(ws + p.at_k));
         }
-        launch_tiles<T, D>(q, sp, group, p.tiles, prefix, Schedule{}, 0, s);
+        launch_tiles<T, D>(q, sp, group, p.tiles, prefix, nullptr, s);
     }
     if (head + p.tail_blocks > 0) {
         const dim3 grid((unsigned)(head + p.tail_blocks));

@@ -176,6 +176,13 @@ struct Tile {
     }
 };
 
+// x, of which the compiler does not know that it is the same in every step of a
+// loop: what is computed from it is not kept in registers between them
+__device__ inline int fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // row r of an accumulator register
 __device__ inline int acc_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
@@ -262,35 +269,22 @@ struct QueryRow {
     }
 };
 
-// What the workgroups of a pass over tiles (of query rows or of keys) do: part
-// `part` of `parts` of tile `tile` of sequence b; the parts of a key tile lie at
-// slot `slot` + part.  With a schedule (Schedule::items: sequence * tiles + tile,
-// part, parts, slot; an item below 0 is none) tiles come longest first, and
-// those of keys may differ in their number of parts; without one later tiles
-// come first, which is the order of their lengths under a causal mask.
-struct Schedule {
-    const int4* items;    // null: none
-    const int2* slots;    // of every sequence * tiles + tile: its first slot, its parts
-};
+// What a workgroup of a pass over tiles (of query rows or of keys) does: part
+// `part` of tile `tile` of sequence b.  order (sequence * tiles + tile): longest
+// first; null: later tiles first, which is that under a causal mask.
 struct Work {
     int64_t b;
-    int tile, part, parts, slot;
-    __device__ inline Work(const int4* items, uint32_t i, int64_t batch, int tiles, int parts_) {
-        if (items) {
-            const int4 it = items[i];
-            const int item = __builtin_amdgcn_readfirstlane(it.x);
-            b = max(item, 0) / tiles;
-            tile = item < 0 ? -1 : item % tiles;
-            part = __builtin_amdgcn_readfirstlane(it.y);
-            parts = __builtin_amdgcn_readfirstlane(it.z);
-            slot = __builtin_amdgcn_readfirstlane(it.w);
+    int tile, part;
+    __device__ inline Work(const int* order, uint32_t i, int64_t batch, int tiles, int parts) {
+        part = (int)(i % (uint32_t)parts);
+        const uint32_t rest = i / (uint32_t)parts;
+        if (order) {
+            const uint32_t item = (uint32_t)__builtin_amdgcn_readfirstlane(order[rest]);
+            b = item / (uint32_t)tiles;
+            tile = (int)(item % (uint32_t)tiles);
         } else {
-            parts = parts_;
-            part = (int)(i % (uint32_t)parts_);
-            const uint32_t rest = i / (uint32_t)parts_;
             b = rest % (uint32_t)batch;
             tile = tiles - 1 - (int)(rest / (uint32_t)batch);
-            slot = ((int)b * tiles + tile) * parts_;
         }
     }
 };
