@@ -190,8 +190,9 @@ class _Call:
         grads = (x for t in (dout, dq, dk, dv) for x in (t.data_ptr(), *t.stride()[:3]))
         head = (*self.rows, out.data_ptr(), *out.stride()[:3], *self.masks, lse.data_ptr(), 0, 0, *grads)
         args, ws, L = _pack_attend(*head, 0, 0, *self.tail), None, lib()
-        if _own_workspace(q.numel() > 2 ** 22 or k.numel() > 2 ** 22):
-            ws, at = _workspace(lambda x: L.frog_attend_workspace(x, 1), args, self.device)
+        n = L.frog_attend_workspace(args, 1)
+        if _own_workspace(n > 2 ** 26):
+            ws, at = _workspace(lambda x: n, args, self.device)
             args = _pack_attend(*head, *at, *self.tail)
         _launch(L.frog_attend_backward, args, self.device)
         return dq, dk, dv
@@ -233,6 +234,9 @@ def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_
     weights: float32 [batch, kv_heads, keys]; the call then also returns these
     plus the weight each key received, summed over queries and the group's
     heads, in a new tensor or in weights_out (may be ``weights``).
+
+    stream: where the work is enqueued (default: the current stream); inputs
+    written on another stream have to be waited for there, as for any kernel.
 
     Returns out [batch, queries, heads, d], followed by lse [batch, heads,
     queries] (return_lse) and the new weights (weights given).  q, k and v

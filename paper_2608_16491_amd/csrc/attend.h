@@ -94,10 +94,18 @@ __device__ inline float fine_tanh(const ScoreParams& s, float y, float r) {
     return s.cap2 * (fabsf(w) < 0.35f ? t : fmaf(-2.f, r, 1.f));
 }
 
+// r of N products (kCapped: z2 = capL - 2 capL r is left to the exponent's
+// multiply-add, and the largest score is the one of the least r)
+template <int N, typename V>
+__device__ inline void cap_shares(const ScoreParams& s, V& z) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = rcp_fast(1.f + exp2_fast(z[i] * s.mul));
+}
+
 // capped z2 of N products, without the distance bias
-template <Scores S, int N, typename V>
+template <int N, typename V>
 __device__ inline void cap_scores(const ScoreParams& s, V& z) {
-    if (S == kAny && s.fine) {
+    if (s.fine) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float y = z[i] * s.mul;

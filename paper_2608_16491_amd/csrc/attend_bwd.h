@@ -8,7 +8,7 @@ namespace frog {
 
 // What the passes that own keys need of 32 query rows at a time, prepared once
 // per call: per (sequence, kv head) and tile of 32 rows a block of floats
-// (lse in log2 units, +inf for a row without keys; delta = dout . out; the
+// (lse in log2 units, less capL for kCapped, +inf for a row without keys; delta = dout . out; the
 // interval, as integers; bias slope and attribute), per (sequence, tile) the
 // least and largest key of the rows' intervals, and the keys all of them see
 // (z > w when a row has none), and a row of zeros that stands for the rows
@@ -22,7 +22,7 @@ struct RowPack {
 };
 
 template <typename T, int D, bool GRAD>
-__global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, RowPack pack, const float* lse) {
+__global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, RowPack pack, const float* lse, float shift) {
     const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
     if (blockIdx.x == 0 && threadIdx.x < 128) ((float*)pack.zeros)[threadIdx.x] = 0.f;
     const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), pairs = a.batch * a.kv_heads;
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, Row
     if (h == 0) {
         // (-inf: no key, or a bias that leaves none a weight)
         const float z = some ? lse[stat] : -INFINITY;
-        out[RowPack::kLse + i] = z > -INFINITY ? z * kLog2e : INFINITY;
+        out[RowPack::kLse + i] = z > -INFINITY ? fmaf(z, kLog2e, -shift) : INFINITY;
         out[RowPack::kLo + i] = __int_as_float(lo);
         out[RowPack::kHi + i] = __int_as_float(hi);
         out[RowPack::kSlope + i] = a.slopes ? a.slopes[q.head] * kLog2e : 0.f;
@@ -125,7 +125,7 @@ struct KeyParts {
 };
 
 // f = 4 r (1 - r), r = 1 / (1 + exp2(c1 dot)): the derivative of the cap, of 16
-// products z, which become the capped scores
+// products z, which become the capped scores (kCapped: r, as in cap_shares)
 template <Scores S>
 __device__ inline void cap_slopes(const ScoreParams& sp, acc16& z, acc16& f) {
     auto each = [&](auto fine) {
@@ -133,7 +133,7 @@ __device__ inline void cap_slopes(const ScoreParams& sp, acc16& z, acc16& f) {
         for (int i = 0; i < 16; ++i) {
             const float y = z[i] * sp.mul, r = rcp_fast(1.f + exp2_fast(y)), r4 = 4.f * r;
             if constexpr (decltype(fine)::value) z[i] = fine_tanh(sp, y, r);
-            else z[i] = fmaf(-2.f * sp.cap2, r, sp.cap2);
+            else z[i] = S == kCapped ? r : fmaf(-2.f * sp.cap2, r, sp.cap2);
             f[i] = fmaf(-r4, r, r4);
         }
     };
@@ -238,11 +238,12 @@ void attend_keys(frog_attend_t a, ScoreParams sp, int group, int key_tiles, RowP
                 }
             }
         }
+        const float mul = KIND == kCapped ? -2.f * sp.cap2 : sp.mul;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const vec<float, 4> lse = *(const vec<float, 4>*)(ps + RowPack::kLse + 8 * i + 4 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[4 * i + e] = weight2(PLAIN ? fmaf(z[4 * i + e], sp.mul, -lse[e]) : z[4 * i + e] - lse[e]);
+            for (int e = 0; e < 4; ++e) z[4 * i + e] = weight2(PLAIN || KIND == kCapped ? fmaf(z[4 * i + e], mul, -lse[e]) : z[4 * i + e] - lse[e]);
         }
         const bool whole = bd.z <= wfirst && bd.w >= wlast;
         if (!whole) {
@@ -504,9 +505,10 @@ void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pa
                 }
             }
             // (all rows here are finite: what no interval meets was cleared)
-            if (j < flo || j + 31 > fhi) mask_scores<1>(z, lo - j, hi - j, lane);
+            if (j < flo || j + 31 > fhi) mask_scores<1>(z, lo - j, hi - j, lane, KIND == kCapped ? INFINITY : -INFINITY);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) z[0][r] = weight2(PLAIN ? fmaf(z[0][r], sp.mul, -lse) : z[0][r] - lse);
+            for (int r = 0; r < 16; ++r)
+                z[0][r] = weight2(PLAIN || KIND == kCapped ? fmaf(z[0][r], KIND == kCapped ? -2.f * sp.cap2 : sp.mul, -lse) : z[0][r] - lse);
             if (capped<KIND>(sp)) z[0] *= f;
             acc16 dp = acc16{} - delta;
 #pragma unroll

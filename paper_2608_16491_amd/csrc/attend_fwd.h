@@ -121,7 +121,10 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
         if constexpr (!PLAIN) {
             if (capped<KIND>(sp)) {
 #pragma unroll
-                for (int n = 0; n < S; ++n) cap_scores<KIND, 16>(sp, z[n]);
+                for (int n = 0; n < S; ++n) {
+                    if constexpr (KIND == kCapped) cap_shares<16>(sp, z[n]);
+                    else cap_scores<16>(sp, z[n]);
+                }
             } else {
 #pragma unroll
                 for (int n = 0; n < S; ++n) z[n] *= sp.mul;
@@ -137,13 +140,13 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
                     }
             }
         }
-        if (j < flo || j + N - 1 > fhi) mask_scores<S>(z, lo - j, hi - j, lane);
+        if (j < flo || j + N - 1 > fhi) mask_scores<S>(z, lo - j, hi - j, lane, KIND == kCapped ? INFINITY : -INFINITY);
         float mx = z[0][0];
 #pragma unroll
         for (int n = 0; n < S; ++n)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) mx = fmaxf(mx, z[n][r]);
-        mx = half_max(PLAIN ? mx * sp.mul : mx);
+            for (int r = 0; r < 16; ++r) mx = KIND == kCapped ? fminf(mx, z[n][r]) : fmaxf(mx, z[n][r]);
+        mx = half_max(PLAIN ? mx * sp.mul : KIND == kCapped ? fmaf(mx, -2.f * sp.cap2, sp.cap2) : mx);
         // the sums are scaled anew only when a row's maximum has grown by more
         // than 2^8: weights up to 256 keep their precision in every type
         if (__any(mx > top + 8.f)) {
@@ -153,11 +156,12 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
 #pragma unroll
             for (int m = 0; m < M; ++m) o[m] *= f;
         }
+        const float mul = KIND == kCapped ? -2.f * sp.cap2 : sp.mul, add = KIND == kCapped ? sp.cap2 - top : -top;
 #pragma unroll
         for (int n = 0; n < S; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                z[n][r] = exp2_fast(PLAIN ? fmaf(z[n][r], sp.mul, -top) : z[n][r] - top);
+                z[n][r] = exp2_fast(PLAIN || KIND == kCapped ? fmaf(z[n][r], mul, add) : z[n][r] - top);
                 sum += z[n][r];
             }
 #pragma unroll
@@ -367,7 +371,7 @@ struct FewPass {
 #pragma unroll
             for (int g = 0; g < RG; ++g) {
                 if (!PLAIN && sp.cap2 > 0.f) {
-                    cap_scores<kAny, 8>(sp, z[g]);
+                    cap_scores<8>(sp, z[g]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) z[g][e] *= sp.mul;

@@ -187,9 +187,9 @@ __device__ inline int fresh(int x) {
 __device__ inline int acc_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
 // Scores of keys outside lo..hi (numbers within the tile; the lane's query)
-// become -inf.
+// become `out`.
 template <int S>
-__device__ inline void mask_scores(acc16 (&z)[S], int lo, int hi, int lane) {
+__device__ inline void mask_scores(acc16 (&z)[S], int lo, int hi, int lane, float out) {
     const int at = 4 * (lane >> 5);
     lo -= at;
     hi -= at;
@@ -198,7 +198,7 @@ __device__ inline void mask_scores(acc16 (&z)[S], int lo, int hi, int lane) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int c = 32 * n + acc_row(r, 0);
-            z[n][r] = c >= lo && c <= hi ? z[n][r] : -INFINITY;
+            z[n][r] = c >= lo && c <= hi ? z[n][r] : out;
         }
 }
 
