@@ -57,10 +57,11 @@ constexpr int64_t kWholeKeys = 1024;
 // (Cutting long tiles into more parts than short ones made dk and dv 319 us
 // there, but their parts' traffic and that of the forward pass took it back.)
 constexpr int64_t kScheduleLength = 2048, kScheduleTiles = 65536;
-SchedulePlan schedule_plan(const frog_attend_t& a, int64_t tiles) {
+SchedulePlan schedule_plan(const frog_attend_t& a, int64_t tiles, int parts) {
     SchedulePlan p{};
     if (!a.lr || std::min(a.keys, a.queries) < kScheduleLength || a.batch * tiles > kScheduleTiles) return p;
     p.tiles = tiles;
+    p.parts = parts;
     p.bytes = a.batch * tiles * 8;
     return p;
 }
@@ -78,7 +79,7 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     const int64_t blocks = pairs * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
     p.splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / std::max<int64_t>(blocks, 1), (a.keys + least - 1) / least));
     if (p.few && p.groups == 1 && a.keys <= kWholeKeys) p.splits = 1;
-    if (!p.few) p.plan = schedule_plan(a, p.tiles);
+    if (!p.few) p.plan = schedule_plan(a, p.tiles, p.splits);
     int64_t at = 0;
     p.plan.at = take(&at, p.plan.bytes);
     if (p.splits > 1) {
@@ -105,8 +106,8 @@ PackPlan pack_plan(const frog_attend_t& a, bool grad) {
     const int64_t blocks = a.batch * a.kv_heads * ((a.keys + kTileRows - 1) / kTileRows);
     p.parts = (int)std::max<int64_t>(1, std::min((1024 + blocks - 1) / std::max<int64_t>(blocks, 1), p.tiles / 8));
     const int64_t key_tiles = (a.keys + kTileRows - 1) / kTileRows, row_tiles = (p.tiles + 3) / 4;
-    p.keys_plan = schedule_plan(a, key_tiles);
-    if (grad) p.rows_plan = schedule_plan(a, row_tiles);
+    p.keys_plan = schedule_plan(a, key_tiles, p.parts);
+    if (grad) p.rows_plan = schedule_plan(a, row_tiles, 1);
     int64_t at = 0;
     p.keys_plan.at = take(&at, p.keys_plan.bytes);
     p.rows_plan.at = take(&at, p.rows_plan.bytes);
@@ -147,12 +148,14 @@ __global__ void fill_lse(float* lse, int64_t n) {
 namespace {
 
 // Tiles longest first, by one workgroup counting in 1,024 classes of equal width
-// (of a class in any order: it changes no result).  order: the tiles, and as
-// many lengths.  length(tile) is called by whole wavefronts (WAVE) or by single
-// threads.
+// (of a class in any order: it changes no result).  The workgroups of the first
+// `wave` tiles take a CU each; those of the next `wave`, which join them there,
+// come shortest first, so that the CU with the longest gets the shortest beside
+// it.  order: the tiles, and as many lengths.  length(tile) is called by whole
+// wavefronts (WAVE) or by single threads.
 constexpr int kSortBlock = 1024;
 template <bool WAVE, typename F>
-__device__ inline void longest_first(int tiles, int* order, F&& length) {
+__device__ inline void longest_first(int tiles, int wave, int* order, F&& length) {
     constexpr int HELD = 4 * kSortBlock;          // lengths kept in LDS, the others' behind the tiles
     __shared__ int held[HELD], hist[kSortBlock], wave_sum[kSortBlock / 64], most;
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
@@ -191,13 +194,16 @@ __device__ inline void longest_first(int tiles, int* order, F&& length) {
     hist[t] = x - own;
     __syncthreads();
     if (writes)
-        for (int i = first; i < tiles; i += step) order[atomicAdd(&hist[bin(i)], 1)] = i;
+        for (int i = first; i < tiles; i += step) {
+            const int at = atomicAdd(&hist[bin(i)], 1), end = min(2 * wave, tiles);
+            order[at >= wave && at < end ? wave + end - 1 - at : at] = i;
+        }
 }
 
 // Lengths of row tiles: the keys from the first to the last that the first,
 // middle and last token of a tile see.
-__global__ __launch_bounds__(kSortBlock) void schedule_row_tiles(frog_attend_t a, int group, int tiles, int* order) {
-    longest_first<false>((int)a.batch * tiles, order, [&](int item) {
+__global__ __launch_bounds__(kSortBlock) void schedule_row_tiles(frog_attend_t a, int group, int tiles, int wave, int* order) {
+    longest_first<false>((int)a.batch * tiles, wave, order, [&](int item) {
         const int64_t b = item / tiles, rows = a.queries * group, r0 = (int64_t)(item % tiles) * kTileRows, r1 = min(rows, r0 + kTileRows) - 1;
         const int64_t t0 = r0 / group, t1 = r1 / group, tokens[3] = {t0, (t0 + t1) / 2, t1};
         int first = INT_MAX, last = -1;
@@ -215,9 +221,9 @@ __global__ __launch_bounds__(kSortBlock) void schedule_row_tiles(frog_attend_t a
 
 // Lengths of key tiles: how many of at most 256 of the sequence's row tiles
 // (evenly spread) see one of its keys.
-__global__ __launch_bounds__(kSortBlock) void schedule_key_tiles(frog_attend_t a, int tiles, const int4* bounds, int row_tiles, int* order) {
+__global__ __launch_bounds__(kSortBlock) void schedule_key_tiles(frog_attend_t a, int tiles, const int4* bounds, int row_tiles, int wave, int* order) {
     const int lane = threadIdx.x & 63, stride = (row_tiles + 255) / 256;
-    longest_first<true>((int)a.batch * tiles, order, [&](int item) {
+    longest_first<true>((int)a.batch * tiles, wave, order, [&](int item) {
         const int4* of = bounds + (int64_t)(item / tiles) * row_tiles;
         const int first = item % tiles * kTileRows, last = (int)min((int64_t)first + kTileRows, a.keys) - 1;
         int n = 0;
@@ -233,12 +239,15 @@ __global__ __launch_bounds__(kSortBlock) void schedule_key_tiles(frog_attend_t a
 
 }  // namespace
 
+// tiles whose workgroups (of all kv heads) are one for each of the 256 CUs
+static int cu_tiles(const frog_attend_t& a, int parts) { return (int)std::max<int64_t>(1, 256 / ((int64_t)a.kv_heads * parts)); }
+
 void schedule_rows(const frog_attend_t& a, const SchedulePlan& p, char* ws, hipStream_t s) {
-    schedule_row_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, a.heads / a.kv_heads, (int)p.tiles, (int*)(ws + p.at));
+    schedule_row_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, a.heads / a.kv_heads, (int)p.tiles, cu_tiles(a, p.parts), (int*)(ws + p.at));
 }
 
 void schedule_keys(const frog_attend_t& a, const SchedulePlan& p, const int4* bounds, int row_tiles, char* ws, hipStream_t s) {
-    schedule_key_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, (int)p.tiles, bounds, row_tiles, (int*)(ws + p.at));
+    schedule_key_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, (int)p.tiles, bounds, row_tiles, cu_tiles(a, p.parts), (int*)(ws + p.at));
 }
 
 int64_t attend_ws(const frog_attend_t& a) { return empty(a) ? 0 : forward_plan(a).bytes; }

@@ -12,6 +12,7 @@ namespace frog {
 // The order in which a pass starts the tiles of a kv head (attend_tile.h: Work).
 struct SchedulePlan {
     int64_t tiles;     // of a sequence; 0: none
+    int parts;         // workgroups of a tile
     int64_t at, bytes;
     int* order(char* ws) const { return tiles ? (int*)(ws + at) : nullptr; }
 };
