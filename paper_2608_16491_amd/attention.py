@@ -9,6 +9,7 @@ import ctypes as C
 import struct
 
 import torch
+from torch.autograd import forward_ad
 
 from . import STORAGE_BF16, STORAGE_F16, STORAGE_F32, _check, lib
 
@@ -117,7 +118,17 @@ def _on(stream, call, inputs):
     return outs
 
 
+def _no_tangent(names, tensors):
+    """No derivative of forward mode enters a kernel: it would be left out of the result."""
+    if getattr(forward_ad, "_current_level", 0) < 0:      # (outside dual levels, without a look at the tensors)
+        return
+    for name, t in zip(names, tensors):
+        if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{name} carries a tangent: forward-mode derivatives are not supported")
+
+
 def _no_gradient(names, tensors):
+    _no_tangent(names, tensors)
     if torch.is_grad_enabled():
         for name, t in zip(names, tensors):
             if t is not None and t.requires_grad:
@@ -212,6 +223,7 @@ class _Attend(torch.autograd.Function):
     def backward(ctx, dout):
         # (the tensors may have moved since: hooks on saved tensors, recomputation)
         q, k, v, out, lse, lr, *bias = ctx.saved_tensors
+        _no_tangent(("the gradient of the output",), (dout,))
         size = 16 // dout.element_size()
         if dout.stride(-1) != 1 or dout.data_ptr() % 16 or any(s % size for s in dout.stride()[:-1]):
             dout = dout.contiguous()
@@ -240,7 +252,9 @@ def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_
 
     Returns out [batch, queries, heads, d], followed by lse [batch, heads,
     queries] (return_lse) and the new weights (weights given).  q, k and v
-    take gradients; lse and weights do not."""
+    take gradients; lse and weights do not, and no argument a tangent of
+    forward mode (ValueError)."""
+    _no_tangent(("q", "k", "v", "slopes", "at_q", "at_k", "weights", "weights_out"), (q, k, v, slopes, at_q, at_k, weights, weights_out))
     mask = (lr, scale, cap, slopes, at_q, at_k)
     call = _Call(q, k, v, *mask)
     if weights is not None:
@@ -276,6 +290,7 @@ def attend_shared(q, k, v, k_pages, v_pages, pages, lengths, *, lr=None, scale=N
     (None: all).  slopes [heads]: scores fall with the distance of the query,
     which stands on the last row of its tail.  Returns out [batch, heads, d],
     and lse [batch, heads] with return_lse."""
+    _no_gradient(("q", "k", "v", "k_pages", "v_pages", "slopes"), (q, k, v, k_pages, v_pages, slopes))
     kind = _values(("q", "k", "v", "k_pages", "v_pages"), (q, k, v, k_pages, v_pages), (3, 3, 3, 4, 4))
     b, h, d = q.shape
     tk, kv, _ = k.shape
@@ -284,7 +299,6 @@ def attend_shared(q, k, v, k_pages, v_pages, pages, lengths, *, lr=None, scale=N
         raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, pages {tuple(k_pages.shape)}, {tuple(v_pages.shape)}: "
                          "[batch, heads, d], twice [prefix, kv_heads, d], twice [num_pages, page, kv_heads, d] are wanted")
     _need(pages.dim() == 2, "pages: [batch, pages_per_request] is wanted")
-    _no_gradient(("q", "k", "v", "k_pages", "v_pages", "slopes"), (q, k, v, k_pages, v_pages, slopes))
     outs = _on(stream, lambda: _attend_shared(kind, q, k, v, k_pages, v_pages, pages, lengths, lr, scale, cap, slopes, return_lse),
                (q, k, v, k_pages, v_pages, pages, lengths, lr, slopes))
     return outs if return_lse else outs[0]
@@ -318,12 +332,12 @@ def evict(k, v, weights, positions, lengths, keep, *, recent=0, stream=None):
     the slots) [batch, heads, slots]; lengths int32 [batch].  Returns new
     (k, v, weights, positions, lengths) with ``keep`` slots; those past a
     length hold 0, 0, 0 and -1."""
+    _no_gradient(("k", "v", "weights"), (k, v, weights))
     kind = _values(("k", "v"), (k, v), (4, 4))
     b, t, h, d = k.shape
     if v.shape != k.shape or not 0 <= recent <= keep <= t:
         raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}, recent {recent}, keep {keep}: the same shape and "
                          "0 <= recent <= keep <= slots are wanted")
-    _no_gradient(("k", "v", "weights"), (k, v, weights))
     return _on(stream, lambda: _evict(kind, k, v, weights, positions, lengths, keep, recent), (k, v, weights, positions, lengths))
 
 

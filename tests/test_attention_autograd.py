@@ -1,0 +1,61 @@
+"""What the attention binding does where torch differentiates around it:
+forward mode, tensors written in place, gradients in unusual memory."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from torch.autograd import forward_ad  # noqa: E402
+
+import paper_2608_16491_amd as F  # noqa: E402
+
+# the refusals that come before any GPU is touched run on the CPU too
+DEVICES = ["cpu", pytest.param("cuda", marks=pytest.mark.gpu)]
+
+
+def tensors(device, b=2, tq=3, tk=20, h=4, kv=2, d=64, dtype=torch.bfloat16, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randn(shape, generator=g).to(dtype).to(device) for shape in ((b, tq, h, d), (b, tk, kv, d), (b, tk, kv, d))]
+
+
+def calls(device):
+    """Every operator with its arguments by name, and those that hold real numbers."""
+    q, k, v = tensors(device)
+    f = dict(device=device, dtype=torch.float32)
+    n = dict(device=device, dtype=torch.int32)
+    attend = dict(q=q, k=k, v=v, slopes=torch.ones(4, **f), at_q=torch.zeros((2, 3), **f), at_k=torch.zeros((2, 20), **f),
+                  weights=torch.zeros((2, 2, 20), **f), weights_out=torch.zeros((2, 2, 20), **f))
+    shared = dict(q=q[:, 0].contiguous(), k=k[0], v=v[0], k_pages=k, v_pages=v, slopes=torch.ones(4, **f))
+    cache = dict(k=k, v=v, weights=torch.zeros((2, 2, 20), **f))
+    return [(F.attend, attend, {}), (F.attend_shared, shared, dict(pages=torch.zeros((2, 1), **n), lengths=torch.ones(2, **n))),
+            (F.evict, cache, dict(positions=None, lengths=torch.full((2,), 20, **n), keep=10))]
+
+
+@pytest.mark.parametrize("device", DEVICES)
+@pytest.mark.parametrize("no_grad", [False, True])
+def test_tangents_are_refused(device, no_grad):
+    for fn, real, others in calls(device):
+        for name in real:
+            with forward_ad.dual_level(), torch.set_grad_enabled(not no_grad):
+                dual = {name: forward_ad.make_dual(real[name], torch.ones_like(real[name]))}
+                with pytest.raises(ValueError, match=f"^{name} carries a tangent"):
+                    fn(**{**real, **dual}, **others)
+
+
+@pytest.mark.gpu
+def test_calls_within_a_dual_level_whose_tensors_have_no_tangent():
+    for fn, real, others in calls("cuda"):
+        want = fn(**real, **others)
+        with forward_ad.dual_level():
+            got = fn(**real, **others)
+        assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.gpu
+def test_a_tangent_of_the_outputs_gradient_is_refused():
+    # forward over reverse, of a factor behind the call
+    q, k, v = (t.requires_grad_() for t in tensors("cuda"))
+    out = F.attend(q, k, v)
+    with forward_ad.dual_level():
+        dout = forward_ad.make_dual(torch.ones_like(out), torch.ones_like(out))
+        with pytest.raises(ValueError, match="carries a tangent"):
+            torch.autograd.grad(out, (q, k, v), dout)
