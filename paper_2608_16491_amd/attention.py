@@ -275,6 +275,8 @@ def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_
         return _Attend.apply(q, k, v, call, mask, weights, new, kept), kept[0], new
 
     out, lse, new = _on(stream, run, (q, k, v, lr, slopes, at_q, at_k, weights, weights_out))
+    if weights_out is not None and not weights_out.is_inference():
+        torch.autograd.graph.increment_version(weights_out)      # (written by address: autograd has to hear of it)
     if not return_lse and weights is None:
         return out
     return (out,) + ((lse,) if return_lse else ()) + ((new,) if weights is not None else ())

@@ -59,3 +59,31 @@ def test_a_tangent_of_the_outputs_gradient_is_refused():
         dout = forward_ad.make_dual(torch.ones_like(out), torch.ones_like(out))
         with pytest.raises(ValueError, match="carries a tangent"):
             torch.autograd.grad(out, (q, k, v), dout)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("same", [False, True])
+def test_weights_written_in_place_are_seen_by_autograd(same):
+    # an earlier product kept the tensor for its gradient: once written, that gradient must not be computed from it
+    q, k, v = tensors("cuda")
+    w, into = (torch.rand((2, 2, 20), device="cuda") for _ in range(2))
+    into = w if same else into
+    x = torch.rand((2, 2, 20), device="cuda", requires_grad=True)
+    y, before = (x * into).sum(), into._version
+    with torch.no_grad():
+        F.attend(q, k, v, weights=w, weights_out=into)
+    assert into._version > before and (same or w._version == 0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    # a view of a larger tensor, of which autograd counts one version for all
+    whole = torch.rand((2, 2, 2, 20), device="cuda")
+    y = (x * whole[1]).sum()
+    F.attend(q, k, v, weights=w, weights_out=whole[0])
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    # tensors without versions are written as before
+    with torch.inference_mode():
+        kept = torch.zeros((2, 2, 20), device="cuda")
+        _, got = F.attend(q, k, v, weights=kept, weights_out=kept)
+    assert got is kept and bool(kept.any())
+    F.attend(q, k, v, weights=w, weights_out=kept)
