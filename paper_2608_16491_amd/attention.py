@@ -226,7 +226,8 @@ class _Attend(torch.autograd.Function):
         _no_tangent(("the gradient of the output",), (dout,))
         size = 16 // dout.element_size()
         if dout.stride(-1) != 1 or dout.data_ptr() % 16 or any(s % size for s in dout.stride()[:-1]):
-            dout = dout.contiguous()
+            # (a copy in new memory: contiguous() returns a tensor that only starts off a boundary as it is)
+            dout = dout.clone(memory_format=torch.contiguous_format)
         call = _Call(q, k, v, lr, ctx.scale, ctx.cap, *bias)
         return (*call.backward(q, k, v, out, lse, dout), None, None, None, None, None)
 

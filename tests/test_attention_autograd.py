@@ -87,3 +87,29 @@ def test_weights_written_in_place_are_seen_by_autograd(same):
         _, got = F.attend(q, k, v, weights=kept, weights_out=kept)
     assert got is kept and bool(kept.any())
     F.attend(q, k, v, weights=w, weights_out=kept)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gradients_handed_in_off_alignment(dtype):
+    q, k, v = (t.requires_grad_() for t in tensors("cuda", dtype=dtype))
+    out = F.attend(q, k, v)
+    g = torch.randn(out.shape, device="cuda").to(dtype)
+    want = torch.autograd.grad(out, (q, k, v), g, retain_graph=True)
+
+    def placed(n):
+        # contiguous, n values behind a boundary
+        t = torch.empty(g.numel() + n, device="cuda", dtype=dtype)[n:].view(g.shape)
+        t.copy_(g)
+        return t
+
+    wide = torch.empty(*g.shape[:-1], 67, device="cuda", dtype=dtype)       # rows 67 values apart
+    wide[..., :64] = g
+    for dout in (placed(0), placed(1), placed(3), placed(4), wide[..., :64], g.transpose(1, 2).contiguous().transpose(1, 2)):
+        got = torch.autograd.grad(out, (q, k, v), dout, retain_graph=True)
+        assert all(torch.equal(a, b) for a, b in zip(want, got)), (dout.data_ptr() % 16, dout.stride())
+    # as a program comes by one: an odd number of values joined in front
+    want = torch.autograd.grad(F.attend(q, k, v).flatten(), (q, k, v), g.flatten())
+    joined = torch.cat([torch.ones(1, device="cuda", dtype=dtype), F.attend(q, k, v).flatten()])
+    got = torch.autograd.grad(joined, (q, k, v), torch.cat([torch.ones(1, device="cuda", dtype=dtype), g.flatten()]))
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
