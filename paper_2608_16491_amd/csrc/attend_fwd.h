@@ -336,7 +336,7 @@ struct FewPass {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const auto at = Keys::of(mine, row_of(e), j, last);
-                vv[e] = load_piece(keys.value(at) + C * c);
+                vv[e] = load_piece<T, C>(keys.value(at) + C * c);
                 if (Keys::kPaged) coming |= (uint32_t)Keys::real(at) << e;
             }
         };
@@ -438,25 +438,6 @@ struct FewPass {
             if (!more) break;
             j64 = next;
         }
-    }
-
-    // D / 16 values from an address of that alignment (4, 8, 12, 16 or 32 bytes)
-    __device__ static inline vec<T, C> load_piece(const T* p) {
-        vec<T, C> x;
-        constexpr int words = C * sizeof(T) / 4;
-        uint32_t r[words];
-        if constexpr (words % 4 == 0) {
-#pragma unroll
-            for (int i = 0; i < words / 4; ++i) *(uint4*)(r + 4 * i) = ((const uint4*)p)[i];
-        } else if constexpr (words % 2 == 0) {
-#pragma unroll
-            for (int i = 0; i < words / 2; ++i) *(uint2*)(r + 2 * i) = ((const uint2*)p)[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < words; ++i) r[i] = ((const uint32_t*)p)[i];
-        }
-        __builtin_memcpy(&x, r, sizeof(x));
-        return x;
     }
 
     // Joins the W wavefronts' results: pairs of halves, through LDS in the

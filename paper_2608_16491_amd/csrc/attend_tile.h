@@ -54,6 +54,28 @@ __device__ inline frag<T> load_frag(const T* p) {   // 16-byte aligned
     }
 }
 
+// C values from an address of their alignment (4, 8, 12, 16, 24 or 32 bytes).  A
+// vector of six takes the memory of eight: what is copied is what was read.
+template <typename T, int C>
+__host__ __device__ inline vec<T, C> load_piece(const T* p) {
+    constexpr int words = C * sizeof(T) / 4;
+    uint32_t r[words];
+    vec<T, C> x;
+    static_assert(sizeof(r) == C * sizeof(T) && sizeof(r) <= sizeof(x), "whole words");
+    if constexpr (words % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < words / 4; ++i) *(uint4*)(r + 4 * i) = ((const uint4*)p)[i];
+    } else if constexpr (words % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < words / 2; ++i) *(uint2*)(r + 2 * i) = ((const uint2*)p)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < words; ++i) r[i] = ((const uint32_t*)p)[i];
+    }
+    __builtin_memcpy(&x, r, sizeof(r));
+    return x;
+}
+
 // max or sum over lanes L and L ^ 32, in both
 __device__ inline float half_max(float x) {
     auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
