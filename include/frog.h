@@ -241,7 +241,8 @@ int frog_search(const frog_index_t* idx, const float* d_queries, int64_t nq,
  * keeps per (device, stream) for the life of the process, grown
  * stream-ordered when a call needs more, so repeated calls allocate nothing;
  * threads enqueueing on one stream take turns, other streams have their own
- * buffer. */
+ * buffer.  (On hipStreamPerThread, a stream of each thread under one handle,
+ * the buffer is allocated for the call and freed after it, in stream order.) */
 int frog_search_ex(const frog_index_t* idx, const float* d_queries, int64_t nq,
                    const double* d_lo, const double* d_hi, int k, int L,
                    const frog_search_params_t* p, int32_t* d_ids, float* d_dists,

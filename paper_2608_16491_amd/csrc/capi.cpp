@@ -852,6 +852,15 @@ Slot* slot_for(hipStream_t stream, hipError_t* err) {
 hipError_t WsLease::acquire(hipStream_t stream, size_t bytes, void** ptr) {
     release();
     hipError_t e = hipSuccess;
+    // One handle that names another stream in every thread: a buffer kept for
+    // it would be shared by streams nothing orders.  The call has one of its
+    // own, from the pool and back to it in the order of the caller's stream.
+    if (stream == hipStreamPerThread) {
+        e = ws_alloc(&own_, bytes, stream);
+        if (e != hipSuccess) own_ = nullptr;
+        *ptr = own_;
+        return e;
+    }
     Slot* sl = slot_for(stream, &e);
     if (!sl) return e;
     sl->mu.lock();
@@ -878,6 +887,10 @@ hipError_t WsLease::acquire(hipStream_t stream, size_t bytes, void** ptr) {
 }
 
 void WsLease::release() {
+    if (own_) {
+        (void)ws_free(own_, hipStreamPerThread);
+        own_ = nullptr;
+    }
     if (!slot_) return;
     slot_->mu.unlock();
     slot_ = nullptr;

@@ -20,7 +20,9 @@ hipError_t ws_free(void* ptr, hipStream_t stream);
 // the buffer's lock while the caller enqueues (two threads on one stream take
 // turns; other streams have buffers of their own).  Earlier uses of a
 // stream's buffer were enqueued on the same stream, so stream order keeps
-// them apart; no event or marker is added to the stream.
+// them apart; no event or marker is added to the stream.  (hipStreamPerThread
+// is as many streams as there are threads: there a lease allocates and frees,
+// stream-ordered, for its call alone.)
 struct Slot;
 
 class WsLease {
@@ -31,11 +33,13 @@ class WsLease {
     ~WsLease() { release(); }
     // a buffer of at least `bytes` on `stream`; *ptr receives it
     hipError_t acquire(hipStream_t stream, size_t bytes, void** ptr);
-    // after the call's last enqueue (also done by the destructor)
+    // after the call's last enqueue, in the thread that made it (also done by
+    // the destructor)
     void release();
 
   private:
     Slot* slot_ = nullptr;
+    void* own_ = nullptr;    // the call's own buffer (hipStreamPerThread)
 };
 
 }  // namespace frog
