@@ -349,7 +349,8 @@ typedef struct {
     void* dv; int64_t dv_stride[3];
     /* workspace of at least frog_attend_workspace() bytes, 256-byte aligned,
      * the caller's until `stream` has run the call; NULL: the library's
-     * buffer of (device, stream), as for frog_search_ex */
+     * buffer of (device, stream), as for frog_search_ex (FROG_EINVAL while
+     * `stream` is captured into a graph: the graph has to keep its own) */
     void* ws;
     int64_t ws_bytes;
     int64_t batch, queries, keys;

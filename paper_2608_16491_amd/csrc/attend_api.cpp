@@ -147,9 +147,15 @@ int with_ws(const A& a, int64_t bytes, hipStream_t stream, F&& launch) {
         if (a.ws_bytes < bytes) return fail(FROG_EINVAL, "workspace of %lld bytes, %lld needed", (long long)a.ws_bytes, (long long)bytes);
         return launch(a.ws);
     }
+    // A graph outlives the call, and the library's buffer may be freed for a
+    // larger one or serve another call between replays.
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    hipError_t e = hipStreamIsCapturing(stream, &capture);
+    if (e != hipSuccess) return fail(FROG_EHIP, "capture status of the stream: %s", hipGetErrorString(e));
+    if (capture != hipStreamCaptureStatusNone) return fail(FROG_EINVAL, "a call under graph capture takes the caller's workspace (%lld bytes)", (long long)bytes);
     WsLease lease;
     void* p = nullptr;
-    hipError_t e = lease.acquire(stream, (size_t)bytes, &p);
+    e = lease.acquire(stream, (size_t)bytes, &p);
     if (e != hipSuccess) return fail(e == hipErrorOutOfMemory ? FROG_ENOMEM : FROG_EHIP, "workspace of %lld bytes: %s", (long long)bytes, hipGetErrorString(e));
     return launch(p);
 }

@@ -61,3 +61,39 @@ def test_search_on_the_stream_of_each_thread():
     torch.cuda.synchronize()
     for a in got:
         assert all(torch.equal(x, y) for x, y in zip(a, want))
+
+
+def test_a_captured_call_takes_the_callers_workspace(monkeypatch):
+    # the binding brings one; without it the call is refused, and so is none that needs no workspace
+    q, k, v, w, lengths = inputs(1, 3000)
+    shared = dict(q=q[:, 0].contiguous(), k=k[0], v=v[0], k_pages=k[:, :64].contiguous(), v_pages=v[:, :64].contiguous(),
+                  pages=torch.zeros((2, 1), device="cuda", dtype=torch.int32), lengths=torch.ones(2, device="cuda", dtype=torch.int32))
+    calls = (lambda: F.attend(q, k, v), lambda: F.attend(q, k, v, weights=w), lambda: F.attend_shared(**shared),
+             lambda: F.evict(k, v, w, None, lengths, 1000))
+    want = [f() for f in calls]
+    small = F.attend(q, k[:, :100].contiguous(), v[:, :100].contiguous())
+    ks, vs = k[:, :100].contiguous(), v[:, :100].contiguous()
+    codes = []
+    with monkeypatch.context() as m:
+        m.setattr(A, "_own_workspace", lambda large: False)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for f in calls:
+                try:
+                    f()
+                except F.FrogError as e:
+                    codes.append(e.code)
+            got = F.attend(q, ks, vs)
+        assert codes == [-1] * 4
+        for _ in range(2):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got, small)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = [f() for f in calls]
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(x, y) for x, y in zip(a if isinstance(a, tuple) else (a,), b if isinstance(b, tuple) else (b,)))
