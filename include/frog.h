@@ -322,7 +322,9 @@ int frog_bruteforce_filtered(const frog_index_t* idx, const float* d_queries, in
  * Strides count values; the last axis (d values) is contiguous.  Every row
  * must start on a 16-byte boundary (pointers and strides), else FROG_EINVAL.
  * d is 32, 64, 96 or 128 (FROG_EUNSUPPORTED otherwise: pad with zeros), and
- * one key of k and v at most 16 MiB from the next.
+ * one key of k and v at most 16 MiB from the next.  A pass of more workgroups
+ * than one launch takes (2^32 threads: 2^31 query rows; of single tokens 2^23
+ * sequences x kv heads) is FROG_EUNSUPPORTED.
  * Calls run on the current HIP device.  The structs may be zeroed first; a
  * zero pointer leaves an optional argument out. */
 typedef struct {

@@ -118,8 +118,8 @@ __device__ inline void cap_scores(const ScoreParams& s, V& z) {
 }
 
 // launchers (attend.hip, evict.hip).  The
-// arguments have been checked (attend_api.cpp); ws holds the bytes of the
-// matching *_ws call.
+// arguments have been checked (attend_api.cpp), and the matching *_ws call, which
+// gives the bytes of ws, has not refused the call's grids (a negative FROG_E*).
 int64_t attend_ws(const frog_attend_t& a);
 int launch_attend(const frog_attend_t& a, void* ws, hipStream_t stream);
 int64_t attend_bwd_ws(const frog_attend_t& a);

@@ -131,11 +131,35 @@ void by_type(int type, F&& f) {
     else f(AttendLaunch<bf16_t>{});
 }
 
-// grids are one number of workgroups, of 512 threads at most; a launch takes
-// fewer than 2^32 threads
-constexpr int64_t kMaxBlocks = 0xffffffffll / 512;
-int check_grid(int64_t blocks) {
-    return blocks > kMaxBlocks ? fail(FROG_EUNSUPPORTED, "%lld workgroups: more than one launch takes", (long long)blocks) : FROG_OK;
+// A launch takes fewer than 2^32 threads.  (Joining passes are not looked at:
+// an axis is cut only where there are a few hundred workgroups.)
+int check_grid(int64_t blocks, int threads = 256) {
+    return blocks > 0xffffffffll / threads ? fail(FROG_EUNSUPPORTED, "%lld workgroups of %d threads: more than one launch takes", (long long)blocks, threads) : FROG_OK;
+}
+
+// the passes that own keys
+int check_keys(const frog_attend_t& a, const PackPlan& p) {
+    const int64_t pairs = a.batch * a.kv_heads;
+    return check_grid(std::max((pairs * p.tiles + 3) / 4, pairs * ((a.keys + kTileRows - 1) / kTileRows) * p.parts));
+}
+
+int check_forward(const frog_attend_t& a, const ForwardPlan& p) {
+    const int64_t pairs = a.batch * a.kv_heads;
+    int rc = p.few ? check_grid(pairs * p.splits, 512) : check_grid(pairs * p.splits * p.tiles);
+    if (rc != FROG_OK || !a.w_out) return rc;
+    return p.few ? check_grid((pairs * p.rows + 3) / 4 + (a.keys + 255) / 256 * pairs) : check_keys(a, pack_plan(a, false));
+}
+
+int check_backward(const frog_attend_t& a, const PackPlan& p) {
+    const int64_t rows = a.queries * (a.heads / a.kv_heads);
+    int rc = check_grid(a.batch * a.kv_heads * ((rows + kTileRows - 1) / kTileRows));
+    return rc != FROG_OK ? rc : check_keys(a, p);
+}
+
+int check_shared(const frog_attend_shared_t& a, const SharedPlan& p) {
+    int rc = check_grid(p.tail_blocks + (p.few ? (int64_t)a.kv_heads * p.head_splits : 0), p.whole ? 512 : 256);
+    if (rc == FROG_OK && !p.whole && !p.few) rc = check_grid((int64_t)a.kv_heads * p.head_splits * p.tiles);
+    return rc != FROG_OK || p.whole ? rc : check_grid((a.batch * a.heads + 3) / 4);
 }
 
 __global__ void fill_lse(float* lse, int64_t n) {
@@ -250,7 +274,12 @@ void schedule_keys(const frog_attend_t& a, const SchedulePlan& p, const int4* bo
     schedule_key_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, (int)p.tiles, bounds, row_tiles, cu_tiles(a, p.parts), (int*)(ws + p.at));
 }
 
-int64_t attend_ws(const frog_attend_t& a) { return empty(a) ? 0 : forward_plan(a).bytes; }
+int64_t attend_ws(const frog_attend_t& a) {
+    if (empty(a)) return 0;
+    const ForwardPlan p = forward_plan(a);
+    const int rc = check_forward(a, p);
+    return rc != FROG_OK ? rc : p.bytes;
+}
 
 int launch_attend(const frog_attend_t& a, void* ws, hipStream_t stream) {
     const int size = a.type == FROG_STORAGE_F32 ? 4 : 2;
@@ -262,14 +291,16 @@ int launch_attend(const frog_attend_t& a, void* ws, hipStream_t stream) {
         return launched("attention launch");
     }
     const ForwardPlan p = forward_plan(a);
-    const int64_t pairs = a.batch * a.kv_heads;
-    int rc = check_grid(std::max(pairs * p.splits * (p.few ? 1 : p.tiles), std::max(pairs * p.rows / 4 + 1, a.w_out ? pairs * (a.keys / kTileRows + 1) : 0)));
-    if (rc != FROG_OK) return rc;
     by_type(a.type, [&](auto l) { l.forward(a, p, (char*)ws, stream); });
     return launched("attention launch");
 }
 
-int64_t attend_bwd_ws(const frog_attend_t& a) { return empty(a) ? 0 : pack_plan(a, true).bytes; }
+int64_t attend_bwd_ws(const frog_attend_t& a) {
+    if (empty(a)) return 0;
+    const PackPlan p = pack_plan(a, true);
+    const int rc = check_backward(a, p);
+    return rc != FROG_OK ? rc : p.bytes;
+}
 
 int launch_attend_bwd(const frog_attend_t& a, void* ws, hipStream_t stream) {
     const int size = a.type == FROG_STORAGE_F32 ? 4 : 2;
@@ -279,11 +310,6 @@ int launch_attend_bwd(const frog_attend_t& a, void* ws, hipStream_t stream) {
         clear(a.dv, a.dv_stride, a.batch, a.keys, a.kv_heads, a.d, size, stream);
         return launched("attention gradient launch");
     }
-    const int64_t pairs = a.batch * a.kv_heads;
-    const PackPlan p = pack_plan(a, true);
-    const int64_t key_tiles = a.keys / kTileRows + 1;
-    int rc = check_grid(pairs * std::max({key_tiles * p.parts, p.tiles, key_tiles * a.d / 4}));
-    if (rc != FROG_OK) return rc;
     by_type(a.type, [&](auto l) { l.backward(a, (char*)ws, stream); });
     return launched("attention gradient launch");
 }
@@ -324,13 +350,16 @@ SharedPlan shared_plan(const frog_attend_shared_t& a) {
     return p;
 }
 
-int64_t attend_shared_ws(const frog_attend_shared_t& a) { return a.batch == 0 ? 0 : shared_plan(a).bytes; }
+int64_t attend_shared_ws(const frog_attend_shared_t& a) {
+    if (a.batch == 0) return 0;
+    const SharedPlan p = shared_plan(a);
+    const int rc = check_shared(a, p);
+    return rc != FROG_OK ? rc : p.bytes;
+}
 
 int launch_attend_shared(const frog_attend_shared_t& a, void* ws, hipStream_t stream) {
     if (a.batch == 0) return FROG_OK;
     const SharedPlan p = shared_plan(a);
-    int rc = check_grid(std::max({p.tail_blocks + (int64_t)a.kv_heads * p.head_splits, (int64_t)a.kv_heads * p.head_splits * p.tiles, a.batch * a.heads / 4 + 1}));
-    if (rc != FROG_OK) return rc;
     by_type(a.type, [&](auto l) { l.shared(a, p, (char*)ws, stream); });
     return launched("shared attention launch");
 }

@@ -141,6 +141,7 @@ int check_evict(const frog_evict_t* a) {
 // around its launches
 template <typename A, typename F>
 int with_ws(const A& a, int64_t bytes, hipStream_t stream, F&& launch) {
+    if (bytes < 0) return (int)bytes;
     if (bytes == 0) return launch(nullptr);
     if (a.ws) {
         if ((uintptr_t)a.ws & 255) return fail(FROG_EINVAL, "the workspace does not start on a 256-byte boundary");
