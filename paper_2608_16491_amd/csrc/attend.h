@@ -16,6 +16,7 @@
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "frog_internal.h"
@@ -115,6 +116,19 @@ __device__ inline void cap_scores(const ScoreParams& s, V& z) {
 #pragma unroll
         for (int i = 0; i < N; ++i) z[i] = fmaf(-2.f * s.cap2, rcp_fast(1.f + exp2_fast(z[i] * s.mul)), s.cap2);
     }
+}
+
+// launch(first, grid) for `total` workgroups, as many at a time as a launch takes
+// (fewer than 2^32 threads); nothing follows a launch that failed.
+template <typename F>
+inline hipError_t in_launches(int64_t total, int threads, F&& launch) {
+    const int64_t most = 0xffffffffll / threads;
+    for (int64_t first = 0; first < total; first += most) {
+        launch(first, dim3((unsigned)std::min(most, total - first)));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // launchers (attend.hip, evict.hip).  The

@@ -42,11 +42,11 @@ __device__ inline int block_scan(int x, int* part) {
     return x + before;
 }
 
-__global__ __launch_bounds__(kBlock) void evict_pick(frog_evict_t a, int32_t* list) {
+__global__ __launch_bounds__(kBlock) void evict_pick(frog_evict_t a, int32_t* list, int64_t first) {
     constexpr int W = kBlock / 64, kBins = 2 * kBlock;
     __shared__ int hist[kBins], part[W], bound[2], counts[2][W];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = blockIdx.x, b = row / a.heads;
+    const int64_t row = first + blockIdx.x, b = row / a.heads;
     const int n = (int)live_rows(a, b), keep = (int)a.keep;
     const int recent = (int)min((int64_t)n, a.recent), old = n - recent;
     const float* w = a.weights + row * a.slots;
@@ -124,8 +124,8 @@ __global__ __launch_bounds__(kBlock) void evict_pick(frog_evict_t a, int32_t* li
     if (row % a.heads == 0 && threadIdx.x == 0) a.lengths_out[b] = min(n, keep);
 }
 
-__global__ __launch_bounds__(256) void evict_copy(frog_evict_t a, const int32_t* list, int size, int pieces) {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, total = a.batch * a.keep * a.heads * pieces;
+__global__ __launch_bounds__(256) void evict_copy(frog_evict_t a, const int32_t* list, int size, int pieces, int64_t first) {
+    const int64_t t = (first + blockIdx.x) * 256 + threadIdx.x, total = a.batch * a.keep * a.heads * pieces;
     if (t >= total) return;
     const int c = (int)(t % pieces);
     const int64_t slot_head = t / pieces;
@@ -159,16 +159,17 @@ int64_t evict_ws(const frog_evict_t& a) { return a.batch * a.heads * a.keep * 4;
 
 int launch_evict(const frog_evict_t& a, void* ws, hipStream_t stream) {
     if (a.batch == 0) return FROG_OK;
+    hipError_t e;
     if (a.keep == 0) {
         evict_nothing<<<dim3((unsigned)((a.batch + 255) / 256)), 256, 0, stream>>>(a);
+        e = hipGetLastError();
     } else {
         const int size = a.type == FROG_STORAGE_F32 ? 4 : 2, pieces = a.d * size / 16;
-        const int64_t total = a.batch * a.keep * a.heads * pieces;
-        if ((total + 255) / 256 > 0x7fffffff) return fail(FROG_EUNSUPPORTED, "too many rows kept");
-        evict_pick<<<dim3((unsigned)(a.batch * a.heads)), kBlock, 0, stream>>>(a, (int32_t*)ws);
-        evict_copy<<<dim3((unsigned)((total + 255) / 256)), 256, 0, stream>>>(a, (const int32_t*)ws, size, pieces);
+        const int64_t copies = (a.batch * a.keep * a.heads * pieces + 255) / 256;
+        int32_t* list = (int32_t*)ws;
+        e = in_launches(a.batch * a.heads, kBlock, [&](int64_t first, dim3 grid) { evict_pick<<<grid, kBlock, 0, stream>>>(a, list, first); });
+        if (e == hipSuccess) e = in_launches(copies, 256, [&](int64_t first, dim3 grid) { evict_copy<<<grid, 256, 0, stream>>>(a, list, size, pieces, first); });
     }
-    hipError_t e = hipGetLastError();
     return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "eviction launch: %s", hipGetErrorString(e));
 }
 

@@ -74,3 +74,46 @@ def test_a_large_batch_of_long_sequences():
     got = torch.autograd.grad(o, x, one[3].expand(b, t, h, d))
     for a, w in zip(got, want[1:]):
         assert all(torch.equal(a[i], w[0]) for i in range(b))
+
+
+@pytest.mark.gpu
+def test_evict_of_more_caches_than_a_launch_takes():
+    # 2^22 workgroups of 1,024 threads are one more than a launch takes
+    b, h, t, d = 2 ** 16 + 1, 64, 2, 8
+    print(f"[gpu] eviction from {b * h} caches", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    k, v = (torch.randn((b, t, h, d), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    w = torch.rand((b, h, t), generator=g, device="cuda")
+    n = torch.randint(0, t + 1, (b,), generator=g, device="cuda", dtype=torch.int32)
+    n[-1] = t
+    ko, vo, wo, po, no = F.evict(k, v, w, None, n, 1)
+    assert torch.equal(no, n.clamp(max=1))
+    best = torch.where(n.view(b, 1) == t, (w[..., 1] > w[..., 0]).int(), torch.where(n.view(b, 1) == 1, 0, -1))     # [b, h]
+    assert torch.equal(po[..., 0], best)
+    take = best.clamp(min=0).long()
+    assert torch.equal(wo, torch.where(best.unsqueeze(-1) >= 0, w.gather(2, take.unsqueeze(-1)), 0.0))
+    rows_of = take.view(b, 1, h, 1).expand(b, 1, h, d)
+    for got, x in ((ko, k), (vo, v)):
+        assert torch.equal(got, torch.where(best.view(b, 1, h, 1) >= 0, x.gather(1, rows_of), 0))
+
+
+@pytest.mark.gpu
+def test_evict_of_more_values_than_a_launch_copies():
+    # 2^32 pieces of 16 bytes and one row more, of a cache whose slots are one row in memory; k and v out are one buffer
+    slots, d = 1025, 2 ** 24
+    print(f"[gpu] eviction of {slots} rows of {d} values", flush=True)
+    row = torch.randn(d, device="cuda")
+    out = torch.full((slots, d), float("nan"), device="cuda")
+    w = torch.rand(slots, device="cuda")
+    n = torch.full((1,), slots, device="cuda", dtype=torch.int32)
+    w_out, at, n_out, ws = torch.empty_like(w), torch.empty(slots, device="cuda", dtype=torch.int32), torch.empty_like(n), torch.empty(slots, device="cuda")
+    a = A.EvictArgs()
+    a.k = a.v = row.data_ptr()
+    a.k_stride = a.v_stride = (0, 0, 0)
+    a.weights, a.lengths, a.k_out, a.v_out, a.weights_out = w.data_ptr(), n.data_ptr(), out.data_ptr(), out.data_ptr(), w_out.data_ptr()
+    a.positions_out, a.lengths_out, a.ws, a.ws_bytes = at.data_ptr(), n_out.data_ptr(), ws.data_ptr(), 4 * slots
+    a.batch, a.slots, a.keep, a.heads, a.d, a.type = 1, slots, slots, 1, d, F.STORAGE_F32
+    assert F.lib().frog_evict(C.byref(a), torch.cuda.current_stream().cuda_stream) == 0, F.lib().frog_last_error()
+    torch.cuda.synchronize()
+    assert int(n_out) == slots and torch.equal(w_out, w) and torch.equal(at, torch.arange(slots, device="cuda", dtype=torch.int32))
+    assert all(torch.equal(out[i], row) for i in range(slots))
