@@ -15,30 +15,29 @@ int64_t take(int64_t* at, int64_t bytes) {
     return here;
 }
 
-int launched(const char* what) {
-    hipError_t e = hipGetLastError();
+int launched(const char* what, hipError_t e = hipGetLastError()) {
     return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-__global__ void copy_weights(const float* in, float* out, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+// (the kernels below take the number of their launch's first workgroup)
+__global__ void copy_weights(const float* in, float* out, int64_t n, int64_t first) {
+    const int64_t i = (first + blockIdx.x) * 256 + threadIdx.x;
     if (i < n) out[i] = in ? in[i] : 0.f;
 }
 
 // a tensor of rows set to 0: [batch][tokens][heads][d values], pieces of 16 bytes
-__global__ void clear_rows(char* p, int64_t s0, int64_t s1, int64_t s2, int64_t tokens, int heads, int pieces, int64_t total) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ void clear_rows(char* p, int64_t s0, int64_t s1, int64_t s2, int64_t tokens, int heads, int pieces, int64_t total, int64_t first) {
+    const int64_t i = (first + blockIdx.x) * 256 + threadIdx.x;
     if (i >= total) return;
     const int c = (int)(i % pieces);
     const int64_t r = i / pieces, h = r % heads, t = r / heads % tokens, b = r / heads / tokens;
     *(uint4*)(p + b * s0 + t * s1 + h * s2 + 16 * c) = make_uint4(0, 0, 0, 0);
 }
 
-void clear(void* p, const int64_t (&st)[3], int64_t batch, int64_t tokens, int heads, int d, int size, hipStream_t s) {
-    const int64_t total = batch * tokens * heads * (d * size / 16);
-    if (total)
-        clear_rows<<<dim3((unsigned)((total + 255) / 256)), 256, 0, s>>>((char*)p, st[0] * size, st[1] * size, st[2] * size, tokens, heads, d * size / 16,
-                                                                         total);
+hipError_t clear(void* p, const int64_t (&st)[3], int64_t batch, int64_t tokens, int heads, int d, int size, hipStream_t s) {
+    const int pieces = d * size / 16;
+    const int64_t total = batch * tokens * heads * pieces, s0 = st[0] * size, s1 = st[1] * size, s2 = st[2] * size;
+    return in_launches((total + 255) / 256, 256, [&](int64_t first, dim3 grid) { clear_rows<<<grid, 256, 0, s>>>((char*)p, s0, s1, s2, tokens, heads, pieces, total, first); });
 }
 
 }  // namespace
@@ -162,8 +161,8 @@ int check_shared(const frog_attend_shared_t& a, const SharedPlan& p) {
     return rc != FROG_OK || p.whole ? rc : check_grid((a.batch * a.heads + 3) / 4);
 }
 
-__global__ void fill_lse(float* lse, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ void fill_lse(float* lse, int64_t n, int64_t first) {
+    const int64_t i = (first + blockIdx.x) * 256 + threadIdx.x;
     if (i < n) lse[i] = -INFINITY;
 }
 
@@ -284,11 +283,12 @@ int64_t attend_ws(const frog_attend_t& a) {
 int launch_attend(const frog_attend_t& a, void* ws, hipStream_t stream) {
     const int size = a.type == FROG_STORAGE_F32 ? 4 : 2;
     if (empty(a)) {
-        clear(a.out, a.out_stride, a.batch, a.queries, a.heads, a.d, size, stream);
         const int64_t rows = a.batch * a.heads * a.queries, cols = a.batch * a.kv_heads * a.keys;
-        if (a.lse && rows) fill_lse<<<dim3((unsigned)((rows + 255) / 256)), 256, 0, stream>>>(a.lse, rows);
-        if (a.w_out && a.w_out != a.w_in && cols) copy_weights<<<dim3((unsigned)((cols + 255) / 256)), 256, 0, stream>>>(a.w_in, a.w_out, cols);
-        return launched("attention launch");
+        hipError_t e = clear(a.out, a.out_stride, a.batch, a.queries, a.heads, a.d, size, stream);
+        if (e == hipSuccess && a.lse) e = in_launches((rows + 255) / 256, 256, [&](int64_t first, dim3 grid) { fill_lse<<<grid, 256, 0, stream>>>(a.lse, rows, first); });
+        if (e == hipSuccess && a.w_out && a.w_out != a.w_in)
+            e = in_launches((cols + 255) / 256, 256, [&](int64_t first, dim3 grid) { copy_weights<<<grid, 256, 0, stream>>>(a.w_in, a.w_out, cols, first); });
+        return launched("attention launch", e);
     }
     const ForwardPlan p = forward_plan(a);
     by_type(a.type, [&](auto l) { l.forward(a, p, (char*)ws, stream); });
@@ -305,10 +305,10 @@ int64_t attend_bwd_ws(const frog_attend_t& a) {
 int launch_attend_bwd(const frog_attend_t& a, void* ws, hipStream_t stream) {
     const int size = a.type == FROG_STORAGE_F32 ? 4 : 2;
     if (empty(a)) {
-        clear(a.dq, a.dq_stride, a.batch, a.queries, a.heads, a.d, size, stream);
-        clear(a.dk, a.dk_stride, a.batch, a.keys, a.kv_heads, a.d, size, stream);
-        clear(a.dv, a.dv_stride, a.batch, a.keys, a.kv_heads, a.d, size, stream);
-        return launched("attention gradient launch");
+        hipError_t e = clear(a.dq, a.dq_stride, a.batch, a.queries, a.heads, a.d, size, stream);
+        if (e == hipSuccess) e = clear(a.dk, a.dk_stride, a.batch, a.keys, a.kv_heads, a.d, size, stream);
+        if (e == hipSuccess) e = clear(a.dv, a.dv_stride, a.batch, a.keys, a.kv_heads, a.d, size, stream);
+        return launched("attention gradient launch", e);
     }
     by_type(a.type, [&](auto l) { l.backward(a, (char*)ws, stream); });
     return launched("attention gradient launch");

@@ -117,3 +117,24 @@ def test_evict_of_more_values_than_a_launch_copies():
     torch.cuda.synchronize()
     assert int(n_out) == slots and torch.equal(w_out, w) and torch.equal(at, torch.arange(slots, device="cuda", dtype=torch.int32))
     assert all(torch.equal(out[i], row) for i in range(slots))
+
+
+@pytest.mark.gpu
+def test_outputs_of_passes_without_keys_or_queries_above_one_launch():
+    # 17 sequences whose outputs lie on one another: 2^32 + 2^28 pieces of 16 bytes are set to 0
+    tokens, heads, d = 2 ** 20, 64, 32
+    print("[gpu] passes without keys and without queries", flush=True)
+    out = torch.full((tokens, heads, d), float("nan"), device="cuda", dtype=torch.bfloat16)
+    stream = torch.cuda.current_stream().cuda_stream
+    strides = (0, heads * d, d)
+    a = attend_args(batch=17, queries=tokens, keys=0, heads=heads, kv_heads=heads, d=d, lse=None, q=out.data_ptr(), q_stride=strides,
+                    out=out.data_ptr(), out_stride=strides)
+    assert F.lib().frog_attend(C.byref(a), stream) == 0, F.lib().frog_last_error()
+    torch.cuda.synchronize()
+    assert not out.any()
+    # 2^32 weights of keys that no query saw
+    w = torch.full((2 ** 32,), float("nan"), device="cuda")
+    a = attend_args(batch=1, queries=0, keys=2 ** 26, heads=64, kv_heads=64, d=32, lse=None, k=out.data_ptr(), v=out.data_ptr(), w_out=w.data_ptr())
+    assert F.lib().frog_attend(C.byref(a), stream) == 0, F.lib().frog_last_error()
+    torch.cuda.synchronize()
+    assert bool((w == 0).all())
