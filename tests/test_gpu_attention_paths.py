@@ -2,6 +2,7 @@
 on long prefixes of few requests and on where a single launch ends; pages
 without a number; and intervals as the filtered search writes them."""
 import itertools
+import math
 
 import pytest
 
@@ -105,3 +106,32 @@ def test_intervals_of_the_filtered_search():
     near(weights, p.view(1, kv, -1, n).sum(2), ref.weights_err, "weights")
     one_token = F.attend(s["q"][:, 7:8].contiguous(), s["k"], s["v"], lr[7:8].contiguous())
     near(one_token, (p @ v).transpose(1, 2)[:, 7:8], ref.out_err[:, 7:8], "one token")
+
+
+@pytest.mark.parametrize("tq", [1, 3, 70, 200])
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (5.0, False), (0.0, True), (5.0, True)])
+@pytest.mark.parametrize("kind", TYPES)
+def test_queries_without_keys_may_hold_anything(kind, cap, bias, tq):
+    # rows of padding between rows that see keys: their q, dout and attribute, and the attributes of keys nobody sees
+    s, opt, dout = one.make(kind, 2, tq, 150, 4, 2, 64, "causal", bias, seed=17)
+    pad = torch.arange(tq, device="cuda") % 3 == 1 if tq > 1 else torch.ones(1, device="cuda", dtype=torch.bool)
+    s["lr"][..., 0], s["lr"][..., 1] = 20, s["lr"][..., 1].clamp(max=110)
+    s["lr"][0, pad] = torch.tensor([70, 60], device="cuda", dtype=torch.int32)
+    what = (math.nan, math.inf, -math.inf)
+    clean = dict(s, q=s["q"].clone()), {n: t.clone() for n, t in opt.items()}, dout.clone()
+    clean[0]["q"][0, pad], clean[2][0, pad] = 0, 0
+    for n, x in enumerate(what):
+        s["q"][0, pad, n], dout[0, pad, n + 1] = x, x
+        if bias:
+            opt["at_q"][0, pad] = x
+            opt["at_k"][:, :, 3 * n:20:2], opt["at_k"][:, :, 111 + n::3] = x, x
+    if bias:
+        clean[1]["at_q"][0, pad], clean[1]["at_k"][:, :, :20], clean[1]["at_k"][:, :, 111:] = 0, 0, 0
+
+    ref = Attention(*(clean[0][n] for n in ("q", "k", "v", "lr")), cap=cap, dout=clean[2], **clean[1])
+    x = [s[n].detach().requires_grad_() for n in ("q", "k", "v")]
+    out, lse, w = F.attend(*x, s["lr"], cap=cap, return_lse=True, weights=torch.zeros((2, 2, 150), device="cuda"), **opt)
+    grads = torch.autograd.grad(out, x, dout)
+    for what, got in zip(("out", "lse", "weights", "dq", "dk", "dv"), (out, lse, w, *grads)):
+        near(got, getattr(ref, what), getattr(ref, what + "_err"), what)
+    assert not out[0, pad].any() and not grads[0][0, pad].any() and bool((lse[0, :, pad] == -math.inf).all())
