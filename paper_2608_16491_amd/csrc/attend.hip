@@ -49,20 +49,44 @@ hipError_t clear(void* p, const int64_t (&st)[3], int64_t batch, int64_t tokens,
 // against 13, but 4 us more on the host; 2,048 keys 10 against 22.
 constexpr int64_t kWholeKeys = 1024;
 
-// Schedules are made where intervals may differ (lr) and both axes are long: a
-// workgroup's work is then anything from one step to hundreds, and the longest
-// one decides.  Documents of 546 to 2,730 tokens, 16 heads, d = 128: forward 142
-// -> 121 us, dq 228 -> 212, dk and dv 503 -> 367, for launches of 6 to 9 us.
-// (Cutting long tiles into more parts than short ones made dk and dv 319 us
-// there, but their parts' traffic and that of the forward pass took it back.)
-constexpr int64_t kScheduleLength = 2048, kScheduleTiles = 65536;
-SchedulePlan schedule_plan(const frog_attend_t& a, int64_t tiles, int parts) {
+// Schedules are made where intervals may differ (lr), both axes are long and
+// there are more workgroups than start at once: a workgroup's work is then
+// anything from one step to hundreds, and the longest one decides.  Sizes alone
+// do not tell packed documents, which win, from causal masks and windows, which
+// the order without a schedule serves as well, so the bounds are set where what
+// documents win is above what the others lose.  One sequence, d = 128, 16 query
+// and 4 kv heads, gradients alone (both schedules, us with and without):
+//   tokens          4,096       8,192         16,384         32,768
+//   documents       205, 205    409, 472      1,307, 1,492   5,352, 5,979
+//   causal          391, 382    1,146, 1,164  4,574, 4,632   17,515, 18,004
+// and the forward pass 66, 60; 104, 114; 289, 308; 1,038, 1,064 and 108, 105; 281,
+// 290; 1,032, 1,025; 4,015, 4,007.  Windows of 512 keys lose 7 us of 64 in the
+// forward pass of 8,192 tokens and 23 of 332 in a step.  At 6,000 tokens documents
+// win 0 to 7 % of a step, causal masks lose 1.5.  One workgroup makes a schedule,
+// so many short sequences lose by it: 64 of 2,048 tokens (2 heads, d = 64) 76 us of
+// 501, 4,096 of them (1 head, d = 32) half of 11 ms.
+constexpr int64_t kScheduleLength = 6144;
+SchedulePlan schedule_plan(const frog_attend_t& a, int64_t tiles, int parts, int64_t least, int64_t most) {
     SchedulePlan p{};
-    if (!a.lr || std::min(a.keys, a.queries) < kScheduleLength || a.batch * tiles > kScheduleTiles) return p;
+    if (!a.lr || std::min(a.keys, a.queries) < kScheduleLength || a.batch * a.kv_heads * tiles < least || a.batch * tiles > most) return p;
     p.tiles = tiles;
     p.parts = parts;
-    p.bytes = a.batch * tiles * 8;
+    p.bytes = a.batch * tiles * 4;
     return p;
+}
+// Row tiles: above two workgroups for each of the 256 CUs, which start all at
+// once (8,192 tokens of 8 heads, 512 workgroups: 79 us with, 73 without).  Their
+// lengths stay in LDS.
+constexpr int64_t kScheduleRowBlocks = 513, kScheduleRowTiles = 4096;
+SchedulePlan schedule_rows_plan(const frog_attend_t& a, int64_t tiles, int parts) {
+    return schedule_plan(a, tiles, parts, kScheduleRowBlocks, kScheduleRowTiles);
+}
+// Key tiles: from one for each CU (cut in parts, so four workgroups; 8,192 tokens
+// of one kv head, 64 tiles: 254 us with, 253 without), and as many as the counting
+// of their rows, a wavefront a tile, takes 30 us for.
+constexpr int64_t kScheduleKeyBlocks = 256, kScheduleKeyTiles = 512;
+SchedulePlan schedule_keys_plan(const frog_attend_t& a, int64_t tiles, int parts) {
+    return schedule_plan(a, tiles, parts, kScheduleKeyBlocks, kScheduleKeyTiles);
 }
 
 ForwardPlan forward_plan(const frog_attend_t& a) {
@@ -78,7 +102,7 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     const int64_t blocks = pairs * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
     p.splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / std::max<int64_t>(blocks, 1), (a.keys + least - 1) / least));
     if (p.few && p.groups == 1 && a.keys <= kWholeKeys) p.splits = 1;
-    if (!p.few) p.plan = schedule_plan(a, p.tiles, p.splits);
+    if (!p.few) p.plan = schedule_rows_plan(a, p.tiles, p.splits);
     int64_t at = 0;
     p.plan.at = take(&at, p.plan.bytes);
     if (p.splits > 1) {
@@ -105,8 +129,8 @@ PackPlan pack_plan(const frog_attend_t& a, bool grad) {
     const int64_t blocks = a.batch * a.kv_heads * ((a.keys + kTileRows - 1) / kTileRows);
     p.parts = (int)std::max<int64_t>(1, std::min((1024 + blocks - 1) / std::max<int64_t>(blocks, 1), p.tiles / 8));
     const int64_t key_tiles = (a.keys + kTileRows - 1) / kTileRows, row_tiles = (p.tiles + 3) / 4;
-    p.keys_plan = schedule_plan(a, key_tiles, p.parts);
-    if (grad) p.rows_plan = schedule_plan(a, row_tiles, 1);
+    p.keys_plan = schedule_keys_plan(a, key_tiles, p.parts);
+    if (grad) p.rows_plan = schedule_rows_plan(a, row_tiles, 1);
     int64_t at = 0;
     p.keys_plan.at = take(&at, p.keys_plan.bytes);
     p.rows_plan.at = take(&at, p.rows_plan.bytes);
@@ -174,13 +198,11 @@ namespace {
 // (of a class in any order: it changes no result).  The workgroups of the first
 // `wave` tiles take a CU each; those of the next `wave`, which join them there,
 // come shortest first, so that the CU with the longest gets the shortest beside
-// it.  order: the tiles, and as many lengths.  length(tile) is called by whole
-// wavefronts (WAVE) or by single threads.
+// it.  length(tile) is called by whole wavefronts (WAVE) or by single threads.
 constexpr int kSortBlock = 1024;
 template <bool WAVE, typename F>
 __device__ inline void longest_first(int tiles, int wave, int* order, F&& length) {
-    constexpr int HELD = 4 * kSortBlock;          // lengths kept in LDS, the others' behind the tiles
-    __shared__ int held[HELD], hist[kSortBlock], wave_sum[kSortBlock / 64], most;
+    __shared__ int held[kScheduleRowTiles], hist[kSortBlock], wave_sum[kSortBlock / 64], most;
     const int t = threadIdx.x, lane = t & 63, w = t >> 6;
     const int first = WAVE ? w : t, step = WAVE ? kSortBlock / 64 : kSortBlock;
     const bool writes = !WAVE || lane == 0;
@@ -190,16 +212,14 @@ __device__ inline void longest_first(int tiles, int wave, int* order, F&& length
     int top = 0;
     for (int i = first; i < tiles; i += step) {
         const int n = length(i);
-        if (writes && i < HELD) held[i] = n;          // read back by the same thread
-        else if (writes) order[tiles + i] = n;
+        if (writes) held[i] = n;          // read back by the same thread
         top = max(top, n);
     }
     if (writes) atomicMax(&most, top);
     __syncthreads();
     const float scale = (float)(kSortBlock - 1) / (float)most;
     auto bin = [&](int i) {
-        const int n = i < HELD ? held[i] : order[tiles + i];
-        return kSortBlock - 1 - min((int)((float)n * scale), kSortBlock - 1);
+        return kSortBlock - 1 - min((int)((float)held[i] * scale), kSortBlock - 1);
     };
     if (writes)
         for (int i = first; i < tiles; i += step) atomicAdd(&hist[bin(i)], 1);

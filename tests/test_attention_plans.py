@@ -1,0 +1,64 @@
+"""Which calls order their tiles by length (a small launch of its own in front
+of a pass): the workspace then holds the order."""
+import ctypes as C
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2608_16491_amd as F  # noqa: E402
+from paper_2608_16491_amd import attention as A  # noqa: E402
+
+
+def workspace(backward, lr, batch, tokens, heads, kv, d=64, keys=None, w=None):
+    a = A.AttendArgs()
+    for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv"):
+        setattr(a, n, 4096)
+        setattr(a, n + "_stride", (0, d * heads, d))
+    a.batch, a.queries, a.keys, a.heads, a.kv_heads, a.d, a.type, a.scale = batch, tokens, keys or tokens, heads, kv, d, 2, 0.125
+    a.lr, a.lse, a.w_out = 4096 if lr else None, 4096, w
+    n = F.lib().frog_attend_workspace(C.byref(a), backward)
+    assert n >= 0, F.lib().frog_last_error()
+    return n
+
+
+# batch, tokens, heads, kv heads, and whether rows (forward) and keys (gradients) are ordered
+@pytest.mark.parametrize("batch,tokens,heads,kv,rows,keys", [
+    (1, 8192, 16, 4, True, True), (1, 8191, 12, 12, True, True), (1, 32768, 16, 4, True, True), (4, 8192, 16, 4, True, True),
+    (1, 4096, 16, 4, False, False), (1, 2048, 32, 8, False, False), (1, 8192, 8, 1, False, False), (1, 131072, 4, 1, True, False),
+    (64, 2048, 2, 2, False, False), (1024, 2048, 2, 2, False, False), (4096, 2048, 1, 1, False, False), (64, 8192, 2, 2, True, False),
+    (65, 8192, 64, 64, False, False)])
+def test_orders_are_made_where_they_pay(batch, tokens, heads, kv, rows, keys):
+    order = [workspace(b, True, batch, tokens, heads, kv) - workspace(b, False, batch, tokens, heads, kv) for b in (0, 1)]
+    tiles = -(-tokens * (heads // kv) // 128) * batch
+    assert order[0] == (-(-4 * tiles // 256) * 256 if rows else 0)
+    key_tiles = -(-tokens // 128) * batch
+    assert order[1] == order[0] + (-(-4 * key_tiles // 256) * 256 if keys else 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mask", ["documents", "one", "lengths", "empty", "wild"])
+@pytest.mark.parametrize("batch,tq,tk", [(1, 6500, 6144), (2, 6144, 6501)])
+def test_ordered_passes(mask, batch, tq, tk):
+    # sizes whose tiles are ordered, each group of heads against the formulas in 64 bits
+    from tests.attention_ref import Attention, intervals, near
+    h, kv, d = 12, 6, 32
+    assert workspace(0, True, batch, tq, h, kv, d, tk) > workspace(0, False, batch, tq, h, kv, d, tk)
+    print(f"[gpu] ordered passes {mask} {batch} x {tq} x {tk}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(tq)
+    q, k, v, dout = (torch.randn(s, generator=g, device="cuda").to(torch.bfloat16) for s in ((batch, tq, h, d), (batch, tk, kv, d), (batch, tk, kv, d), (batch, tq, h, d)))
+    lr = intervals("causal" if mask == "one" else mask, batch, tq, tk, 5).cuda()
+    if mask == "one":
+        # a few rows see every key, the others one
+        lr[:, :, 0] = lr[:, :, 1] = lr[:, :, 1].clamp(min=0)
+        lr[:, 700:704, 0], lr[:, 700:704, 1] = 0, tk - 1
+    x = [t.requires_grad_() for t in (q, k, v)]
+    out, lse, w = F.attend(*x, lr, return_lse=True, weights=torch.zeros((batch, kv, tk), device="cuda"))
+    grads = torch.autograd.grad(out, x, dout)
+    for b in range(batch):
+        for i in range(kv):
+            hs = slice(i * h // kv, (i + 1) * h // kv)
+            ref = Attention(q[b:b + 1, :, hs].detach(), k[b:b + 1, :, i:i + 1].detach(), v[b:b + 1, :, i:i + 1].detach(), lr[b:b + 1], dout=dout[b:b + 1, :, hs])
+            got = (out[b:b + 1, :, hs], lse[b:b + 1, hs], w[b:b + 1, i:i + 1], grads[0][b:b + 1, :, hs], grads[1][b:b + 1, :, i:i + 1], grads[2][b:b + 1, :, i:i + 1])
+            for what, y in zip(("out", "lse", "weights", "dq", "dk", "dv"), got):
+                near(y, getattr(ref, what), getattr(ref, what + "_err"), f"{mask} {what}")
