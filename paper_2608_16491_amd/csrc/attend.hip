@@ -42,12 +42,19 @@ hipError_t clear(void* p, const int64_t (&st)[3], int64_t batch, int64_t tokens,
 
 }  // namespace
 
-// Up to so many keys a few-rows pass is not split: one launch, eight
-// wavefronts a workgroup, four steps each.  A CU takes in about 60 GB/s, so a
-// workgroup's step of 256 keys of 128 bf16 values costs 2.3 us; split over
-// CUs and joined by a second launch 1,001 keys take 12 us of device time
-// against 13, but 4 us more on the host; 2,048 keys 10 against 22.
-constexpr int64_t kWholeKeys = 1024;
+// A few-rows pass over at most kWholeKeys keys that is not split: one launch
+// instead of two, but a workgroup walks all keys of a kv head, and a CU takes in
+// about 60 GB/s.  With 256 workgroups or more that is at least as fast at every
+// size (256 caches of 1,024 keys, bf16, d = 128: 26 us, split 30).  With fewer it
+// is where the keys of a kv head are at most kWholeBytes, both by the host's clock
+// and on the device alone, as in a replayed graph (us, whole and split; device in
+// brackets): bf16, d = 128, 512 keys 12.0, 14.0 (9.1, 8.9), 1,024 keys 15.5, 14.3
+// (13.4, 8.8); d = 64, 1,024 keys 12.3, 14.1 (9.2, 7.7); fp32, d = 128, 256 keys 13.7,
+// 14.6 (11.6, 11.8), 512 keys 20.0, 14.7 (18.0, 11.8).
+constexpr int64_t kWholeKeys = 1024, kWholeBytes = 128 << 10;
+bool whole_pays(int64_t keys, int64_t blocks, int d, int type) {
+    return keys <= kWholeKeys && (blocks >= 256 || keys * d * (type == FROG_STORAGE_F32 ? 4 : 2) <= kWholeBytes);
+}
 
 // Schedules are made where intervals may differ (lr), both axes are long and
 // there are more workgroups than start at once: a workgroup's work is then
@@ -101,7 +108,9 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     // (128 keys; 256 of the tiles', whose parts cost 4 D bytes a row)
     const int64_t blocks = pairs * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
     p.splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / std::max<int64_t>(blocks, 1), (a.keys + least - 1) / least));
-    if (p.few && p.groups == 1 && a.keys <= kWholeKeys) p.splits = 1;
+    // (with key weights too, where a second launch follows in any case, so that
+    // they do not change the output: 512 keys 17.3 us whole, 16.3 split)
+    if (p.few && p.groups == 1 && whole_pays(a.keys, pairs, a.d, a.type)) p.splits = 1;
     if (!p.few) p.plan = schedule_rows_plan(a, p.tiles, p.splits);
     int64_t at = 0;
     p.plan.at = take(&at, p.plan.bytes);
@@ -338,10 +347,15 @@ SharedPlan shared_plan(const frog_attend_shared_t& a) {
     SharedPlan p{};
     const int64_t group = a.heads / a.kv_heads, rows = a.batch * group, all = a.batch * a.heads;
     const int64_t most = a.pages_per_request * a.page;
-    if (a.prefix + most <= kWholeKeys && a.batch * a.prefix <= 16 * kWholeKeys) {
+    const int whole_groups = group <= 16 ? 1 : 2;
+    const int64_t whole_blocks = a.batch * a.kv_heads * ((group + 16 * whole_groups - 1) / (16 * whole_groups));
+    // (the prefix of more than 32 rows would take tiles, one more launch: 16
+    // requests over 900 and 60 keys, bf16, d = 128: 18.6 us whole, 23.6 in parts)
+    if (a.prefix + most <= kWholeKeys && a.batch * a.prefix <= 16 * kWholeKeys &&
+        ((a.prefix > 0 && rows > 32) || whole_pays(a.prefix + most, whole_blocks, a.d, a.type))) {
         p.whole = true;
-        p.groups = group <= 16 ? 1 : 2;
-        p.tail_blocks = a.batch * a.kv_heads * ((group + 16 * p.groups - 1) / (16 * p.groups));
+        p.groups = whole_groups;
+        p.tail_blocks = whole_blocks;
         return p;
     }
     // parts as in forward_plan

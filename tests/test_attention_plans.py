@@ -62,3 +62,39 @@ def test_ordered_passes(mask, batch, tq, tk):
             got = (out[b:b + 1, :, hs], lse[b:b + 1, hs], w[b:b + 1, i:i + 1], grads[0][b:b + 1, :, hs], grads[1][b:b + 1, :, i:i + 1], grads[2][b:b + 1, :, i:i + 1])
             for what, y in zip(("out", "lse", "weights", "dq", "dk", "dv"), got):
                 near(y, getattr(ref, what), getattr(ref, what + "_err"), f"{mask} {what}")
+
+
+F32, BF16 = 0, 2
+
+
+# batch, keys, heads, kv heads, d, type, key weights, and whether one launch takes all (no workspace)
+@pytest.mark.parametrize("batch,keys,heads,kv,d,type_,weights,whole", [
+    (1, 128, 16, 4, 128, F32, False, True), (1, 256, 16, 4, 128, F32, False, True), (1, 257, 16, 4, 128, F32, False, False),
+    (1, 512, 16, 4, 128, BF16, False, True), (1, 513, 16, 4, 128, BF16, False, False), (1, 1024, 16, 4, 64, BF16, False, True),
+    (1, 1025, 16, 4, 32, BF16, False, False), (64, 1024, 16, 4, 128, F32, False, True), (63, 1024, 16, 4, 128, BF16, False, False),
+    (1, 512, 16, 4, 128, BF16, True, True), (1, 700, 16, 4, 128, BF16, True, False), (64, 512, 16, 4, 128, BF16, True, True)])
+def test_short_caches_are_cut_where_that_pays(batch, keys, heads, kv, d, type_, weights, whole):
+    a = A.AttendArgs()
+    for n in ("q", "k", "v", "out"):
+        setattr(a, n, 4096)
+        setattr(a, n + "_stride", (0, d * heads, d))
+    a.batch, a.queries, a.keys, a.heads, a.kv_heads, a.d, a.type, a.scale = batch, 1, keys, heads, kv, d, type_, 0.125
+    scores = 0
+    if weights:
+        a.w_out = a.lse = 4096
+        scores = -(-batch * heads * keys * 4 // 256) * 256
+    assert (F.lib().frog_attend_workspace(C.byref(a), 0) == scores) == whole
+
+
+@pytest.mark.parametrize("batch,prefix,tail,heads,kv,d,type_,whole", [
+    (4, 700, 64, 16, 4, 64, BF16, True), (4, 400, 112, 16, 4, 128, BF16, True), (4, 401, 112, 16, 4, 128, BF16, False), (4, 200, 57, 16, 4, 128, F32, False),
+    (16, 900, 64, 16, 4, 128, F32, True), (4, 0, 520, 16, 4, 128, BF16, False), (64, 0, 1000, 16, 4, 128, BF16, True), (4, 960, 65, 16, 4, 32, BF16, False)])
+def test_short_shared_prefixes_are_cut_where_that_pays(batch, prefix, tail, heads, kv, d, type_, whole):
+    a = A.SharedArgs()
+    for n in ("q", "k", "v", "out"):
+        setattr(a, n, 4096)
+        setattr(a, n + "_stride", (d * heads, d))
+    a.k_pages = a.v_pages = a.pages = a.lengths = 4096
+    a.k_pages_stride = a.v_pages_stride = (d * heads, d * heads, d)
+    a.batch, a.prefix, a.num_pages, a.pages_per_request, a.page, a.heads, a.kv_heads, a.d, a.type, a.scale = batch, prefix, 4, tail, 1, heads, kv, d, type_, 0.125
+    assert (F.lib().frog_attend_shared_workspace(C.byref(a)) == 0) == whole

@@ -30,7 +30,8 @@ SHARED = [(3, 3000, 100, 8, 2, 128, 16),     # at most 16 query rows a kv head o
           (2, 200, 100, 70, 2, 32, 5), (3, 0, 60, 33, 1, 96, 16),
           (2, 2600, 300, 40, 1, 64, 16),     # the same over a long prefix and long tails
           (5, 1500, 400, 20, 1, 128, 32), (4, 1200, 1300, 48, 1, 32, 16),
-          (2, 1000, 24, 4, 2, 64, 8), (2, 1001, 24, 4, 2, 64, 8)]   # prefix and tail of 1,024 rows, and one more
+          (2, 1000, 24, 4, 2, 64, 8), (2, 1001, 24, 4, 2, 64, 8),
+          (4, 400, 112, 16, 4, 128, 16), (4, 420, 112, 16, 4, 128, 16), (4, 0, 700, 8, 2, 128, 16)]   # prefix and tail of 1,024 rows, and one more
 
 
 @pytest.mark.parametrize("kind", TYPES)
@@ -67,7 +68,8 @@ def test_pages_without_a_number_count_as_no_rows(kind, prefix, width, h, kv):
 
 # b, tq, tk, h, kv, d: 17 to 32 query rows a kv head, in one part and in many; a single launch's last key and one more
 FEW = [(1, 5, 3000, 8, 2, 128), (2, 1, 2500, 20, 1, 64), (1, 1, 1500, 32, 1, 96), (3, 8, 129, 8, 2, 32), (2, 3, 700, 10, 1, 128),
-       (1, 2, 1024, 8, 2, 64), (1, 2, 1025, 8, 2, 64), (1, 33, 300, 1, 1, 64)]
+       (1, 2, 1024, 8, 2, 64), (1, 2, 1025, 8, 2, 64), (1, 33, 300, 1, 1, 64),
+       (64, 1, 1000, 4, 4, 64), (2, 1, 600, 8, 2, 128), (1, 3, 500, 4, 1, 128)]
 
 
 @pytest.mark.parametrize("kind", TYPES)
