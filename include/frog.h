@@ -312,8 +312,9 @@ int frog_bruteforce_filtered(const frog_index_t* idx, const float* d_queries, in
  * Values are fp32, fp16 or bf16 (FROG_STORAGE_*); products, softmax
  * statistics and sums are fp32.  With 16-bit values p and the gradient of x
  * are rounded to the type as factors of the second products, and each output
- * once; an fp16 gradient of x below 6e-8 is lost, so scale the loss where
- * training in fp16.
+ * once; an fp16 gradient of x (p times the difference of two dot products with
+ * dout) below 6e-8 is lost and above 65,504 infinite, so scale the loss where
+ * training in fp16.  The gradients use out as it was rounded.
  *
  * Rows no interval meets are not read into any result: a cache's unused tail
  * may hold anything.  Rows some interval meets must be finite (a NaN or

@@ -133,8 +133,14 @@ PackPlan pack_plan(const frog_attend_t& a, bool grad) {
     // Parts of the query rows until there are four workgroups for each of the
     // 256 CUs, which hold two at a time, of 8 tiles at least: a workgroup's keys
     // see anything from all rows to a few (causal: the first keys twice the
-    // mean).  Their fp32 sums cost 16 d bytes a key and part.  (Two instead of
-    // four: a causal step of 8,192 tokens 1.78 -> 1.48 ms; three: 1.57.)
+    // mean).  Their fp32 sums cost 16 d bytes a key and part.  Two, four and eight
+    // workgroups a CU, us a step, 16 and 4 heads of d = 128:
+    //   tokens       4,096           8,192                 16,384
+    //   causal       542, 483, 558   1,726, 1,441, 1,504   7,002, 5,599, 5,346
+    //   documents    402, 347, 408   695, 541, 574         1,612, 1,163, 1,094
+    //   window       179, 202, 267   302, 329, 402         516, 568, 640
+    //   every key    722, 757, 869   2,638, 2,672, 2,794   10,234, 10,276, 10,489
+    // Equal work pays 5 to 20 % for the others' gain; sizes do not tell them apart.
     const int64_t blocks = a.batch * a.kv_heads * ((a.keys + kTileRows - 1) / kTileRows);
     p.parts = (int)std::max<int64_t>(1, std::min((1024 + blocks - 1) / std::max<int64_t>(blocks, 1), p.tiles / 8));
     const int64_t key_tiles = (a.keys + kTileRows - 1) / kTileRows, row_tiles = (p.tiles + 3) / 4;

@@ -21,6 +21,11 @@ struct RowPack {
     int tiles;
 };
 
+// delta is a 32-bit sum over the output as it was rounded to the type: where a
+// row's weight lies on few keys, dout . v - delta is small beside both, and the
+// rounding shows.  dq and dk of bf16 causal rows are off by 0.0037 of their norm at
+// 2 tokens, 0.0026 at 64, 0.0025 from 257 on (0.0017: computed in 32 bits and
+// rounded once).  The output in more bits would have to be kept for it.
 template <typename T, int D, bool GRAD>
 __global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, RowPack pack, const float* lse, float shift) {
     const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
@@ -149,9 +154,11 @@ __device__ inline void cap_slopes(const ScoreParams& sp, acc16& z, acc16& f) {
 // registers given up before the next, two wavefronts a SIMD of 16-bit rows run
 // without spilling (d = 128: 242 to 256 registers), one's products beside the
 // other's exponentials.  Documents of 546 to 2,730 tokens, 16 heads, capped: 320
-// us with one, 287 with two (one waited 38 % of its cycles, its vector
-// instructions took 36 %, its products 21 %); every key of 8,192 seen, no cap:
-// a step 2.79 -> 2.66 ms.
+// us with one, 285 with two (with 1.5 of them on average, vector instructions
+// active 43 % of the time, products 18 %); every key of 8,192 seen, no cap: a step
+// 2.79 -> 2.66 ms, 750 to 825 TFLOP/s here (fp32, 4,096 tokens: 100).
+//   Of 16-bit rows p and dx = p (dp - delta) are rounded to the type as factors of
+// the second products, as in attend_tile; an fp16 dx above 65,504 is infinite.
 //   GRAD: dk = sum dx q, dv = sum p dout.  Else: w_out = w_in + sum p.
 template <typename T, int D, Scores KIND, bool GRAD, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
@@ -392,11 +399,11 @@ __global__ __launch_bounds__(256) void keys_join(frog_attend_t a, ScoreParams sp
 
 // dq: one workgroup of W wavefronts, 32 query rows each (a lane owns a query),
 // over the keys of their intervals in tiles of N, double buffered.  Three
-// products a score and the exponentials beside them: 1,089 TFLOP/s at 8,192
-// tokens, 16 heads, d = 128, every key seen, before its addresses were computed
-// anew (fresh) in every step; that takes 30 registers and all spills from it:
-// capped documents of 546 to 2,730 tokens 212 -> 163 us, every key seen without a
-// cap 3 % slower.
+// products a score and the exponentials beside them: 1,020 to 1,050 TFLOP/s at
+// 8,192 tokens, 16 heads, d = 128, every key seen (fp32, 4,096 tokens: 113).
+// Addresses computed anew (fresh) in every step take 30 registers and all spills
+// from it: capped documents of 546 to 2,730 tokens 212 -> 163 us, every key seen
+// without a cap 3 % slower.  dx is rounded as in attend_keys.
 template <typename T, int D, Scores KIND, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
 void attend_dq(frog_attend_t a, ScoreParams sp, int group, int tiles, RowPack pack, const int* order) {

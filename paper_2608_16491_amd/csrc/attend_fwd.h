@@ -22,9 +22,16 @@ constexpr float kLow = -FLT_MAX;   // running maximum of a row that has seen no 
 // intervals in tiles of N: scores transposed (keys x queries) so that a lane
 // owns a query, one pass with the running maximum and sum, keys and values
 // double buffered in LDS by direct loads.  Bound by the matrix cores and the
-// exponentials beside them, two wavefronts a SIMD: 1,070 TFLOP/s at 8,192 tokens,
-// 16 heads, d = 128, bf16, every key seen; a cap costs 1.2 to 1.4 times the time
-// (three transcendentals a score instead of one).
+// exponentials beside them, two wavefronts a SIMD: 1,000 to 1,070 TFLOP/s at 8,192
+// tokens, 16 heads, d = 128, bf16, every key seen (534 to 551 us); a cap costs 1.2
+// to 1.4 times the time (three transcendentals a score instead of one).  fp32: 118
+// TFLOP/s at 4,096 tokens.  Documents of unequal lengths leave a SIMD 1.0 to 1.3
+// wavefronts on average, which is what they are bound by.
+//   Weights of 16-bit rows are rounded to the type as factors of the second
+// product (relative to the running maximum, so at most 2^8); their sum is of the
+// 32-bit ones.  Exact to 32 bits they would be two factors, 1.5 times the
+// products.  It takes the output from 0.0016 of its norm off (rounded once) to
+// 0.0021 in bf16.  kAny of d = 128 spills 9 registers.
 template <typename T, int D, Scores KIND, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
 void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts parts, const int* order) {
@@ -283,7 +290,8 @@ struct FewRows {
 // LDS: a lane loads 16 bytes of a key row as it stands in the left factor of
 // the scores, and D / 16 values each of 8 value rows, whose transposition is
 // a renaming of registers and one exchange of 16-bit halves; the output's
-// columns come out as d = 4 (L/16) + r times D/16 plus e.
+// columns come out as d = 4 (L/16) + r times D/16 plus e.  Weights of 16-bit rows
+// are rounded as in attend_tile.
 template <typename T, int D, int RG>
 struct FewPass {
     static constexpr int K = D / 32, C = D / 16;
@@ -507,8 +515,11 @@ struct FewPass {
 
 // One workgroup per (sequence, kv head, part of the keys) for at most 16 RG
 // query rows.  Bound by HBM, 4.4 TB/s over 24 caches to 40,000 keys of 8 kv heads
-// (443 us); a short cache by its chain of steps (1,001 keys 14 us).  KEEP: scores [batch][heads][queries][keys] receive every score in
-// log2 units for the key weights.
+// (443 us), fp32 5.8 over 16 of 10,000; a short cache by its chain of steps (1,001
+// keys 6 us, and 4 for the join).  fp32 rows of d = 128 spill 16 to 45 registers
+// in two groups (8 caches of 10,000, 2 kv heads of 32: 78 us, 2.1 TB/s; bf16 45, 1.8).
+// KEEP: scores [batch][heads][queries][keys] receive every score in log2 units
+// for the key weights.
 template <typename T, int D, int RG, int W, bool PLAIN, bool KEEP>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RG == 1 && sizeof(T) == 2 ? 2 : 1))) void attend_few(frog_attend_t a, ScoreParams sp, int group, Parts parts, float* scores) {
     __shared__ __attribute__((aligned(16))) float lds[FewPass<T, D, RG>::kJoin(W)], tops[W * RG * 16], sums[W * RG * 16];
@@ -584,8 +595,9 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RG == 1 
 // tails, for few rows: workgroups below `head` take a part of the prefix for
 // the rows of all requests (at most 16 RG per kv head; none when the prefix is
 // left to attend_tile), the others a part of one request's tail for 16 RG rows
-// of a kv head's group.  Bound by HBM: 100 tails to 2,000 rows, 8 kv heads, d =
-// 128, bf16, 106 us (3.9 TB/s).
+// of a kv head's group.  Bound by HBM and, at d = 128, by its registers (15 to 24
+// spilled; fp32 in two groups 87 to 123): 100 tails to 2,000 rows, 8 kv heads, d =
+// 128, bf16, 112 to 120 us (3.7 to 3.4 TB/s).
 template <typename T, int D, int RG, bool PLAIN>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RG == 1 && sizeof(T) == 2 ? 2 : 1))) void shared_few(frog_attend_shared_t a, ScoreParams sp, int group, int head, Parts prefix, Parts tail) {
     constexpr int W = 4;
@@ -666,7 +678,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RG == 1 && 
 
 // The same where prefix and tails are short: one workgroup does both for 16 RG
 // rows of a (request, kv head) and nothing is left to join (the prefix comes
-// from L2 for all requests but the first).
+// from L2 for all requests but the first).  d = 128 spills 5 to 15 registers, fp32
+// in two groups 88 to 109.
 template <typename T, int D, int RG, int W, bool PLAIN>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RG == 1 && sizeof(T) == 2 ? 2 : 1))) void shared_whole(frog_attend_shared_t a, ScoreParams sp, int group) {
     __shared__ __attribute__((aligned(16))) float lds[FewPass<T, D, RG>::kJoin(W)], tops[W * RG * 16], sums[W * RG * 16];
@@ -712,7 +725,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RG == 1 
                             (const T*)a.q + b * a.q_stride[0] + hk * group * a.q_stride[1]};
     pass(tail, 0, len - 1, (float)(len - 1));
 #pragma unroll
-    for (int g = 0; g < RG; ++g) f.row.lo[g] = f.row.hi[g] = 0;   // (rows past the group have the sum 0)
+    for (int g = 0; g < RG; ++g) f.row.lo[g] = f.row.hi[g] = 0;   // (rows past the group hold sums of steps without a mask, and are not written)
     f.template join<W>(lds, tops, sums, w, lane);
     for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * W) {
         const int r = i / (D / 4), d = i % (D / 4) * 4, h = hk * group + row0 + r;

@@ -48,7 +48,7 @@ SharedPlan shared_plan(const frog_attend_shared_t& a);
 // and how the passes that own keys are cut
 struct PackPlan {
     int64_t tiles, rows, bounds, zeros, o, bytes;
-    int parts;                // of the query rows, without a schedule
+    int parts;                // of the query rows, the same of every key tile
     SchedulePlan keys_plan, rows_plan;
 };
 PackPlan pack_plan(const frog_attend_t& a, bool grad);
