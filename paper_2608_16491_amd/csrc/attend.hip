@@ -42,6 +42,13 @@ hipError_t clear(void* p, const int64_t (&st)[3], int64_t batch, int64_t tokens,
 
 }  // namespace
 
+constexpr int64_t kCUs = 256;
+
+// parts, at most `most`, of each of `blocks` workgroups until there are `want`
+int parts_until(int64_t want, int64_t blocks, int64_t most) {
+    return (int)std::max<int64_t>(1, std::min((want + blocks - 1) / std::max<int64_t>(blocks, 1), most));
+}
+
 // A few-rows pass over at most kWholeKeys keys that is not split: one launch
 // instead of two, but a workgroup walks all keys of a kv head, and a CU takes in
 // about 60 GB/s.  With 256 workgroups or more that is at least as fast at every
@@ -53,7 +60,7 @@ hipError_t clear(void* p, const int64_t (&st)[3], int64_t batch, int64_t tokens,
 // 14.6 (11.6, 11.8), 512 keys 20.0, 14.7 (18.0, 11.8).
 constexpr int64_t kWholeKeys = 1024, kWholeBytes = 128 << 10;
 bool whole_pays(int64_t keys, int64_t blocks, int d, int type) {
-    return keys <= kWholeKeys && (blocks >= 256 || keys * d * (type == FROG_STORAGE_F32 ? 4 : 2) <= kWholeBytes);
+    return keys <= kWholeKeys && (blocks >= kCUs || keys * d * (type == FROG_STORAGE_F32 ? 4 : 2) <= kWholeBytes);
 }
 
 // Schedules are made where intervals may differ (lr), both axes are long and
@@ -84,14 +91,14 @@ SchedulePlan schedule_plan(const frog_attend_t& a, int64_t tiles, int parts, int
 // Row tiles: above two workgroups for each of the 256 CUs, which start all at
 // once (8,192 tokens of 8 heads, 512 workgroups: 79 us with, 73 without).  Their
 // lengths stay in LDS.
-constexpr int64_t kScheduleRowBlocks = 513, kScheduleRowTiles = 4096;
+constexpr int64_t kScheduleRowBlocks = 2 * kCUs + 1, kScheduleRowTiles = 4096;
 SchedulePlan schedule_rows_plan(const frog_attend_t& a, int64_t tiles, int parts) {
     return schedule_plan(a, tiles, parts, kScheduleRowBlocks, kScheduleRowTiles);
 }
 // Key tiles: from one for each CU (cut in parts, so four workgroups; 8,192 tokens
 // of one kv head, 64 tiles: 254 us with, 253 without), and as many as the counting
 // of their rows, a wavefront a tile, takes 30 us for.
-constexpr int64_t kScheduleKeyBlocks = 256, kScheduleKeyTiles = 512;
+constexpr int64_t kScheduleKeyBlocks = kCUs, kScheduleKeyTiles = 512;
 SchedulePlan schedule_keys_plan(const frog_attend_t& a, int64_t tiles, int parts) {
     return schedule_plan(a, tiles, parts, kScheduleKeyBlocks, kScheduleKeyTiles);
 }
@@ -106,8 +113,8 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     // parts of the keys until the card's 256 CUs have four workgroups each
     // (two of the larger tile's), none of less than a step of its wavefronts
     // (128 keys; 256 of the tiles', whose parts cost 4 D bytes a row)
-    const int64_t blocks = pairs * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
-    p.splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / std::max<int64_t>(blocks, 1), (a.keys + least - 1) / least));
+    const int64_t blocks = pairs * (p.few ? 1 : p.tiles), want = p.few ? 4 * kCUs : 2 * kCUs, least = p.few ? 128 : 256;
+    p.splits = parts_until(want, blocks, (a.keys + least - 1) / least);
     // (with key weights too, where a second launch follows in any case, so that
     // they do not change the output: 512 keys 17.3 us whole, 16.3 split)
     if (p.few && p.groups == 1 && whole_pays(a.keys, pairs, a.d, a.type)) p.splits = 1;
@@ -142,7 +149,7 @@ PackPlan pack_plan(const frog_attend_t& a, bool grad) {
     //   every key    722, 757, 869   2,638, 2,672, 2,794   10,234, 10,276, 10,489
     // Equal work pays 5 to 20 % for the others' gain; sizes do not tell them apart.
     const int64_t blocks = a.batch * a.kv_heads * ((a.keys + kTileRows - 1) / kTileRows);
-    p.parts = (int)std::max<int64_t>(1, std::min((1024 + blocks - 1) / std::max<int64_t>(blocks, 1), p.tiles / 8));
+    p.parts = parts_until(4 * kCUs, blocks, p.tiles / 8);
     const int64_t key_tiles = (a.keys + kTileRows - 1) / kTileRows, row_tiles = (p.tiles + 3) / 4;
     p.keys_plan = schedule_keys_plan(a, key_tiles, p.parts);
     if (grad) p.rows_plan = schedule_rows_plan(a, row_tiles, 1);
@@ -298,7 +305,7 @@ __global__ __launch_bounds__(kSortBlock) void schedule_key_tiles(frog_attend_t a
 }  // namespace
 
 // tiles whose workgroups (of all kv heads) are one for each of the 256 CUs
-static int cu_tiles(const frog_attend_t& a, int parts) { return (int)std::max<int64_t>(1, 256 / ((int64_t)a.kv_heads * parts)); }
+static int cu_tiles(const frog_attend_t& a, int parts) { return (int)std::max<int64_t>(1, kCUs / ((int64_t)a.kv_heads * parts)); }
 
 void schedule_rows(const frog_attend_t& a, const SchedulePlan& p, char* ws, hipStream_t s) {
     schedule_row_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, a.heads / a.kv_heads, (int)p.tiles, cu_tiles(a, p.parts), (int*)(ws + p.at));
@@ -368,13 +375,13 @@ SharedPlan shared_plan(const frog_attend_shared_t& a) {
     if (a.prefix > 0) {
         p.few = rows <= 32;
         p.tiles = (int)((rows + kTileRows - 1) / kTileRows);
-        const int64_t blocks = (int64_t)a.kv_heads * (p.few ? 1 : p.tiles), want = p.few ? 1024 : 512, least = p.few ? 128 : 256;
-        p.head_splits = (int)std::max<int64_t>(1, std::min((want + blocks - 1) / blocks, (a.prefix + least - 1) / least));
+        const int64_t blocks = (int64_t)a.kv_heads * (p.few ? 1 : p.tiles), want = p.few ? 4 * kCUs : 2 * kCUs, least = p.few ? 128 : 256;
+        p.head_splits = parts_until(want, blocks, (a.prefix + least - 1) / least);
     }
     p.groups = std::max(p.few ? rows : 0, std::min<int64_t>(group, 32)) <= 16 ? 1 : 2;
     if (most > 0) {
         const int64_t blocks = a.batch * a.kv_heads * ((group + 16 * p.groups - 1) / (16 * p.groups));
-        p.tail_splits = (int)std::max<int64_t>(1, std::min((1024 + blocks - 1) / blocks, (most + 127) / 128));
+        p.tail_splits = parts_until(4 * kCUs, blocks, (most + 127) / 128);
         p.tail_blocks = blocks * p.tail_splits;
     }
     int64_t at = 0;
