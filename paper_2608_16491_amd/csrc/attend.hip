@@ -51,16 +51,20 @@ int parts_until(int64_t want, int64_t blocks, int64_t most) {
 
 // A few-rows pass over at most kWholeKeys keys that is not split: one launch
 // instead of two, but a workgroup walks all keys of a kv head, and a CU takes in
-// about 60 GB/s.  With 256 workgroups or more that is at least as fast at every
-// size (256 caches of 1,024 keys, bf16, d = 128: 26 us, split 30).  With fewer it
-// is where the keys of a kv head are at most kWholeBytes, both by the host's clock
-// and on the device alone, as in a replayed graph (us, whole and split; device in
-// brackets): bf16, d = 128, 512 keys 12.0, 14.0 (9.1, 8.9), 1,024 keys 15.5, 14.3
-// (13.4, 8.8); d = 64, 1,024 keys 12.3, 14.1 (9.2, 7.7); fp32, d = 128, 256 keys 13.7,
-// 14.6 (11.6, 11.8), 512 keys 20.0, 14.7 (18.0, 11.8).
-constexpr int64_t kWholeKeys = 1024, kWholeBytes = 128 << 10;
-bool whole_pays(int64_t keys, int64_t blocks, int d, int type) {
-    return keys <= kWholeKeys && (blocks >= kCUs || keys * d * (type == FROG_STORAGE_F32 ? 4 : 2) <= kWholeBytes);
+// about 60 GB/s (fp32, whose workgroups have half the wavefronts: 40).  With 256
+// workgroups or more that is at least as fast at every size (256 caches of 1,024
+// keys, bf16, d = 128: 26 us, split 30).  With fewer it is as long as it takes no
+// more than the host takes for two launches, 14 us: while the keys of a kv head
+// are at most kWholeBytes (fp32: half of it).  us a call in a stream of calls,
+// whole and split, and by the device alone, as in a replayed graph: bf16, d = 128,
+// 512 keys 12.0, 14.0 and 9.1, 8.9; 1,001 keys 13.9, 14.8 and 13.4, 8.8 (what a
+// program that replays graphs loses); 1,300 keys 18.2, 14.3; fp32, d = 128, 256 keys
+// 13.7, 14.6 and 11.6, 11.8; 512 keys 20.0, 14.7 and 18.0, 11.8; 1,024 keys 31.3, 14.6.
+// A shared prefix and a tail are two such passes: 4 requests over 700 and 60 keys,
+// bf16, d = 128, 16.1, 16.2; over 900 and 60 18.0, 16.0.
+constexpr int64_t kWholeKeys = 1024, kWholeBytes = 256 << 10, kWholeSharedBytes = 192 << 10;
+bool whole_pays(int64_t keys, int64_t blocks, int d, int type, int64_t bytes) {
+    return keys <= kWholeKeys && (blocks >= kCUs || keys * d * (type == FROG_STORAGE_F32 ? 8 : 2) <= bytes);
 }
 
 // Schedules are made where intervals may differ (lr), both axes are long and
@@ -117,7 +121,7 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     p.splits = parts_until(want, blocks, (a.keys + least - 1) / least);
     // (with key weights too, where a second launch follows in any case, so that
     // they do not change the output: 512 keys 17.3 us whole, 16.3 split)
-    if (p.few && p.groups == 1 && whole_pays(a.keys, pairs, a.d, a.type)) p.splits = 1;
+    if (p.few && p.groups == 1 && whole_pays(a.keys, pairs, a.d, a.type, kWholeBytes)) p.splits = 1;
     if (!p.few) p.plan = schedule_rows_plan(a, p.tiles, p.splits);
     int64_t at = 0;
     p.plan.at = take(&at, p.plan.bytes);
@@ -365,7 +369,7 @@ SharedPlan shared_plan(const frog_attend_shared_t& a) {
     // (the prefix of more than 32 rows would take tiles, one more launch: 16
     // requests over 900 and 60 keys, bf16, d = 128: 18.6 us whole, 23.6 in parts)
     if (a.prefix + most <= kWholeKeys && a.batch * a.prefix <= 16 * kWholeKeys &&
-        ((a.prefix > 0 && rows > 32) || whole_pays(a.prefix + most, whole_blocks, a.d, a.type))) {
+        ((a.prefix > 0 && rows > 32) || whole_pays(a.prefix + most, whole_blocks, a.d, a.type, kWholeSharedBytes))) {
         p.whole = true;
         p.groups = whole_groups;
         p.tail_blocks = whole_blocks;

@@ -516,7 +516,7 @@ struct FewPass {
 // One workgroup per (sequence, kv head, part of the keys) for at most 16 RG
 // query rows.  Bound by HBM, 4.4 TB/s over 24 caches to 40,000 keys of 8 kv heads
 // (443 us), fp32 5.8 over 16 of 10,000; a short cache by its chain of steps (1,001
-// keys 6 us, and 4 for the join).  fp32 rows of d = 128 spill 16 to 45 registers
+// keys 13.4 us; split 6, and 4 for the join).  fp32 rows of d = 128 spill 16 to 45 registers
 // in two groups (8 caches of 10,000, 2 kv heads of 32: 78 us, 2.1 TB/s; bf16 45, 1.8).
 // KEEP: scores [batch][heads][queries][keys] receive every score in log2 units
 // for the key weights.
