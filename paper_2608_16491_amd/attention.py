@@ -26,7 +26,7 @@ class AttendArgs(C.Structure):
                 ("at_q", _P), ("at_q_stride", _I), ("at_k", _P), ("at_k_stride", _I * 2), ("lse", _P), ("w_in", _P), ("w_out", _P),
                 *_rows("dout", 3), *_rows("dq", 3), *_rows("dk", 3), *_rows("dv", 3), ("ws", _P), ("ws_bytes", _I), ("batch", _I),
                 ("queries", _I), ("keys", _I), ("heads", _D), ("kv_heads", _D), ("d", _D), ("type", _D), ("scale", C.c_float),
-                ("cap", C.c_float)]
+                ("cap", C.c_float), ("out_low", _P)]
 
 
 class SharedArgs(C.Structure):
@@ -183,28 +183,31 @@ class _Call:
         self.masks = lrs + bias
         self.tail = (b, tq, tk, h, kv, d, kind, d ** -0.5 if scale is None else scale, cap)
 
-    def forward(self, q, want_lse, w_in, w_out):
+    def forward(self, q, want_lse, w_in, w_out, want_low=False):
         b, tq, h, d, tk, kv = self.shape
         out = torch.empty((b, tq, h, d), dtype=q.dtype, device=self.device)
+        low = torch.empty_like(out) if want_low else None
         lse = torch.empty((b, h, tq), dtype=torch.float32, device=self.device) if want_lse else None
         head = (*self.rows, out.data_ptr(), tq * h * d, h * d, d, *self.masks, 0 if lse is None else lse.data_ptr(),
                 0 if w_in is None else w_in.data_ptr(), 0 if w_out is None else w_out.data_ptr(), *_NO_GRADS)
-        args, ws, L = _pack_attend(*head, 0, 0, *self.tail), None, lib()
+        tail = (*self.tail, 0 if low is None else low.data_ptr())
+        args, ws, L = _pack_attend(*head, 0, 0, *tail), None, lib()
         if _own_workspace(w_out is not None and max(q.numel() // d, kv * 64) * tk > 2 ** 22):
             ws, at = _workspace(lambda x: L.frog_attend_workspace(x, 0), args, self.device)
-            args = _pack_attend(*head, *at, *self.tail)
+            args = _pack_attend(*head, *at, *tail)
         _launch(L.frog_attend, args, self.device)
-        return out, lse
+        return out, lse, low
 
-    def backward(self, q, k, v, out, lse, dout):
+    def backward(self, q, k, v, out, low, lse, dout):
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=self.device) for t in (q, k, v))
         grads = (x for t in (dout, dq, dk, dv) for x in (t.data_ptr(), *t.stride()[:3]))
         head = (*self.rows, out.data_ptr(), *out.stride()[:3], *self.masks, lse.data_ptr(), 0, 0, *grads)
-        args, ws, L = _pack_attend(*head, 0, 0, *self.tail), None, lib()
+        tail = (*self.tail, 0 if low is None else low.data_ptr())
+        args, ws, L = _pack_attend(*head, 0, 0, *tail), None, lib()
         n = L.frog_attend_workspace(args, 1)
         if _own_workspace(n > 2 ** 26):
             ws, at = _workspace(lambda x: n, args, self.device)
-            args = _pack_attend(*head, *at, *self.tail)
+            args = _pack_attend(*head, *at, *tail)
         _launch(L.frog_attend_backward, args, self.device)
         return dq, dk, dv
 
@@ -212,24 +215,27 @@ class _Call:
 class _Attend(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, v, call, mask, w_in, w_out, kept):
-        out, lse = call.forward(q, True, w_in, w_out)
+        # (16-bit rows: the gradient takes the output with what its rounding left)
+        out, lse, low = call.forward(q, True, w_in, w_out, q.element_size() == 2)
         kept.append(lse)
         lr, ctx.scale, ctx.cap, *bias = mask
-        ctx.save_for_backward(q, k, v, out, lse, lr, *bias)
+        ctx.save_for_backward(q, k, v, out, low, lse, lr, *bias)
         return out
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout):
         # (the tensors may have moved since: hooks on saved tensors, recomputation)
-        q, k, v, out, lse, lr, *bias = ctx.saved_tensors
+        q, k, v, out, low, lse, lr, *bias = ctx.saved_tensors
         _no_tangent(("the gradient of the output",), (dout,))
         size = 16 // dout.element_size()
         if dout.stride(-1) != 1 or dout.data_ptr() % 16 or any(s % size for s in dout.stride()[:-1]):
             # (a copy in new memory: contiguous() returns a tensor that only starts off a boundary as it is)
             dout = dout.clone(memory_format=torch.contiguous_format)
+        if low is not None and low.stride() != out.stride():       # (read at the same places)
+            out, low = out.contiguous(), low.contiguous()
         call = _Call(q, k, v, lr, ctx.scale, ctx.cap, *bias)
-        return (*call.backward(q, k, v, out, lse, dout), None, None, None, None, None)
+        return (*call.backward(q, k, v, out, low, lse, dout), None, None, None, None, None)
 
 
 def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_k=None, weights=None, weights_out=None,
@@ -255,7 +261,8 @@ def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_
     queries] (return_lse) and the new weights (weights given).  q, k and v
     take gradients; lse and weights do not, and no argument a tangent of
     forward mode (ValueError)."""
-    _no_tangent(("q", "k", "v", "slopes", "at_q", "at_k", "weights", "weights_out"), (q, k, v, slopes, at_q, at_k, weights, weights_out))
+    if getattr(forward_ad, "_current_level", 0) >= 0:
+        _no_tangent(("q", "k", "v", "slopes", "at_q", "at_k", "weights", "weights_out"), (q, k, v, slopes, at_q, at_k, weights, weights_out))
     mask = (lr, scale, cap, slopes, at_q, at_k)
     call = _Call(q, k, v, *mask)
     if weights is not None:
@@ -271,7 +278,7 @@ def attend(q, k, v, lr=None, *, scale=None, cap=0.0, slopes=None, at_q=None, at_
     def run():
         new = torch.empty_like(weights) if weights is not None and weights_out is None else weights_out
         if not grad:
-            return (*call.forward(q, return_lse, weights, new), new)
+            return (*call.forward(q, return_lse, weights, new)[:2], new)
         kept = []
         return _Attend.apply(q, k, v, call, mask, weights, new, kept), kept[0], new
 

@@ -331,6 +331,7 @@ int launch_attend(const frog_attend_t& a, void* ws, hipStream_t stream) {
     if (empty(a)) {
         const int64_t rows = a.batch * a.heads * a.queries, cols = a.batch * a.kv_heads * a.keys;
         hipError_t e = clear(a.out, a.out_stride, a.batch, a.queries, a.heads, a.d, size, stream);
+        if (e == hipSuccess && a.out_low && size == 2) e = clear(a.out_low, a.out_stride, a.batch, a.queries, a.heads, a.d, size, stream);
         if (e == hipSuccess && a.lse) e = in_launches((rows + 255) / 256, 256, [&](int64_t first, dim3 grid) { fill_lse<<<grid, 256, 0, stream>>>(a.lse, rows, first); });
         if (e == hipSuccess && a.w_out && a.w_out != a.w_in)
             e = in_launches((cols + 255) / 256, 256, [&](int64_t first, dim3 grid) { copy_weights<<<grid, 256, 0, stream>>>(a.w_in, a.w_out, cols, first); });

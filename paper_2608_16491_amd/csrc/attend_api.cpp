@@ -61,6 +61,7 @@ int check_attend(const frog_attend_t* a, bool backward) {
     if (a->queries > 0) {
         TRY(check_rows("q", a->q, a->q_stride, rows, size));
         TRY(check_rows("out", a->out, a->out_stride, rows, size));
+        if (a->out_low && size == 2) TRY(check_rows("out_low", a->out_low, a->out_stride, rows, size));
     }
     if (a->keys > 0) {
         TRY(check_rows("k", a->k, a->k_stride, cols, size));

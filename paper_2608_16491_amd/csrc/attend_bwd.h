@@ -21,13 +21,18 @@ struct RowPack {
     int tiles;
 };
 
-// delta is a 32-bit sum over the output as it was rounded to the type: where a
-// row's weight lies on few keys, dout . v - delta is small beside both, and the
-// rounding shows.  dq and dk of bf16 causal rows are off by 0.0037 of their norm at
-// 2 tokens, 0.0026 at 64, 0.0025 from 257 on (0.0017: computed in 32 bits and
-// rounded once).  The output in more bits would have to be kept for it.
+// delta is a 32-bit sum over the output and what its rounding left (out_low).
+// Where a row's weight lies on few keys, dout . v - delta is small beside both: from
+// the rounded output alone dq and dk of 16-bit causal rows were off by 2.7 times a
+// single rounding at 2 tokens, 1.7 at 64 and 1.5 at 2,500 (1.41, the square root of
+// 2, is what rounding dx leaves).  The output itself is a sum of rounded weights,
+// which few keys do not average out (still 1.53 at 2 tokens): of 16-bit rows that
+// see at most kSummedKeys keys delta is sum p (dout . v), by its definition.
+// 8,192 tokens, 16 heads, d = 128, bf16: 18 us (100 MB), 26 where a wavefront has
+// such rows and is the last to end.
+constexpr int kSummedKeys = 16;
 template <typename T, int D, bool GRAD>
-__global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, RowPack pack, const float* lse, float shift) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void pack_rows(frog_attend_t a, ScoreParams sp, int group, RowPack pack, const float* lse, float shift) {
     const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
     if (blockIdx.x == 0 && threadIdx.x < 128) ((float*)pack.zeros)[threadIdx.x] = 0.f;
     const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), pairs = a.batch * a.kv_heads;
@@ -42,11 +47,14 @@ __global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, Row
     if (!some) lo = 1, hi = 0;
     float* out = pack.rows + at * RowPack::kFloats;
     const int64_t stat = (b * a.heads + q.head) * a.queries + q.token;
+    // (-inf: no key, or a bias that leaves none a weight)
+    const float lse2 = some && lse[stat] > -INFINITY ? lse[stat] * kLog2e : INFINITY;
     if constexpr (GRAD) {
         // a piece of 16 bytes a lane, LANES lanes a row (a power of two; D = 96
         // leaves some without one), as many rows at once as fit
         constexpr int PER = 16 / sizeof(T), PIECES = D / PER, LANES = PIECES <= 4 ? 4 : PIECES <= 8 ? 8 : PIECES <= 16 ? 16 : 32, AT = 64 / LANES;
         const int piece = lane % LANES;
+        const bool few = sizeof(T) == 2 && some && hi - lo < kSummedKeys;
 #pragma unroll
         for (int r0 = 0; r0 < 32; r0 += AT) {
             const int r = r0 + lane / LANES;
@@ -55,21 +63,62 @@ __global__ __launch_bounds__(256) void pack_rows(frog_attend_t a, int group, Row
             if (piece < PIECES) {
                 const vec<T, PER> u = *(const vec<T, PER>*)((const T*)a.dout + b * a.dout_stride[0] + qr.token * a.dout_stride[1] +
                                                             qr.head * a.dout_stride[2] + piece * PER);
-                const vec<T, PER> v = *(const vec<T, PER>*)((const T*)a.out + b * a.out_stride[0] + qr.token * a.out_stride[1] +
-                                                            qr.head * a.out_stride[2] + piece * PER);
+                const int64_t at_out = b * a.out_stride[0] + qr.token * a.out_stride[1] + qr.head * a.out_stride[2] + piece * PER;
+                const vec<T, PER> v = *(const vec<T, PER>*)((const T*)a.out + at_out);
 #pragma unroll
                 for (int e = 0; e < PER; ++e) delta = fmaf((float)u[e], (float)v[e], delta);
+                if (sizeof(T) == 2 && a.out_low) {
+                    const vec<T, PER> low = *(const vec<T, PER>*)((const T*)a.out_low + at_out);
+#pragma unroll
+                    for (int e = 0; e < PER; ++e) delta = fmaf((float)u[e], (float)low[e], delta);
+                }
             }
 #pragma unroll
             for (int o = LANES / 2; o; o >>= 1) delta += __shfl_xor(delta, o);
-            const int seen = __shfl(some, r);   // row r's lane
-            if (piece == 0) out[RowPack::kDelta + r] = seen ? delta : 0.f;
+            const int state = __shfl(few ? 2 : some ? 1 : 0, r);   // row r's lane
+            if (piece == 0 && state < 2) out[RowPack::kDelta + r] = state ? delta : 0.f;
+        }
+        if constexpr (sizeof(T) == 2) {
+            // the others, from the least of their keys on 32 at a time, as in
+            // attend_keys: a lane owns a row, so the sums stay in it
+            float delta = 0.f;
+            for (bool left = few; __any(left);) {
+                const int first = col_min(left ? lo : INT_MAX), j = min(first + i, (int)a.keys - 1);
+                const T* kp = (const T*)a.k + b * a.k_stride[0] + hk * a.k_stride[2] + j * a.k_stride[1] + 8 * h;
+                const T* vp = (const T*)a.v + b * a.v_stride[0] + hk * a.v_stride[2] + j * a.v_stride[1] + 8 * h;
+                const T* qp = (const T*)a.q + b * a.q_stride[0] + q.token * a.q_stride[1] + q.head * a.q_stride[2] + 8 * h;
+                const T* gp = (const T*)a.dout + b * a.dout_stride[0] + q.token * a.dout_stride[1] + q.head * a.dout_stride[2] + 8 * h;
+                acc16 z = acc16{}, dp = acc16{};
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) {
+                    z = mma(load_frag(kp + 16 * s), load_frag(qp + 16 * s), z);
+                    dp = mma(load_frag(vp + 16 * s), load_frag(gp + 16 * s), dp);
+                }
+                if (sp.cap2 > 0.f) cap_scores<16>(sp, z);
+                else z *= sp.mul;
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int key = first + acc_row(r, lane);
+                    float x = z[r] - lse2;
+                    if (a.slopes) {
+                        const float ak = a.at_k[b * a.at_k_stride[0] + hk * a.at_k_stride[1] + min(key, (int)a.keys - 1)];
+                        x = fmaf(-(a.slopes[q.head] * kLog2e), fabsf(a.at_q[b * a.at_q_stride + q.token] - ak), x);
+                    }
+                    // (a key that the row does not see may hold anything)
+                    sum += key >= lo && key <= hi ? weight2(x) * dp[r] : 0.f;
+                }
+                sum = half_sum(sum);
+                if (left && hi < first + 32) {
+                    delta = sum;
+                    left = false;
+                }
+            }
+            if (few && h == 0) out[RowPack::kDelta + i] = delta;
         }
     }
     if (h == 0) {
-        // (-inf: no key, or a bias that leaves none a weight)
-        const float z = some ? lse[stat] : -INFINITY;
-        out[RowPack::kLse + i] = z > -INFINITY ? fmaf(z, kLog2e, -shift) : INFINITY;
+        out[RowPack::kLse + i] = lse2 < INFINITY ? fmaf(lse[stat], kLog2e, -shift) : INFINITY;
         out[RowPack::kLo + i] = __int_as_float(lo);
         out[RowPack::kHi + i] = __int_as_float(hi);
         out[RowPack::kSlope + i] = a.slopes ? a.slopes[q.head] * kLog2e : 0.f;

@@ -222,7 +222,7 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
         }
         return;
     }
-    T* out = (T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2];
+    const int64_t to = b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2] + 4 * (lane >> 5);
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
@@ -230,8 +230,19 @@ void attend_tile(frog_attend_t a, ScoreParams sp, int group, int tiles, Parts pa
             vec<T, 4> y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = sum > 0.f ? (T)(o[m][4 * i + e] * inv) : (T)0.f;
-            *(vec<T, 4>*)(out + 32 * m + 8 * i + 4 * (lane >> 5)) = y;
+            *(vec<T, 4>*)((T*)a.out + to + 32 * m + 8 * i) = y;
         }
+    if (sizeof(T) == 2 && a.out_low) {
+#pragma unroll
+        for (int m = 0; m < M; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                vec<T, 4> y;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) y[e] = sum > 0.f ? rounded_off<T>(o[m][4 * i + e] * inv) : (T)0.f;
+                *(vec<T, 4>*)((T*)a.out_low + to + 32 * m + 8 * i) = y;
+            }
+    }
     if (a.lse && lane < 32) a.lse[(b * a.heads + q.head) * a.queries + q.token] = sum > 0.f ? (top + __log2f(sum)) * kLn2 : -INFINITY;
 }
 
@@ -582,10 +593,11 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RG == 1 
             if (d == 0) parts.ml[at] = make_float2(tops[r], sum);
         } else {
             const QueryRow q(r, group, hk);
-            vec<T, 4> t;
+            const int64_t to = b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2] + d;
+            vec<float, 4> t;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) t[e] = sum > 0.f ? (T)(y[e] * inv) : (T)0.f;
-            *(vec<T, 4>*)((T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2] + d) = t;
+            for (int e = 0; e < 4; ++e) t[e] = sum > 0.f ? y[e] * inv : 0.f;
+            put_rounded<T, 4>((T*)a.out + to, a.out_low ? (T*)a.out_low + to : nullptr, t);
             if (a.lse && d == 0) a.lse[(b * a.heads + q.head) * a.queries + q.token] = sum > 0.f ? (tops[r] + __log2f(sum)) * kLn2 : -INFINITY;
         }
     }
@@ -788,13 +800,13 @@ struct Joined {
         }
     }
     template <typename T>
-    __device__ inline void write(T* out, int lane) const {
+    __device__ inline void write(T* out, T* low, int lane) const {
         const float inv = sum > 0.f ? 1.f / sum : 0.f;
         if (lane * V >= D) return;
-        vec<T, V> t;
+        vec<float, V> t;
 #pragma unroll
-        for (int v = 0; v < V; ++v) t[v] = (T)(y[v] * inv);
-        *(vec<T, V>*)(out + lane * V) = t;
+        for (int v = 0; v < V; ++v) t[v] = y[v] * inv;
+        put_rounded<T, V>(out + lane * V, low ? low + lane * V : nullptr, t);
     }
     __device__ inline float lse() const { return sum > 0.f ? (top + __log2f(sum)) * kLn2 : -INFINITY; }
 };
@@ -807,7 +819,8 @@ __device__ inline void join_row(const frog_attend_t& a, int group, const Parts& 
     const QueryRow q(i % rows, group, (int)(x % a.kv_heads));
     Joined<D> y;
     y.add(parts, i, lane);
-    y.write((T*)a.out + b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2], lane);
+    const int64_t to = b * a.out_stride[0] + q.token * a.out_stride[1] + q.head * a.out_stride[2];
+    y.write((T*)a.out + to, a.out_low ? (T*)a.out_low + to : nullptr, lane);
     if (a.lse && lane == 0) a.lse[(b * a.heads + q.head) * a.queries + q.token] = y.lse();
 }
 
@@ -878,7 +891,7 @@ __global__ __launch_bounds__(256) void shared_join(frog_attend_shared_t a, int g
     Joined<D> y;
     y.add(prefix, (h / group * a.batch + b) * group + h % group, lane);
     y.add(tail, i, lane);
-    y.write((T*)a.out + b * a.out_stride[0] + h * a.out_stride[1], lane);
+    y.write((T*)a.out + b * a.out_stride[0] + h * a.out_stride[1], (T*)nullptr, lane);
     if (a.lse && lane == 0) a.lse[i] = y.lse();
 }
 

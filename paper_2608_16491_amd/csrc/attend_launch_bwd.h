@@ -10,8 +10,9 @@ template <typename T, int D, bool GRAD>
 RowPack launch_pack(const frog_attend_t& a, const PackPlan& p, const float* lse, char* pack, hipStream_t s) {
     const RowPack r{(float*)(pack + p.rows), (int4*)(pack + p.bounds), pack + p.zeros, (int)p.tiles};
     const int64_t waves = a.batch * a.kv_heads * p.tiles;
-    const float shift = scores_of(a.scale, a.cap, a.slopes, a.type) == kCapped ? score_params(a.scale, a.cap, a.type).cap2 : 0.f;
-    pack_rows<T, D, GRAD><<<dim3((unsigned)((waves + 3) / 4)), 256, 0, s>>>(a, a.heads / a.kv_heads, r, lse, shift);
+    const ScoreParams sp = score_params(a.scale, a.cap, a.type);
+    const float shift = scores_of(a.scale, a.cap, a.slopes, a.type) == kCapped ? sp.cap2 : 0.f;
+    pack_rows<T, D, GRAD><<<dim3((unsigned)((waves + 3) / 4)), 256, 0, s>>>(a, sp, a.heads / a.kv_heads, r, lse, shift);
     return r;
 }
 

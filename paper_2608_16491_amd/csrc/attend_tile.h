@@ -76,6 +76,27 @@ __host__ __device__ inline vec<T, C> load_piece(const T* p) {
     return x;
 }
 
+// what the rounding of x to the type leaves of it
+template <typename T>
+__device__ inline T rounded_off(float x) { return (T)(x - (float)(T)x); }
+
+// N values of the output, and what their rounding left (frog_attend_t::out_low;
+// none where `low` is null or rows are fp32)
+template <typename T, int N, typename V>
+__device__ inline void put_rounded(T* out, T* low, const V& x) {
+    vec<T, N> y;
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = (T)x[e];
+    *(vec<T, N>*)out = y;
+    if constexpr (sizeof(T) == 2) {
+        if (!low) return;
+        vec<T, N> r;
+#pragma unroll
+        for (int e = 0; e < N; ++e) r[e] = rounded_off<T>(x[e]);
+        *(vec<T, N>*)low = r;
+    }
+}
+
 // max or sum over lanes L and L ^ 32, in both
 __device__ inline float half_max(float x) {
     auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
