@@ -310,9 +310,9 @@ int frog_bruteforce_filtered(const frog_index_t* idx, const float* d_queries, in
  *   lse = log sum exp z,  p = exp(z - lse),  out = sum p v
  * over the keys of the interval; out = 0 and lse = -inf for an empty one.
  * Values are fp32, fp16 or bf16 (FROG_STORAGE_*); products, softmax
- * statistics and sums are fp32.  With 16-bit values p and the gradient of x
- * are rounded to the type as factors of the second products, and each output
- * once; an fp16 gradient of x (p times the difference of two dot products with
+ * statistics and sums are fp32.  With 16-bit values p (of more than 32 query
+ * rows a kv head) and the gradient of x are rounded to the type as factors of
+ * the second products, and each output once; an fp16 gradient of x (p times the difference of two dot products with
  * dout) below 6e-8 is lost and above 65,504 infinite, so scale the loss where
  * training in fp16.
  *

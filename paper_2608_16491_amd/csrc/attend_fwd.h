@@ -302,7 +302,9 @@ struct FewRows {
 // the scores, and D / 16 values each of 8 value rows, whose transposition is
 // a renaming of registers and one exchange of 16-bit halves; the output's
 // columns come out as d = 4 (L/16) + r times D/16 plus e.  Weights of 16-bit rows
-// are rounded as in attend_tile.
+// are two factors of the second product, the rounded weight and what that left:
+// beside the reads of the cache the second product is nearly free (1,001 keys 13.7
+// -> 13.9 us, 16 caches to 10,000 unchanged), and the output's only rounding is its own.
 template <typename T, int D, int RG>
 struct FewPass {
     static constexpr int K = D / 32, C = D / 16;
@@ -386,7 +388,7 @@ struct FewPass {
                 for (int e = 0; e < 8; ++e) ak[e] = at_key(min(j + row_of(e), last));
             }
             uint32_t met = 0;
-            frag<T> p[RG];
+            frag<T> p[RG], low[RG];
 #pragma unroll
             for (int g = 0; g < RG; ++g) {
                 if (!PLAIN && sp.cap2 > 0.f) {
@@ -427,8 +429,12 @@ struct FewPass {
                     y[e] = exp2_fast(z[g][e] - row.top[g]);
                     row.sum[g] += y[e];
                 }
-                if constexpr (sizeof(T) == 4) p[g] = y;
-                else p[g] = __builtin_convertvector(y, frag<T>);
+                if constexpr (sizeof(T) == 4) {
+                    p[g] = y;
+                } else {
+                    p[g] = __builtin_convertvector(y, frag<T>);
+                    low[g] = __builtin_convertvector(y - __builtin_convertvector(p[g], vec<float, 8>), frag<T>);
+                }
             }
             if constexpr (MASKED) {
                 // values of keys that no row sees may be anything, and must not
@@ -441,7 +447,10 @@ struct FewPass {
             for (int e = 0; e < C; ++e) {
                 const frag<T> vf{vv[0][e], vv[1][e], vv[2][e], vv[3][e], vv[4][e], vv[5][e], vv[6][e], vv[7][e]};
 #pragma unroll
-                for (int g = 0; g < RG; ++g) o[g][e] = mma(vf, p[g], o[g][e]);
+                for (int g = 0; g < RG; ++g) {
+                    o[g][e] = mma(vf, p[g], o[g][e]);
+                    if constexpr (sizeof(T) == 2) o[g][e] = mma(vf, low[g], o[g][e]);
+                }
             }
             if (more) {
                 load_values(next);
@@ -607,7 +616,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RG == 1 
 // tails, for few rows: workgroups below `head` take a part of the prefix for
 // the rows of all requests (at most 16 RG per kv head; none when the prefix is
 // left to attend_tile), the others a part of one request's tail for 16 RG rows
-// of a kv head's group.  Bound by HBM and, at d = 128, by its registers (15 to 24
+// of a kv head's group.  Bound by HBM and, at d = 128, by its registers (15 to 21
 // spilled; fp32 in two groups 87 to 123): 100 tails to 2,000 rows, 8 kv heads, d =
 // 128, bf16, 112 to 120 us (3.7 to 3.4 TB/s).
 template <typename T, int D, int RG, bool PLAIN>
@@ -690,7 +699,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(RG == 1 && 
 
 // The same where prefix and tails are short: one workgroup does both for 16 RG
 // rows of a (request, kv head) and nothing is left to join (the prefix comes
-// from L2 for all requests but the first).  d = 128 spills 5 to 15 registers, fp32
+// from L2 for all requests but the first).  d = 128 spills 5 to 11 registers, fp32
 // in two groups 88 to 109.
 template <typename T, int D, int RG, int W, bool PLAIN>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RG == 1 && sizeof(T) == 2 ? 2 : 1))) void shared_whole(frog_attend_shared_t a, ScoreParams sp, int group) {

@@ -74,3 +74,30 @@ def test_what_the_rounding_of_the_output_left(dtype, tq, tk):
     assert both < off(out, Attention(q, k, v).out)
     a.out_low = low.data_ptr() + 2
     assert F.lib().frog_attend_workspace(C.byref(a), 0) == -1
+
+
+@pytest.mark.parametrize("b,tq,tk,h,kv,d", [(8, 1, 100, 16, 4, 64), (16, 1, 1001, 16, 4, 128), (8, 1, 5000, 32, 8, 96), (4, 5, 3000, 8, 2, 128), (64, 2, 300, 8, 8, 32)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+def test_16_bit_outputs_of_few_rows(dtype, b, tq, tk, h, kv, d):
+    # nothing is rounded on the way but the output: an error of 32-bit sums, 2^-15 and less of the rounding's, only
+    # moves values that lie as near to a tie
+    g = torch.Generator(device="cuda").manual_seed(tk)
+    q, k, v = ((torch.randn(s, generator=g, device="cuda") * std).to(dtype) for s, std in (((b, tq, h, d), 1.5), ((b, tk, kv, d), 1.0), ((b, tk, kv, d), 1.0)))
+    ref = Attention(q, k, v)
+    assert off(F.attend(q, k, v), ref.out) < 1.05 * off(ref.out.to(dtype), ref.out)
+    out, w = F.attend(q, k, v, weights=torch.zeros((b, kv, tk), device="cuda"), cap=20.0)
+    ref = Attention(q, k, v, cap=20.0)
+    assert off(out, ref.out) < 1.05 * off(ref.out.to(dtype), ref.out)
+
+
+@pytest.mark.parametrize("b,prefix,tail,h,kv,d", [(4, 700, 60, 16, 4, 64), (3, 3000, 200, 8, 2, 128), (6, 3000, 100, 8, 2, 96), (3, 0, 900, 40, 1, 64)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+def test_16_bit_outputs_over_a_shared_prefix(dtype, b, prefix, tail, h, kv, d):
+    g = torch.Generator(device="cuda").manual_seed(prefix)
+    q, k, v = ((torch.randn(s, generator=g, device="cuda") * std).to(dtype) for s, std in (((b, h, d), 1.5), ((prefix, kv, d), 1.0), ((prefix, kv, d), 1.0)))
+    pages = torch.randperm(b * tail, generator=g, device="cuda").to(torch.int32).view(b, tail)
+    kp, vp = (torch.randn((b * tail, 1, kv, d), generator=g, device="cuda").to(dtype) for _ in range(2))
+    out = F.attend_shared(q, k, v, kp, vp, pages, torch.full((b,), tail, device="cuda", dtype=torch.int32))
+    own = [torch.cat([x.expand(b, prefix, kv, d), p[pages.long(), 0]], 1) for x, p in ((k, kp), (v, vp))]
+    ref = Attention(q.unsqueeze(1), *own)
+    assert off(out.unsqueeze(1), ref.out) < 1.05 * off(ref.out.to(dtype), ref.out)
