@@ -67,44 +67,46 @@ bool whole_pays(int64_t keys, int64_t blocks, int d, int type, int64_t bytes) {
     return keys <= kWholeKeys && (blocks >= kCUs || keys * d * (type == FROG_STORAGE_F32 ? 8 : 2) <= bytes);
 }
 
-// Schedules are made where intervals may differ (lr), both axes are long and
-// there are more workgroups than start at once: a workgroup's work is then
-// anything from one step to hundreds, and the longest one decides.  Sizes alone
-// do not tell packed documents, which win, from causal masks and windows, which
-// the order without a schedule serves as well, so the bounds are set where what
-// documents win is above what the others lose.  One sequence, d = 128, 16 query
-// and 4 kv heads, gradients alone (both schedules, us with and without):
-//   tokens          4,096       8,192         16,384         32,768
-//   documents       205, 205    409, 472      1,307, 1,492   5,352, 5,979
-//   causal          391, 382    1,146, 1,164  4,574, 4,632   17,515, 18,004
-// and the forward pass 66, 60; 104, 114; 289, 308; 1,038, 1,064 and 108, 105; 281,
-// 290; 1,032, 1,025; 4,015, 4,007.  Windows of 512 keys lose 7 us of 64 in the
-// forward pass of 8,192 tokens and 23 of 332 in a step.  At 6,000 tokens documents
-// win 0 to 7 % of a step, causal masks lose 1.5.  One workgroup makes a schedule,
-// so many short sequences lose by it: 64 of 2,048 tokens (2 heads, d = 64) 76 us of
-// 501, 4,096 of them (1 head, d = 32) half of 11 ms.
-constexpr int64_t kScheduleLength = 6144;
+// Schedules are made where intervals may differ (lr), and a call is long enough
+// for what they win: a workgroup's work is anything from one step to hundreds, and
+// the longest one decides.  Sizes alone do not tell packed documents, which win,
+// from windows and causal masks, which the order without a schedule serves as well
+// (16-bit rows), so the bounds are set where documents win about what the others
+// lose; a launch costs 6 to 10 us.  One sequence, bf16, d = 128, 16 query and 4 kv
+// heads, forward and gradients, us with and without:
+//   tokens     4,096              6,000              8,192               16,384
+//   documents  68, 61; 216, 216   64, 70; 278, 299   105, 115; 432, 497  292, 312; 1,354, 1,546
+//   causal     99, 97; 400, 392   166, 159; 697, 686 286, 293; 1,178, 1,196  1,048, 1,043; 4,566, 4,707
+//   window     38, 32; 176, 166   52, 45; 244, 231   63, 56; 281, 262    111, 102; 504, 468
+// The same lengths of narrower rows are worth less (d = 64, two sequences of 6,144
+// tokens: 81, 85; 290, 333), fp32 rows some 16 times as much (4,096 tokens, d = 64:
+// documents 134, 157; 434, 518, causal masks 325, 406; 1,207, 1,381): kScheduleWork
+// in query-key pairs times d.  Short sequences balance by their number (4 of 3,000
+// tokens: 85, 82; 345, 354).  One workgroup makes a schedule, so its tiles are
+// bounded: of 64 sequences of 2,048 tokens it took 72 us of 500, of 4,096 half of
+// 11 ms, of 8 of 8,192 (512 tiles of keys) as much as it won.
+constexpr double kScheduleWork = 60e9;
+constexpr int64_t kScheduleRowTiles = 1024, kScheduleKeyTiles = 256;
 SchedulePlan schedule_plan(const frog_attend_t& a, int64_t tiles, int parts, int64_t least, int64_t most) {
     SchedulePlan p{};
-    if (!a.lr || std::min(a.keys, a.queries) < kScheduleLength || a.batch * a.kv_heads * tiles < least || a.batch * tiles > most) return p;
+    const bool f32 = a.type == FROG_STORAGE_F32;
+    const int64_t length = std::min(a.keys, a.queries);
+    if (!a.lr || length < (f32 ? 2048 : 4096) || a.batch * a.kv_heads * tiles < least || a.batch * tiles > most) return p;
+    if ((double)a.batch * a.heads * length * length * a.d * (f32 ? 16 : 1) < kScheduleWork) return p;
     p.tiles = tiles;
     p.parts = parts;
     p.bytes = a.batch * tiles * 4;
     return p;
 }
-// Row tiles: above two workgroups for each of the 256 CUs, which start all at
-// once (8,192 tokens of 8 heads, 512 workgroups: 79 us with, 73 without).  Their
-// lengths stay in LDS.
-constexpr int64_t kScheduleRowBlocks = 2 * kCUs + 1, kScheduleRowTiles = 4096;
-SchedulePlan schedule_rows_plan(const frog_attend_t& a, int64_t tiles, int parts) {
-    return schedule_plan(a, tiles, parts, kScheduleRowBlocks, kScheduleRowTiles);
+// Row tiles: above two workgroups for each CU, which start all at once (16-bit rows,
+// 512 workgroups: 79 us with, 73 without).  fp32 workgroups differ by so much that
+// one a CU is enough in the forward pass (256 workgroups, causal: 188, 224).
+SchedulePlan schedule_rows_plan(const frog_attend_t& a, int64_t tiles, int parts, bool forward) {
+    return schedule_plan(a, tiles, parts, a.type == FROG_STORAGE_F32 ? (forward ? kCUs : kCUs + 1) : 2 * kCUs + 1, kScheduleRowTiles);
 }
-// Key tiles: from one for each CU (cut in parts, so four workgroups; 8,192 tokens
-// of one kv head, 64 tiles: 254 us with, 253 without), and as many as the counting
-// of their rows, a wavefront a tile, takes 30 us for.
-constexpr int64_t kScheduleKeyBlocks = kCUs, kScheduleKeyTiles = 512;
+// Key tiles are cut in parts: half a tile (fp32: a quarter) for each CU and more.
 SchedulePlan schedule_keys_plan(const frog_attend_t& a, int64_t tiles, int parts) {
-    return schedule_plan(a, tiles, parts, kScheduleKeyBlocks, kScheduleKeyTiles);
+    return schedule_plan(a, tiles, parts, a.type == FROG_STORAGE_F32 ? kCUs / 4 : kCUs / 2 + 1, kScheduleKeyTiles);
 }
 
 ForwardPlan forward_plan(const frog_attend_t& a) {
@@ -122,7 +124,7 @@ ForwardPlan forward_plan(const frog_attend_t& a) {
     // (with key weights too, where a second launch follows in any case, so that
     // they do not change the output: 512 keys 17.3 us whole, 16.3 split)
     if (p.few && p.groups == 1 && whole_pays(a.keys, pairs, a.d, a.type, kWholeBytes)) p.splits = 1;
-    if (!p.few) p.plan = schedule_rows_plan(a, p.tiles, p.splits);
+    if (!p.few) p.plan = schedule_rows_plan(a, p.tiles, p.splits, true);
     int64_t at = 0;
     p.plan.at = take(&at, p.plan.bytes);
     if (p.splits > 1) {
@@ -156,7 +158,7 @@ PackPlan pack_plan(const frog_attend_t& a, bool grad) {
     p.parts = parts_until(4 * kCUs, blocks, p.tiles / 8);
     const int64_t key_tiles = (a.keys + kTileRows - 1) / kTileRows, row_tiles = (p.tiles + 3) / 4;
     p.keys_plan = schedule_keys_plan(a, key_tiles, p.parts);
-    if (grad) p.rows_plan = schedule_rows_plan(a, row_tiles, 1);
+    if (grad) p.rows_plan = schedule_rows_plan(a, row_tiles, 1, false);
     int64_t at = 0;
     p.keys_plan.at = take(&at, p.keys_plan.bytes);
     p.rows_plan.at = take(&at, p.rows_plan.bytes);
@@ -308,15 +310,19 @@ __global__ __launch_bounds__(kSortBlock) void schedule_key_tiles(frog_attend_t a
 
 }  // namespace
 
-// tiles whose workgroups (of all kv heads) are one for each of the 256 CUs
-static int cu_tiles(const frog_attend_t& a, int parts) { return (int)std::max<int64_t>(1, kCUs / ((int64_t)a.kv_heads * parts)); }
-
-void schedule_rows(const frog_attend_t& a, const SchedulePlan& p, char* ws, hipStream_t s) {
-    schedule_row_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, a.heads / a.kv_heads, (int)p.tiles, cu_tiles(a, p.parts), (int*)(ws + p.at));
+// tiles whose workgroups (of all kv heads) are one for each of the 256 CUs; all of
+// them where a CU holds one workgroup (shortest first after the longest, a causal
+// pass of 4,096 fp32 tokens, d = 128, took 770 us instead of 639)
+static int cu_tiles(const frog_attend_t& a, const SchedulePlan& p, bool alone) {
+    return alone ? (int)(a.batch * p.tiles) : (int)std::max<int64_t>(1, kCUs / ((int64_t)a.kv_heads * p.parts));
 }
 
-void schedule_keys(const frog_attend_t& a, const SchedulePlan& p, const int4* bounds, int row_tiles, char* ws, hipStream_t s) {
-    schedule_key_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, (int)p.tiles, bounds, row_tiles, cu_tiles(a, p.parts), (int*)(ws + p.at));
+void schedule_rows(const frog_attend_t& a, const SchedulePlan& p, bool alone, char* ws, hipStream_t s) {
+    schedule_row_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, a.heads / a.kv_heads, (int)p.tiles, cu_tiles(a, p, alone), (int*)(ws + p.at));
+}
+
+void schedule_keys(const frog_attend_t& a, const SchedulePlan& p, bool alone, const int4* bounds, int row_tiles, char* ws, hipStream_t s) {
+    schedule_key_tiles<<<dim3(1), kSortBlock, 0, s>>>(a, (int)p.tiles, bounds, row_tiles, cu_tiles(a, p, alone), (int*)(ws + p.at));
 }
 
 int64_t attend_ws(const frog_attend_t& a) {

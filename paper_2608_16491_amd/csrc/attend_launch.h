@@ -54,9 +54,9 @@ struct PackPlan {
 PackPlan pack_plan(const frog_attend_t& a, bool grad);
 
 // Write the schedule of tiles of kTileRows query rows, or of as many keys
-// (bounds, row_tiles: RowPack).
-void schedule_rows(const frog_attend_t& a, const SchedulePlan& p, char* ws, hipStream_t s);
-void schedule_keys(const frog_attend_t& a, const SchedulePlan& p, const int4* bounds, int row_tiles, char* ws, hipStream_t s);
+// (bounds, row_tiles: RowPack).  alone: a CU holds one workgroup of the pass.
+void schedule_rows(const frog_attend_t& a, const SchedulePlan& p, bool alone, char* ws, hipStream_t s);
+void schedule_keys(const frog_attend_t& a, const SchedulePlan& p, bool alone, const int4* bounds, int row_tiles, char* ws, hipStream_t s);
 
 // f(a constant of this kind), for rows of type T (fp32 rows are never kCapped)
 template <typename T, typename F>

@@ -21,7 +21,7 @@ void launch_keys(const frog_attend_t& a, const ScoreParams& sp, const PackPlan& 
     const int group = a.heads / a.kv_heads, tiles = (int)((a.keys + kTileRows - 1) / kTileRows);
     const KeyParts parts{(float*)(pack + p.o), p.parts};
     const int* order = p.keys_plan.order(pack);
-    if (order) schedule_keys(a, p.keys_plan, r.bounds, r.tiles, pack, s);
+    if (order) schedule_keys(a, p.keys_plan, sizeof(T) == 4 && D >= 96, r.bounds, r.tiles, pack, s);
     const dim3 grid((unsigned)(a.batch * a.kv_heads * tiles * p.parts));
     by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) {
         attend_keys<T, D, decltype(kind)::value, GRAD, 4><<<grid, 256, 0, s>>>(a, sp, group, tiles, r, parts, order);
@@ -47,7 +47,7 @@ void launch_backward(const frog_attend_t& a, char* pack, hipStream_t s) {
     const int qt = (int)((a.queries * group + kTileRows - 1) / kTileRows);
     launch_keys<T, D, true>(a, sp, p, r, pack, s);
     const int* order = p.rows_plan.order(pack);
-    if (order) schedule_rows(a, p.rows_plan, pack, s);
+    if (order) schedule_rows(a, p.rows_plan, sizeof(T) == 4 && D >= 128, pack, s);
     const dim3 qg((unsigned)(a.batch * a.kv_heads * qt));
     by_scores<T>(scores_of(a.scale, a.cap, a.slopes, a.type), [&](auto kind) { attend_dq<T, D, decltype(kind)::value, 4><<<qg, 256, 0, s>>>(a, sp, group, qt, r, order); });
 }

@@ -27,7 +27,7 @@ void launch_forward(const frog_attend_t& a, const ForwardPlan& p, char* ws, hipS
     if (a.w_out && !a.lse) b.lse = (float*)(ws + p.lse);
     if (!p.few) {
         const int* order = p.plan.order(ws);
-        if (order) schedule_rows(a, p.plan, ws, s);
+        if (order) schedule_rows(a, p.plan, sizeof(T) == 4 && D >= 96, ws, s);
         launch_tiles<T, D>(b, sp, group, p.tiles, parts, order, s);
         if (p.splits > 1) attend_join<T, D><<<dim3((unsigned)((parts.total + 3) / 4)), 256, 0, s>>>(b, group, parts);
         if (a.w_out) AttendLaunch<T>::weigh(b, b.lse, ws + p.pack, s);

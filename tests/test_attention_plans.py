@@ -10,43 +10,50 @@ import paper_2608_16491_amd as F  # noqa: E402
 from paper_2608_16491_amd import attention as A  # noqa: E402
 
 
-def workspace(backward, lr, batch, tokens, heads, kv, d=64, keys=None, w=None):
+F32, BF16 = 0, 2
+
+
+def workspace(backward, lr, batch, tokens, heads, kv, d, type_=BF16, keys=None):
     a = A.AttendArgs()
     for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv"):
         setattr(a, n, 4096)
         setattr(a, n + "_stride", (0, d * heads, d))
-    a.batch, a.queries, a.keys, a.heads, a.kv_heads, a.d, a.type, a.scale = batch, tokens, keys or tokens, heads, kv, d, 2, 0.125
-    a.lr, a.lse, a.w_out = 4096 if lr else None, 4096, w
+    a.batch, a.queries, a.keys, a.heads, a.kv_heads, a.d, a.type, a.scale = batch, tokens, keys or tokens, heads, kv, d, type_, 0.125
+    a.lr, a.lse = 4096 if lr else None, 4096
     n = F.lib().frog_attend_workspace(C.byref(a), backward)
     assert n >= 0, F.lib().frog_last_error()
     return n
 
 
-# batch, tokens, heads, kv heads, and whether rows (forward) and keys (gradients) are ordered
-@pytest.mark.parametrize("batch,tokens,heads,kv,rows,keys", [
-    (1, 8192, 16, 4, True, True), (1, 8191, 12, 12, True, True), (1, 32768, 16, 4, True, True), (4, 8192, 16, 4, True, True),
-    (1, 4096, 16, 4, False, False), (1, 2048, 32, 8, False, False), (1, 8192, 8, 1, False, False), (1, 131072, 4, 1, True, False),
-    (64, 2048, 2, 2, False, False), (1024, 2048, 2, 2, False, False), (4096, 2048, 1, 1, False, False), (64, 8192, 2, 2, True, False),
-    (65, 8192, 64, 64, False, False)])
-def test_orders_are_made_where_they_pay(batch, tokens, heads, kv, rows, keys):
-    order = [workspace(b, True, batch, tokens, heads, kv) - workspace(b, False, batch, tokens, heads, kv) for b in (0, 1)]
-    tiles = -(-tokens * (heads // kv) // 128) * batch
-    assert order[0] == (-(-4 * tiles // 256) * 256 if rows else 0)
-    key_tiles = -(-tokens // 128) * batch
-    assert order[1] == order[0] + (-(-4 * key_tiles // 256) * 256 if keys else 0)
+# batch, tokens, heads, kv heads, d, type, and whether rows (forward), keys and rows (gradients) are ordered
+@pytest.mark.parametrize("batch,tokens,heads,kv,d,type_,rows,keys,dq", [
+    (1, 8192, 16, 4, 128, BF16, True, True, True), (1, 8191, 12, 12, 96, BF16, True, True, True), (1, 32768, 16, 4, 128, BF16, True, True, True),
+    (4, 8192, 16, 4, 64, BF16, True, True, True), (1, 4096, 16, 4, 128, BF16, False, False, False), (1, 2048, 32, 8, 128, BF16, False, False, False),
+    (1, 8192, 8, 1, 64, BF16, False, False, False), (1, 16384, 8, 1, 64, BF16, True, False, True), (64, 2048, 4, 4, 64, BF16, False, False, False),
+    (1024, 2048, 2, 2, 64, BF16, False, False, False), (4096, 2048, 1, 1, 32, BF16, False, False, False), (8, 8192, 8, 2, 64, BF16, False, False, False),
+    (1, 4096, 16, 4, 64, F32, True, True, True), (1, 4096, 8, 8, 64, F32, True, True, False), (1, 2048, 8, 8, 64, F32, False, False, False),
+    (1, 1500, 32, 4, 128, F32, False, False, False), (16, 2048, 4, 4, 64, F32, True, True, True)])
+def test_orders_are_made_where_they_pay(batch, tokens, heads, kv, d, type_, rows, keys, dq):
+    order = [workspace(b, True, batch, tokens, heads, kv, d, type_) - workspace(b, False, batch, tokens, heads, kv, d, type_) for b in (0, 1)]
+    row_tiles, key_tiles = -(-tokens * (heads // kv) // 128) * batch, -(-tokens // 128) * batch
+    size = [-(-4 * n // 256) * 256 for n in (row_tiles, key_tiles)]
+    assert order[0] == (size[0] if rows else 0)
+    assert order[1] == (size[0] if dq else 0) + (size[1] if keys else 0)
 
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("mask", ["documents", "one", "lengths", "empty", "wild"])
-@pytest.mark.parametrize("batch,tq,tk", [(1, 6500, 6144), (2, 6144, 6501)])
-def test_ordered_passes(mask, batch, tq, tk):
+@pytest.mark.parametrize("type_,batch,tq,tk,d", [(BF16, 1, 6500, 6144, 128), (F32, 1, 2600, 2500, 96), (F32, 2, 2100, 2304, 64)])
+def test_ordered_passes(mask, type_, batch, tq, tk, d):
     # sizes whose tiles are ordered, each group of heads against the formulas in 64 bits
     from tests.attention_ref import Attention, intervals, near
-    h, kv, d = 12, 6, 32
-    assert workspace(0, True, batch, tq, h, kv, d, tk) > workspace(0, False, batch, tq, h, kv, d, tk)
+    h, kv = 14, 7
+    for backward in (0, 1):
+        assert workspace(backward, True, batch, tq, h, kv, d, type_, tk) > workspace(backward, False, batch, tq, h, kv, d, type_, tk)
     print(f"[gpu] ordered passes {mask} {batch} x {tq} x {tk}", flush=True)
     g = torch.Generator(device="cuda").manual_seed(tq)
-    q, k, v, dout = (torch.randn(s, generator=g, device="cuda").to(torch.bfloat16) for s in ((batch, tq, h, d), (batch, tk, kv, d), (batch, tk, kv, d), (batch, tq, h, d)))
+    q, k, v, dout = (torch.randn(s, generator=g, device="cuda").to(torch.bfloat16 if type_ == BF16 else torch.float32)
+                     for s in ((batch, tq, h, d), (batch, tk, kv, d), (batch, tk, kv, d), (batch, tq, h, d)))
     lr = intervals("causal" if mask == "one" else mask, batch, tq, tk, 5).cuda()
     if mask == "one":
         # a few rows see every key, the others one
@@ -62,9 +69,6 @@ def test_ordered_passes(mask, batch, tq, tk):
             got = (out[b:b + 1, :, hs], lse[b:b + 1, hs], w[b:b + 1, i:i + 1], grads[0][b:b + 1, :, hs], grads[1][b:b + 1, :, i:i + 1], grads[2][b:b + 1, :, i:i + 1])
             for what, y in zip(("out", "lse", "weights", "dq", "dk", "dv"), got):
                 near(y, getattr(ref, what), getattr(ref, what + "_err"), f"{mask} {what}")
-
-
-F32, BF16 = 0, 2
 
 
 # batch, keys, heads, kv heads, d, type, key weights, and whether one launch takes all (no workspace)
