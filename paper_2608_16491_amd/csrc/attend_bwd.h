@@ -28,8 +28,8 @@ struct RowPack {
 // 2, is what rounding dx leaves).  The output itself is a sum of rounded weights,
 // which few keys do not average out (still 1.53 at 2 tokens): of 16-bit rows that
 // see at most kSummedKeys keys delta is sum p (dout . v), by its definition.
-// 8,192 tokens, 16 heads, d = 128, bf16: 18 us (100 MB), 26 where a wavefront has
-// such rows and is the last to end.
+// 8,192 tokens, 16 heads, d = 128, bf16: 18 us (100 MB), 23 where a wavefront has
+// such rows (26 with the tiles of one kv head after another).
 constexpr int kSummedKeys = 16;
 template <typename T, int D, bool GRAD>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void pack_rows(frog_attend_t a, ScoreParams sp, int group, RowPack pack, const float* lse, float shift) {
@@ -37,15 +37,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void p
     if (blockIdx.x == 0 && threadIdx.x < 128) ((float*)pack.zeros)[threadIdx.x] = 0.f;
     const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), pairs = a.batch * a.kv_heads;
     if (at >= pairs * pack.tiles) return;
-    const int64_t x = at / pack.tiles, b = x / a.kv_heads;
-    const int tile = (int)(at % pack.tiles), hk = (int)(x % a.kv_heads);
+    // (earlier tiles first: there the rows stand that take longest, see below)
+    const int64_t x = at % pairs, b = x / a.kv_heads;
+    const int tile = (int)(at / pairs), hk = (int)(x % a.kv_heads);
     const int64_t rows = a.queries * group, row = (int64_t)tile * 32 + i;
     const QueryRow q(min(row, rows - 1), group, hk);
     int lo, hi;
     interval(a, b, q.token, &lo, &hi);
     const bool some = row < rows && lo <= hi;
     if (!some) lo = 1, hi = 0;
-    float* out = pack.rows + at * RowPack::kFloats;
+    float* out = pack.rows + (x * pack.tiles + tile) * RowPack::kFloats;
     const int64_t stat = (b * a.heads + q.head) * a.queries + q.token;
     // (-inf: no key, or a bias that leaves none a weight)
     const float lse2 = some && lse[stat] > -INFINITY ? lse[stat] * kLog2e : INFINITY;
