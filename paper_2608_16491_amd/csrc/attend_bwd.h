@@ -208,7 +208,8 @@ __device__ inline void cap_slopes(const ScoreParams& sp, acc16& z, acc16& f) {
 // active 43 % of the time, products 18 %); every key of 8,192 seen, no cap: a step
 // 2.79 -> 2.66 ms, 750 to 825 TFLOP/s here (fp32, 4,096 tokens: 100).
 //   Of 16-bit rows p and dx = p (dp - delta) are rounded to the type as factors of
-// the second products, as in attend_tile; an fp16 dx above 65,504 is infinite.
+// the second products, as in attend_tile (dx in two factors here and in attend_dq:
+// 8,192 causal tokens, d = 64, 678 -> 785 us); an fp16 dx above 65,504 is infinite.
 //   GRAD: dk = sum dx q, dv = sum p dout.  Else: w_out = w_in + sum p.
 template <typename T, int D, Scores KIND, bool GRAD, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1)))
