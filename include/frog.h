@@ -6,7 +6,8 @@
  * 2608.16491) on one AMD GPU, plus the host-side index construction that
  * produces its input and an exhaustive filtered search used as ground truth;
  * and attention over rows kept in attribute order, each query over one rank
- * interval of them, with the upkeep of the cache that holds the rows.
+ * interval of them, with the upkeep of the cache that holds the rows, and a
+ * cache in 8-bit pages with the attention that reads all or chosen ones of them.
  *
  * Conventions for every entry point:
  *   - Return value: FROG_OK (0) or a negative FROG_E* code.  frog_last_error()
@@ -441,6 +442,133 @@ typedef struct {
 
 int64_t frog_evict_workspace(const frog_evict_t* a);
 int frog_evict(const frog_evict_t* a, void* stream);
+
+/* ---------------------------------------------------------- cache in pages
+ *
+ * Keys and values of many requests in 8 bits: a row of d values is d codes and
+ * one power of two.  With a the row's largest magnitude, L = 448 for e4m3 codes
+ * and 127 for int8, and e the least integer >= -100 with a <= L 2^e,
+ *   code = x 2^-e rounded to nearest, ties to even;   the row's value: code 2^e
+ * (exact in bf16, and in any type of more bits that holds its magnitude; int8
+ * rows above 127 2^121 may have values of 2^128, which are infinite).  The
+ * power is kept as the byte e + 127; a row that is not finite has the byte 255
+ * and codes 0, and its value is NaN.
+ * A page holds `page` rows of every kv head.  Row t of a request is row t % page
+ * of the page pages[request][t / page]: pages is a table
+ * [batch][pages_per_request] of page numbers.  Entries past a request's length
+ * are not read into a result, lengths are clipped to [0, pages_per_request *
+ * page], and an entry outside [0, num_pages) counts as no rows.  One token that
+ * is decoded several times at once (a draft of the next tokens) is several
+ * requests of the same pages with lengths that grow by one.
+ * `bounds` are, per page and kv head, the least and the largest value of every
+ * channel of the keys written to the page since its row 0 was: whatever a
+ * request's rows are, q . k of a page's rows is at most
+ * sum max(q least, q largest).  (NaN where a row was not finite.)
+ * d is 32, 64, 96 or 128 (FROG_EUNSUPPORTED otherwise); page 16, 32, 64, 128 or
+ * 256.  The arrays are packed, on 16-byte boundaries, fewer than 2^35 rows of
+ * one head each.  Rows outside the cache are strided as in the attention section. */
+enum { FROG_CACHE_E4M3 = 0, FROG_CACHE_INT8 = 1 };
+
+typedef struct {
+    void* k;                 /* [num_pages][kv_heads][page][d] codes */
+    void* v;
+    uint8_t* k_exp;          /* [num_pages][kv_heads][page] */
+    uint8_t* v_exp;
+    void* bounds;            /* [num_pages][kv_heads][2][d] bf16, least and largest; NULL: not kept */
+    int64_t num_pages;
+    int32_t kv_heads, page, d, storage;
+} frog_cache_t;
+
+/* Append rows to the requests: the rows [starts[b], starts[b + 1]) of k and v
+ * become the last rows of request b, whose length with them is lengths[b].
+ * starts NULL: tokens / batch rows each.  A row before the request's start or
+ * past its pages, or of a page that is none, is not written.  starts ascend and
+ * end at `tokens` at most (rows outside are not read).  A page that two
+ * requests write in one call holds a mixture of both. */
+typedef struct {
+    frog_cache_t cache;
+    const void* k; int64_t k_stride[2];        /* [tokens, kv_heads, d]: token, head */
+    const void* v; int64_t v_stride[2];
+    const int32_t* starts;                     /* [batch + 1]; NULL: equal shares */
+    const int32_t* pages;                      /* [batch][pages_per_request] */
+    const int32_t* lengths;                    /* [batch], the new rows included */
+    int64_t batch, tokens, pages_per_request;
+    int32_t type;                              /* of k and v: FROG_STORAGE_* */
+} frog_cache_write_t;
+
+int frog_cache_write(const frog_cache_write_t* a, void* stream);
+
+/* The rows of the requests, rounded to the type of k and v (a magnitude the type
+ * does not hold is infinite); 0 past a length.  All `slots` rows of every
+ * request are written. */
+typedef struct {
+    frog_cache_t cache;
+    void* k; int64_t k_stride[3];              /* [batch, slots, kv_heads, d]: request, row, head */
+    void* v; int64_t v_stride[3];
+    const int32_t* pages;
+    const int32_t* lengths;
+    int64_t batch, slots, pages_per_request;
+    int32_t type;
+} frog_cache_read_t;
+
+int frog_cache_read(const frog_cache_read_t* a, void* stream);
+
+/* The pages worth a token's look: of the pages that hold rows of request b, for
+ * every kv head `keep` (all, where there are no more): the first `first`, the
+ * newest `recent`, and of the others those with the largest bound on the scores
+ * of the head's query heads, summed over them: with Q+ and Q- the sums over the
+ * heads of max(q, 0) and min(q, 0),
+ *   sum over channels of Q+ largest + Q- least
+ * (for finite bounds the sum over heads and channels of max(q least, q largest)),
+ * summed in 64 bits and rounded once to 32 (equal sums: the lower page; NaN
+ * counts as the largest; a page that is none as the smallest).  chosen lists
+ * them ascending, as numbers within the request (0 .. pages_per_request - 1),
+ * and holds -1 behind them.
+ * first + recent <= keep. */
+typedef struct {
+    frog_cache_t cache;                        /* k, v and their powers may be NULL */
+    const void* q; int64_t q_stride[2];        /* [batch, heads, d]: request, head */
+    const int32_t* pages;
+    const int32_t* lengths;
+    int32_t* chosen;                           /* [batch][kv_heads][keep], written */
+    void* ws;                                  /* as for frog_attend */
+    int64_t ws_bytes;
+    int64_t batch, pages_per_request, keep, first, recent;
+    int32_t heads, type;
+} frog_select_pages_t;
+
+int64_t frog_select_pages_workspace(const frog_select_pages_t* a);
+int frog_select_pages(const frog_select_pages_t* a, void* stream);
+
+/* Attention of one token per request over its pages, or over the chosen ones of
+ * them, with the formulas and options of the attention section.  The query
+ * stands at lengths[b] - 1 (its distance to a key is the difference of the
+ * numbers as floats: exact up to 2^24).  lr (optional) limits the rows a
+ * request sees.  chosen (optional) [batch][kv_heads][num_chosen]: pages of the
+ * request by their numbers within it, in any order; an entry outside [0,
+ * pages_per_request) is none, and a page listed twice counts twice.  Codes and
+ * powers enter the products exactly; queries, weights and sums are as exact as
+ * 32 bits for fp32 queries, and for 16-bit ones weights are held to 2^-16.  The
+ * rows' magnitudes must stay below 2^100, those behind a length may be anything. */
+typedef struct {
+    frog_cache_t cache;
+    const void* q; int64_t q_stride[2];        /* [batch, heads, d]: request, head */
+    const int32_t* pages;
+    const int32_t* lengths;
+    const int32_t* chosen;                     /* NULL: every page */
+    const int32_t* lr;                         /* [batch][2]; NULL: every row */
+    const float* slopes;                       /* [heads]; NULL: no distance bias */
+    void* out; int64_t out_stride[2];
+    float* lse;                                /* [batch][heads]; NULL: not wanted */
+    void* ws;                                  /* as for frog_attend */
+    int64_t ws_bytes;
+    int64_t batch, pages_per_request, num_chosen;
+    int32_t heads, type;
+    float scale, cap;
+} frog_attend_paged_t;
+
+int64_t frog_attend_paged_workspace(const frog_attend_paged_t* a);
+int frog_attend_paged(const frog_attend_paged_t* a, void* stream);
 
 /* Message of the last failure on this thread ("" if none). */
 const char* frog_last_error(void);

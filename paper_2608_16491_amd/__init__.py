@@ -33,6 +33,8 @@ SYMBOLS = (
     "frog_search_ex", "frog_search_noalloc", "frog_index_prepare_sample", "frog_bruteforce_filtered",
     "frog_attend", "frog_attend_backward", "frog_attend_workspace", "frog_attend_shared",
     "frog_attend_shared_workspace", "frog_evict", "frog_evict_workspace",
+    "frog_cache_write", "frog_cache_read", "frog_select_pages", "frog_select_pages_workspace",
+    "frog_attend_paged", "frog_attend_paged_workspace",
     "frog_last_error",
 )
 
@@ -110,11 +112,11 @@ def lib() -> C.CDLL:
     L.frog_index_prepare_sample.argtypes = [P, C.c_uint64]
     L.frog_bruteforce_filtered.restype = i32
     L.frog_bruteforce_filtered.argtypes = [P, P, i64, P, P, i32, P, P, P, P]
-    for name in ("frog_attend", "frog_attend_shared", "frog_evict"):
+    for name in ("frog_attend", "frog_attend_shared", "frog_evict", "frog_select_pages", "frog_attend_paged"):
         for fn, args, res in ((name, [P, P], i32), (name + "_workspace", [P] + [i32] * (name == "frog_attend"), i64)):
             getattr(L, fn).argtypes, getattr(L, fn).restype = args, res
-    L.frog_attend_backward.restype = i32
-    L.frog_attend_backward.argtypes = [P, P]
+    for name in ("frog_attend_backward", "frog_cache_write", "frog_cache_read"):
+        getattr(L, name).argtypes, getattr(L, name).restype = [P, P], i32
     _lib = L
     return L
 
@@ -330,12 +332,15 @@ def bruteforce(index: Index, Q, lo, hi, k: int, stream=None):
 # ------------------------------------------------------------------ attention
 
 _ATTENTION = ("attend", "attend_shared", "evict")
+_PAGED = ("PagedCache", "cache_write", "cache_read", "select_pages", "attend_paged")
 
 
 def __getattr__(name):
-    # attend, attend_shared and evict need torch, which this module imports
-    # only where a call does
+    # these need torch, which this module imports only where a call does
     if name in _ATTENTION:
         from . import attention
         return getattr(attention, name)
+    if name in _PAGED:
+        from . import paged
+        return getattr(paged, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

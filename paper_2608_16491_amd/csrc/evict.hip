@@ -11,6 +11,7 @@
 // us, copy 120 (5.0 TB/s read and written).
 
 #include "attend.h"
+#include "pick.h"
 
 namespace frog {
 namespace {
@@ -26,26 +27,8 @@ __device__ inline uint32_t code_of(float w) {
 
 __device__ inline int64_t live_rows(const frog_evict_t& a, int64_t b) { return max((int64_t)0, min((int64_t)a.lengths[b], a.slots)); }
 
-// inclusive prefix sum over the workgroup (part: a value per wavefront)
-__device__ inline int block_scan(int x, int* part) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-    }
-    if (lane == 63) part[w] = x;
-    __syncthreads();
-    int before = 0;
-#pragma unroll
-    for (int i = 0; i < kBlock / 64 - 1; ++i) before += i < w ? part[i] : 0;
-    return x + before;
-}
-
 __global__ __launch_bounds__(kBlock) void evict_pick(frog_evict_t a, int32_t* list, int64_t first) {
-    constexpr int W = kBlock / 64, kBins = 2 * kBlock;
-    __shared__ int hist[kBins], part[W], bound[2], counts[2][W];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ PickSpace<kBlock> space;
     const int64_t row = first + blockIdx.x, b = row / a.heads;
     const int n = (int)live_rows(a, b), keep = (int)a.keep;
     const int recent = (int)min((int64_t)n, a.recent), old = n - recent;
@@ -54,72 +37,13 @@ __global__ __launch_bounds__(kBlock) void evict_pick(frog_evict_t a, int32_t* li
     // of the `old` first rows the `want` heaviest: those above `code`, and the
     // first `ties` equal to it
     const int want = min(old, keep - recent);
-    uint32_t code = 0;
-    int ties = 0;
-    if (want > 0 && want < old) {
-        ties = want;
-        constexpr int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
-#pragma unroll
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = shifts[pass], top = shift + bits[pass];
-            hist[threadIdx.x] = hist[threadIdx.x + kBlock] = 0;
-            __syncthreads();
-            for (int i = threadIdx.x; i < old; i += kBlock) {
-                const uint32_t c = code_of(w[i]);
-                if (pass == 0 || (c >> (top & 31)) == (code >> (top & 31))) atomicAdd(&hist[(c >> shift) & ((1u << bits[pass]) - 1)], 1);
-            }
-            __syncthreads();
-            // two bins a thread, from the largest digit down
-            const int d = kBins - 1 - 2 * (int)threadIdx.x, above = hist[d], sum = above + hist[d - 1];
-            const int upto = block_scan(sum, part), before = upto - sum;
-            if (before < ties && upto >= ties) {
-                const bool first = before + above >= ties;
-                bound[0] = first ? d : d - 1;
-                bound[1] = ties - before - (first ? 0 : above);
-            }
-            __syncthreads();
-            code |= (uint32_t)bound[0] << shift;
-            ties = bound[1];
-        }
-    }
-    // piece of the wavefront: whole groups of 64 slots
-    const int each = ((n + 64 * W - 1) / (64 * W)) * 64, from = min(n, wave * each), to = min(n, from + each);
-    auto kind = [&](int i) {   // 2: kept, 1: equal to the last kept, 0: not kept
-        if (i >= to) return 0;
+    const Bound bound = largest<kBlock>(old, want, [&](int i) { return code_of(w[i]); }, space);
+    list_kept<kBlock>(n, bound.ties, [&](int i) {   // 2: kept, 1: equal to the last kept, 0: not kept
         if (i >= old || want == old) return 2;
         if (want == 0) return 0;
         const uint32_t c = code_of(w[i]);
-        return c > code ? 2 : c == code ? 1 : 0;
-    };
-    int sure = 0, even = 0;
-    for (int i = from; i < to; i += 64) {
-        const int k = kind(i + lane);
-        sure += __popcll(__ballot(k == 2));
-        even += __popcll(__ballot(k == 1));
-    }
-    if (lane == 0) {
-        counts[0][wave] = sure;
-        counts[1][wave] = even;
-    }
-    __syncthreads();
-    int at = 0, seen = 0;      // slots listed, and equals passed, before the piece
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-        if (i >= wave) break;
-        at += counts[0][i];
-        seen += counts[1][i];
-    }
-    at += min(seen, ties);
-    const uint64_t below = (1ull << lane) - 1;
-    for (int i = from; i < to; i += 64) {
-        const int k = kind(i + lane);
-        const uint64_t equal = __ballot(k == 1);
-        const bool in = k == 2 || (k == 1 && seen + __popcll(equal & below) < ties);
-        const uint64_t kept = __ballot(in);
-        if (in) out[at + __popcll(kept & below)] = i + lane;
-        at += __popcll(kept);
-        seen += __popcll(equal);
-    }
+        return c > bound.code ? 2 : c == bound.code ? 1 : 0;
+    }, out, space);
     for (int i = min(n, keep) + threadIdx.x; i < keep; i += kBlock) out[i] = -1;
     if (row % a.heads == 0 && threadIdx.x == 0) a.lengths_out[b] = min(n, keep);
 }

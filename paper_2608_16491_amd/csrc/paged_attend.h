@@ -1,0 +1,444 @@
+// Attention of one token per request over a cache in 8-bit pages: the kernels
+// (instantiated per query type by paged_attend_*.hip) and how a call is cut.
+//
+// With code k = c 2^e and its row's power apart, a score is (q . c) 2^e: codes of
+// both kinds are exact in bf16 (int8 7 bits, e4m3 4), so the products run on the
+// bf16 matrix cores, q in one factor (bf16), two (fp16: 8 + 8 bits hold its 11)
+// or three (fp32), and the power multiplies the sum.  A value's power multiplies
+// its weight instead, and p 2^e enters the second product in two factors (16-bit
+// queries: a weight is off by 2^-16 of itself at most) or three.
+#pragma once
+
+#include "attend_tile.h"
+#include "paged.h"
+
+namespace frog {
+
+constexpr int kTile = 16;             // keys of a tile; a step of a wavefront takes two
+constexpr int kMostTiles = 256;       // of a workgroup's part of the cache
+constexpr float kNoneSeen = -FLT_MAX; // running maximum of a row that has seen no key
+
+// How a call is cut: parts of `chunk` tiles a workgroup, in parts of at most `tiles` tiles a request;
+// `blocks` workgroups share the query rows of a kv head
+struct PagedPlan {
+    int64_t tiles;
+    int chunk, parts, blocks, wide, waves;   // wide: two column tiles of 16 query rows
+};
+
+// Partial results (o null: one part, which writes the outputs itself): part s of
+// row b * heads + h at [s * rows + row], o unnormalised
+struct PagedParts {
+    float* o;
+    float2* ml;
+    int64_t rows;
+};
+
+// The tiles request b's token walks, [first, end), and the rows it sees, [lo, hi]:
+// tiles of the request's own pages in order, or of the listed pages
+struct Walk {
+    int64_t first, end;
+    int lo, hi, last;     // last: where the query stands
+    __device__ inline Walk(const frog_attend_paged_t& a, int64_t b) {
+        lo = 0;
+        hi = last = (int)rows_of(a.lengths, b, a.pages_per_request, a.cache.page) - 1;
+        if (a.lr) {
+            lo = max(lo, a.lr[2 * b]);
+            hi = min(hi, a.lr[2 * b + 1]);
+        }
+        first = a.chosen ? 0 : lo / kTile;
+        end = lo > hi ? first : a.chosen ? a.num_chosen * (a.cache.page / kTile) : (int64_t)hi / kTile + 1;
+    }
+};
+
+// two floats whose upper halves are bf16 already
+__device__ inline uint32_t upper_halves(float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); }
+
+// eight codes as a factor
+template <bool INT8>
+__device__ inline frag<bf16_t> factor_of(uint32_t x, uint32_t y) {
+    vec<uint32_t, 4> r;
+    if constexpr (INT8) {
+        const vec<float, 4> a = values_of<true>(x), b = values_of<true>(y);
+        r = vec<uint32_t, 4>{upper_halves(a[0], a[1]), upper_halves(a[2], a[3]), upper_halves(b[0], b[1]), upper_halves(b[2], b[3])};
+    } else {
+        r = vec<uint32_t, 4>{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, false)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, true)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.f, false)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.f, true))};
+    }
+    return __builtin_bit_cast(frag<bf16_t>, r);
+}
+
+// byte N of the words of two rows, as a pair
+template <bool INT8, int N>
+__device__ inline uint32_t pair_of(uint32_t a, uint32_t b) {
+    if constexpr (INT8) {
+        return upper_halves((float)(int8_t)(a >> (8 * N)), (float)(int8_t)(b >> (8 * N)));
+    } else {
+        const uint32_t x = __builtin_amdgcn_perm(b, a, N < 2 ? 0x05010400 : 0x07030602);
+        return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, (N & 1) != 0));
+    }
+}
+
+// x in F factors of bf16
+template <int F>
+__device__ inline void split_factors(const vec<float, 8>& x, frag<bf16_t> (&f)[F]) {
+    vec<float, 8> rest = x;
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+        f[i] = __builtin_convertvector(rest, frag<bf16_t>);
+        if (i + 1 < F) rest -= __builtin_convertvector(f[i], vec<float, 8>);
+    }
+}
+
+// What a lane holds of a step's rows, as loaded.  Keys: of row lane % 16 of each
+// tile the pieces that its quarter of the wavefront multiplies.  Values: of rows
+// 4 (lane / 16) .. + 3 the bytes whose channels are row lane % 16 of the second
+// product's left factor; slots of the quarter's 8 rows stand in the order of the
+// score registers, so that no lane exchanges a value and nothing goes through LDS.
+template <int D>
+struct Rows {
+    static constexpr int kV = D >= 96 ? 2 : 1;   // words of a value row
+    uint32_t k[2][D / 16], v[2][4][kV], ke[2], ve[2];
+
+    // first of the eight channels of product s
+    __device__ static inline int channel(int s, int quarter) {
+        if constexpr (D % 64 == 0) return 64 * (s / 2) + 16 * quarter + 8 * (s % 2);
+        else return 32 * s + 8 * quarter;
+    }
+    __device__ inline void load(const frog_cache_t& c, int64_t block0, int64_t block1, int lane) {
+        const int col = lane & 15, quarter = lane >> 4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t row = (t ? block1 : block0) * kTile;
+            const uint8_t* kp = (const uint8_t*)c.k + row * D;
+            const uint8_t* vp = (const uint8_t*)c.v + row * D;
+            if constexpr (D % 64 == 0) {
+#pragma unroll
+                for (int i = 0; i < D / 64; ++i) *(uint4*)&k[t][4 * i] = *(const uint4*)(kp + (uint32_t)(col * D + 16 * quarter) + 64 * i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 32; ++i) *(uint2*)&k[t][2 * i] = *(const uint2*)(kp + (uint32_t)(col * D + 8 * quarter) + 32 * i);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t at = (uint32_t)(4 * quarter * D) + e * D;
+                if constexpr (D == 128) *(uint2*)v[t][e] = *(const uint2*)(vp + at + 8 * col);
+                else if constexpr (D == 32) v[t][e][0] = *(const uint16_t*)(vp + at + 2 * col);
+                else v[t][e][0] = *(const uint32_t*)(vp + at + 4 * col);
+                if constexpr (D == 96) v[t][e][1] = *(const uint16_t*)(vp + at + 64 + 2 * col);
+            }
+            ke[t] = *(const uint32_t*)(c.k_exp + row + 4 * quarter);
+            ve[t] = *(const uint32_t*)(c.v_exp + row + 4 * quarter);
+        }
+    }
+};
+
+// N channels of row i of the second product (value m of it stands for channel_of(i, m))
+template <int D>
+__device__ inline int out_channel(int i, int m) {
+    if constexpr (D == 96) return m < 4 ? 4 * i + m : 64 + 2 * i + m - 4;
+    else return D / 16 * i + m;
+}
+
+// One workgroup of W wavefronts a (request, kv head, part of its rows).  Bound by
+// HBM: conversions and softmax take about a third of the cycles that the read
+// of the rows does, so the loads of the next step are only kept in registers.
+template <typename T, bool INT8, int D, bool PLAIN, int NQ, int W>
+__global__ __launch_bounds__(64 * W) void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedParts parts, int64_t first_item) {
+    constexpr int QF = sizeof(T) == 4 ? 3 : std::is_same<T, bf16_t>::value ? 1 : 2, PF = sizeof(T) == 4 ? 3 : 2;
+    constexpr int M = D / 16, S = D / 32;
+    __shared__ int block_of[kMostTiles], place_of[kMostTiles];
+    __shared__ float tops[W][16 * NQ], sums[W][16 * NQ];
+    __shared__ float joined[W / 2][NQ * M * 4][64];
+    const frog_cache_t& c = a.cache;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
+    int64_t item = first_item + blockIdx.x;
+    const int h = (int)(item % c.kv_heads);
+    item /= c.kv_heads;
+    const int rows0 = (int)(item % plan.blocks) * 16 * NQ;
+    item /= plan.blocks;
+    const int part = (int)(item % plan.parts);
+    const int64_t b = item / plan.parts;
+    const Walk walk(a, b);
+    const int64_t first = walk.first + (int64_t)part * plan.chunk;
+    const int count = (int)max((int64_t)0, min((int64_t)plan.chunk, walk.end - first));
+    if (count == 0 && parts.o) return;
+    const int group = a.heads / c.kv_heads, tiles = c.page / kTile;
+    for (int i = threadIdx.x; i < ((count + 1) & ~1); i += 64 * W) {
+        int block = -1, place = 0;
+        if (i < count) {
+            const int64_t entry = (first + i) / tiles;
+            const int sub = (int)((first + i) % tiles);
+            const int64_t logical = a.chosen ? a.chosen[(b * c.kv_heads + h) * a.num_chosen + entry] : entry;
+            if (logical >= 0 && logical < a.pages_per_request) {
+                place = (int)logical * c.page + sub * kTile;
+                if (place <= walk.hi && place + kTile > walk.lo) {
+                    const int page = page_of(a.pages, b, a.pages_per_request, logical, c.num_pages);
+                    if (page >= 0) block = (page * c.kv_heads + h) * tiles + sub;
+                }
+            }
+        }
+        block_of[i] = block;
+        place_of[i] = place;
+    }
+    frag<bf16_t> qf[NQ][S][QF];
+    float slope[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        const int head = h * group + min(rows0 + 16 * n + col, group - 1);
+        const T* p = (const T*)a.q + b * a.q_stride[0] + head * a.q_stride[1];
+#pragma unroll
+        for (int s = 0; s < S; ++s) {
+            const frag<T> x = load_frag(p + Rows<D>::channel(s, quarter));
+            if constexpr (QF == 1) qf[n][s][0] = x;
+            else split_factors<QF>(__builtin_convertvector(x, vec<float, 8>), qf[n][s]);
+        }
+        slope[n] = !PLAIN && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+    }
+    acc4 o[NQ][M];
+    float top[NQ], sum[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        top[n] = kNoneSeen;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int m = 0; m < M; ++m) o[n][m] = acc4{};
+    }
+    __syncthreads();
+
+    struct Step {
+        int block[2], place[2];
+    };
+    auto look = [&](int i) {
+        Step s;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            s.block[t] = __builtin_amdgcn_readfirstlane(block_of[i + t]);
+            s.place[t] = __builtin_amdgcn_readfirstlane(place_of[i + t]);
+        }
+        return s;
+    };
+    auto step = [&](Rows<D>& r, const Step& at) __attribute__((always_inline)) {
+        if (at.block[0] < 0 && at.block[1] < 0) return;
+        vec<float, 8> z[NQ], up;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            acc4 x[NQ];
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) x[n] = acc4{};
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const frag<bf16_t> k = factor_of<INT8>(r.k[t][2 * s], r.k[t][2 * s + 1]);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                    for (int f = 0; f < QF; ++f) x[n] = mma(k, qf[n][s][f], x[n]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float power = power_of((r.ke[t] >> (8 * e)) & 255) * (PLAIN ? sp.mul : 1.f);
+                up[4 * t + e] = power_of((r.ve[t] >> (8 * e)) & 255);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) z[n][4 * t + e] = x[n][e] * power;
+            }
+        }
+        if constexpr (!PLAIN) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                if (sp.cap2 > 0.f) cap_scores<8>(sp, z[n]);
+                else z[n] *= sp.mul;
+                if (a.slopes) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int place = at.place[e / 4] + 4 * quarter + e % 4;
+                        z[n][e] -= slope[n] * fabsf((float)(walk.last - place));
+                    }
+                }
+            }
+        }
+        // rows outside lo .. hi, and of tiles that are none, may hold anything
+        bool whole = true;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) whole &= at.block[t] >= 0 && at.place[t] >= walk.lo && at.place[t] + kTile - 1 <= walk.hi;
+        if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int place = at.place[e / 4] + 4 * quarter + e % 4;
+                const bool seen = at.block[e / 4] >= 0 && place >= walk.lo && place <= walk.hi;
+                up[e] = seen ? up[e] : 0.f;
+#pragma unroll
+                for (int i = 0; i < Rows<D>::kV; ++i) r.v[e / 4][e % 4][i] = seen ? r.v[e / 4][e % 4][i] : 0;
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) z[n][e] = seen ? z[n][e] : -INFINITY;
+            }
+        }
+        frag<bf16_t> pf[NQ][PF];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+            float most = z[n][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) most = fmaxf(most, z[n][e]);
+            // the maximum is renewed where it grew by more than 2^8
+            if (__any(most > top[n] + 8.f)) {
+                const float now = quarter_max(fmaxf(most, top[n])), down = exp2_fast(top[n] - now);
+                top[n] = now;
+                sum[n] *= down;
+#pragma unroll
+                for (int m = 0; m < M; ++m) o[n][m] *= down;
+            }
+            vec<float, 8> p;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = exp2_fast(z[n][e] - top[n]);
+                sum[n] += p[e];
+            }
+            split_factors<PF>(p * up, pf[n]);
+        }
+        auto product = [&](auto byte, int word, int m) __attribute__((always_inline)) {
+            constexpr int B = decltype(byte)::value;
+            const vec<uint32_t, 4> x{pair_of<INT8, B>(r.v[0][0][word], r.v[0][1][word]), pair_of<INT8, B>(r.v[0][2][word], r.v[0][3][word]),
+                                     pair_of<INT8, B>(r.v[1][0][word], r.v[1][1][word]), pair_of<INT8, B>(r.v[1][2][word], r.v[1][3][word])};
+            const frag<bf16_t> v = __builtin_bit_cast(frag<bf16_t>, x);
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int f = 0; f < PF; ++f) o[n][m] = mma(v, pf[n][f], o[n][m]);
+        };
+#pragma unroll
+        for (int m = 0; m < M; m += 4) {
+            product(std::integral_constant<int, 0>(), m / 4, m);
+            product(std::integral_constant<int, 1>(), m / 4, m + 1);
+            if (m + 2 < M) product(std::integral_constant<int, 2>(), m / 4, m + 2);
+            if (m + 3 < M) product(std::integral_constant<int, 3>(), m / 4, m + 3);
+        }
+    };
+
+    // (the loads of a step that is none read block 0: a cache has one)
+    auto fetch = [&](Rows<D>& r, const Step& at) __attribute__((always_inline)) { r.load(c, max(at.block[0], 0), max(at.block[1], 0), lane); };
+    int i = 2 * w;
+    if (i < count) {
+        Rows<D> r0, r1;
+        Step s0 = look(i), s1;
+        fetch(r0, s0);
+        while (true) {
+            const int j = min(i + 2 * W, (count - 1) & ~1);
+            s1 = look(j);
+            fetch(r1, s1);
+            step(r0, s0);
+            i += 2 * W;
+            if (i >= count) break;
+            s0 = look(min(i + 2 * W, (count - 1) & ~1));
+            fetch(r0, s0);
+            step(r1, s1);
+            i += 2 * W;
+            if (i >= count) break;
+        }
+    }
+
+    // the wavefronts' results, joined pair by pair
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        sum[n] = quarter_sum(sum[n]);
+        if (quarter == 0) {
+            tops[w][16 * n + col] = top[n];
+            sums[w][16 * n + col] = sum[n];
+        }
+    }
+    __syncthreads();
+    float all[NQ], total[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        all[n] = kNoneSeen;
+#pragma unroll
+        for (int i = 0; i < W; ++i) all[n] = fmaxf(all[n], tops[i][16 * n + col]);
+        total[n] = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) total[n] += sums[i][16 * n + col] * exp2_fast(tops[i][16 * n + col] - all[n]);
+        const float down = exp2_fast(top[n] - all[n]);
+#pragma unroll
+        for (int m = 0; m < M; ++m) o[n][m] *= down;
+    }
+#pragma unroll
+    for (int half = W / 2; half; half /= 2) {
+        if (w >= half && w < 2 * half) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) joined[w - half][(n * M + m) * 4 + e][lane] = o[n][m][e];
+        }
+        __syncthreads();
+        if (w < half) {
+#pragma unroll
+            for (int n = 0; n < NQ; ++n)
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n][m][e] += joined[w][(n * M + m) * 4 + e][lane];
+        }
+        __syncthreads();
+    }
+    if (w) return;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n) {
+        if (rows0 + 16 * n + col >= group) continue;
+        const int head = h * group + rows0 + 16 * n + col;
+        const int64_t row = b * a.heads + head;
+        if (parts.o) {
+            float* to = parts.o + (part * parts.rows + row) * D;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int m = 0; m < M; m += 2)
+                    *(float2*)(to + out_channel<D>(4 * quarter + e, m)) = make_float2(o[n][m][e], o[n][m + 1][e]);
+            if (quarter == 0) parts.ml[part * parts.rows + row] = make_float2(all[n], total[n]);
+        } else {
+            T* to = (T*)a.out + b * a.out_stride[0] + head * a.out_stride[1];
+            const float scale = total[n] == 0.f ? 0.f : 1.f / total[n];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int m = 0; m < M; m += 2)
+                    *(vec<T, 2>*)(to + out_channel<D>(4 * quarter + e, m)) = vec<T, 2>{(T)(o[n][m][e] * scale), (T)(o[n][m + 1][e] * scale)};
+            if (quarter == 0 && a.lse) a.lse[row] = total[n] == 0.f ? -INFINITY : (all[n] + log2f(total[n])) * kLn2;
+        }
+    }
+}
+
+// launchers of one query type
+hipError_t launch_paged_bf16(const frog_attend_paged_t& a, const PagedPlan& plan, const PagedParts& parts, hipStream_t stream);
+hipError_t launch_paged_f16(const frog_attend_paged_t& a, const PagedPlan& plan, const PagedParts& parts, hipStream_t stream);
+hipError_t launch_paged_f32(const frog_attend_paged_t& a, const PagedPlan& plan, const PagedParts& parts, hipStream_t stream);
+
+template <typename T, bool INT8, int D>
+hipError_t launch_paged(const frog_attend_paged_t& a, const PagedPlan& plan, const PagedParts& parts, hipStream_t stream) {
+    const ScoreParams sp = score_params(a.scale, a.cap, a.type);
+    const int64_t items = a.batch * plan.parts * plan.blocks * a.cache.kv_heads;
+    auto run = [&](auto kernel, int threads) {
+        return in_launches(items, threads, [&](int64_t first, dim3 grid) { kernel<<<grid, threads, 0, stream>>>(a, sp, plan, parts, first); });
+    };
+    const bool plain = a.cap == 0.f && !a.slopes;
+    if constexpr (sizeof(T) == 2) {
+        if (plan.wide) return plain ? run(paged_attend<T, INT8, D, true, 2, 4>, 256) : run(paged_attend<T, INT8, D, false, 2, 4>, 256);
+    }
+    if (plan.waves == 16) return plain ? run(paged_attend<T, INT8, D, true, 1, 16>, 1024) : run(paged_attend<T, INT8, D, false, 1, 16>, 1024);
+    return plain ? run(paged_attend<T, INT8, D, true, 1, 4>, 256) : run(paged_attend<T, INT8, D, false, 1, 4>, 256);
+}
+
+template <typename T>
+hipError_t launch_paged_type(const frog_attend_paged_t& a, const PagedPlan& plan, const PagedParts& parts, hipStream_t stream) {
+    auto codes = [&](auto d) {
+        return a.cache.storage == FROG_CACHE_INT8 ? launch_paged<T, true, decltype(d)::value>(a, plan, parts, stream)
+                                                  : launch_paged<T, false, decltype(d)::value>(a, plan, parts, stream);
+    };
+    switch (a.cache.d) {
+        case 32: return codes(std::integral_constant<int, 32>());
+        case 64: return codes(std::integral_constant<int, 64>());
+        case 96: return codes(std::integral_constant<int, 96>());
+        default: return codes(std::integral_constant<int, 128>());
+    }
+}
+
+}  // namespace frog

@@ -1,0 +1,97 @@
+// Attention over 8-bit pages: how a call is cut into workgroups, and the join of
+// the parts (kernels: paged_attend.h).
+
+#include "paged_attend.h"
+
+namespace frog {
+namespace {
+
+// A workgroup a row of queries: maximum and sums of its parts, then their
+// outputs, D / 64 channels a lane.
+__global__ __launch_bounds__(256) void paged_join(frog_attend_paged_t a, PagedPlan plan, PagedParts parts, int64_t first) {
+    const int lane = threadIdx.x & 63, d = a.cache.d;
+    const int64_t row = (first + blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (row >= parts.rows) return;
+    const int64_t b = row / a.heads;
+    const int head = (int)(row % a.heads);
+    const Walk walk(a, b);
+    const int live = (int)((walk.end - walk.first + plan.chunk - 1) / plan.chunk);
+    float all = kNoneSeen;
+    for (int s = lane; s < live; s += 64) all = fmaxf(all, parts.ml[s * parts.rows + row].x);
+    for (int o = 32; o; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
+    float total = 0.f, x[2] = {0.f, 0.f};
+    for (int s0 = 0; s0 < live; s0 += 64) {
+        float2 ml = make_float2(kNoneSeen, 0.f);
+        if (s0 + lane < live) ml = parts.ml[(s0 + lane) * parts.rows + row];
+        const float share = exp2_fast(ml.x - all);
+        total += ml.y * share;
+        const int n = min(64, live - s0);
+        for (int s = 0; s < n; ++s) {
+            const float f = __shfl(share, s);
+            const float* from = parts.o + ((s0 + s) * parts.rows + row) * d;
+            if (lane < d) x[0] += f * from[lane];
+            if (lane + 64 < d) x[1] += f * from[lane + 64];
+        }
+    }
+    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+    const float scale = total == 0.f ? 0.f : 1.f / total;
+    const int64_t at = b * a.out_stride[0] + head * a.out_stride[1] + lane;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (lane + 64 * i >= d) break;
+        const float y = x[i] * scale;
+        if (a.type == FROG_STORAGE_F32) ((float*)a.out)[at + 64 * i] = y;
+        else if (a.type == FROG_STORAGE_F16) ((f16_t*)a.out)[at + 64 * i] = (f16_t)y;
+        else ((bf16_t*)a.out)[at + 64 * i] = (bf16_t)y;
+    }
+    if (lane == 0 && a.lse) a.lse[row] = total == 0.f ? -INFINITY : (all + log2f(total)) * kLn2;
+}
+
+PagedPlan plan_of(const frog_attend_paged_t& a) {
+    PagedPlan p;
+    const int group = a.heads / a.cache.kv_heads;
+    p.wide = a.type != FROG_STORAGE_F32 && group > 16;
+    p.blocks = (group + (p.wide ? 31 : 15)) / (p.wide ? 32 : 16);
+    p.tiles = (a.chosen ? a.num_chosen : a.pages_per_request) * (a.cache.page / kTile);
+    if (a.cache.num_pages == 0) p.tiles = 0;
+    const int64_t pairs = a.batch * a.cache.kv_heads * p.blocks;
+    p.waves = 4;
+    if (p.tiles <= 64 && !p.wide) {
+        p.waves = 16;
+        p.chunk = 64;
+        p.parts = 1;
+        return p;
+    }
+    // parts of 128 to 4,096 rows, about 2,048 workgroups
+    const int64_t each = (pairs * p.tiles + 2047) / 2048;
+    p.chunk = (int)std::min<int64_t>(kMostTiles, std::max<int64_t>(8, (each + 7) / 8 * 8));
+    p.parts = (int)std::max<int64_t>(1, (p.tiles + p.chunk - 1) / p.chunk);
+    return p;
+}
+
+}  // namespace
+
+int64_t attend_paged_ws(const frog_attend_paged_t& a) {
+    if (a.batch == 0) return 0;
+    const PagedPlan p = plan_of(a);
+    return p.parts == 1 ? 0 : p.parts * a.batch * a.heads * (int64_t)(a.cache.d + 2) * 4;
+}
+
+int launch_attend_paged(const frog_attend_paged_t& args, void* ws, hipStream_t stream) {
+    if (args.batch == 0) return FROG_OK;
+    frog_attend_paged_t a = args;
+    const PagedPlan p = plan_of(a);
+    if (p.tiles == 0) a.pages_per_request = 0;      // no rows: outputs of 0
+    PagedParts parts{};
+    parts.rows = a.batch * a.heads;
+    if (p.parts > 1) {
+        parts.ml = (float2*)ws;
+        parts.o = (float*)(parts.ml + p.parts * parts.rows);
+    }
+    hipError_t e = a.type == FROG_STORAGE_F32 ? launch_paged_f32(a, p, parts, stream) : a.type == FROG_STORAGE_F16 ? launch_paged_f16(a, p, parts, stream) : launch_paged_bf16(a, p, parts, stream);
+    if (e == hipSuccess && p.parts > 1)
+        e = in_launches((parts.rows + 3) / 4, 256, [&](int64_t first, dim3 grid) { paged_join<<<grid, 256, 0, stream>>>(a, p, parts, first); });
+    return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "attention over pages launch: %s", hipGetErrorString(e));
+}
+
+}  // namespace frog

@@ -1,0 +1,204 @@
+// Rows into a cache in 8-bit pages and back (include/frog.h: frog_cache_write,
+// frog_cache_read).  Both move every byte once and are bound by HBM.
+
+#include "paged.h"
+
+namespace frog {
+namespace {
+
+constexpr int kBlock = 256, kWaves = kBlock / 64;
+
+// first new row of request b
+__device__ inline int64_t start_of(const frog_cache_write_t& a, int64_t b) {
+    const int64_t each = a.tokens / a.batch;
+    return a.starts ? max((int64_t)0, min((int64_t)a.starts[b], a.tokens)) : b * each;
+}
+
+// One workgroup a (page with new rows, kv head): the page's bounds are then its
+// own, without atomics, and the same every run.  Request b's pages are work
+// items from start / page + 2 b on, at least as many as its rows can meet (n
+// rows meet at most n / page + 2 pages), so the host needs no lengths; the
+// request of an item is found by a search over 64 requests at a time.  A row
+// takes 4, 8 or 16 lanes, which find its largest magnitude among themselves.
+template <typename T, bool INT8, int D>
+__global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, int64_t first) {
+    using S = RowSplit<D>;
+    constexpr int C = S::kEach;
+    __shared__ float least[kWaves][D], most[kWaves][D];
+    __shared__ int broken;
+    const frog_cache_t& c = a.cache;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t item = (first + blockIdx.x) / c.kv_heads;
+    const int h = (int)((first + blockIdx.x) % c.kv_heads);
+    int64_t b = 0;
+    for (int64_t len = a.batch; len > 1;) {
+        const int64_t step = (len + 63) / 64, i = lane * step;
+        const bool before = i < len && start_of(a, b + i) / c.page + 2 * (b + i) <= item;
+        const int64_t at = max(0, __popcll(__ballot(before)) - 1) * step;
+        b += at;
+        len = min(step, len - at);
+    }
+    const int64_t start = start_of(a, b), count = max((int64_t)0, start_of(a, b + 1) - start);
+    const int64_t length = a.lengths[b], before = length - count;       // rows the request had
+    const int64_t from = max((int64_t)0, before), to = min(length, a.pages_per_request * c.page);
+    const int64_t logical = from / c.page + (item - (start / c.page + 2 * b));
+    const int64_t r0 = max(from, logical * c.page), r1 = min(to, (logical + 1) * c.page);
+    if (logical < 0 || r0 >= r1) return;
+    const int page = page_of(a.pages, b, a.pages_per_request, logical, c.num_pages);
+    if (page < 0) return;
+
+    const int64_t block = (int64_t)page * c.kv_heads + h;
+    const int sub = lane / S::kLanes, at = (lane % S::kLanes) * C;
+    float lo[C], hi[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) lo[i] = INFINITY, hi[i] = -INFINITY;
+    int bad = 0;
+    for (int64_t r = r0 + w * S::kRows + sub; r - sub < r1; r += kWaves * S::kRows) {
+        const bool live = r < r1;
+        const int64_t token = start + (live ? r : r0) - before;
+        const T* src[2] = {(const T*)a.k + token * a.k_stride[0] + h * a.k_stride[1] + at, (const T*)a.v + token * a.v_stride[0] + h * a.v_stride[1] + at};
+        float x[2][C];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) load_values(src[t], x[t]);
+        const int64_t row = block * c.page + r % c.page;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < C; ++i) top = max(top, __float_as_uint(x[t][i]) & 0x7FFFFFFFu);
+            top = over_row<S::kLanes>(top, [](uint32_t p, uint32_t q) { return max(p, q); });
+            const int byte = power_byte<INT8>(top);
+            const float down = power_of(254 - byte);
+            Words<C / 4> codes;
+#pragma unroll
+            for (int i = 0; i < C / 4; ++i)
+                codes.w[i] = byte == kNoRow ? 0 : codes_of<INT8>(x[t][4 * i] * down, x[t][4 * i + 1] * down, x[t][4 * i + 2] * down, x[t][4 * i + 3] * down);
+            if (live) {
+                store_words((uint8_t*)(t ? c.v : c.k) + row * D + at, codes);
+                if (at == 0) (t ? c.v_exp : c.k_exp)[row] = (uint8_t)byte;
+            }
+            if (t == 0 && c.bounds && live) {
+                bad |= byte == kNoRow;
+                const float up = power_of(byte);
+#pragma unroll
+                for (int i = 0; i < C / 4; ++i) {
+                    const vec<float, 4> y = values_of<INT8>(codes.w[i]) * up;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        lo[4 * i + e] = fminf(lo[4 * i + e], y[e]);
+                        hi[4 * i + e] = fmaxf(hi[4 * i + e], y[e]);
+                    }
+                }
+            }
+        }
+    }
+    if (!c.bounds) return;
+    // over the wavefront's rows (lanes of the same channels), then the wavefronts
+    if (threadIdx.x == 0) broken = 0;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+#pragma unroll
+        for (int o = S::kLanes; o < 64; o <<= 1) {
+            lo[i] = fminf(lo[i], __shfl_xor(lo[i], o));
+            hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], o));
+        }
+        if (sub == 0) least[w][at + i] = lo[i], most[w][at + i] = hi[i];
+    }
+    __syncthreads();
+    if (__any(bad) && lane == 0) broken = 1;
+    __syncthreads();
+    if (threadIdx.x >= 2 * D) return;
+    const bool high = threadIdx.x >= D;
+    const int i = threadIdx.x - (high ? D : 0);
+    bf16_t* p = (bf16_t*)c.bounds + (block * 2 + (high ? 1 : 0)) * D + i;
+    float x = high ? most[0][i] : least[0][i];
+#pragma unroll
+    for (int n = 1; n < kWaves; ++n) x = high ? fmaxf(x, most[n][i]) : fminf(x, least[n][i]);
+    // (a page begun at its row 0 forgets what it held)
+    const float old = r0 % c.page ? (float)*p : x;
+    x = high ? fmaxf(x, old) : fminf(x, old);
+    *p = (bf16_t)(broken || old != old ? NAN : x);
+}
+
+// One workgroup 16 rows of a request (of one page) with all their heads, in the
+// order of the outputs.
+template <typename T, bool INT8, int D>
+__global__ __launch_bounds__(kBlock) void cache_read(frog_cache_read_t a, int64_t first) {
+    using S = RowSplit<D>;
+    constexpr int C = S::kEach;
+    const frog_cache_t& c = a.cache;
+    const int64_t blocks = (a.slots + 15) / 16, item = first + blockIdx.x, b = item / blocks, s0 = item % blocks * 16;
+    const int rows = (int)min((int64_t)16, a.slots - s0);
+    const int64_t length = rows_of(a.lengths, b, a.pages_per_request, c.page);
+    const int page = s0 < length ? page_of(a.pages, b, a.pages_per_request, s0 / c.page, c.num_pages) : -1;
+    const int live = page < 0 ? 0 : (int)min((int64_t)rows, length - s0);
+    const int sub = threadIdx.x / S::kLanes, at = (threadIdx.x % S::kLanes) * C;
+    for (int i = sub; i < rows * c.kv_heads; i += kBlock / S::kLanes) {
+        const int s = i / c.kv_heads, h = i - s * c.kv_heads;
+        const int64_t row = ((int64_t)page * c.kv_heads + h) * c.page + s0 % c.page + s;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            T y[C] = {};
+            if (s < live) {
+                const Words<C / 4> codes = load_words<C / 4>((const uint8_t*)(t ? c.v : c.k) + row * D + at);
+                const float up = power_of((t ? c.v_exp : c.k_exp)[row]);
+#pragma unroll
+                for (int n = 0; n < C / 4; ++n) {
+                    const vec<float, 4> x = values_of<INT8>(codes.w[n]) * up;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[4 * n + e] = (T)x[e];
+                }
+            }
+            T* out = t ? (T*)a.v + b * a.v_stride[0] + (s0 + s) * a.v_stride[1] + h * a.v_stride[2]
+                       : (T*)a.k + b * a.k_stride[0] + (s0 + s) * a.k_stride[1] + h * a.k_stride[2];
+            Words<C * sizeof(T) / 4> words;
+            __builtin_memcpy(words.w, y, sizeof(y));
+            store_words(out + at, words);
+        }
+    }
+}
+
+// f(row type, whether codes are int8, d) as compile-time values
+template <typename F>
+void of_kind(int type, int storage, int d, F&& f) {
+    auto width = [&](auto t, auto i8) {
+        if (d == 32) f(t, i8, std::integral_constant<int, 32>());
+        else if (d == 64) f(t, i8, std::integral_constant<int, 64>());
+        else if (d == 96) f(t, i8, std::integral_constant<int, 96>());
+        else f(t, i8, std::integral_constant<int, 128>());
+    };
+    auto codes = [&](auto t) {
+        if (storage == FROG_CACHE_INT8) width(t, std::true_type());
+        else width(t, std::false_type());
+    };
+    if (type == FROG_STORAGE_F32) codes(float());
+    else if (type == FROG_STORAGE_F16) codes(f16_t());
+    else codes(bf16_t());
+}
+
+}  // namespace
+
+int launch_cache_write(const frog_cache_write_t& a, hipStream_t stream) {
+    if (a.batch == 0 || a.tokens == 0 || a.cache.num_pages == 0 || a.pages_per_request == 0) return FROG_OK;
+    const int64_t items = a.tokens / a.cache.page + 2 * a.batch;
+    hipError_t e = hipSuccess;
+    of_kind(a.type, a.cache.storage, a.cache.d, [&](auto t, auto i8, auto d) {
+        e = in_launches(items * a.cache.kv_heads, kBlock, [&](int64_t first, dim3 grid) {
+            cache_write<decltype(t), i8.value, d.value><<<grid, kBlock, 0, stream>>>(a, first);
+        });
+    });
+    return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "cache write launch: %s", hipGetErrorString(e));
+}
+
+int launch_cache_read(const frog_cache_read_t& a, hipStream_t stream) {
+    if (a.batch == 0 || a.slots == 0) return FROG_OK;
+    hipError_t e = hipSuccess;
+    of_kind(a.type, a.cache.storage, a.cache.d, [&](auto t, auto i8, auto d) {
+        e = in_launches(a.batch * ((a.slots + 15) / 16), kBlock, [&](int64_t first, dim3 grid) {
+            cache_read<decltype(t), i8.value, d.value><<<grid, kBlock, 0, stream>>>(a, first);
+        });
+    });
+    return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "cache read launch: %s", hipGetErrorString(e));
+}
+
+}  // namespace frog
