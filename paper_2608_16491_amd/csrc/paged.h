@@ -117,6 +117,9 @@ __device__ inline void store_words(void* p, const Words<N>& r) {
     }
 }
 
+// pages are powers of two: row t stands in page t >> shift
+__device__ inline int shift_of(int page) { return __builtin_ctz((unsigned)page); }
+
 // rows of request b, clipped to its pages
 __device__ inline int64_t rows_of(const int32_t* lengths, int64_t b, int64_t pages_per_request, int page) {
     return max((int64_t)0, min((int64_t)lengths[b], pages_per_request * page));

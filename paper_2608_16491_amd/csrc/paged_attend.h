@@ -14,7 +14,7 @@
 
 namespace frog {
 
-constexpr int kTile = 16;             // keys of a tile; a step of a wavefront takes two
+constexpr int kTile = 16, kTileShift = 4;   // keys of a tile; a step of a wavefront takes two
 constexpr int kMostTiles = 256;       // of a workgroup's part of the cache
 constexpr float kNoneSeen = -FLT_MAX; // running maximum of a row that has seen no key
 
@@ -46,7 +46,7 @@ struct Walk {
             hi = min(hi, a.lr[2 * b + 1]);
         }
         first = a.chosen ? 0 : lo / kTile;
-        end = lo > hi ? first : a.chosen ? a.num_chosen * (a.cache.page / kTile) : (int64_t)hi / kTile + 1;
+        end = lo > hi ? first : a.chosen ? a.num_chosen * (a.cache.page / kTile) : hi / kTile + 1;
     }
 };
 
@@ -106,30 +106,38 @@ struct Rows {
         if constexpr (D % 64 == 0) return 64 * (s / 2) + 16 * quarter + 8 * (s % 2);
         else return 32 * s + 8 * quarter;
     }
-    __device__ inline void load(const frog_cache_t& c, int64_t block0, int64_t block1, int lane) {
+    // (blocks: of 16 rows of one head)
+    __device__ inline void load_keys(const frog_cache_t& c, const int (&block)[2], int lane) {
         const int col = lane & 15, quarter = lane >> 4;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int64_t row = (t ? block1 : block0) * kTile;
-            const uint8_t* kp = (const uint8_t*)c.k + row * D;
-            const uint8_t* vp = (const uint8_t*)c.v + row * D;
+            const int64_t row = (int64_t)max(block[t], 0) * kTile;
+            const uint8_t* p = (const uint8_t*)c.k + row * D;
             if constexpr (D % 64 == 0) {
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) *(uint4*)&k[t][4 * i] = *(const uint4*)(kp + (uint32_t)(col * D + 16 * quarter) + 64 * i);
+                for (int i = 0; i < D / 64; ++i) *(uint4*)&k[t][4 * i] = *(const uint4*)(p + (uint32_t)(col * D + 16 * quarter) + 64 * i);
             } else {
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) *(uint2*)&k[t][2 * i] = *(const uint2*)(kp + (uint32_t)(col * D + 8 * quarter) + 32 * i);
+                for (int i = 0; i < D / 32; ++i) *(uint2*)&k[t][2 * i] = *(const uint2*)(p + (uint32_t)(col * D + 8 * quarter) + 32 * i);
             }
+            ke[t] = *(const uint32_t*)(c.k_exp + row + 4 * quarter);
+        }
+    }
+    __device__ inline void load_values(const frog_cache_t& c, const int (&block)[2], int lane) {
+        const int col = lane & 15, quarter = lane >> 4;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t row = (int64_t)max(block[t], 0) * kTile;
+            const uint8_t* p = (const uint8_t*)c.v + row * D;
+            ve[t] = *(const uint32_t*)(c.v_exp + row + 4 * quarter);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t at = (uint32_t)(4 * quarter * D) + e * D;
-                if constexpr (D == 128) *(uint2*)v[t][e] = *(const uint2*)(vp + at + 8 * col);
-                else if constexpr (D == 32) v[t][e][0] = *(const uint16_t*)(vp + at + 2 * col);
-                else v[t][e][0] = *(const uint32_t*)(vp + at + 4 * col);
-                if constexpr (D == 96) v[t][e][1] = *(const uint16_t*)(vp + at + 64 + 2 * col);
+                if constexpr (D == 128) *(uint2*)v[t][e] = *(const uint2*)(p + at + 8 * col);
+                else if constexpr (D == 32) v[t][e][0] = *(const uint16_t*)(p + at + 2 * col);
+                else v[t][e][0] = *(const uint32_t*)(p + at + 4 * col);
+                if constexpr (D == 96) v[t][e][1] = *(const uint16_t*)(p + at + 64 + 2 * col);
             }
-            ke[t] = *(const uint32_t*)(c.k_exp + row + 4 * quarter);
-            ve[t] = *(const uint32_t*)(c.v_exp + row + 4 * quarter);
         }
     }
 };
@@ -145,37 +153,41 @@ __device__ inline int out_channel(int i, int m) {
 // HBM: conversions and softmax take about a third of the cycles that the read
 // of the rows does, so the loads of the next step are only kept in registers.
 template <typename T, bool INT8, int D, bool PLAIN, int NQ, int W>
-__global__ __launch_bounds__(64 * W) void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedParts parts, int64_t first_item) {
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NQ == 2 || sizeof(T) == 4 ? 2 : W == 16 ? 4 : 3)))
+void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedParts parts, uint32_t first_item) {
     constexpr int QF = sizeof(T) == 4 ? 3 : std::is_same<T, bf16_t>::value ? 1 : 2, PF = sizeof(T) == 4 ? 3 : 2;
     constexpr int M = D / 16, S = D / 32;
     __shared__ int block_of[kMostTiles], place_of[kMostTiles];
-    __shared__ float tops[W][16 * NQ], sums[W][16 * NQ];
-    __shared__ float joined[W / 2][NQ * M * 4][64];
+    __shared__ float tops[W][16 * NQ], sums[W][16 * NQ], most[16 * NQ], total[16 * NQ];
+    __shared__ __attribute__((aligned(16))) float joined[W][16 * NQ * D];
     const frog_cache_t& c = a.cache;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
-    int64_t item = first_item + blockIdx.x;
-    const int h = (int)(item % c.kv_heads);
-    item /= c.kv_heads;
-    const int rows0 = (int)(item % plan.blocks) * 16 * NQ;
-    item /= plan.blocks;
-    const int part = (int)(item % plan.parts);
-    const int64_t b = item / plan.parts;
+    uint32_t item = first_item + blockIdx.x;
+    const int h = (int)(item % (uint32_t)c.kv_heads);
+    item /= (uint32_t)c.kv_heads;
+    int rows0 = 0;
+    if (plan.blocks > 1) {
+        rows0 = (int)(item % (uint32_t)plan.blocks) * 16 * NQ;
+        item /= (uint32_t)plan.blocks;
+    }
+    const int part = (int)(item % (uint32_t)plan.parts);
+    const int64_t b = item / (uint32_t)plan.parts;
     const Walk walk(a, b);
     const int64_t first = walk.first + (int64_t)part * plan.chunk;
     const int count = (int)max((int64_t)0, min((int64_t)plan.chunk, walk.end - first));
     if (count == 0 && parts.o) return;
-    const int group = a.heads / c.kv_heads, tiles = c.page / kTile;
+    const int group = a.heads / c.kv_heads, shift = shift_of(c.page) - kTileShift;      // a page's tiles: 1 << shift
     for (int i = threadIdx.x; i < ((count + 1) & ~1); i += 64 * W) {
         int block = -1, place = 0;
         if (i < count) {
-            const int64_t entry = (first + i) / tiles;
-            const int sub = (int)((first + i) % tiles);
+            const int64_t entry = (first + i) >> shift;
+            const int sub = (int)(first + i) & ((1 << shift) - 1);
             const int64_t logical = a.chosen ? a.chosen[(b * c.kv_heads + h) * a.num_chosen + entry] : entry;
             if (logical >= 0 && logical < a.pages_per_request) {
                 place = (int)logical * c.page + sub * kTile;
                 if (place <= walk.hi && place + kTile > walk.lo) {
                     const int page = page_of(a.pages, b, a.pages_per_request, logical, c.num_pages);
-                    if (page >= 0) block = (page * c.kv_heads + h) * tiles + sub;
+                    if (page >= 0) block = (page * c.kv_heads + h << shift) + sub;
                 }
             }
         }
@@ -219,8 +231,7 @@ __global__ __launch_bounds__(64 * W) void paged_attend(frog_attend_paged_t a, Sc
         }
         return s;
     };
-    auto step = [&](Rows<D>& r, const Step& at) __attribute__((always_inline)) {
-        if (at.block[0] < 0 && at.block[1] < 0) return;
+    auto step = [&](Rows<D>& r, const Step& at, const Step& next, bool more) __attribute__((always_inline)) {
         vec<float, 8> z[NQ], up;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -238,11 +249,13 @@ __global__ __launch_bounds__(64 * W) void paged_attend(frog_attend_paged_t a, Sc
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float power = power_of((r.ke[t] >> (8 * e)) & 255) * (PLAIN ? sp.mul : 1.f);
-                up[4 * t + e] = power_of((r.ve[t] >> (8 * e)) & 255);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) z[n][4 * t + e] = x[n][e] * power;
             }
         }
+        if (more) r.load_keys(c, next.block, lane);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) up[e] = power_of((r.ve[e / 4] >> (8 * (e % 4))) & 255);
         if constexpr (!PLAIN) {
 #pragma unroll
             for (int n = 0; n < NQ; ++n) {
@@ -314,29 +327,25 @@ __global__ __launch_bounds__(64 * W) void paged_attend(frog_attend_paged_t a, Sc
         }
     };
 
-    // (the loads of a step that is none read block 0: a cache has one)
-    auto fetch = [&](Rows<D>& r, const Step& at) __attribute__((always_inline)) { r.load(c, max(at.block[0], 0), max(at.block[1], 0), lane); };
-    int i = 2 * w;
-    if (i < count) {
-        Rows<D> r0, r1;
-        Step s0 = look(i), s1;
-        fetch(r0, s0);
-        while (true) {
-            const int j = min(i + 2 * W, (count - 1) & ~1);
-            s1 = look(j);
-            fetch(r1, s1);
-            step(r0, s0);
-            i += 2 * W;
-            if (i >= count) break;
-            s0 = look(min(i + 2 * W, (count - 1) & ~1));
-            fetch(r0, s0);
-            step(r1, s1);
-            i += 2 * W;
-            if (i >= count) break;
+    // a step's keys are loaded behind the scores of the one before, its values
+    // behind the products of it (a tile that is none reads block 0: a cache has one)
+    if (2 * w < count) {
+        Rows<D> r;
+        Step now = look(2 * w);
+        r.load_keys(c, now.block, lane);
+        r.load_values(c, now.block, lane);
+        for (int i = 2 * w; i < count; i += 2 * W) {
+            const bool more = i + 2 * W < count;
+            const Step next = more ? look(i + 2 * W) : now;
+            step(r, now, next, more);
+            if (more) r.load_values(c, next.block, lane);
+            now = next;
         }
     }
 
-    // the wavefronts' results, joined pair by pair
+    // the wavefronts' results: maxima and sums, then every wavefront's outputs of
+    // the rows there are, added by all threads
+    const int rows = min(group - rows0, 16 * NQ);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         sum[n] = quarter_sum(sum[n]);
@@ -346,64 +355,50 @@ __global__ __launch_bounds__(64 * W) void paged_attend(frog_attend_paged_t a, Sc
         }
     }
     __syncthreads();
-    float all[NQ], total[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        all[n] = kNoneSeen;
+        float all = kNoneSeen, sum_all = 0.f;
 #pragma unroll
-        for (int i = 0; i < W; ++i) all[n] = fmaxf(all[n], tops[i][16 * n + col]);
-        total[n] = 0.f;
+        for (int i = 0; i < W; ++i) all = fmaxf(all, tops[i][16 * n + col]);
+        if (w == 0) {
 #pragma unroll
-        for (int i = 0; i < W; ++i) total[n] += sums[i][16 * n + col] * exp2_fast(tops[i][16 * n + col] - all[n]);
-        const float down = exp2_fast(top[n] - all[n]);
-#pragma unroll
-        for (int m = 0; m < M; ++m) o[n][m] *= down;
-    }
-#pragma unroll
-    for (int half = W / 2; half; half /= 2) {
-        if (w >= half && w < 2 * half) {
-#pragma unroll
-            for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                for (int m = 0; m < M; ++m)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) joined[w - half][(n * M + m) * 4 + e][lane] = o[n][m][e];
+            for (int i = 0; i < W; ++i) sum_all += sums[i][16 * n + col] * exp2_fast(tops[i][16 * n + col] - all);
+            if (quarter == 0) {
+                most[16 * n + col] = all;
+                total[16 * n + col] = sum_all;
+            }
         }
-        __syncthreads();
-        if (w < half) {
+        const float down = exp2_fast(top[n] - all);
+        if (16 * n + col < rows) {
 #pragma unroll
-            for (int n = 0; n < NQ; ++n)
+            for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int m = 0; m < M; ++m)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[n][m][e] += joined[w][(n * M + m) * 4 + e][lane];
+                for (int m = 0; m < M; m += 2)
+                    *(float2*)&joined[w][(16 * n + col) * D + out_channel<D>(4 * quarter + e, m)] = make_float2(o[n][m][e] * down, o[n][m + 1][e] * down);
         }
-        __syncthreads();
     }
-    if (w) return;
+    __syncthreads();
+    const int64_t row0 = b * a.heads + h * group + rows0;
+    for (int i = threadIdx.x; i < rows * (D / 2); i += 64 * W) {
+        float2 x = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        if (rows0 + 16 * n + col >= group) continue;
-        const int head = h * group + rows0 + 16 * n + col;
-        const int64_t row = b * a.heads + head;
+        for (int n = 0; n < W; ++n) {
+            const float2 y = *(const float2*)&joined[n][2 * i];
+            x.x += y.x;
+            x.y += y.y;
+        }
+        const int row = i / (D / 2), channel = 2 * (i % (D / 2));
         if (parts.o) {
-            float* to = parts.o + (part * parts.rows + row) * D;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int m = 0; m < M; m += 2)
-                    *(float2*)(to + out_channel<D>(4 * quarter + e, m)) = make_float2(o[n][m][e], o[n][m + 1][e]);
-            if (quarter == 0) parts.ml[part * parts.rows + row] = make_float2(all[n], total[n]);
+            *(float2*)(parts.o + (part * parts.rows + row0 + row) * D + channel) = x;
         } else {
-            T* to = (T*)a.out + b * a.out_stride[0] + head * a.out_stride[1];
-            const float scale = total[n] == 0.f ? 0.f : 1.f / total[n];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int m = 0; m < M; m += 2)
-                    *(vec<T, 2>*)(to + out_channel<D>(4 * quarter + e, m)) = vec<T, 2>{(T)(o[n][m][e] * scale), (T)(o[n][m + 1][e] * scale)};
-            if (quarter == 0 && a.lse) a.lse[row] = total[n] == 0.f ? -INFINITY : (all[n] + log2f(total[n])) * kLn2;
+            const float scale = total[row] == 0.f ? 0.f : 1.f / total[row];
+            *(vec<T, 2>*)((T*)a.out + b * a.out_stride[0] + (h * group + rows0 + row) * a.out_stride[1] + channel) = vec<T, 2>{(T)(x.x * scale), (T)(x.y * scale)};
         }
+    }
+    if (threadIdx.x < rows) {
+        const float all = most[threadIdx.x], sum_all = total[threadIdx.x];
+        if (parts.o) parts.ml[part * parts.rows + row0 + threadIdx.x] = make_float2(all, sum_all);
+        else if (a.lse) a.lse[row0 + threadIdx.x] = sum_all == 0.f ? -INFINITY : (all + log2f(sum_all)) * kLn2;
     }
 }
 
@@ -417,7 +412,7 @@ hipError_t launch_paged(const frog_attend_paged_t& a, const PagedPlan& plan, con
     const ScoreParams sp = score_params(a.scale, a.cap, a.type);
     const int64_t items = a.batch * plan.parts * plan.blocks * a.cache.kv_heads;
     auto run = [&](auto kernel, int threads) {
-        return in_launches(items, threads, [&](int64_t first, dim3 grid) { kernel<<<grid, threads, 0, stream>>>(a, sp, plan, parts, first); });
+        return in_launches(items, threads, [&](int64_t first, dim3 grid) { kernel<<<grid, threads, 0, stream>>>(a, sp, plan, parts, (uint32_t)first); });
     };
     const bool plain = a.cap == 0.f && !a.slopes;
     if constexpr (sizeof(T) == 2) {

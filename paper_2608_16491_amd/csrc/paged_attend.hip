@@ -12,10 +12,10 @@ __global__ __launch_bounds__(256) void paged_join(frog_attend_paged_t a, PagedPl
     const int lane = threadIdx.x & 63, d = a.cache.d;
     const int64_t row = (first + blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (row >= parts.rows) return;
-    const int64_t b = row / a.heads;
-    const int head = (int)(row % a.heads);
+    const int64_t b = (uint32_t)row / (uint32_t)a.heads;      // (rows are fewer than 2^31)
+    const int head = (int)((uint32_t)row % (uint32_t)a.heads);
     const Walk walk(a, b);
-    const int live = (int)((walk.end - walk.first + plan.chunk - 1) / plan.chunk);
+    const int live = ((int)(walk.end - walk.first) + plan.chunk - 1) / plan.chunk;
     float all = kNoneSeen;
     for (int s = lane; s < live; s += 64) all = fmaxf(all, parts.ml[s * parts.rows + row].x);
     for (int o = 32; o; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
@@ -25,12 +25,22 @@ __global__ __launch_bounds__(256) void paged_join(frog_attend_paged_t a, PagedPl
         if (s0 + lane < live) ml = parts.ml[(s0 + lane) * parts.rows + row];
         const float share = exp2_fast(ml.x - all);
         total += ml.y * share;
+        // (parts past the last one repeat it, with a share of 0)
         const int n = min(64, live - s0);
-        for (int s = 0; s < n; ++s) {
-            const float f = __shfl(share, s);
-            const float* from = parts.o + ((s0 + s) * parts.rows + row) * d;
-            if (lane < d) x[0] += f * from[lane];
-            if (lane + 64 < d) x[1] += f * from[lane + 64];
+        for (int s = 0; s < n; s += 8) {
+            float y[8][2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float* from = parts.o + ((s0 + min(s + i, n - 1)) * parts.rows + row) * d;
+                y[i][0] = from[min(lane, d - 1)];
+                y[i][1] = d > 64 ? from[min(lane + 64, d - 1)] : 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float f = s + i < n ? __shfl(share, s + i) : 0.f;
+                x[0] += f * y[i][0];
+                x[1] += f * y[i][1];
+            }
         }
     }
     for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
@@ -74,6 +84,7 @@ PagedPlan plan_of(const frog_attend_paged_t& a) {
 int64_t attend_paged_ws(const frog_attend_paged_t& a) {
     if (a.batch == 0) return 0;
     const PagedPlan p = plan_of(a);
+    if (a.batch * p.blocks * a.cache.kv_heads > 0x7fffffff / p.parts) return fail(FROG_EUNSUPPORTED, "more than 2^31 workgroups");
     return p.parts == 1 ? 0 : p.parts * a.batch * a.heads * (int64_t)(a.cache.d + 2) * 4;
 }
 

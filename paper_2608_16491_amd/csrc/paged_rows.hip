@@ -10,8 +10,7 @@ constexpr int kBlock = 256, kWaves = kBlock / 64;
 
 // first new row of request b
 __device__ inline int64_t start_of(const frog_cache_write_t& a, int64_t b) {
-    const int64_t each = a.tokens / a.batch;
-    return a.starts ? max((int64_t)0, min((int64_t)a.starts[b], a.tokens)) : b * each;
+    return a.starts ? max((int64_t)0, min((int64_t)a.starts[b], a.tokens)) : b * (int64_t)((uint32_t)a.tokens / (uint32_t)a.batch);      // (both below 2^31)
 }
 
 // One workgroup a (page with new rows, kv head): the page's bounds are then its
@@ -21,19 +20,20 @@ __device__ inline int64_t start_of(const frog_cache_write_t& a, int64_t b) {
 // request of an item is found by a search over 64 requests at a time.  A row
 // takes 4, 8 or 16 lanes, which find its largest magnitude among themselves.
 template <typename T, bool INT8, int D>
-__global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, int64_t first) {
+__global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, uint32_t first) {
     using S = RowSplit<D>;
     constexpr int C = S::kEach;
     __shared__ float least[kWaves][D], most[kWaves][D];
     __shared__ int broken;
     const frog_cache_t& c = a.cache;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t item = (first + blockIdx.x) / c.kv_heads;
-    const int h = (int)((first + blockIdx.x) % c.kv_heads);
+    const int shift = shift_of(c.page);
+    const uint32_t item = (first + blockIdx.x) / (uint32_t)c.kv_heads;
+    const int h = (int)((first + blockIdx.x) % (uint32_t)c.kv_heads);
     int64_t b = 0;
     for (int64_t len = a.batch; len > 1;) {
         const int64_t step = (len + 63) / 64, i = lane * step;
-        const bool before = i < len && start_of(a, b + i) / c.page + 2 * (b + i) <= item;
+        const bool before = i < len && (start_of(a, b + i) >> shift) + 2 * (b + i) <= item;
         const int64_t at = max(0, __popcll(__ballot(before)) - 1) * step;
         b += at;
         len = min(step, len - at);
@@ -41,8 +41,8 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, int6
     const int64_t start = start_of(a, b), count = max((int64_t)0, start_of(a, b + 1) - start);
     const int64_t length = a.lengths[b], before = length - count;       // rows the request had
     const int64_t from = max((int64_t)0, before), to = min(length, a.pages_per_request * c.page);
-    const int64_t logical = from / c.page + (item - (start / c.page + 2 * b));
-    const int64_t r0 = max(from, logical * c.page), r1 = min(to, (logical + 1) * c.page);
+    const int64_t logical = (from >> shift) + ((int64_t)item - ((start >> shift) + 2 * b));
+    const int64_t r0 = max(from, logical << shift), r1 = min(to, (logical + 1) << shift);
     if (logical < 0 || r0 >= r1) return;
     const int page = page_of(a.pages, b, a.pages_per_request, logical, c.num_pages);
     if (page < 0) return;
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, int6
         float x[2][C];
 #pragma unroll
         for (int t = 0; t < 2; ++t) load_values(src[t], x[t]);
-        const int64_t row = block * c.page + r % c.page;
+        const int64_t row = (block << shift) + (r & (c.page - 1));
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             uint32_t top = 0;
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, int6
 #pragma unroll
     for (int n = 1; n < kWaves; ++n) x = high ? fmaxf(x, most[n][i]) : fminf(x, least[n][i]);
     // (a page begun at its row 0 forgets what it held)
-    const float old = r0 % c.page ? (float)*p : x;
+    const float old = r0 & (c.page - 1) ? (float)*p : x;
     x = high ? fmaxf(x, old) : fminf(x, old);
     *p = (bf16_t)(broken || old != old ? NAN : x);
 }
@@ -123,19 +123,21 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, int6
 // One workgroup 16 rows of a request (of one page) with all their heads, in the
 // order of the outputs.
 template <typename T, bool INT8, int D>
-__global__ __launch_bounds__(kBlock) void cache_read(frog_cache_read_t a, int64_t first) {
+__global__ __launch_bounds__(kBlock) void cache_read(frog_cache_read_t a, uint32_t first) {
     using S = RowSplit<D>;
     constexpr int C = S::kEach;
     const frog_cache_t& c = a.cache;
-    const int64_t blocks = (a.slots + 15) / 16, item = first + blockIdx.x, b = item / blocks, s0 = item % blocks * 16;
+    const int shift = shift_of(c.page);
+    const uint32_t blocks = (uint32_t)((a.slots + 15) / 16), item = first + blockIdx.x;
+    const int64_t b = item / blocks, s0 = (int64_t)(item % blocks) * 16;
     const int rows = (int)min((int64_t)16, a.slots - s0);
     const int64_t length = rows_of(a.lengths, b, a.pages_per_request, c.page);
-    const int page = s0 < length ? page_of(a.pages, b, a.pages_per_request, s0 / c.page, c.num_pages) : -1;
+    const int page = s0 < length ? page_of(a.pages, b, a.pages_per_request, s0 >> shift, c.num_pages) : -1;
     const int live = page < 0 ? 0 : (int)min((int64_t)rows, length - s0);
     const int sub = threadIdx.x / S::kLanes, at = (threadIdx.x % S::kLanes) * C;
     for (int i = sub; i < rows * c.kv_heads; i += kBlock / S::kLanes) {
         const int s = i / c.kv_heads, h = i - s * c.kv_heads;
-        const int64_t row = ((int64_t)page * c.kv_heads + h) * c.page + s0 % c.page + s;
+        const int64_t row = (((int64_t)page * c.kv_heads + h) << shift) + (s0 & (c.page - 1)) + s;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             T y[C] = {};
@@ -181,10 +183,11 @@ void of_kind(int type, int storage, int d, F&& f) {
 int launch_cache_write(const frog_cache_write_t& a, hipStream_t stream) {
     if (a.batch == 0 || a.tokens == 0 || a.cache.num_pages == 0 || a.pages_per_request == 0) return FROG_OK;
     const int64_t items = a.tokens / a.cache.page + 2 * a.batch;
+    if (items > 0xffffffffll / a.cache.kv_heads) return fail(FROG_EUNSUPPORTED, "more than 2^32 workgroups");
     hipError_t e = hipSuccess;
     of_kind(a.type, a.cache.storage, a.cache.d, [&](auto t, auto i8, auto d) {
         e = in_launches(items * a.cache.kv_heads, kBlock, [&](int64_t first, dim3 grid) {
-            cache_write<decltype(t), i8.value, d.value><<<grid, kBlock, 0, stream>>>(a, first);
+            cache_write<decltype(t), i8.value, d.value><<<grid, kBlock, 0, stream>>>(a, (uint32_t)first);
         });
     });
     return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "cache write launch: %s", hipGetErrorString(e));
@@ -192,10 +195,11 @@ int launch_cache_write(const frog_cache_write_t& a, hipStream_t stream) {
 
 int launch_cache_read(const frog_cache_read_t& a, hipStream_t stream) {
     if (a.batch == 0 || a.slots == 0) return FROG_OK;
+    if (a.batch > 0xffffffffll / ((a.slots + 15) / 16)) return fail(FROG_EUNSUPPORTED, "more than 2^32 workgroups");
     hipError_t e = hipSuccess;
     of_kind(a.type, a.cache.storage, a.cache.d, [&](auto t, auto i8, auto d) {
         e = in_launches(a.batch * ((a.slots + 15) / 16), kBlock, [&](int64_t first, dim3 grid) {
-            cache_read<decltype(t), i8.value, d.value><<<grid, kBlock, 0, stream>>>(a, first);
+            cache_read<decltype(t), i8.value, d.value><<<grid, kBlock, 0, stream>>>(a, (uint32_t)first);
         });
     });
     return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "cache read launch: %s", hipGetErrorString(e));

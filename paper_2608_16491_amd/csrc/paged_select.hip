@@ -6,7 +6,7 @@
 // with Q+ (Q-) the sum of the heads' positive (negative) parts, so a page costs
 // two multiply-adds a channel whatever the group.  They are done in 64 bits and
 // rounded once: which page is the last one chosen does not depend on the order of
-// a sum.  The scores' codes are then sorted out as eviction does with its weights.
+// a sum.  The last score kept is then found among their codes (pick.h).
 // Bound by the read of the bounds, 4 d bytes a page and kv head.
 
 #include "paged.h"
@@ -16,18 +16,9 @@ namespace frog {
 namespace {
 
 constexpr int kBlock = 1024;
-constexpr int kFused = 2048;        // most pages of a request scored and chosen by one workgroup
+constexpr int kFused = 512;        // most pages of a request scored and chosen by one workgroup
 constexpr int kChunk = 128;         // else: pages a workgroup scores
 constexpr int kScoreBlock = 256;
-constexpr uint32_t kAlways = 0xFFFFFFFFu, kNaN = 0xFFFFFFFEu;
-
-// codes order like the scores; -0 equals 0
-__device__ inline uint32_t score_code(float s) {
-    if (s != s) return kNaN;
-    const uint32_t u = __float_as_uint(s + 0.f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-
 template <int CTRL>
 __device__ inline double moved(double x) {
     const uint64_t u = __builtin_bit_cast(uint64_t, x);
@@ -45,106 +36,179 @@ __device__ inline double row_sum(double x) {
     return x;
 }
 
-// Pages that hold rows of request b
-__device__ inline int live_pages(const frog_select_pages_t& a, int64_t b) {
-    return (int)((rows_of(a.lengths, b, a.pages_per_request, a.cache.page) + a.cache.page - 1) / a.cache.page);
+// What request b's lists are made of: `n` pages hold rows; `want` are listed; of
+// those from `from` on `count` have to be scored, of which `pick` are taken.
+struct Lists {
+    int n, want, from, count, pick;
+    __device__ inline Lists(const frog_select_pages_t& a, int64_t b) {
+        n = (int)((rows_of(a.lengths, b, a.pages_per_request, a.cache.page) + a.cache.page - 1) >> shift_of(a.cache.page));
+        want = (int)min((int64_t)n, a.keep);
+        const bool all = n <= a.keep;
+        from = all ? 0 : (int)a.first;
+        count = all ? 0 : n - from - (int)a.recent;
+        pick = all ? 0 : want - from - (int)a.recent;
+        if (pick == 0) count = 0;
+    }
+};
+
+// Q+ and Q- of (request b, kv head h) into LDS
+template <typename T, int D>
+__device__ inline void sum_queries(const frog_select_pages_t& a, int64_t b, int h, double (&parts)[2][D]) {
+    const int i = threadIdx.x, group = a.heads / a.cache.kv_heads;
+    if (i < D) {
+        const T* q = (const T*)a.q + b * a.q_stride[0] + (int64_t)h * group * a.q_stride[1] + i;
+        double up = 0.0, down = 0.0;
+        for (int g0 = 0; g0 < group; g0 += 8) {      // eight heads' loads at a time
+            float x[8];
+#pragma unroll
+            for (int g = 0; g < 8; ++g) x[g] = (float)q[(int64_t)min(g0 + g, group - 1) * a.q_stride[1]];
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                // (a NaN goes into both)
+                const float y = g0 + g < group ? x[g] : 0.f;
+                up += y < 0.f ? 0.0 : (double)y;
+                down += y > 0.f ? 0.0 : (double)y;
+            }
+        }
+        parts[0][i] = up;
+        parts[1][i] = down;
+    }
+    __syncthreads();
 }
 
 // Codes of pages p0 .. p1 - 1 of (request b, kv head h) by WAVES wavefronts, put(p, code) from one lane each.
 template <typename T, int D, int WAVES, typename F>
-__device__ inline void score_pages(const frog_select_pages_t& a, int64_t b, int h, int n, int p0, int p1, F&& put) {
+__device__ inline void score_pages(const frog_select_pages_t& a, int64_t b, int h, int p0, int p1, double (&parts)[2][D], F&& put) {
     using S = RowSplit<D>;
-    constexpr int C = S::kEach, U = 4;      // U pages of a row of lanes in flight
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, sub = lane / S::kLanes, at = (lane % S::kLanes) * C;
-    const int group = a.heads / a.cache.kv_heads;
-    double up[C], down[C];
-#pragma unroll
-    for (int i = 0; i < C; ++i) up[i] = down[i] = 0.0;
-    for (int g = 0; g < group; ++g) {
-        float x[C];
-        load_values((const T*)a.q + b * a.q_stride[0] + (int64_t)(h * group + g) * a.q_stride[1] + at, x);
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            // (a NaN goes into both)
-            up[i] += x[i] < 0.f ? 0.0 : (double)x[i];
-            down[i] += x[i] > 0.f ? 0.0 : (double)x[i];
-        }
-    }
+    constexpr int C = S::kEach, U = D == 96 ? 2 : 4;      // U pages of a row of lanes in flight
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), sub = lane / S::kLanes, at = (lane % S::kLanes) * C;
     const int32_t* table = a.pages + b * a.pages_per_request;
     const uint16_t* bounds = (const uint16_t*)a.cache.bounds + (int64_t)h * 2 * D + at;
     const int64_t stride = (int64_t)a.cache.kv_heads * 2 * D;
-    for (int p = p0 + w * S::kRows; p < p1; p += WAVES * S::kRows * U) {
+    constexpr int kApart = WAVES * S::kRows;
+    struct Pages {
         int page[U];
         Words<C / 2> least[U], most[U];
+    };
+    auto look = [&](int (&page)[U], int p) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) page[u] = table[min(p + u * WAVES * S::kRows + sub, p1 - 1)];
+        for (int u = 0; u < U; ++u) page[u] = table[min(p + u * kApart + sub, p1 - 1)];
+    };
+    auto fetch = [&](Pages& x) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const uint16_t* src = bounds + max((int64_t)0, min((int64_t)page[u], a.cache.num_pages - 1)) * stride;
-            least[u] = load_words<C / 2>(src);
-            most[u] = load_words<C / 2>(src + D);
+            const uint16_t* src = bounds + max((int64_t)0, min((int64_t)x.page[u], a.cache.num_pages - 1)) * stride;
+            x.least[u] = load_words<C / 2>(src);
+            x.most[u] = load_words<C / 2>(src + D);
+        }
+    };
+    // page numbers two steps ahead, bounds one: what the workgroup waits for first is on its way beside the queries
+    Pages now, next;
+    int p = p0 + w * S::kRows;
+    look(now.page, p);
+    look(next.page, p + U * kApart);
+    fetch(now);
+    sum_queries<T, D>(a, b, h, parts);
+    double up[C], down[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) up[i] = parts[0][at + i], down[i] = parts[1][at + i];
+    for (; p < p1; p += U * kApart) {
+        int far[U];
+        if (p + U * kApart < p1) {
+            fetch(next);
+            look(far, p + 2 * U * kApart);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            if (p + u * kApart >= p1) break;
             double s = 0.0;
 #pragma unroll
             for (int i = 0; i < C / 2; ++i)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t x = least[u].w[i], y = most[u].w[i];
+                    const uint32_t x = now.least[u].w[i], y = now.most[u].w[i];
                     s = __builtin_fma(down[2 * i + e], (double)__uint_as_float(e ? x & 0xFFFF0000u : x << 16), s);
                     s = __builtin_fma(up[2 * i + e], (double)__uint_as_float(e ? y & 0xFFFF0000u : y << 16), s);
                 }
             s = row_sum<S::kLanes>(s);
-            const int i = p + u * WAVES * S::kRows + sub;
-            if (at == 0 && i < p1) {
-                const bool none = page[u] < 0 || page[u] >= a.cache.num_pages;
-                put(i, i < a.first || i >= n - a.recent ? kAlways : none ? 0u : score_code((float)s));
-            }
+            const int i = p + u * kApart + sub;
+            if (at == 0 && i < p1) put(i, now.page[u] < 0 || now.page[u] >= a.cache.num_pages ? 0u : score_code((float)s));
         }
+        now = next;
+#pragma unroll
+        for (int u = 0; u < U; ++u) next.page[u] = far[u];
     }
 }
 
-// the list of (request, kv head) x from the codes of its n pages
-template <typename F>
-__device__ inline void choose(const frog_select_pages_t& a, int64_t x, int n, F&& code_at, PickSpace<kBlock>& space) {
-    const int want = (int)min((int64_t)n, a.keep);
+// the pages of list x that are chosen whatever their score, and the end of the list
+__device__ inline void put_sure(const frog_select_pages_t& a, int64_t x, const Lists& l) {
     int32_t* out = a.chosen + x * a.keep;
-    const Bound bound = largest<kBlock>(n, want, code_at, space);
-    list_kept<kBlock>(n, bound.ties, [&](int i) {
-        if (want == n) return 2;
-        const uint32_t c = code_at(i);
-        return c > bound.code ? 2 : c == bound.code ? 1 : 0;
-    }, out, space);
-    for (int64_t i = want + threadIdx.x; i < a.keep; i += kBlock) out[i] = -1;
+    const int recent = l.want - l.from - l.pick;      // (all of them, where all are listed)
+    for (int i = threadIdx.x; i < l.from; i += kBlock) out[i] = i;
+    for (int i = threadIdx.x; i < recent; i += kBlock) out[l.from + l.pick + i] = l.n - recent + i;
+    for (int64_t i = l.want + threadIdx.x; i < a.keep; i += kBlock) out[i] = -1;
 }
 
 // One workgroup a (request, kv head), the codes in LDS.
 template <typename T, int D>
 __global__ __launch_bounds__(kBlock) void select_whole(frog_select_pages_t a, int64_t first) {
-    __shared__ PickSpace<kBlock> space;
+    __shared__ FewSpace<kBlock> space;
     __shared__ uint32_t codes[kFused];
-    const int64_t x = first + blockIdx.x, b = x / a.cache.kv_heads;
-    const int n = live_pages(a, b);
-    if (n > a.keep) score_pages<T, D, kBlock / 64>(a, b, (int)(x % a.cache.kv_heads), n, 0, n, [&](int p, uint32_t c) { codes[p] = c; });
+    __shared__ double parts[2][D];
+    const int64_t x = first + blockIdx.x, b = (uint32_t)x / (uint32_t)a.cache.kv_heads;
+    const Lists l(a, b);
+    put_sure(a, x, l);
+    if (l.count == 0) return;
+    score_pages<T, D, kBlock / 64>(a, b, (int)((uint32_t)x % (uint32_t)a.cache.kv_heads), l.from, l.from + l.count, parts, [&](int p, uint32_t c) { codes[p - l.from] = c; });
     __syncthreads();
-    choose(a, x, n, [&](int i) { return codes[i]; }, space);
+    constexpr int R = 1;
+    static_assert(kFused <= R * kBlock, "a code a thread");
+    uint32_t code[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int i = 64 * (R * (threadIdx.x >> 6) + r) + (threadIdx.x & 63);
+        code[r] = i < l.count ? codes[i] : 0;
+    }
+    pick_few<kBlock, R>(code, l.count, l.pick, l.from, a.chosen + x * a.keep + l.from, space);
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kScoreBlock) void select_score(frog_select_pages_t a, uint32_t* codes, int chunks, int64_t first) {
-    const int64_t item = first + blockIdx.x, x = item / chunks, b = x / a.cache.kv_heads;
-    const int n = live_pages(a, b), p0 = (int)(item % chunks) * kChunk;
-    if (p0 >= n || n <= a.keep) return;
-    uint32_t* to = codes + x * a.pages_per_request;
-    score_pages<T, D, kScoreBlock / 64>(a, b, (int)(x % a.cache.kv_heads), n, p0, min(n, p0 + kChunk), [&](int p, uint32_t c) { to[p] = c; });
+__global__ __launch_bounds__(kScoreBlock) void select_score(frog_select_pages_t a, uint32_t* codes, int chunks, uint32_t first) {
+    __shared__ double parts[2][D];
+    const uint32_t item = first + blockIdx.x;
+    const int64_t x = item / (uint32_t)chunks, b = (uint32_t)x / (uint32_t)a.cache.kv_heads;
+    const Lists l(a, b);
+    const int p0 = (int)(item % (uint32_t)chunks) * kChunk;
+    if (p0 >= l.count) return;
+    uint32_t* to = codes + x * a.pages_per_request - l.from;
+    score_pages<T, D, kScoreBlock / 64>(a, b, (int)((uint32_t)x % (uint32_t)a.cache.kv_heads), l.from + p0, l.from + min(l.count, p0 + kChunk), parts, [&](int p, uint32_t c) { to[p] = c; });
 }
 
+// R codes a thread in registers; R = 0: from memory
+template <int R>
 __global__ __launch_bounds__(kBlock) void select_choose(frog_select_pages_t a, const uint32_t* codes, int64_t first) {
-    __shared__ PickSpace<kBlock> space;
+    __shared__ typename std::conditional<R == 0, PickSpace<kBlock>, FewSpace<kBlock>>::type space;
     const int64_t x = first + blockIdx.x;
+    const Lists l(a, (uint32_t)x / (uint32_t)a.cache.kv_heads);
+    put_sure(a, x, l);
+    if (l.count == 0) return;
     const uint32_t* from = codes + x * a.pages_per_request;
-    choose(a, x, live_pages(a, x / a.cache.kv_heads), [&](int i) { return from[i]; }, space);
+    int32_t* out = a.chosen + x * a.keep + l.from;
+    if constexpr (R == 0) {
+        const Bound bound = largest<kBlock>(l.count, l.pick, [&](int i) { return from[i]; }, space);
+        list_kept<kBlock>(l.count, bound.ties, [&](int i) { return from[i] > bound.code ? 2 : from[i] == bound.code ? 1 : 0; }, out, space);
+        // (the list counts from the first page scored)
+        __syncthreads();
+        for (int i = threadIdx.x; i < l.pick; i += kBlock) out[i] += l.from;
+    } else {
+        uint32_t code[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int i = 64 * (R * (threadIdx.x >> 6) + r) + (threadIdx.x & 63);
+            code[r] = i < l.count ? from[i] : 0;
+        }
+        pick_few<kBlock, R>(code, l.count, l.pick, l.from, out, space);
+    }
 }
 
 // One launch while one workgroup takes a request's pages.
@@ -155,9 +219,13 @@ hipError_t launch(const frog_select_pages_t& a, uint32_t* codes, hipStream_t str
     const int64_t pairs = a.batch * a.cache.kv_heads;
     if (whole(a)) return in_launches(pairs, kBlock, [&](int64_t first, dim3 grid) { select_whole<T, D><<<grid, kBlock, 0, stream>>>(a, first); });
     const int chunks = (int)((a.pages_per_request + kChunk - 1) / kChunk);
-    const hipError_t e = in_launches(pairs * chunks, kScoreBlock, [&](int64_t first, dim3 grid) { select_score<T, D><<<grid, kScoreBlock, 0, stream>>>(a, codes, chunks, first); });
+    const hipError_t e = in_launches(pairs * chunks, kScoreBlock, [&](int64_t first, dim3 grid) { select_score<T, D><<<grid, kScoreBlock, 0, stream>>>(a, codes, chunks, (uint32_t)first); });
     if (e != hipSuccess) return e;
-    return in_launches(pairs, kBlock, [&](int64_t first, dim3 grid) { select_choose<<<grid, kBlock, 0, stream>>>(a, codes, first); });
+    return in_launches(pairs, kBlock, [&](int64_t first, dim3 grid) {
+        if (a.pages_per_request <= 2 * kBlock) select_choose<2><<<grid, kBlock, 0, stream>>>(a, codes, first);
+        else if (a.pages_per_request <= 8 * kBlock) select_choose<8><<<grid, kBlock, 0, stream>>>(a, codes, first);
+        else select_choose<0><<<grid, kBlock, 0, stream>>>(a, codes, first);
+    });
 }
 
 template <typename T>
@@ -179,6 +247,7 @@ __global__ __launch_bounds__(256) void select_nothing(frog_select_pages_t a, int
 
 int64_t select_pages_ws(const frog_select_pages_t& a) {
     if (a.batch == 0 || a.keep == 0 || a.cache.num_pages == 0 || whole(a)) return 0;
+    if (a.batch * a.cache.kv_heads > 0xffffffffll / ((a.pages_per_request + kChunk - 1) / kChunk)) return fail(FROG_EUNSUPPORTED, "more than 2^32 workgroups");
     return a.batch * a.cache.kv_heads * a.pages_per_request * 4;
 }
 

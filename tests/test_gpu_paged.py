@@ -230,20 +230,44 @@ def test_select_ties_and_what_is_not_a_number():
             assert torch.equal(got.cpu(), ref.select(x, pages, lengths, keep, 0, 1)), keep
 
 
-def test_select_many_pages():
-    # more pages than one workgroup keeps: scored by one launch, chosen by another
+@pytest.mark.parametrize("width", [2100, 3100, 8200])
+def test_select_many_pages(width):
+    # more pages than one workgroup keeps: scored by one launch, chosen by another, from registers or from memory
     g = torch.Generator().manual_seed(6)
-    b, width, kv, d = 2, 3100, 2, 64
+    b, kv, d = 2, 2, 64
     pages, total = table(g, b, width)
     cache = F.PagedCache.empty(total, kv, d, page=16)
-    cache.bounds.copy_(torch.randn(cache.bounds.shape, generator=g).sort(2)[0])
     q = rand_rows(g, "bf16", b, 6, d)
-    ref = Cache(cache)
-    for n in ([width * 16, 5000], [0, 1], [width * 16 + 99, 2100 * 16]):
-        n = torch.tensor(n, dtype=torch.int32)
-        for keep in (1, 200, 2999):
-            got = F.select_pages(q.cuda(), cache, pages.cuda(), n.cuda(), keep, first=1 if keep > 1 else 0)
-            assert torch.equal(got.cpu(), ref.select(q, pages, n, keep, 1 if keep > 1 else 0, 1))
+    for kind in ("all differ", "few values", "one value"):
+        x = torch.randn(cache.bounds.shape, generator=g).sort(2)[0]
+        # (of equal bounds only some pages' differ)
+        x = x if kind == "all differ" else x[:1] * torch.ones((total, 1, 1, 1)) if kind == "one value" else x[torch.arange(total) % 7]
+        cache.bounds.copy_(x)
+        ref = Cache(cache)
+        for n in ([width * 16, 5000], [0, 1], [width * 16 + 99, 2080 * 16]):
+            n = torch.tensor(n, dtype=torch.int32)
+            for keep in (1, 2, 200, 2050):
+                first = 1 if keep > 1 else 0
+                got = F.select_pages(q.cuda(), cache, pages.cuda(), n.cuda(), keep, first=first)
+                assert torch.equal(got.cpu(), ref.select(q, pages, n, keep, first, 1)), (kind, n, keep)
+
+
+@pytest.mark.parametrize("width", [3, 63, 64, 65, 130, 1025, 2048])
+def test_select_counts(width):
+    # every number of pages kept about a wavefront's and a workgroup's share, scores with and without equals
+    g = torch.Generator().manual_seed(width)
+    pages, total = table(g, 1, width)
+    cache = F.PagedCache.empty(total, 1, 32, page=16, storage="int8")
+    q = rand_rows(g, "fp16", 1, 2, 32)
+    n = torch.tensor([width * 16 - 5], dtype=torch.int32)
+    for spread in (1, 3, total):
+        cache.bounds.copy_(torch.randn(cache.bounds.shape, generator=g).sort(2)[0][torch.arange(total) % spread])
+        ref = Cache(cache)
+        for keep in sorted({1, 2, 3, width // 3, width // 2, width - 2, width - 1, width, width + 1} - {0}):
+            for first, recent in ((0, 0), (0, 1), (1, keep - 1), (keep // 2, keep - keep // 2)):
+                if first + recent <= keep:
+                    got = F.select_pages(q.cuda(), cache, pages.cuda(), n.cuda(), keep, first=first, recent=recent)
+                    assert torch.equal(got.cpu(), ref.select(q, pages, n, keep, first, recent)), (spread, keep, first, recent)
 
 
 # ------------------------------------------------------------------ attention
