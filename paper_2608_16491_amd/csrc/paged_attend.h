@@ -91,6 +91,95 @@ __device__ inline void split_factors(const vec<float, 8>& x, frag<bf16_t> (&f)[F
     }
 }
 
+// Columns of the score tiles: with at most G = 2, 4 or 8 query rows, rows repeat
+// along the 16 columns, and the 8 scores a lane has of one are shared out: lane
+// G j + g takes the E = G / 2 of part j, whose weights the others get from it.
+// x of part J, in all lanes of the row of 16 that have the same g
+template <int G, int J>
+__device__ inline uint32_t from_part(uint32_t x) { return (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, (J * G) << 5 | 0x10 | (G - 1)); }
+
+// the part's own E of eight values
+template <int E>
+__device__ inline vec<float, E> own_part(vec<float, 8> x, int part) {
+    vec<float, E> y;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        y[e] = x[e];
+#pragma unroll
+        for (int j = 1; j < 8 / E; ++j) y[e] = part == j ? x[j * E + e] : y[e];
+    }
+    return y;
+}
+
+// What the weights' two factors cost in products: where at most eight rows repeat
+// along the columns, the first stands in columns 0 .. 7 of one product and the
+// second in 8 .. 15, and the halves are added at the end (1,001 keys, four rows, d = 128:
+// half of the second product's 16 matrix instructions a step).
+template <int E, int F>
+constexpr bool kHalves = E < 8 && F == 2;
+template <int E, int F>
+constexpr int kChains = kHalves<E, F> ? 1 : F;
+
+// the factors of all eight weights from the part's own
+template <int E, int F>
+__device__ inline void share_factors(const vec<float, E>& p, frag<bf16_t> (&f)[kChains<E, F>], int col) {
+    if constexpr (E == 8) {
+        split_factors<F>(p, f);
+    } else {
+        constexpr int G = 2 * E;
+        vec<float, E> rest = p;
+        vec<bf16_t, E> own[F];
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+            own[i] = __builtin_convertvector(rest, vec<bf16_t, E>);
+            if (i + 1 < F) rest -= __builtin_convertvector(own[i], vec<float, E>);
+        }
+        auto gather = [](const uint32_t (&x)[E], uint32_t (&w)[8]) {
+            // value e of part j: weight E j + e
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                w[e] = from_part<G, 0>(x[e]);
+                w[E + e] = from_part<G, 1>(x[e]);
+                if constexpr (E <= 2) {
+                    w[2 * E + e] = from_part<G, 2>(x[e]);
+                    w[3 * E + e] = from_part<G, 3>(x[e]);
+                }
+                if constexpr (E == 1) {
+                    w[4] = from_part<G, 4>(x[e]);
+                    w[5] = from_part<G, 5>(x[e]);
+                    w[6] = from_part<G, 6>(x[e]);
+                    w[7] = from_part<G, 7>(x[e]);
+                }
+            }
+        };
+        uint32_t x[E], w[8];
+        vec<uint32_t, 4> a;
+        if constexpr (F == 2) {
+            // both factors of a weight in one word; a column takes its half of it
+            const uint32_t half = col < 8 ? 0x05040100 : 0x07060302;
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = __builtin_bit_cast(uint32_t, vec<bf16_t, 2>{own[0][e], own[1][e]});
+            gather(x, w);
+#pragma unroll
+            for (int n = 0; n < 4; ++n) a[n] = __builtin_amdgcn_perm(w[2 * n + 1], w[2 * n], half);
+            f[0] = __builtin_bit_cast(frag<bf16_t>, a);
+        } else {
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const bf16_t y = own[i][e];      // (a bit cast of an element takes the vector's first)
+                    x[e] = __builtin_bit_cast(uint16_t, y);
+                }
+                gather(x, w);
+#pragma unroll
+                for (int n = 0; n < 4; ++n) a[n] = __builtin_amdgcn_perm(w[2 * n + 1], w[2 * n], 0x05040100);
+                f[i] = __builtin_bit_cast(frag<bf16_t>, a);
+            }
+        }
+    }
+}
+
 // What a lane holds of a step's rows, as loaded.  Keys: of row lane % 16 of each
 // tile the pieces that its quarter of the wavefront multiplies.  Values: of rows
 // 4 (lane / 16) .. + 3 the bytes whose channels are row lane % 16 of the second
@@ -152,16 +241,19 @@ __device__ inline int out_channel(int i, int m) {
 // One workgroup of W wavefronts a (request, kv head, part of its rows).  Bound by
 // HBM: conversions and softmax take about a third of the cycles that the read
 // of the rows does, so the loads of the next step are only kept in registers.
-template <typename T, bool INT8, int D, bool PLAIN, int NQ, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NQ == 2 || sizeof(T) == 4 ? 2 : W == 16 ? 4 : 3)))
+template <typename T, bool INT8, int D, bool PLAIN, int E, int NQ, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NQ == 2 || sizeof(T) == 4 ? 2 : W == 16 || E < 8 ? 4 : 3)))
 void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedParts parts, uint32_t first_item) {
     constexpr int QF = sizeof(T) == 4 ? 3 : std::is_same<T, bf16_t>::value ? 1 : 2, PF = sizeof(T) == 4 ? 3 : 2;
-    constexpr int M = D / 16, S = D / 32;
+    constexpr int M = D / 16, S = D / 32, G = 2 * E;
+    static_assert(E == 8 || NQ == 1, "shared scores are of one column tile");
     __shared__ int block_of[kMostTiles], place_of[kMostTiles];
     __shared__ float tops[W][16 * NQ], sums[W][16 * NQ], most[16 * NQ], total[16 * NQ];
-    __shared__ __attribute__((aligned(16))) float joined[W][16 * NQ * D];
+    // (rows apart by eight banks)
+    constexpr int kRows = E < 8 ? G : 16 * NQ, kApart = D + 8;
+    __shared__ __attribute__((aligned(16))) float joined[W][kRows * kApart];
     const frog_cache_t& c = a.cache;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quarter = lane >> 4, own = col / G;
     uint32_t item = first_item + blockIdx.x;
     const int h = (int)(item % (uint32_t)c.kv_heads);
     item /= (uint32_t)c.kv_heads;
@@ -198,7 +290,7 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
     float slope[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        const int head = h * group + min(rows0 + 16 * n + col, group - 1);
+        const int head = h * group + min(rows0 + 16 * n + col % G, group - 1);
         const T* p = (const T*)a.q + b * a.q_stride[0] + head * a.q_stride[1];
 #pragma unroll
         for (int s = 0; s < S; ++s) {
@@ -232,41 +324,50 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
         return s;
     };
     auto step = [&](Rows<D>& r, const Step& at, const Step& next, bool more) __attribute__((always_inline)) {
-        vec<float, 8> z[NQ], up;
+        vec<float, 8> x[NQ];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            acc4 x[NQ];
+            acc4 y[NQ];
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) x[n] = acc4{};
+            for (int n = 0; n < NQ; ++n) y[n] = acc4{};
 #pragma unroll
             for (int s = 0; s < S; ++s) {
                 const frag<bf16_t> k = factor_of<INT8>(r.k[t][2 * s], r.k[t][2 * s + 1]);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                    for (int f = 0; f < QF; ++f) x[n] = mma(k, qf[n][s][f], x[n]);
+                    for (int f = 0; f < QF; ++f) y[n] = mma(k, qf[n][s][f], y[n]);
             }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float power = power_of((r.ke[t] >> (8 * e)) & 255) * (PLAIN ? sp.mul : 1.f);
+            for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) z[n][4 * t + e] = x[n][e] * power;
-            }
+                for (int e = 0; e < 4; ++e) x[n][4 * t + e] = y[n][e];
         }
+        // of the own scores: the powers' bytes, and where their keys stand
+        const uint32_t ke0 = r.ke[0], ke1 = r.ke[1];
         if (more) r.load_keys(c, next.block, lane);
+        auto byte_of = [&](uint32_t exps0, uint32_t exps1, int e) {
+            if constexpr (E == 8) return ((e / 4 ? exps1 : exps0) >> (8 * (e % 4))) & 255;
+            else return ((E * own >= 4 ? exps1 : exps0) >> (8 * ((E * own & 3) + e))) & 255;
+        };
+        auto tile_of = [&](int e) { return E == 8 ? e / 4 : E * own / 4; };
+        auto place_of_key = [&](int e) {
+            return (tile_of(e) ? at.place[1] : at.place[0]) + 4 * quarter + (E == 8 ? e % 4 : (E * own & 3) + e);
+        };
+        vec<float, E> z[NQ], up;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) up[e] = power_of((r.ve[e / 4] >> (8 * (e % 4))) & 255);
-        if constexpr (!PLAIN) {
+        for (int e = 0; e < E; ++e) up[e] = power_of(byte_of(r.ve[0], r.ve[1], e));
 #pragma unroll
-            for (int n = 0; n < NQ; ++n) {
-                if (sp.cap2 > 0.f) cap_scores<8>(sp, z[n]);
+        for (int n = 0; n < NQ; ++n) {
+            z[n] = own_part<E>(x[n], own);
+#pragma unroll
+            for (int e = 0; e < E; ++e) z[n][e] *= power_of(byte_of(ke0, ke1, e)) * (PLAIN ? sp.mul : 1.f);
+            if constexpr (!PLAIN) {
+                if (sp.cap2 > 0.f) cap_scores<E>(sp, z[n]);
                 else z[n] *= sp.mul;
                 if (a.slopes) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int place = at.place[e / 4] + 4 * quarter + e % 4;
-                        z[n][e] -= slope[n] * fabsf((float)(walk.last - place));
-                    }
+                    for (int e = 0; e < E; ++e) z[n][e] -= slope[n] * fabsf((float)(walk.last - place_of_key(e)));
                 }
             }
         }
@@ -279,34 +380,43 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
             for (int e = 0; e < 8; ++e) {
                 const int place = at.place[e / 4] + 4 * quarter + e % 4;
                 const bool seen = at.block[e / 4] >= 0 && place >= walk.lo && place <= walk.hi;
-                up[e] = seen ? up[e] : 0.f;
 #pragma unroll
                 for (int i = 0; i < Rows<D>::kV; ++i) r.v[e / 4][e % 4][i] = seen ? r.v[e / 4][e % 4][i] : 0;
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int place = place_of_key(e);
+                const bool seen = (tile_of(e) ? at.block[1] : at.block[0]) >= 0 && place >= walk.lo && place <= walk.hi;
+                up[e] = seen ? up[e] : 0.f;
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) z[n][e] = seen ? z[n][e] : -INFINITY;
             }
         }
-        frag<bf16_t> pf[NQ][PF];
+        frag<bf16_t> pf[NQ][kChains<E, PF>];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
             float most = z[n][0];
 #pragma unroll
-            for (int e = 1; e < 8; ++e) most = fmaxf(most, z[n][e]);
+            for (int e = 1; e < E; ++e) most = fmaxf(most, z[n][e]);
             // the maximum is renewed where it grew by more than 2^8
             if (__any(most > top[n] + 8.f)) {
-                const float now = quarter_max(fmaxf(most, top[n])), down = exp2_fast(top[n] - now);
+                float now = fmaxf(most, top[n]);
+#pragma unroll
+                for (int i = G; i < 16; i *= 2) now = fmaxf(now, __shfl_xor(now, i));
+                now = quarter_max(now);
+                const float down = exp2_fast(top[n] - now);
                 top[n] = now;
                 sum[n] *= down;
 #pragma unroll
                 for (int m = 0; m < M; ++m) o[n][m] *= down;
             }
-            vec<float, 8> p;
+            vec<float, E> p;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < E; ++e) {
                 p[e] = exp2_fast(z[n][e] - top[n]);
                 sum[n] += p[e];
             }
-            split_factors<PF>(p * up, pf[n]);
+            share_factors<E, PF>(p * up, pf[n], col);
         }
         auto product = [&](auto byte, int word, int m) __attribute__((always_inline)) {
             constexpr int B = decltype(byte)::value;
@@ -316,7 +426,7 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int f = 0; f < PF; ++f) o[n][m] = mma(v, pf[n][f], o[n][m]);
+                for (int f = 0; f < kChains<E, PF>; ++f) o[n][m] = mma(v, pf[n][f], o[n][m]);
         };
 #pragma unroll
         for (int m = 0; m < M; m += 4) {
@@ -348,6 +458,8 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
     const int rows = min(group - rows0, 16 * NQ);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
+#pragma unroll
+        for (int i = G; i < 16; i *= 2) sum[n] += __shfl_xor(sum[n], i);
         sum[n] = quarter_sum(sum[n]);
         if (quarter == 0) {
             tops[w][16 * n + col] = top[n];
@@ -369,25 +481,31 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
             }
         }
         const float down = exp2_fast(top[n] - all);
+        if constexpr (kHalves<E, PF>) {
+#pragma unroll
+            for (int m = 0; m < M; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[n][m][e] += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(o[n][m][e]), 0x128, 0xF, 0xF, true));   // column ^ 8
+        }
         if (16 * n + col < rows) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
                 for (int m = 0; m < M; m += 2)
-                    *(float2*)&joined[w][(16 * n + col) * D + out_channel<D>(4 * quarter + e, m)] = make_float2(o[n][m][e] * down, o[n][m + 1][e] * down);
+                    *(float2*)&joined[w][(16 * n + col) * kApart + out_channel<D>(4 * quarter + e, m)] = make_float2(o[n][m][e] * down, o[n][m + 1][e] * down);
         }
     }
     __syncthreads();
     const int64_t row0 = b * a.heads + h * group + rows0;
     for (int i = threadIdx.x; i < rows * (D / 2); i += 64 * W) {
+        const int row = i / (D / 2), channel = 2 * (i % (D / 2));
         float2 x = make_float2(0.f, 0.f);
 #pragma unroll
         for (int n = 0; n < W; ++n) {
-            const float2 y = *(const float2*)&joined[n][2 * i];
+            const float2 y = *(const float2*)&joined[n][row * kApart + channel];
             x.x += y.x;
             x.y += y.y;
         }
-        const int row = i / (D / 2), channel = 2 * (i % (D / 2));
         if (parts.o) {
             *(float2*)(parts.o + (part * parts.rows + row0 + row) * D + channel) = x;
         } else {
@@ -416,10 +534,18 @@ hipError_t launch_paged(const frog_attend_paged_t& a, const PagedPlan& plan, con
     };
     const bool plain = a.cap == 0.f && !a.slopes;
     if constexpr (sizeof(T) == 2) {
-        if (plan.wide) return plain ? run(paged_attend<T, INT8, D, true, 2, 4>, 256) : run(paged_attend<T, INT8, D, false, 2, 4>, 256);
+        if (plan.wide) return plain ? run(paged_attend<T, INT8, D, true, 8, 2, 4>, 256) : run(paged_attend<T, INT8, D, false, 8, 2, 4>, 256);
     }
-    if (plan.waves == 16) return plain ? run(paged_attend<T, INT8, D, true, 1, 16>, 1024) : run(paged_attend<T, INT8, D, false, 1, 16>, 1024);
-    return plain ? run(paged_attend<T, INT8, D, true, 1, 4>, 256) : run(paged_attend<T, INT8, D, false, 1, 4>, 256);
+    auto shared = [&](auto each) {
+        constexpr int E = decltype(each)::value;
+        if (plan.waves == 16) return plain ? run(paged_attend<T, INT8, D, true, E, 1, 16>, 1024) : run(paged_attend<T, INT8, D, false, E, 1, 16>, 1024);
+        return plain ? run(paged_attend<T, INT8, D, true, E, 1, 4>, 256) : run(paged_attend<T, INT8, D, false, E, 1, 4>, 256);
+    };
+    const int group = a.heads / a.cache.kv_heads;
+    if (group <= 2) return shared(std::integral_constant<int, 1>());
+    if (group <= 4) return shared(std::integral_constant<int, 2>());
+    if (group <= 8) return shared(std::integral_constant<int, 4>());
+    return shared(std::integral_constant<int, 8>());
 }
 
 template <typename T>
