@@ -336,11 +336,13 @@ _PAGED = ("PagedCache", "cache_write", "cache_read", "select_pages", "attend_pag
 
 
 def __getattr__(name):
-    # these need torch, which this module imports only where a call does
+    # these need torch, which this module imports only where a call does; once
+    # looked up they are ordinary names of the module
     if name in _ATTENTION:
-        from . import attention
-        return getattr(attention, name)
-    if name in _PAGED:
-        from . import paged
-        return getattr(paged, name)
-    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+        from . import attention as source
+    elif name in _PAGED:
+        from . import paged as source
+    else:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    globals()[name] = value = getattr(source, name)
+    return value

@@ -242,7 +242,7 @@ __device__ inline int out_channel(int i, int m) {
 // HBM: conversions and softmax take about a third of the cycles that the read
 // of the rows does, so the loads of the next step are only kept in registers.
 template <typename T, bool INT8, int D, bool PLAIN, int E, int NQ, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NQ == 2 || sizeof(T) == 4 ? 2 : W == 16 || E < 8 ? 4 : 3)))
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NQ == 2 || sizeof(T) == 4 ? 2 : W == 8 ? 2 : E < 8 ? 4 : 3)))
 void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedParts parts, uint32_t first_item) {
     constexpr int QF = sizeof(T) == 4 ? 3 : std::is_same<T, bf16_t>::value ? 1 : 2, PF = sizeof(T) == 4 ? 3 : 2;
     constexpr int M = D / 16, S = D / 32, G = 2 * E;
@@ -538,7 +538,7 @@ hipError_t launch_paged(const frog_attend_paged_t& a, const PagedPlan& plan, con
     }
     auto shared = [&](auto each) {
         constexpr int E = decltype(each)::value;
-        if (plan.waves == 16) return plain ? run(paged_attend<T, INT8, D, true, E, 1, 16>, 1024) : run(paged_attend<T, INT8, D, false, E, 1, 16>, 1024);
+        if (plan.waves == 8) return plain ? run(paged_attend<T, INT8, D, true, E, 1, 8>, 512) : run(paged_attend<T, INT8, D, false, E, 1, 8>, 512);
         return plain ? run(paged_attend<T, INT8, D, true, E, 1, 4>, 256) : run(paged_attend<T, INT8, D, false, E, 1, 4>, 256);
     };
     const int group = a.heads / a.cache.kv_heads;

@@ -90,8 +90,9 @@ class PagedCache:
         return (self.k.data_ptr(), self.v.data_ptr(), self.k_exp.data_ptr(), self.v_exp.data_ptr(), 0 if b is None else b.data_ptr(),
                 *self._tail)
 
-    def _inputs(self):
-        return (self.k, self.v, self.k_exp, self.v_exp, self.bounds)
+    def _run(self, call, stream, *inputs):
+        """`call()`, enqueued on `stream` (None: the current one)."""
+        return call() if stream is None else _on(stream, call, (self.k, self.v, self.k_exp, self.v_exp, self.bounds, *inputs))
 
 
 def _table(cache, pages, lengths):
@@ -133,7 +134,7 @@ def cache_write(cache, k, v, pages, lengths, *, starts=None, stream=None):
         _launch(lib().frog_cache_write, args, cache.device)
         return ()
 
-    _on(stream, run, (k, v, pages, lengths, starts, *cache._inputs()))
+    cache._run(run, stream, k, v, pages, lengths, starts)
     if cache._written:
         increment_version(cache._written)      # (written by address: autograd has to hear of it)
 
@@ -156,7 +157,7 @@ def cache_read(cache, pages, lengths, slots=None, *, dtype=torch.bfloat16, strea
                                                   kind), cache.device)
         return k, v
 
-    return _on(stream, run, (cache.k, pages, lengths, *cache._inputs()[1:]))
+    return cache._run(run, stream, pages, lengths)
 
 
 def select_pages(q, cache, pages, lengths, keep, *, first=0, recent=1, stream=None):
@@ -183,7 +184,7 @@ def select_pages(q, cache, pages, lengths, keep, *, first=0, recent=1, stream=No
         _launch(L.frog_select_pages, args, cache.device)
         return (chosen,)
 
-    return _on(stream, run, (q, pages, lengths, *cache._inputs()))[0]
+    return cache._run(run, stream, q, pages, lengths)[0]
 
 
 def attend_paged(q, cache, pages, lengths, *, chosen=None, lr=None, scale=None, cap=0.0, slopes=None, return_lse=False, stream=None):
@@ -220,5 +221,5 @@ def attend_paged(q, cache, pages, lengths, *, chosen=None, lr=None, scale=None, 
         _launch(L.frog_attend_paged, args, cache.device)
         return out, lse
 
-    out, lse = _on(stream, run, (q, pages, lengths, chosen, lr, slopes, *cache._inputs()))
+    out, lse = cache._run(run, stream, q, pages, lengths, chosen, lr, slopes)
     return (out, lse) if return_lse else out

@@ -94,6 +94,21 @@ def test_workspaces():
     assert L.frog_attend_paged(C.byref(a), None) == -1
 
 
+@pytest.mark.parametrize("heads", [2, 8, 34, 66, 512])
+@pytest.mark.parametrize("kind", [0, 1, 2])
+def test_workspaces_of_every_cut(heads, kind):
+    # no rows at all, one row, many: parts times (output, maximum and sum) of every query row, or none
+    for batch in (1, 300, 5000):
+        for pages in (0, 1, 5, 64, 65, 1000, 2 ** 20):
+            for chosen in (None, 4096):
+                for num in (0, 1, 100, 2 ** 20):
+                    a = args(G.PagedArgs, heads=heads, type=kind, batch=batch, pages_per_request=pages, chosen=chosen, num_chosen=num)
+                    n = F.lib().frog_attend_paged_workspace(C.byref(a))
+                    assert n >= 0 and n % (batch * heads * (64 + 2) * 4) == 0
+                    rows = (num if chosen else pages) * 16
+                    assert n == 0 if rows <= 128 else n <= batch * heads * 66 * 4 * max(1, rows // 128 + 1)
+
+
 def test_the_binding_refuses_what_is_on_no_gpu():
     k = torch.zeros(2, 1, 16, 32, dtype=torch.int8)
     e = torch.zeros(2, 1, 16, dtype=torch.uint8)
