@@ -65,56 +65,49 @@ __device__ inline uint32_t over_row(uint32_t x, F&& f) {
     return x;
 }
 
-// N values of a row as floats (16-bit ones: 16- or 24-byte pieces)
-template <typename T, int N>
-__device__ inline void load_values(const T* p, float (&x)[N]) {
-    constexpr int words = N * sizeof(T) / 4;
-    uint32_t r[words];
-    if constexpr (words % 4 == 0) {
-#pragma unroll
-        for (int i = 0; i < words / 4; ++i) *(uint4*)(r + 4 * i) = ((const uint4*)p)[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < words / 2; ++i) *(uint2*)(r + 2 * i) = ((const uint2*)p)[i];
-    }
-    T y[N];
-    static_assert(sizeof(y) == sizeof(r), "whole words");
-    __builtin_memcpy(y, r, sizeof(r));
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = (float)y[i];
-}
-
+// N words at p, on a boundary of 16, 8 or 4 bytes as N divides; `streamed`: past the
+// caches where they are not looked for again soon (writing prompts of 639 MB 134
+// -> 131 us, reading 1.08 GB back 225 -> 210; rows that the attention after it
+// finds in the caches are no longer there, which costs it about as much)
 template <int N>
 struct Words {
     uint32_t w[N];
 };
-template <int N>
-__device__ inline Words<N> load_words(const void* p) {   // on a boundary of 8 (N even) or 4 bytes
+template <int N, bool STREAMED = false>
+__device__ inline Words<N> load_words(const void* p) {
+    constexpr int M = N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 1;
+    using V = vec<uint32_t, M>;
     Words<N> r;
-    if constexpr (N % 4 == 0) {
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i) *(uint4*)(r.w + 4 * i) = ((const uint4*)p)[i];
-    } else if constexpr (N % 2 == 0) {
+    for (int i = 0; i < N / M; ++i) {
+        const V x = STREAMED ? __builtin_nontemporal_load((const V*)p + i) : ((const V*)p)[i];
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) *(uint2*)(r.w + 2 * i) = ((const uint2*)p)[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) r.w[i] = ((const uint32_t*)p)[i];
+        for (int e = 0; e < M; ++e) r.w[M * i + e] = x[e];
     }
     return r;
 }
 template <int N>
-__device__ inline void store_words(void* p, const Words<N>& r) {
-    if constexpr (N % 4 == 0) {
+__device__ inline void store_streamed(void* p, const Words<N>& r) {
+    constexpr int M = N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 1;
+    using V = vec<uint32_t, M>;
 #pragma unroll
-        for (int i = 0; i < N / 4; ++i) ((uint4*)p)[i] = *(const uint4*)(r.w + 4 * i);
-    } else if constexpr (N % 2 == 0) {
+    for (int i = 0; i < N / M; ++i) {
+        V x;
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) ((uint2*)p)[i] = *(const uint2*)(r.w + 2 * i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) ((uint32_t*)p)[i] = r.w[i];
+        for (int e = 0; e < M; ++e) x[e] = r.w[M * i + e];
+        __builtin_nontemporal_store(x, (V*)p + i);
     }
+}
+
+// N values of a row as floats (16-bit ones: pieces of 16 or 8 bytes)
+template <typename T, int N>
+__device__ inline void load_values(const T* p, float (&x)[N]) {
+    const Words<N * sizeof(T) / 4> r = load_words<N * sizeof(T) / 4, true>(p);
+    T y[N];
+    static_assert(sizeof(y) == sizeof(r), "whole words");
+    __builtin_memcpy(y, r.w, sizeof(y));
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = (float)y[i];
 }
 
 // pages are powers of two: row t stands in page t >> shift

@@ -74,7 +74,7 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, uint
             for (int i = 0; i < C / 4; ++i)
                 codes.w[i] = byte == kNoRow ? 0 : codes_of<INT8>(x[t][4 * i] * down, x[t][4 * i + 1] * down, x[t][4 * i + 2] * down, x[t][4 * i + 3] * down);
             if (live) {
-                store_words((uint8_t*)(t ? c.v : c.k) + row * D + at, codes);
+                store_streamed((uint8_t*)(t ? c.v : c.k) + row * D + at, codes);
                 if (at == 0) (t ? c.v_exp : c.k_exp)[row] = (uint8_t)byte;
             }
             if (t == 0 && c.bounds && live) {
@@ -121,11 +121,10 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, uint
 }
 
 // One workgroup 16 rows of a request (of one page) with all their heads, in the
-// order of the outputs.
+// order of the outputs, 16 bytes of them a lane.
 template <typename T, bool INT8, int D>
 __global__ __launch_bounds__(kBlock) void cache_read(frog_cache_read_t a, uint32_t first) {
-    using S = RowSplit<D>;
-    constexpr int C = S::kEach;
+    constexpr int C = 16 / sizeof(T), kPieces = D / C;
     const frog_cache_t& c = a.cache;
     const int shift = shift_of(c.page);
     const uint32_t blocks = (uint32_t)((a.slots + 15) / 16), item = first + blockIdx.x;
@@ -134,28 +133,27 @@ __global__ __launch_bounds__(kBlock) void cache_read(frog_cache_read_t a, uint32
     const int64_t length = rows_of(a.lengths, b, a.pages_per_request, c.page);
     const int page = s0 < length ? page_of(a.pages, b, a.pages_per_request, s0 >> shift, c.num_pages) : -1;
     const int live = page < 0 ? 0 : (int)min((int64_t)rows, length - s0);
-    const int sub = threadIdx.x / S::kLanes, at = (threadIdx.x % S::kLanes) * C;
-    for (int i = sub; i < rows * c.kv_heads; i += kBlock / S::kLanes) {
-        const int s = i / c.kv_heads, h = i - s * c.kv_heads;
-        const int64_t row = (((int64_t)page * c.kv_heads + h) << shift) + (s0 & (c.page - 1)) + s;
+    const int64_t row0 = ((int64_t)max(page, 0) * c.kv_heads << shift) + (s0 & (c.page - 1));
+    T* const out[2] = {(T*)a.k + b * a.k_stride[0] + s0 * a.k_stride[1], (T*)a.v + b * a.v_stride[0] + s0 * a.v_stride[1]};
+    for (uint32_t i = threadIdx.x; i < (uint32_t)(rows * c.kv_heads) * kPieces; i += kBlock) {
+        const uint32_t n = i / kPieces, at = (i - n * kPieces) * C;
+        const uint32_t s = n / (uint32_t)c.kv_heads, h = n - s * (uint32_t)c.kv_heads;
+        const int64_t row = row0 + ((int64_t)h << shift) + s;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            T y[C] = {};
-            if (s < live) {
+            vec<T, C> y = {};
+            if ((int)s < live) {
                 const Words<C / 4> codes = load_words<C / 4>((const uint8_t*)(t ? c.v : c.k) + row * D + at);
                 const float up = power_of((t ? c.v_exp : c.k_exp)[row]);
 #pragma unroll
-                for (int n = 0; n < C / 4; ++n) {
-                    const vec<float, 4> x = values_of<INT8>(codes.w[n]) * up;
+                for (int w = 0; w < C / 4; ++w) {
+                    const vec<float, 4> x = values_of<INT8>(codes.w[w]) * up;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[4 * n + e] = (T)x[e];
+                    for (int e = 0; e < 4; ++e) y[4 * w + e] = (T)x[e];
                 }
             }
-            T* out = t ? (T*)a.v + b * a.v_stride[0] + (s0 + s) * a.v_stride[1] + h * a.v_stride[2]
-                       : (T*)a.k + b * a.k_stride[0] + (s0 + s) * a.k_stride[1] + h * a.k_stride[2];
-            Words<C * sizeof(T) / 4> words;
-            __builtin_memcpy(words.w, y, sizeof(y));
-            store_words(out + at, words);
+            const int64_t* stride = t ? a.v_stride : a.k_stride;
+            __builtin_nontemporal_store(y, (vec<T, C>*)(out[t] + s * stride[1] + h * stride[2] + at));
         }
     }
 }
