@@ -87,6 +87,18 @@ __device__ inline Words<N> load_words(const void* p) {
     return r;
 }
 template <int N>
+__device__ inline void store_words(void* p, const Words<N>& r) {
+    constexpr int M = N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 1;
+    using V = vec<uint32_t, M>;
+#pragma unroll
+    for (int i = 0; i < N / M; ++i) {
+        V x;
+#pragma unroll
+        for (int e = 0; e < M; ++e) x[e] = r.w[M * i + e];
+        ((V*)p)[i] = x;
+    }
+}
+template <int N>
 __device__ inline void store_streamed(void* p, const Words<N>& r) {
     constexpr int M = N % 4 == 0 ? 4 : N % 2 == 0 ? 2 : 1;
     using V = vec<uint32_t, M>;

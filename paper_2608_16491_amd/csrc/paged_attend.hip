@@ -6,11 +6,16 @@
 namespace frog {
 namespace {
 
-// A workgroup a row of queries: maximum and sums of its parts, then their
-// outputs, D / 64 channels a lane.
-__global__ __launch_bounds__(256) void paged_join(frog_attend_paged_t a, PagedPlan plan, PagedParts parts, int64_t first) {
-    const int lane = threadIdx.x & 63, d = a.cache.d;
-    const int64_t row = (first + blockIdx.x) * 4 + (threadIdx.x >> 6);
+constexpr int kJoin1 = 8, kJoin4 = 32;     // most parts that one wavefront, or four, join
+
+// A query row's maximum and sum over its parts, then their outputs, D / 64 channels
+// a lane, eight parts in flight: by one wavefront, or where there are many parts
+// by the 16 of a workgroup, whose shares meet in LDS.
+template <int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void paged_join(frog_attend_paged_t a, PagedPlan plan, PagedParts parts, int64_t first) {
+    __shared__ float shares[WAVES][128];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, d = a.cache.d;
+    const int64_t row = WAVES == 1 ? (first + blockIdx.x) * 4 + w : first + blockIdx.x;
     if (row >= parts.rows) return;
     const int64_t b = (uint32_t)row / (uint32_t)a.heads;      // (rows are fewer than 2^31)
     const int head = (int)((uint32_t)row % (uint32_t)a.heads);
@@ -20,30 +25,40 @@ __global__ __launch_bounds__(256) void paged_join(frog_attend_paged_t a, PagedPl
     for (int s = lane; s < live; s += 64) all = fmaxf(all, parts.ml[s * parts.rows + row].x);
     for (int o = 32; o; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
     float total = 0.f, x[2] = {0.f, 0.f};
-    for (int s0 = 0; s0 < live; s0 += 64) {
-        float2 ml = make_float2(kNoneSeen, 0.f);
-        if (s0 + lane < live) ml = parts.ml[(s0 + lane) * parts.rows + row];
-        const float share = exp2_fast(ml.x - all);
-        total += ml.y * share;
-        // (parts past the last one repeat it, with a share of 0)
-        const int n = min(64, live - s0);
-        for (int s = 0; s < n; s += 8) {
-            float y[8][2];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float* from = parts.o + ((s0 + min(s + i, n - 1)) * parts.rows + row) * d;
-                y[i][0] = from[min(lane, d - 1)];
-                y[i][1] = d > 64 ? from[min(lane + 64, d - 1)] : 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float f = s + i < n ? __shfl(share, s + i) : 0.f;
-                x[0] += f * y[i][0];
-                x[1] += f * y[i][1];
-            }
-        }
+    for (int s = lane; s < live; s += 64) {
+        const float2 ml = parts.ml[s * parts.rows + row];
+        total += ml.y * exp2_fast(ml.x - all);
     }
     for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+    // (parts past the wavefront's last one repeat it, with a share of 0)
+    const int each = (live + WAVES - 1) / WAVES, from = WAVES == 1 ? 0 : w * each, to = WAVES == 1 ? live : min(live, from + each);
+    for (int s = from; s < to; s += 8) {
+        float y[8][2], share[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t at = (int64_t)min(s + i, to - 1) * parts.rows + row;
+            share[i] = s + i < to ? exp2_fast(parts.ml[at].x - all) : 0.f;
+            y[i][0] = parts.o[at * d + min(lane, d - 1)];
+            y[i][1] = d > 64 ? parts.o[at * d + min(lane + 64, d - 1)] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[0] += share[i] * y[i][0];
+            x[1] += share[i] * y[i][1];
+        }
+    }
+    if constexpr (WAVES > 1) {
+        shares[w][lane] = x[0];
+        shares[w][lane + 64] = x[1];
+        __syncthreads();
+        if (w) return;
+        x[0] = x[1] = 0.f;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            x[0] += shares[i][lane];
+            x[1] += shares[i][lane + 64];
+        }
+    }
     const float scale = total == 0.f ? 0.f : 1.f / total;
     const int64_t at = b * a.out_stride[0] + head * a.out_stride[1] + lane;
 #pragma unroll
@@ -74,17 +89,27 @@ PagedPlan plan_of(const frog_attend_paged_t& a) {
         p.chunk = 64;
         return p;
     }
-    // Lists of pages are equally long: workgroups for every CU do (48 requests of 64
-    // pages of 64 rows, 8 kv heads: 384 workgroups 77 us, in six parts 82 + 5).  Of
-    // requests of all lengths many workgroups end early, and the longest one of
-    // few decides (24 requests to 5,000 rows, 12 kv heads: parts of 512 to 1,024
-    // rows 22 us, of 2,048 27, of 4,096 38).
-    const int64_t want = a.chosen ? 384 : 1536;
+    // Lists of pages are equally long: a workgroup a list, where that fills the CUs
+    // (48 requests of 64 pages of 64 rows, 8 kv heads: 77 us, in two parts 76 + 5, in
+    // six 82 + 5).
     if (a.chosen && pairs >= 256 && p.tiles <= kMostTiles) {
         p.chunk = kMostTiles;
         return p;
     }
-    const int64_t each = std::min<int64_t>(kMostTiles, std::max<int64_t>(8, (pairs * p.tiles + want - 1) / want));
+    // Else a workgroup begins (about 4 us) for 16 to 64 tiles (1 us for 8), more of
+    // them where there is more to do, since the longest request decides and the
+    // parts are read again; of very large calls for 128.  Tiles a part, us of a
+    // call (bf16, e4m3, requests of all lengths up to the one named):
+    //   rows, requests, heads, d       16     24     32     48     64     96    128
+    //   60,000   1  32 / 8   128     36.4   32.8   31.0   31.5   28.5   30.0   30.0
+    //   10,000   1  32 / 8   128     14.8   15.3   15.3   16.6   18.2   21.7   25.3
+    //    8,000  16  48 / 2   128     26.9   20.9   22.1   25.4   25.1   28.9   33.2
+    //    4,000  48  16 / 2   128     23.7   21.7   22.3   21.0   23.4   26.1   26.7
+    //    8,000  32   8 / 8    32     26.5   23.1   22.5   21.4   23.9   24.0   25.0
+    //    3,000 128  32 / 8   128    107.5  101.5   96.7  110.0   97.6  111.2  121.9
+    //   40,000  32  32 / 8   128    306.3  289.9  279.7  268.6  263.0  252.6  254.8
+    const int64_t work = pairs * p.tiles;
+    const int64_t each = work > 400000 ? 128 : std::min<int64_t>(64, std::max<int64_t>(16, work / 500));
     p.parts = (int)((p.tiles + each - 1) / each);
     p.chunk = (int)((p.tiles + p.parts - 1) / p.parts + 7) / 8 * 8;
     p.parts = (int)((p.tiles + p.chunk - 1) / p.chunk);
@@ -112,8 +137,15 @@ int launch_attend_paged(const frog_attend_paged_t& args, void* ws, hipStream_t s
         parts.o = (float*)(parts.ml + p.parts * parts.rows);
     }
     hipError_t e = a.type == FROG_STORAGE_F32 ? launch_paged_f32(a, p, parts, stream) : a.type == FROG_STORAGE_F16 ? launch_paged_f16(a, p, parts, stream) : launch_paged_bf16(a, p, parts, stream);
-    if (e == hipSuccess && p.parts > 1)
-        e = in_launches((parts.rows + 3) / 4, 256, [&](int64_t first, dim3 grid) { paged_join<<<grid, 256, 0, stream>>>(a, p, parts, first); });
+    if (e == hipSuccess && p.parts > 1) {
+        // eight parts of a row are in flight at once in a wavefront
+        if (p.parts <= kJoin1)
+            e = in_launches((parts.rows + 3) / 4, 256, [&](int64_t first, dim3 grid) { paged_join<1><<<grid, 256, 0, stream>>>(a, p, parts, first); });
+        else if (p.parts <= kJoin4)
+            e = in_launches(parts.rows, 256, [&](int64_t first, dim3 grid) { paged_join<4><<<grid, 256, 0, stream>>>(a, p, parts, first); });
+        else
+            e = in_launches(parts.rows, 1024, [&](int64_t first, dim3 grid) { paged_join<16><<<grid, 1024, 0, stream>>>(a, p, parts, first); });
+    }
     return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "attention over pages launch: %s", hipGetErrorString(e));
 }
 

@@ -13,23 +13,23 @@ __device__ inline int64_t start_of(const frog_cache_write_t& a, int64_t b) {
     return a.starts ? max((int64_t)0, min((int64_t)a.starts[b], a.tokens)) : b * (int64_t)((uint32_t)a.tokens / (uint32_t)a.batch);      // (both below 2^31)
 }
 
-// One workgroup a (page with new rows, kv head): the page's bounds are then its
-// own, without atomics, and the same every run.  Request b's pages are work
-// items from start / page + 2 b on, at least as many as its rows can meet (n
-// rows meet at most n / page + 2 pages), so the host needs no lengths; the
-// request of an item is found by a search over 64 requests at a time.  A row
-// takes 4, 8 or 16 lanes, which find its largest magnitude among themselves.
-template <typename T, bool INT8, int D>
-__global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, uint32_t first) {
+// WAVES wavefronts of a workgroup take a (page with new rows, kv head): the page's
+// bounds are then their own, without atomics, and the same every run.  Request b's
+// pages are work items from start / page + 2 b on, at least as many as its rows can
+// meet (n rows meet at most n / page + 2 pages), so the host needs no lengths; the
+// request of an item is found by a search over 64 requests at a time.  A row takes
+// 4, 8 or 16 lanes, which find its largest magnitude among themselves.
+template <typename T, bool INT8, int D, int WAVES>
+__global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, int64_t units, uint32_t first) {
     using S = RowSplit<D>;
     constexpr int C = S::kEach;
-    __shared__ float least[kWaves][D], most[kWaves][D];
-    __shared__ int broken;
     const frog_cache_t& c = a.cache;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = w % WAVES;
     const int shift = shift_of(c.page);
-    const uint32_t item = (first + blockIdx.x) / (uint32_t)c.kv_heads;
-    const int h = (int)((first + blockIdx.x) % (uint32_t)c.kv_heads);
+    const uint32_t unit = (first + blockIdx.x) * (kWaves / WAVES) + w / WAVES;
+    if (unit >= units) return;
+    const uint32_t item = unit / (uint32_t)c.kv_heads;
+    const int h = (int)(unit % (uint32_t)c.kv_heads);
     int64_t b = 0;
     for (int64_t len = a.batch; len > 1;) {
         const int64_t step = (len + 63) / 64, i = lane * step;
@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, uint
 #pragma unroll
     for (int i = 0; i < C; ++i) lo[i] = INFINITY, hi[i] = -INFINITY;
     int bad = 0;
-    for (int64_t r = r0 + w * S::kRows + sub; r - sub < r1; r += kWaves * S::kRows) {
+    for (int64_t r = r0 + mine * S::kRows + sub; r - sub < r1; r += WAVES * S::kRows) {
         const bool live = r < r1;
         const int64_t token = start + (live ? r : r0) - before;
         const T* src[2] = {(const T*)a.k + token * a.k_stride[0] + h * a.k_stride[1] + at, (const T*)a.v + token * a.v_stride[0] + h * a.v_stride[1] + at};
@@ -94,30 +94,52 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, uint
     }
     if (!c.bounds) return;
     // over the wavefront's rows (lanes of the same channels), then the wavefronts
-    if (threadIdx.x == 0) broken = 0;
+    bool broken = __any(bad);
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
+    for (int i = 0; i < C; ++i)
 #pragma unroll
         for (int o = S::kLanes; o < 64; o <<= 1) {
             lo[i] = fminf(lo[i], __shfl_xor(lo[i], o));
             hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], o));
         }
-        if (sub == 0) least[w][at + i] = lo[i], most[w][at + i] = hi[i];
-    }
-    __syncthreads();
-    if (__any(bad) && lane == 0) broken = 1;
-    __syncthreads();
-    if (threadIdx.x >= 2 * D) return;
-    const bool high = threadIdx.x >= D;
-    const int i = threadIdx.x - (high ? D : 0);
-    bf16_t* p = (bf16_t*)c.bounds + (block * 2 + (high ? 1 : 0)) * D + i;
-    float x = high ? most[0][i] : least[0][i];
+    if constexpr (WAVES > 1) {
+        __shared__ float least[WAVES][D], most[WAVES][D];
+        __shared__ int any[WAVES];
+        if (sub == 0) {
 #pragma unroll
-    for (int n = 1; n < kWaves; ++n) x = high ? fmaxf(x, most[n][i]) : fminf(x, least[n][i]);
+            for (int i = 0; i < C; ++i) least[mine][at + i] = lo[i], most[mine][at + i] = hi[i];
+            if (lane == 0) any[mine] = broken;
+        }
+        __syncthreads();
+        if (mine) return;
+#pragma unroll
+        for (int n = 1; n < WAVES; ++n) {
+            broken |= any[n] != 0;
+#pragma unroll
+            for (int i = 0; i < C; ++i) lo[i] = fminf(lo[i], least[n][at + i]), hi[i] = fmaxf(hi[i], most[n][at + i]);
+        }
+    }
+    if (sub) return;
     // (a page begun at its row 0 forgets what it held)
-    const float old = r0 & (c.page - 1) ? (float)*p : x;
-    x = high ? fmaxf(x, old) : fminf(x, old);
-    *p = (bf16_t)(broken || old != old ? NAN : x);
+    bf16_t* p = (bf16_t*)c.bounds + block * 2 * D + at;
+    const bool begun = (r0 & (c.page - 1)) == 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const Words<C / 2> old = load_words<C / 2>(p + t * D);
+        Words<C / 2> now;
+#pragma unroll
+        for (int i = 0; i < C / 2; ++i) {
+            float y[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float x = t ? hi[2 * i + e] : lo[2 * i + e];
+                const float was = begun ? x : __uint_as_float(e ? old.w[i] & 0xFFFF0000u : old.w[i] << 16);
+                y[e] = broken || was != was ? NAN : t ? fmaxf(x, was) : fminf(x, was);
+            }
+            now.w[i] = __builtin_bit_cast(uint32_t, vec<bf16_t, 2>{(bf16_t)y[0], (bf16_t)y[1]});
+        }
+        store_words(p + t * D, now);
+    }
 }
 
 // One workgroup 16 rows of a request (of one page) with all their heads, in the
@@ -181,12 +203,19 @@ void of_kind(int type, int storage, int d, F&& f) {
 int launch_cache_write(const frog_cache_write_t& a, hipStream_t stream) {
     if (a.batch == 0 || a.tokens == 0 || a.cache.num_pages == 0 || a.pages_per_request == 0) return FROG_OK;
     const int64_t items = a.tokens / a.cache.page + 2 * a.batch;
-    if (items > 0xffffffffll / a.cache.kv_heads) return fail(FROG_EUNSUPPORTED, "more than 2^32 workgroups");
+    if (items > 0xfffffffbll / a.cache.kv_heads) return fail(FROG_EUNSUPPORTED, "more than 2^32 pages of a head");
+    const int64_t units = items * a.cache.kv_heads;
     hipError_t e = hipSuccess;
     of_kind(a.type, a.cache.storage, a.cache.d, [&](auto t, auto i8, auto d) {
-        e = in_launches(items * a.cache.kv_heads, kBlock, [&](int64_t first, dim3 grid) {
-            cache_write<decltype(t), i8.value, d.value><<<grid, kBlock, 0, stream>>>(a, (uint32_t)first);
-        });
+        auto run = [&](auto kernel, int waves) {
+            const int each = kWaves / waves;
+            e = in_launches((units + each - 1) / each, kBlock, [&](int64_t first, dim3 grid) { kernel<<<grid, kBlock, 0, stream>>>(a, units, (uint32_t)first); });
+        };
+        // a page whose rows a wavefront has in four rounds is one's alone (8 prompts to
+        // 8,000 rows, 8 heads, pages of 16, d = 64: 29 us, by four 55; d = 128, pages of 32, twice
+        // the rounds: 53 us, by four 47)
+        if (a.cache.page <= 4 * RowSplit<d.value>::kRows) run(cache_write<decltype(t), i8.value, d.value, 1>, 1);
+        else run(cache_write<decltype(t), i8.value, d.value, kWaves>, kWaves);
     });
     return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "cache write launch: %s", hipGetErrorString(e));
 }
