@@ -1,7 +1,8 @@
 """The attention operators together, as a serving program and a training step
 use them: prompts read with their key weights recorded, tokens decoded against
 caches that are shortened to their heaviest rows when they are full, a batch
-decoded over one common prefix, and the gradients of packed documents.
+decoded over one common prefix, the gradients of packed documents, and a batch
+decoded over the chosen pages of a cache in 8 bits.
 
     python examples/attention_cache.py
 """
@@ -82,9 +83,30 @@ def train(sizes=(70, 130, 56), seed=2):
     return out.detach(), q.grad, k.grad, v.grad
 
 
+def paged(prompts=(150, 900, 40), steps=20, keep=8, page=16, storage="int8", seed=3):
+    """Prompts of several lengths written into a cache of 8-bit pages, then `steps` tokens each, which look at `keep` pages:
+    the first, the newest, and those with the largest bound on their scores.  Returns the last step's arguments and output."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    batch, width = len(prompts), -(-(max(prompts) + steps) // page)
+    cache = F.PagedCache.empty(batch * width, KV_HEADS, D, page=page, storage=storage)
+    pages = torch.arange(batch * width, device="cuda", dtype=torch.int32).view(batch, width)
+    starts = torch.tensor([0, *prompts], device="cuda").cumsum(0).to(torch.int32)
+    lengths = torch.tensor(prompts, device="cuda", dtype=torch.int32)
+    F.cache_write(cache, rows(g, sum(prompts), KV_HEADS, D), rows(g, sum(prompts), KV_HEADS, D), pages, lengths, starts=starts)
+    for _ in range(steps):
+        lengths += 1
+        F.cache_write(cache, rows(g, batch, KV_HEADS, D), rows(g, batch, KV_HEADS, D), pages, lengths)
+        q = rows(g, batch, HEADS, D)
+        chosen = F.select_pages(q, cache, pages, lengths, keep, first=1)
+        out = F.attend_paged(q, cache, pages, lengths, chosen=chosen)
+    return q, cache, pages, lengths, chosen, out
+
+
 if __name__ == "__main__":
     *_, args, out, weights = decode()
     print("decoded:", tuple(out.shape), "rows seen:", int(args["lr"][0, 0, 1]) + 1, "weight recorded:", float(weights.sum()))
     out, lse = shared()
     print("shared prefix:", tuple(out.shape), "log sums:", [round(x, 2) for x in lse[:, 0].tolist()])
     print("trained:", [tuple(t.shape) for t in train()])
+    *_, lengths, chosen, out = paged()
+    print("paged:", tuple(out.shape), "rows:", lengths.tolist(), "pages of the first:", chosen[0, 0].tolist())

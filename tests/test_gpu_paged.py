@@ -8,7 +8,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 import paper_2608_16491_amd as F  # noqa: E402
-from tests.attention_ref import near  # noqa: E402
+from tests.attention_ref import Attention, near  # noqa: E402
 from tests.paged_ref import Cache  # noqa: E402
 
 TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
@@ -469,6 +469,54 @@ def test_a_cache_beyond_32_bit_offsets():
     assert all(torch.equal(x, y) for x, y in zip(F.cache_read(cache, pages.cuda(), n.cuda()), F.cache_read(small, own.cuda(), n.cuda())))
 
 
+@pytest.mark.parametrize("b,most,h,kv,d,page", [(1, 20_000, 4, 1, 32, 16), (2, 9000, 6, 2, 64, 128), (1, 6000, 20, 1, 32, 64), (20, 1500, 3, 3, 32, 16)])
+def test_every_cut(b, most, h, kv, d, page):
+    """Parts joined by one wavefront, by four, by sixteen; requests far shorter than the longest."""
+    say("cut", b, most, h, kv, d, page)
+    lengths = [most] + [(i * 977) % most for i in range(1, b)]
+    cache, _, _, pages, n, _ = filled("fp16", "int8", b, most, kv, d, page, lengths=lengths, bounds=False)
+    q = torch.randn((b, h, d), generator=torch.Generator().manual_seed(4)).half()
+    check(q, cache, pages, n)
+    lr = torch.stack([n // 3, n - 1 - n // 5], -1).to(torch.int32)
+    check(q, cache, pages, n, lr=lr, cap=20.0)
+    # the same rows by a list of all pages, in another order
+    chosen = torch.randperm(pages.shape[1], generator=torch.Generator().manual_seed(5)).to(torch.int32).expand(b, kv, -1).contiguous()
+    check(q, cache, pages, n, chosen=chosen)
+
+
+def test_large_calls():
+    # above 400,000 tiles (longer parts), and lists of pages for more than 256 (request, kv head) pairs (one workgroup
+    # each): some requests against 64 bits, over the rows read back, which are exact in 32
+    g = torch.Generator(device="cuda").manual_seed(3)
+    b, kv, d, page, width = 72, 4, 64, 64, 400
+    cache = F.PagedCache.empty(b * width // 8, kv, d, page=page, storage="int8", bounds=False)
+    for x in (cache.k, cache.v):
+        x.random_(-127, 128, generator=g)
+    for x in (cache.k_exp, cache.v_exp):
+        x.random_(118, 124, generator=g)
+    pages = torch.randint(0, cache.shape[0], (b, width), generator=g, device="cuda", dtype=torch.int32)
+    n = torch.randint(1, width * page + 1, (b,), generator=g, device="cuda", dtype=torch.int32)
+    q = torch.randn((b, 3 * kv, d), generator=g, device="cuda")
+    chosen = torch.randint(0, width, (b, kv, 60), generator=g, device="cuda", dtype=torch.int32)
+    whole = F.attend_paged(q, cache, pages, n)
+    some = F.attend_paged(q, cache, pages, n, chosen=chosen)
+    for i in (0, 17, 71):
+        k, v = F.cache_read(cache, pages[i:i + 1], n[i:i + 1], dtype=torch.float32)
+        m = int(n[i])
+        ref = Attention(q[i].view(1, 1, 3 * kv, d), k[:, :m], v[:, :m])
+        # (queries of 32 bits enter in three factors: sums of three times as many products)
+        near(whole[i].view(ref.out.shape), ref.out, 3 * ref.out_err, f"request {i}")
+        for j in range(kv):
+            at = (chosen[i, j].long().unsqueeze(1) * page + torch.arange(page, device="cuda")).flatten()
+            at = at[at < m]
+            got = some[i, 3 * j:3 * j + 3]
+            if len(at) == 0:
+                assert not got.any()
+                continue
+            ref = Attention(q[i, 3 * j:3 * j + 3].view(1, 1, 3, d), k[:, at, j:j + 1], v[:, at, j:j + 1])
+            near(got.view(ref.out.shape), ref.out, 3 * ref.out_err, f"request {i}, kv head {j}")
+
+
 # ------------------------------------------------------------------ together
 
 def test_a_conversation():
@@ -495,3 +543,18 @@ def test_a_conversation():
         check(q.cpu(), cache, pages.cpu(), n.cpu(), chosen=some.cpu())
         n += 1
         F.cache_write(cache, *(torch.randn((b, kv, d), generator=g, device="cuda").bfloat16() for _ in range(2)), pages, n)
+
+
+def test_the_example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "attention_cache.py")
+    spec = importlib.util.spec_from_file_location("attention_cache", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    q, cache, pages, n, chosen, out = example.paged()
+    assert n.tolist() == [170, 920, 60]
+    ref = Cache(cache)
+    assert torch.equal(chosen.cpu(), ref.select(q, pages.cpu(), n.cpu(), 8, 1, 1))
+    want, err, _, _ = ref.attend(q.cpu(), pages.cpu(), n.cpu(), chosen.cpu())
+    near(out.cpu(), want, err, "out")

@@ -109,6 +109,25 @@ def test_workspaces_of_every_cut(heads, kind):
                     assert n == 0 if rows <= 128 else n <= batch * heads * 66 * 4 * max(1, rows // 128 + 1)
 
 
+def test_sizes_above_a_launch_are_refused():
+    # before anything is enqueued, by the workspace query too where there is one
+    L = F.lib()
+    assert L.frog_cache_read(C.byref(args(G.ReadArgs, batch=2 ** 20, slots=2 ** 17)), None) == -7 and b"workgroups" in L.frog_last_error()
+    assert L.frog_cache_write(C.byref(args(G.WriteArgs, **{"cache.kv_heads": 65535, "batch": 2 ** 16, "tokens": 2 ** 16, "cache.num_pages": 1})), None) == -7
+    big = args(G.PagedArgs, batch=2 ** 20, pages_per_request=2 ** 22, chosen=None)
+    assert L.frog_attend_paged_workspace(C.byref(big)) == -7 and L.frog_attend_paged(C.byref(big), None) == -7
+    big = args(G.SelectArgs, batch=2 ** 22, pages_per_request=2 ** 24)
+    assert L.frog_select_pages_workspace(C.byref(big)) == -7 and L.frog_select_pages(C.byref(big), None) == -7
+
+
+def test_a_cache_keeps_its_tensors():
+    # (their sizes are what the kernels go by)
+    for name in ("k", "v", "k_exp", "v_exp", "bounds", "shape", "device"):
+        assert isinstance(getattr(F.PagedCache, name), property) and getattr(F.PagedCache, name).fset is None
+    with pytest.raises(AttributeError):
+        F.no_such_name
+
+
 def test_the_binding_refuses_what_is_on_no_gpu():
     k = torch.zeros(2, 1, 16, 32, dtype=torch.int8)
     e = torch.zeros(2, 1, 16, dtype=torch.uint8)
