@@ -54,6 +54,7 @@ def _packer(cls):
 _pack_attend, _pack_shared, _pack_evict = (_packer(c) for c in (AttendArgs, SharedArgs, EvictArgs))
 # the raw handle of the current stream, without the stream object built around it where torch offers that
 _current = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _need(ok, text):
@@ -87,7 +88,7 @@ def _values(names, tensors, dims):
 def _launch(fn, args, device):
     """Enqueue on the device's current stream."""
     index = device.index
-    if torch.cuda.current_device() == index:
+    if _device() == index:
         rc = fn(args, _current(index))
     else:
         with torch.cuda.device(index):

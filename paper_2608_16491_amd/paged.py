@@ -103,14 +103,17 @@ def _table(cache, pages, lengths):
     if pages.dim() != 2:
         raise ValueError("pages: [batch, pages_per_request] is wanted")
     b, width = pages.shape
-    return _plain("pages", pages, torch.int32, (b, width), cache.k), _plain("lengths", lengths, torch.int32, (b,), cache.k), b, width
+    like = cache._tensors[0]
+    return _plain("pages", pages, torch.int32, (b, width), like), _plain("lengths", lengths, torch.int32, (b,), like), b, width
 
 
 def _query(q, cache, batch):
-    kind = _values(("q",), (q,), (3,))
-    b, h, d = q.shape
-    if b != batch or d != cache.shape[3] or q.get_device() != cache.device.index:
-        raise ValueError(f"q {tuple(q.shape)} on {q.device}: [{batch}, heads, {cache.shape[3]}] on {cache.device} is wanted")
+    kind, d = _TYPES.get(q.dtype), cache._tail[3]
+    if kind is None or q.dim() != 3 or q.shape[0] != batch or q.shape[2] != d or q.get_device() != cache._tensors[0].get_device():
+        raise ValueError(f"q {tuple(q.shape)} of {q.dtype} on {q.device}: [{batch}, heads, {d}] of float32, float16 or bfloat16 on "
+                         f"{cache.device} is wanted")
+    if q.stride(2) != 1:
+        raise ValueError("q: the last axis must have stride 1")
     return kind
 
 
@@ -126,15 +129,15 @@ def cache_write(cache, k, v, pages, lengths, *, starts=None, stream=None):
     those of the new rows, else they widen the old ones."""
     _no_gradient(("k", "v"), (k, v))
     kind = _values(("k", "v"), (k, v), (3, 3))
-    t, (_, h, _, d) = k.shape[0], cache.shape
-    if k.shape != (t, h, d) or v.shape != k.shape or k.get_device() != cache.device.index:
+    t, (_, h, _, d) = k.shape[0], cache._tail[:4]
+    if k.shape != (t, h, d) or v.shape != k.shape or k.get_device() != cache._tensors[0].get_device():
         raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)} on {k.device}: twice [tokens, {h}, {d}] on {cache.device} are wanted")
     table, rows, b, width = _table(cache, pages, lengths)
     args = _pack_write(*cache._head(), k.data_ptr(), *k.stride()[:2], v.data_ptr(), *v.stride()[:2],
                        0 if starts is None else _plain("starts", starts, torch.int32, (b + 1,), k), table, rows, b, t, width, kind)
 
     def run():
-        _launch(lib().frog_cache_write, args, cache.device)
+        _launch(lib().frog_cache_write, args, k.device)
         return ()
 
     cache._run(run, stream, k, v, pages, lengths, starts)
@@ -147,17 +150,19 @@ def cache_read(cache, pages, lengths, slots=None, *, dtype=torch.bfloat16, strea
     request: k, v [batch, slots, kv_heads, d] of ``dtype``, 0 past a length; as
     :func:`attend` takes them."""
     kind = _TYPES.get(dtype)
-    _need(kind is not None, f"dtype {dtype}: float32, float16 or bfloat16")
+    if kind is None:
+        raise ValueError(f"dtype {dtype}: float32, float16 or bfloat16")
     table, rows, b, width = _table(cache, pages, lengths)
-    _, h, page, d = cache.shape
+    _, h, page, d, _ = cache._tail
     slots = width * page if slots is None else slots
     _need(slots >= 0, "slots is negative")
 
     def run():
-        k, v = (torch.empty((b, slots, h, d), dtype=dtype, device=cache.device) for _ in range(2))
+        k = torch.empty((b, slots, h, d), dtype=dtype, device=pages.device)
+        v = torch.empty_like(k)
         strides = (slots * h * d, h * d, d)
         _launch(lib().frog_cache_read, _pack_read(*cache._head(), k.data_ptr(), *strides, v.data_ptr(), *strides, table, rows, b, slots, width,
-                                                  kind), cache.device)
+                                                  kind), pages.device)
         return k, v
 
     return cache._run(run, stream, pages, lengths)
@@ -173,18 +178,20 @@ def select_pages(q, cache, pages, lengths, keep, *, first=0, recent=1, stream=No
     _no_gradient(("q",), (q,))
     table, rows, b, width = _table(cache, pages, lengths)
     kind = _query(q, cache, b)
+    kv = cache._tail[1]
     _need(cache.bounds is not None, "the cache keeps no bounds")
-    _need(0 <= first and 0 <= recent and first + recent <= keep, f"first {first}, recent {recent}, keep {keep}: first + recent <= keep is wanted")
+    if not (0 <= first and 0 <= recent and first + recent <= keep):
+        raise ValueError(f"first {first}, recent {recent}, keep {keep}: first + recent <= keep is wanted")
 
     def run():
-        chosen = torch.empty((b, cache.shape[1], keep), dtype=torch.int32, device=cache.device)
+        chosen = lengths.new_empty((b, kv, keep))
         head = (*cache._head(), q.data_ptr(), *q.stride()[:2], table, rows, chosen.data_ptr())
         tail = (b, width, keep, first, recent, q.shape[1], kind)
         args, ws, L = _pack_select(*head, 0, 0, *tail), None, lib()
-        if _own_workspace(b * cache.shape[1] * width > 2 ** 24):
-            ws, at = _workspace(L.frog_select_pages_workspace, args, cache.device)
+        if _own_workspace(b * kv * width > 2 ** 24):
+            ws, at = _workspace(L.frog_select_pages_workspace, args, q.device)
             args = _pack_select(*head, *at, *tail)
-        _launch(L.frog_select_pages, args, cache.device)
+        _launch(L.frog_select_pages, args, q.device)
         return (chosen,)
 
     return cache._run(run, stream, q, pages, lengths)[0]
@@ -202,7 +209,7 @@ def attend_paged(q, cache, pages, lengths, *, chosen=None, lr=None, scale=None, 
     _no_gradient(("q", "slopes"), (q, slopes))
     table, rows, b, width = _table(cache, pages, lengths)
     kind = _query(q, cache, b)
-    h, (_, kv, page, d) = q.shape[1], cache.shape
+    h, kv, page, d = q.shape[1], *cache._tail[1:4]
     num = 0
     if chosen is not None:
         num = chosen.shape[-1] if chosen.dim() else 0
@@ -210,8 +217,8 @@ def attend_paged(q, cache, pages, lengths, *, chosen=None, lr=None, scale=None, 
         chosen_at = _plain("chosen", chosen, torch.int32, (b, kv, num), q) or rows
 
     def run():
-        out = torch.empty((b, h, d), dtype=q.dtype, device=cache.device)
-        lse = torch.empty((b, h), dtype=torch.float32, device=cache.device) if return_lse else None
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        lse = torch.empty((b, h), dtype=torch.float32, device=q.device) if return_lse else None
         head = (*cache._head(), q.data_ptr(), *q.stride()[:2], table, rows, 0 if chosen is None else chosen_at,
                 0 if lr is None else _plain("lr", lr, torch.int32, (b, 2), q),
                 0 if slopes is None else _plain("slopes", slopes, torch.float32, (h,), q), out.data_ptr(), h * d, d,
@@ -219,9 +226,9 @@ def attend_paged(q, cache, pages, lengths, *, chosen=None, lr=None, scale=None, 
         tail = (b, width, num, h, kind, d ** -0.5 if scale is None else scale, cap)
         args, ws, L = _pack_paged(*head, 0, 0, *tail), None, lib()
         if _own_workspace(q.numel() * width * page > 2 ** 36):
-            ws, at = _workspace(L.frog_attend_paged_workspace, args, cache.device)
+            ws, at = _workspace(L.frog_attend_paged_workspace, args, q.device)
             args = _pack_paged(*head, *at, *tail)
-        _launch(L.frog_attend_paged, args, cache.device)
+        _launch(L.frog_attend_paged, args, q.device)
         return out, lse
 
     out, lse = cache._run(run, stream, q, pages, lengths, chosen, lr, slopes)
