@@ -119,6 +119,10 @@ template <int E, int F>
 constexpr bool kHalves = E < 8 && F == 2;
 template <int E, int F>
 constexpr int kChains = kHalves<E, F> ? 1 : F;
+// (the same for the queries' factors in the first product, whose halves are added at once)
+
+// x of column ^ 8
+__device__ inline float other_half(float x) { return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), 0x128, 0xF, 0xF, true)); }
 
 // the factors of all eight weights from the part's own
 template <int E, int F>
@@ -286,7 +290,7 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
         block_of[i] = block;
         place_of[i] = place;
     }
-    frag<bf16_t> qf[NQ][S][QF];
+    frag<bf16_t> qf[NQ][S][kChains<E, QF>];
     float slope[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
@@ -295,8 +299,15 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
 #pragma unroll
         for (int s = 0; s < S; ++s) {
             const frag<T> x = load_frag(p + Rows<D>::channel(s, quarter));
-            if constexpr (QF == 1) qf[n][s][0] = x;
-            else split_factors<QF>(__builtin_convertvector(x, vec<float, 8>), qf[n][s]);
+            if constexpr (QF == 1) {
+                qf[n][s][0] = x;
+            } else if constexpr (kHalves<E, QF>) {
+                frag<bf16_t> both[QF];
+                split_factors<QF>(__builtin_convertvector(x, vec<float, 8>), both);
+                qf[n][s][0] = col < 8 ? both[0] : both[1];
+            } else {
+                split_factors<QF>(__builtin_convertvector(x, vec<float, 8>), qf[n][s]);
+            }
         }
         slope[n] = !PLAIN && a.slopes ? a.slopes[head] * kLog2e : 0.f;
     }
@@ -336,12 +347,12 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
 #pragma unroll
                 for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                    for (int f = 0; f < QF; ++f) y[n] = mma(k, qf[n][s][f], y[n]);
+                    for (int f = 0; f < kChains<E, QF>; ++f) y[n] = mma(k, qf[n][s][f], y[n]);
             }
 #pragma unroll
             for (int n = 0; n < NQ; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[n][4 * t + e] = y[n][e];
+                for (int e = 0; e < 4; ++e) x[n][4 * t + e] = kHalves<E, QF> ? y[n][e] + other_half(y[n][e]) : y[n][e];
         }
         // of the own scores: the powers' bytes, and where their keys stand
         const uint32_t ke0 = r.ke[0], ke1 = r.ke[1];
@@ -485,7 +496,7 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
 #pragma unroll
             for (int m = 0; m < M; ++m)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[n][m][e] += __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(o[n][m][e]), 0x128, 0xF, 0xF, true));   // column ^ 8
+                for (int e = 0; e < 4; ++e) o[n][m][e] += other_half(o[n][m][e]);
         }
         if (16 * n + col < rows) {
 #pragma unroll

@@ -91,8 +91,9 @@ PagedPlan plan_of(const frog_attend_paged_t& a) {
     }
     // Lists of pages are equally long: a workgroup a list, where that fills the CUs
     // (48 requests of 64 pages of 64 rows, 8 kv heads: 77 us, in two parts 76 + 5, in
-    // six 82 + 5).
-    if (a.chosen && pairs >= 256 && p.tiles <= kMostTiles) {
+    // six 82 + 5).  So are short requests of many (64 to 2,000 rows, 8 kv heads: 30.4 us,
+    // in two parts 36.8).
+    if (p.tiles <= (a.chosen ? pairs >= 256 ? kMostTiles : 0 : pairs >= 512 ? 128 : 0)) {
         p.chunk = kMostTiles;
         return p;
     }
@@ -103,13 +104,14 @@ PagedPlan plan_of(const frog_attend_paged_t& a) {
     //   rows, requests, heads, d       16     24     32     48     64     96    128
     //   60,000   1  32 / 8   128     36.4   32.8   31.0   31.5   28.5   30.0   30.0
     //   10,000   1  32 / 8   128     14.8   15.3   15.3   16.6   18.2   21.7   25.3
+    //    4,000   4  32 / 8   128     14.0   14.7   14.3   16.0   17.7   21.2   24.7
     //    8,000  16  48 / 2   128     26.9   20.9   22.1   25.4   25.1   28.9   33.2
+    //   16,000   8  32 / 8   128     35.0   34.5   36.0   36.0   40.2   42.4   38.7
     //    4,000  48  16 / 2   128     23.7   21.7   22.3   21.0   23.4   26.1   26.7
-    //    8,000  32   8 / 8    32     26.5   23.1   22.5   21.4   23.9   24.0   25.0
-    //    3,000 128  32 / 8   128    107.5  101.5   96.7  110.0   97.6  111.2  121.9
+    //    8,000  32  32 / 8   128     70.5   65.0   64.4   63.4   66.2   67.3   75.1
     //   40,000  32  32 / 8   128    306.3  289.9  279.7  268.6  263.0  252.6  254.8
-    const int64_t work = pairs * p.tiles;
-    const int64_t each = work > 400000 ? 128 : std::min<int64_t>(64, std::max<int64_t>(16, work / 500));
+    const int64_t work = pairs * p.tiles, most = pairs <= 16 ? 64 : 48;
+    const int64_t each = work > 400000 ? 128 : std::min<int64_t>(most, std::max<int64_t>(16, work / 500));
     p.parts = (int)((p.tiles + each - 1) / each);
     p.chunk = (int)((p.tiles + p.parts - 1) / p.parts + 7) / 8 * 8;
     p.parts = (int)((p.tiles + p.chunk - 1) / p.chunk);
