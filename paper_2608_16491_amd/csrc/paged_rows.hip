@@ -49,6 +49,20 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, int6
 
     const int64_t block = (int64_t)page * c.kv_heads + h;
     const int sub = lane / S::kLanes, at = (lane % S::kLanes) * C;
+    // the page's bounds so far, on their way beside the rows: of a lane's channels,
+    // or where wavefronts join, of a thread's
+    const bool begun = (r0 & (c.page - 1)) == 0;
+    uint16_t* const bounds = (uint16_t*)c.bounds + block * 2 * D;
+    Words<C / 2> was[2];
+    uint16_t was_one = 0;
+    if (c.bounds && !begun) {
+        if constexpr (WAVES == 1) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) was[t] = load_words<C / 2>(bounds + t * D + at);
+        } else {
+            was_one = bounds[min((int)threadIdx.x, 2 * D - 1)];
+        }
+    }
     float lo[C], hi[C];
 #pragma unroll
     for (int i = 0; i < C; ++i) lo[i] = INFINITY, hi[i] = -INFINITY;
@@ -102,43 +116,40 @@ __global__ __launch_bounds__(kBlock) void cache_write(frog_cache_write_t a, int6
             lo[i] = fminf(lo[i], __shfl_xor(lo[i], o));
             hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], o));
         }
+    // (a page begun at its row 0 forgets what it held)
+    auto widened = [&](float x, uint32_t old, bool high) {
+        const float y = begun ? x : __uint_as_float(old << 16);
+        return (bf16_t)(broken || y != y ? NAN : high ? fmaxf(x, y) : fminf(x, y));
+    };
     if constexpr (WAVES > 1) {
-        __shared__ float least[WAVES][D], most[WAVES][D];
+        __shared__ float ends[2][WAVES][D];
         __shared__ int any[WAVES];
         if (sub == 0) {
 #pragma unroll
-            for (int i = 0; i < C; ++i) least[mine][at + i] = lo[i], most[mine][at + i] = hi[i];
+            for (int i = 0; i < C; ++i) ends[0][mine][at + i] = lo[i], ends[1][mine][at + i] = hi[i];
             if (lane == 0) any[mine] = broken;
         }
         __syncthreads();
-        if (mine) return;
+        if (threadIdx.x >= 2 * D) return;
+        const bool high = threadIdx.x >= D;
+        const int i = threadIdx.x - (high ? D : 0);
+        float x = ends[high][0][i];
 #pragma unroll
-        for (int n = 1; n < WAVES; ++n) {
-            broken |= any[n] != 0;
+        for (int n = 1; n < WAVES; ++n) x = high ? fmaxf(x, ends[1][n][i]) : fminf(x, ends[0][n][i]);
 #pragma unroll
-            for (int i = 0; i < C; ++i) lo[i] = fminf(lo[i], least[n][at + i]), hi[i] = fmaxf(hi[i], most[n][at + i]);
-        }
-    }
-    if (sub) return;
-    // (a page begun at its row 0 forgets what it held)
-    bf16_t* p = (bf16_t*)c.bounds + block * 2 * D + at;
-    const bool begun = (r0 & (c.page - 1)) == 0;
+        for (int n = 0; n < WAVES; ++n) broken |= any[n] != 0;
+        ((bf16_t*)bounds)[threadIdx.x] = widened(x, was_one, high);
+    } else if (sub == 0) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const Words<C / 2> old = load_words<C / 2>(p + t * D);
-        Words<C / 2> now;
+        for (int t = 0; t < 2; ++t) {
+            Words<C / 2> now;
 #pragma unroll
-        for (int i = 0; i < C / 2; ++i) {
-            float y[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float x = t ? hi[2 * i + e] : lo[2 * i + e];
-                const float was = begun ? x : __uint_as_float(e ? old.w[i] & 0xFFFF0000u : old.w[i] << 16);
-                y[e] = broken || was != was ? NAN : t ? fmaxf(x, was) : fminf(x, was);
+            for (int i = 0; i < C / 2; ++i) {
+                const float* x = t ? hi : lo;
+                now.w[i] = __builtin_bit_cast(uint32_t, vec<bf16_t, 2>{widened(x[2 * i], was[t].w[i] & 0xFFFF, t), widened(x[2 * i + 1], was[t].w[i] >> 16, t)});
             }
-            now.w[i] = __builtin_bit_cast(uint32_t, vec<bf16_t, 2>{(bf16_t)y[0], (bf16_t)y[1]});
+            store_words(bounds + t * D + at, now);
         }
-        store_words(p + t * D, now);
     }
 }
 
@@ -213,8 +224,9 @@ int launch_cache_write(const frog_cache_write_t& a, hipStream_t stream) {
         };
         // a page whose rows a wavefront has in four rounds is one's alone (8 prompts to
         // 8,000 rows, 8 heads, pages of 16, d = 64: 29 us, by four 55; d = 128, pages of 32, twice
-        // the rounds: 53 us, by four 47)
-        if (a.cache.page <= 4 * RowSplit<d.value>::kRows) run(cache_write<decltype(t), i8.value, d.value, 1>, 1);
+        // the rounds: 53 us, by four 47), unless there are few of them, whose time is
+        // one page's (1,400 fp32 rows, 3 heads, pages of 16, d = 96: 9.9 us, by four 6.9)
+        if (units >= 4096 && a.cache.page <= 4 * RowSplit<d.value>::kRows) run(cache_write<decltype(t), i8.value, d.value, 1>, 1);
         else run(cache_write<decltype(t), i8.value, d.value, kWaves>, kWaves);
     });
     return e == hipSuccess ? FROG_OK : fail(FROG_EHIP, "cache write launch: %s", hipGetErrorString(e));
