@@ -242,9 +242,18 @@ __device__ inline int out_channel(int i, int m) {
     else return D / 16 * i + m;
 }
 
-// One workgroup of W wavefronts a (request, kv head, part of its rows).  Bound by
-// HBM: conversions and softmax take about a third of the cycles that the read
-// of the rows does, so the loads of the next step are only kept in registers.
+// One workgroup of W wavefronts a (request, kv head, part of its rows).  A step of
+// a wavefront is two tiles: their scores (keys x queries), one pass of the running
+// maximum and sum, the second product with the values as they were loaded.  Many
+// long requests are bound by HBM (32 of up to 40,000 rows, 32 / 8 heads, d = 128: 1.36
+// GB in 248 us, 5.5 TB/s; vector instructions 30 % of the CUs' busy time, products a
+// tenth); few query rows over d = 64 with a cap by vector instructions (65 %), of
+// which half turn int8 codes into bf16; a single short request by the chain of
+// a step (about 1 us).
+//   W = 4 with at most 128 registers (d = 128, up to eight query rows), four
+// wavefronts a SIMD: a step's loads need only be one step ahead.  Two steps ahead
+// took 78 us for 77 (chosen pages) and 11.2 for 10.4 (1,001 rows); W = 8 and 16 for
+// long requests 5 to 20 % more, W = 2 the same for twice the parts.
 template <typename T, bool INT8, int D, bool PLAIN, int E, int NQ, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(NQ == 2 || sizeof(T) == 4 ? 2 : W == 8 ? 2 : E < 8 ? 4 : 3)))
 void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedParts parts, uint32_t first_item) {
@@ -283,7 +292,7 @@ void paged_attend(frog_attend_paged_t a, ScoreParams sp, PagedPlan plan, PagedPa
                 place = (int)logical * c.page + sub * kTile;
                 if (place <= walk.hi && place + kTile > walk.lo) {
                     const int page = page_of(a.pages, b, a.pages_per_request, logical, c.num_pages);
-                    if (page >= 0) block = (page * c.kv_heads + h << shift) + sub;
+                    if (page >= 0) block = ((page * c.kv_heads + h) << shift) + sub;
                 }
             }
         }

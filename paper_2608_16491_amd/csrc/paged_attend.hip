@@ -21,31 +21,41 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void paged_join(frog
     const int head = (int)((uint32_t)row % (uint32_t)a.heads);
     const Walk walk(a, b);
     const int live = ((int)(walk.end - walk.first) + plan.chunk - 1) / plan.chunk;
-    float all = kNoneSeen;
-    for (int s = lane; s < live; s += 64) all = fmaxf(all, parts.ml[s * parts.rows + row].x);
-    for (int o = 32; o; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
-    float total = 0.f, x[2] = {0.f, 0.f};
-    for (int s = lane; s < live; s += 64) {
-        const float2 ml = parts.ml[s * parts.rows + row];
-        total += ml.y * exp2_fast(ml.x - all);
-    }
-    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
-    // (parts past the wavefront's last one repeat it, with a share of 0)
     const int each = (live + WAVES - 1) / WAVES, from = WAVES == 1 ? 0 : w * each, to = WAVES == 1 ? live : min(live, from + each);
-    for (int s = from; s < to; s += 8) {
-        float y[8][2], share[8];
+    // (parts past the wavefront's last one repeat it, with a share of 0)
+    float y[8][2], top[8];
+    auto fetch = [&](int s) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int64_t at = (int64_t)min(s + i, to - 1) * parts.rows + row;
-            share[i] = s + i < to ? exp2_fast(parts.ml[at].x - all) : 0.f;
+            top[i] = parts.ml[at].x;
             y[i][0] = parts.o[at * d + min(lane, d - 1)];
             y[i][1] = d > 64 ? parts.o[at * d + min(lane + 64, d - 1)] : 0.f;
         }
+    };
+    if (from < to) fetch(from);
+    float all = kNoneSeen, total = 0.f;
+    float2 ml = make_float2(kNoneSeen, 0.f);
+    if (lane < live) ml = parts.ml[lane * parts.rows + row];
+    all = ml.x;
+    for (int s = lane + 64; s < live; s += 64) all = fmaxf(all, parts.ml[s * parts.rows + row].x);
+    for (int o = 32; o; o >>= 1) all = fmaxf(all, __shfl_xor(all, o));
+    total = ml.y * exp2_fast(ml.x - all);
+    for (int s = lane + 64; s < live; s += 64) {
+        const float2 more = parts.ml[s * parts.rows + row];
+        total += more.y * exp2_fast(more.x - all);
+    }
+    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+    float x[2] = {0.f, 0.f};
+    for (int s = from; s < to;) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[0] += share[i] * y[i][0];
-            x[1] += share[i] * y[i][1];
+            const float share = s + i < to ? exp2_fast(top[i] - all) : 0.f;
+            x[0] += share * y[i][0];
+            x[1] += share * y[i][1];
         }
+        s += 8;
+        if (s < to) fetch(s);
     }
     if constexpr (WAVES > 1) {
         shares[w][lane] = x[0];
