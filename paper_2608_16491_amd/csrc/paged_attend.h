@@ -235,7 +235,8 @@ struct Rows {
     }
 };
 
-// N channels of row i of the second product (value m of it stands for channel_of(i, m))
+// the channel that value m of row i of the second product stands for (two
+// neighbouring ones from an even m on)
 template <int D>
 __device__ inline int out_channel(int i, int m) {
     if constexpr (D == 96) return m < 4 ? 4 * i + m : 64 + 2 * i + m - 4;
@@ -246,8 +247,8 @@ __device__ inline int out_channel(int i, int m) {
 // a wavefront is two tiles: their scores (keys x queries), one pass of the running
 // maximum and sum, the second product with the values as they were loaded.  Many
 // long requests are bound by HBM (32 of up to 40,000 rows, 32 / 8 heads, d = 128: 1.36
-// GB in 248 us, 5.5 TB/s; vector instructions 30 % of the CUs' busy time, products a
-// tenth); few query rows over d = 64 with a cap by vector instructions (65 %), of
+// GB in 248 us, 5.5 TB/s; vector instructions 30 % of the CUs' busy time, products
+// 8 %); few query rows over d = 64 with a cap by vector instructions (65 %), of
 // which half turn int8 codes into bf16; a single short request by the chain of
 // a step (about 1 us).
 //   W = 4 with at most 128 registers (d = 128, up to eight query rows), four

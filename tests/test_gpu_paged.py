@@ -344,6 +344,60 @@ def test_what_no_token_sees_may_hold_anything(kind, store):
     near(lse.cpu(), ref[2], ref[3], "lse")
 
 
+@pytest.mark.parametrize("page,most", [(16, 300), (64, 3000)])
+def test_entries_that_are_no_page_and_lengths_past_the_table(page, most):
+    cache, _, _, pages, n, _ = filled("bf16", "int8", 4, most, 2, 64, page, lengths=[most, most - 1, most // 2, 5], seed=1)
+    pages[0, 2], pages[1, 0], pages[1, -1], pages[2, 1] = -1, cache.shape[0], -2 ** 31, 2 ** 31 - 1
+    pages[3] = -1                                    # a request of no page at all
+    n = n + torch.tensor([page * 9, 2 ** 30, 0, 0], dtype=torch.int32)
+    q = torch.randn((4, 6, 64), generator=torch.Generator().manual_seed(1)).bfloat16()
+    ref = Cache(cache)
+    full = pages.shape[1] * page
+    check(q, cache, pages, n)
+    check(q, cache, pages, n, lr=torch.tensor([[0, full], [page // 2, full - 2], [page, 2 * page - 1], [0, 4]], dtype=torch.int32))
+    for keep in (1, 3, pages.shape[1]):
+        got = F.select_pages(q.cuda(), cache, pages.cuda(), n.cuda(), keep)
+        assert torch.equal(got.cpu(), ref.select(q, pages, n, keep, 0, 1))
+        check(q, cache, pages, n, chosen=got.cpu())
+    for got, want in zip(F.cache_read(cache, pages.cuda(), n.cuda(), full + 20), ref.read(pages, n, full + 20, torch.bfloat16)):
+        assert torch.equal(got.cpu(), want)
+    n[:] = torch.tensor([-1, -2 ** 31, 0, 0], dtype=torch.int32)
+    out, lse = F.attend_paged(q.cuda(), cache, pages.cuda(), n.cuda(), return_lse=True)
+    assert not out.any() and (lse == -math.inf).all()
+    assert (F.select_pages(q.cuda(), cache, pages.cuda(), n.cuda(), 2) == -1).all()
+
+
+def test_arguments_are_refused():
+    cache, _, _, pages, n, _ = filled("bf16", "int8", 2, 50, 2, 64, 16, lengths=[50, 20])
+    pages, n = pages.cuda(), n.cuda()
+    q, k = torch.randn(2, 4, 64, device="cuda").bfloat16(), torch.randn(2, 2, 64, device="cuda").bfloat16()
+    bad = [lambda: F.attend_paged(q[:1], cache, pages, n), lambda: F.attend_paged(q[..., :32], cache, pages, n), lambda: F.attend_paged(q.double(), cache, pages, n),
+           lambda: F.attend_paged(q.cpu(), cache, pages, n), lambda: F.attend_paged(q, cache, pages.long(), n), lambda: F.attend_paged(q, cache, pages, n[:1]),
+           lambda: F.attend_paged(q, cache, pages.t(), n), lambda: F.attend_paged(q, cache, pages, n, chosen=pages), lambda: F.attend_paged(q, cache, pages, n, lr=pages),
+           lambda: F.attend_paged(q, cache, pages, n, slopes=torch.ones(3, device="cuda")), lambda: F.attend_paged(q.requires_grad_(), cache, pages, n),
+           lambda: F.attend_paged(q.detach().transpose(1, 2).contiguous().transpose(1, 2), cache, pages, n),
+           lambda: F.select_pages(q.detach(), cache, pages, n, 2, first=2), lambda: F.select_pages(q.detach(), cache, pages, n, 2, recent=-1),
+           lambda: F.select_pages(q.detach(), F.PagedCache(cache.k, cache.v, cache.k_exp, cache.v_exp), pages, n, 2),
+           lambda: F.cache_write(cache, k, k[:1], pages, n), lambda: F.cache_write(cache, k[..., :32], k[..., :32], pages, n),
+           lambda: F.cache_write(cache, k, k.half(), pages, n), lambda: F.cache_write(cache, k, k, pages, n, starts=n),
+           lambda: F.cache_write(cache, k.clone().requires_grad_(), k, pages, n), lambda: F.cache_read(cache, pages, n, -1),
+           lambda: F.cache_read(cache, pages, n, dtype=torch.float64), lambda: F.PagedCache(cache.k, cache.v[:1], cache.k_exp, cache.v_exp),
+           lambda: F.PagedCache(cache.k, cache.v, cache.k_exp, cache.v_exp.int()), lambda: F.PagedCache(cache.k.transpose(0, 1), cache.v, cache.k_exp, cache.v_exp),
+           lambda: F.PagedCache.empty(2, 1, 64, page=48), lambda: F.PagedCache.empty(2, 1, 80)]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            print("not refused:", i)
+    q = q.detach()
+    three = torch.randn(3, 2, 64, device="cuda").bfloat16()
+    for f in (lambda: F.cache_write(cache, three, three, pages, n),                                         # no equal shares
+              lambda: F.attend_paged(torch.randn(2, 3, 64, device="cuda"), cache, pages, n),                # 3 heads over 2
+              lambda: F.attend_paged(torch.randn(2, 4, 72, device="cuda")[..., 3:67], cache, pages, n),     # rows off a boundary
+              lambda: F.attend_paged(q, cache, pages, n, cap=-1.0)):
+        with pytest.raises(F.FrogError):
+            f()
+
+
 def test_a_row_that_is_not_a_number_reaches_who_sees_it():
     cache, _, _, pages, n, _ = filled("bf16", "e4m3", 2, 100, 2, 64, 16, lengths=[100, 90], bounds=False)
     x = torch.full((2, 2, 64), math.nan)
@@ -448,6 +502,30 @@ def test_two_graphs_do_not_share_a_workspace():
                 graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(x, y) for x, y in zip(outs, want))
+
+
+def test_threads_on_streams_of_their_own():
+    import threading
+    cache, _, _, pages, n, _ = filled("bf16", "int8", 3, 9000, 2, 64, 16, seed=2)
+    pages, n = pages.cuda(), n.cuda()
+    qs = [torch.randn((3, 4, 64), generator=torch.Generator().manual_seed(i)).bfloat16().cuda() for i in range(3)]
+    want = [(F.attend_paged(q, cache, pages, n), F.select_pages(q, cache, pages, n, 20)) for q in qs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                got = F.attend_paged(qs[i], cache, pages, n), F.select_pages(qs[i], cache, pages, n, 20)
+                torch.cuda.current_stream().synchronize()
+                wrong.extend(i for x, y in zip(got, want[i]) if not torch.equal(x, y))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
 
 
 def test_a_cache_beyond_32_bit_offsets():
