@@ -101,9 +101,10 @@ PagedPlan plan_of(const frog_attend_paged_t& a) {
     }
     // Lists of pages are equally long: a workgroup a list, where that fills the CUs
     // (48 requests of 64 pages of 64 rows, 8 kv heads: 77 us, in two parts 76 + 5, in
-    // six 82 + 5).  So are short requests of many (64 to 2,000 rows, 8 kv heads: 30.4 us,
-    // in two parts 36.8).
-    if (p.tiles <= (a.chosen ? pairs >= 256 ? kMostTiles : 0 : pairs >= 512 ? 128 : 0)) {
+    // six 82 + 5).  So are requests to 4,096 rows of many pairs, long and short ones side
+    // by side (8 kv heads, 64 requests to 2,000 rows 30.4 us, in two parts 36.8; 128 to 3,000
+    // 91, in three to six 89 to 108; 200 to 2,500 106, 101 to 135; 64 to 4,000 67, 64 to 85).
+    if (pairs >= (a.chosen ? 256 : 512) && p.tiles <= kMostTiles) {
         p.chunk = kMostTiles;
         return p;
     }
