@@ -117,6 +117,12 @@ def _query(q, cache, batch):
     return kind
 
 
+def _most_workspace(batch, heads, d, rows):
+    """Bytes that an attention call over ``rows`` rows a request takes at most: a part has 256 of them or more, and keeps an
+    output, a maximum and a sum of every query row."""
+    return batch * heads * (d + 2) * 4 * -(-rows // 256)
+
+
 def cache_write(cache, k, v, pages, lengths, *, starts=None, stream=None):
     """Append rows to the requests of a cache, quantised.
 
@@ -225,7 +231,9 @@ def attend_paged(q, cache, pages, lengths, *, chosen=None, lr=None, scale=None, 
                 0 if lse is None else lse.data_ptr())
         tail = (b, width, num, h, kind, d ** -0.5 if scale is None else scale, cap)
         args, ws, L = _pack_paged(*head, 0, 0, *tail), None, lib()
-        if _own_workspace(q.numel() * width * page > 2 ** 36):
+        # (the listed pages, or else the table's width, are what a call is cut by)
+        most = _most_workspace(b, h, d, (width if chosen is None else num) * page)
+        if _own_workspace(most > 2 ** 26 and L.frog_attend_paged_workspace(args) > 2 ** 26):
             ws, at = _workspace(L.frog_attend_paged_workspace, args, q.device)
             args = _pack_paged(*head, *at, *tail)
         _launch(L.frog_attend_paged, args, q.device)
