@@ -62,3 +62,131 @@ def test_only_workspaces_to_64_mib_stay_with_the_library(monkeypatch, b, h, kv, 
     small = F.attend_paged(q, cache, pages[:, :1].contiguous(), n)
     assert small[-1].any() and not small[:-1].any()
     assert torch.equal(out, small)
+
+
+# ------------------------------------------------------------------ many small pages written
+
+LIMIT = {"e4m3": 448.0, "int8": 127.0}
+ONE_WAVE = {32: 64, 64: 32, 96: 32, 128: 16}      # largest page whose rows a wavefront has in four rounds
+
+
+def quantised(x, store):
+    """Codes (float64) and bytes of rows in float64: the least power of at least -100 that the largest magnitude fits."""
+    fine = torch.isfinite(x).all(-1)
+    x = torch.where(fine.unsqueeze(-1), x, 0.0)
+    a = x.abs().amax(-1)
+    e = torch.ceil(torch.log2((a / LIMIT[store]).clamp(min=2.0 ** -110)))
+    e = torch.where(a > LIMIT[store] * torch.exp2(e), e + 1, e)
+    e = torch.where(a <= LIMIT[store] * torch.exp2(e - 1), e - 1, e).clamp(min=-100)
+    y = x * torch.exp2(-e).unsqueeze(-1)
+    if store == "e4m3":
+        unit = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+        y = torch.round(y / unit) * unit
+    else:
+        y = torch.round(y)
+    return y, torch.where(fine, e + 127, 255.0)
+
+
+class Arrays:
+    """The cache's arrays in 64 bits on the host, all rows of a call at a time."""
+
+    def __init__(self, cache):
+        self.store = "int8" if cache.k.dtype == torch.int8 else "e4m3"
+        self.of(cache)
+
+    def of(self, cache):
+        self.t = {x: getattr(cache, x).cpu().float().double() for x in ("k", "v", "k_exp", "v_exp", "bounds")}
+
+    def write(self, k, v, pages, lengths, starts):
+        num, kv, page, d = self.t["k"].shape
+        b, width = pages.shape
+        starts, lengths = starts.long(), lengths.long()
+        token = torch.arange(int(starts[0]), int(starts[-1]))
+        request = torch.searchsorted(starts[1:].contiguous(), token, right=True)
+        place = lengths[request] - starts[request + 1] + token
+        inside = (place >= 0) & (place < width * page)
+        at = torch.where(inside, pages[request, (place // page).clamp(0, width - 1)].long(), -1)
+        inside &= (at >= 0) & (at < num)
+        token, at, row = token[inside], at[inside], place[inside] % page
+        for x, t in (("k", k), ("v", v)):
+            codes, byte = quantised(t[token].double(), self.store)
+            self.t[x][at, :, row] = codes
+            self.t[x + "_exp"][at, :, row] = byte
+            if x == "k":
+                value = torch.where((byte == 255).unsqueeze(-1), torch.nan, codes * torch.exp2(byte - 127).unsqueeze(-1))
+                old = self.t["bounds"]
+                begun = at[row == 0]
+                old[begun, :, 0], old[begun, :, 1] = torch.inf, -torch.inf
+                index = at.view(-1, 1, 1).expand_as(value)
+                # (amin and amax hand a NaN on)
+                least = old[:, :, 0].contiguous().scatter_reduce_(0, index, value, "amin")
+                most = old[:, :, 1].contiguous().scatter_reduce_(0, index, value, "amax")
+                # a head with a row that is not finite has no bounds in any channel
+                lost = torch.zeros((num, kv), dtype=torch.bool)
+                lost[at] |= False
+                lost.view(-1)[(at.unsqueeze(1) * kv + torch.arange(kv))[byte == 255]] = True
+                least[lost], most[lost] = torch.nan, torch.nan
+                self.t["bounds"] = torch.stack([least, most], 2)
+
+    def same(self, cache):
+        for x, want in self.t.items():
+            got = getattr(cache, x).cpu().float().double()
+            assert torch.equal(torch.isnan(got), torch.isnan(want)), x
+            wrong = (got.nan_to_num(0.0) != want.nan_to_num(0.0)).nonzero()
+            assert len(wrong) == 0, (x, len(wrong), wrong[:3].tolist())
+
+
+@pytest.mark.parametrize("store", ["e4m3", "int8"])
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16, torch.float32], ids=["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("d,page", [(32, 16), (32, 64), (64, 16), (64, 32), (96, 16), (96, 32), (128, 16)])
+def test_many_small_pages(kind, store, d, page):
+    """Pages that a wavefront writes alone: prompts, pieces and single rows behind them, in a call of 4,096 (page, head) and more."""
+    say("small pages", kind, store, d, page)
+    assert page <= ONE_WAVE[d]
+    b, kv, width = 300, 7, max(2, 64 // page)
+    g = torch.Generator().manual_seed(d + page)
+    total = b * width + 5
+    pages = torch.randperm(total, generator=g)[: b * width].view(b, width).to(torch.int32)
+    pages[3, 1], pages[8, 0], pages[9, -1] = -1, total, -2 ** 31
+    cache = F.PagedCache.empty(total, kv, d, page=page, storage=store)
+    ref = Arrays(cache)
+    n = torch.zeros(b, dtype=torch.long)
+    for step, most in enumerate((40, 1, 20, page)):
+        new = torch.randint(0, most + 1, (b,), generator=g) if step != 1 else torch.ones(b, dtype=torch.long)
+        new[0], new[1] = most, 0
+        n = (n + new).clamp(max=width * page)
+        length = n.clone()
+        if step == 2:
+            length[5], length[6], length[7] = new[5] - 3, 2 ** 30, -1    # rows before a request's start, past its pages, of none
+        starts = torch.cat([torch.zeros(1, dtype=torch.long), new.cumsum(0)]).to(torch.int32)
+        tokens = int(starts[-1])
+        assert (tokens // page + 2 * b) * kv >= 4096
+        k, v = (torch.randn((tokens, kv, d), generator=g) * torch.exp(torch.randn((tokens, kv, 1), generator=g)) for _ in range(2))
+        k[..., 1] *= 7.0
+        if step != 1:
+            k[tokens // 2, 2, d - 1], k[tokens // 3, 0, 0], v[tokens // 2 + 1, 1, 5] = torch.nan, -torch.inf, torch.inf
+        k, v = k.to(kind), v.to(kind)
+        F.cache_write(cache, k.cuda(), v.cuda(), pages.cuda(), length.to(torch.int32).cuda(), starts=starts.cuda())
+        ref.write(k, v, pages, length, starts)
+        ref.same(cache)
+
+
+@pytest.mark.parametrize("store", ["e4m3", "int8"])
+def test_small_pages_in_one_call_or_several(store):
+    """The same rows by one wavefront a page and, in calls of fewer requests, by four."""
+    b, kv, d, page = 520, 4, 64, 32
+    g = torch.Generator().manual_seed(4)
+    n = torch.randint(1, 2 * page + 1, (b,), generator=g)
+    pages = torch.randperm(2 * b, generator=g).view(b, 2).to(torch.int32).cuda()
+    one, many = (F.PagedCache.empty(2 * b, kv, d, page=page, storage=store) for _ in range(2))
+    k, v = (torch.randn((int(n.sum()), kv, d), generator=g).half().cuda() for _ in range(2))
+    starts = torch.cat([torch.zeros(1, dtype=torch.long), n.cumsum(0)])
+    length = n.to(torch.int32).cuda()
+    assert (len(k) // page + 2 * b) * kv >= 4096
+    F.cache_write(one, k, v, pages, length, starts=starts.to(torch.int32).cuda())
+    for i in range(0, b, 65):
+        s = starts[i:i + 66]
+        assert (int(s[-1] - s[0]) // page + 130) * kv < 4096
+        F.cache_write(many, k[s[0]:s[-1]], v[s[0]:s[-1]], pages[i:i + 65], length[i:i + 65], starts=(s - s[0]).to(torch.int32).cuda())
+    for x in ("k", "v", "k_exp", "v_exp", "bounds"):
+        assert torch.equal(getattr(one, x).view(torch.uint8), getattr(many, x).view(torch.uint8)), x
