@@ -9,6 +9,8 @@ pytestmark = pytest.mark.gpu
 
 import paper_2608_16491_amd as F  # noqa: E402
 from paper_2608_16491_amd import paged as G  # noqa: E402
+from tests.attention_ref import near  # noqa: E402
+from tests.paged_ref import Cache  # noqa: E402
 
 
 def say(*what):
@@ -190,3 +192,37 @@ def test_small_pages_in_one_call_or_several(store):
         F.cache_write(many, k[s[0]:s[-1]], v[s[0]:s[-1]], pages[i:i + 65], length[i:i + 65], starts=(s - s[0]).to(torch.int32).cuda())
     for x in ("k", "v", "k_exp", "v_exp", "bounds"):
         assert torch.equal(getattr(one, x).view(torch.uint8), getattr(many, x).view(torch.uint8)), x
+
+
+# ------------------------------------------------------------------ many requests that are not split
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16, torch.float32], ids=["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("h,kv,d,page,width", [(2, 2, 32, 16, 65), (8, 2, 128, 64, 64), (8, 1, 96, 256, 16), (26, 2, 64, 32, 100),
+                                               (36, 2, 128, 16, 256), (40, 1, 64, 128, 32)])
+def test_requests_of_many_pairs_are_whole(kind, h, kv, d, page, width):
+    """512 and more (request, kv head) pairs, tables of 65 to 256 tiles: a workgroup walks a whole request."""
+    say("whole requests", kind, h, kv, d, page, width)
+    b, rows = 512 // kv + 3, width * page
+    assert 64 < rows // 16 <= 256 and b * kv >= 512
+    # (pages that many requests read)
+    g = torch.Generator().manual_seed(h + d)
+    total = 40 * 64 // page + 30
+    cache = F.PagedCache.empty(total, kv, d, page=page, storage="int8" if h % 8 else "e4m3", bounds=False)
+    k, v = ((torch.randn((total * page, kv, d), generator=g) * torch.exp(0.5 * torch.randn((total * page, kv, 1), generator=g))).to(kind).cuda() for _ in range(2))
+    F.cache_write(cache, k, v, torch.arange(total, dtype=torch.int32).view(1, -1).cuda(), torch.tensor([total * page], dtype=torch.int32).cuda())
+    pages = torch.randint(0, total, (b, width), generator=g, dtype=torch.int32)
+    pages[5, width // 2] = -1
+    n = torch.randint(1, rows + 1, (b,), generator=g, dtype=torch.int32)
+    n[0], n[1], n[2], n[3], n[4], n[5] = rows, 0, rows - 1, 1, 2 ** 30, rows - 17
+    q = (torch.randn((b, h, d), generator=g) * 1.2).to(kind)
+    lo = torch.randint(-5, rows, (b,), generator=g, dtype=torch.int32)
+    lr = torch.stack([lo, lo + torch.randint(-1, rows, (b,), generator=g, dtype=torch.int32)], -1)
+    lr[0], lr[2] = torch.tensor([0, rows - 1]), torch.tensor([rows - 2, rows + 9])
+    slopes = torch.exp2(-8.0 * torch.arange(1, h + 1) / h)
+    at, ref = [0, 1, 2, 3, 4, 5, b // 3, b // 2, b - 1], Cache(cache)
+    for kw in ({}, {"lr": lr}, {"lr": lr, "cap": 12.0, "slopes": slopes}):
+        args = {x: y.cuda() if torch.is_tensor(y) else y for x, y in kw.items()}
+        out, lse = F.attend_paged(q.cuda(), cache, pages.cuda(), n.cuda(), return_lse=True, **args)
+        want, err, lw, le = ref.attend(q[at], pages[at], n[at], **{x: y[at] if x == "lr" else y for x, y in kw.items()})
+        near(out[at].cpu(), want, err, f"out {list(kw)}")
+        near(lse[at].cpu(), lw, le, f"lse {list(kw)}")
