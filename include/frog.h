@@ -457,7 +457,10 @@ int frog_evict(const frog_evict_t* a, void* stream);
  * of the page pages[request][t / page]: pages is a table
  * [batch][pages_per_request] of page numbers.  Entries past a request's length
  * are not read into a result, lengths are clipped to [0, pages_per_request *
- * page], and an entry outside [0, num_pages) counts as no rows.  One token that
+ * page], and an entry outside [0, num_pages) counts as no rows.  Calls are cut
+ * into workgroups by the width of the table (or of the lists of chosen pages),
+ * since the lengths are on the device: one much wider than the longest request
+ * costs time and workspace.  One token that
  * is decoded several times at once (a draft of the next tokens) is several
  * requests of the same pages with lengths that grow by one.
  * `bounds` are, per page and kv head, the least and the largest value of every
@@ -483,8 +486,9 @@ typedef struct {
  * become the last rows of request b, whose length with them is lengths[b].
  * starts NULL: tokens / batch rows each.  A row before the request's start or
  * past its pages, or of a page that is none, is not written.  starts ascend and
- * end at `tokens` at most (rows outside are not read).  A page that two
- * requests write in one call holds a mixture of both. */
+ * end at `tokens` at most (rows outside are not read).  A page that is written
+ * at two places of one call (by two requests, or listed twice by one) holds a
+ * mixture of both, its bounds too. */
 typedef struct {
     frog_cache_t cache;
     const void* k; int64_t k_stride[2];        /* [tokens, kv_heads, d]: token, head */
@@ -524,7 +528,10 @@ int frog_cache_read(const frog_cache_read_t* a, void* stream);
  * counts as the largest; a page that is none as the smallest).  chosen lists
  * them ascending, as numbers within the request (0 .. pages_per_request - 1),
  * and holds -1 behind them.
- * first + recent <= keep. */
+ * first + recent <= keep.  The bound is one of q . k: what frog_attend_paged may
+ * do to scores besides is not in it.  A cap keeps the order of one head's; a
+ * distance bias does not, with a negative scale the largest bounds are the
+ * smallest scores, and pages outside lr are chosen like others. */
 typedef struct {
     frog_cache_t cache;                        /* k, v and their powers may be NULL */
     const void* q; int64_t q_stride[2];        /* [batch, heads, d]: request, head */
@@ -546,7 +553,8 @@ int frog_select_pages(const frog_select_pages_t* a, void* stream);
  * numbers as floats: exact up to 2^24).  lr (optional) limits the rows a
  * request sees.  chosen (optional) [batch][kv_heads][num_chosen]: pages of the
  * request by their numbers within it, in any order; an entry outside [0,
- * pages_per_request) is none, and a page listed twice counts twice.  Codes and
+ * pages_per_request) is none, and a page listed twice counts twice; an entry
+ * that is none, or whose rows are not seen, takes as long as a page.  Codes and
  * powers enter the products exactly; queries, weights and sums are as exact as
  * 32 bits for fp32 queries, and for 16-bit ones weights are held to 2^-16.  The
  * rows' magnitudes must stay below 2^100, those behind a length may be anything. */

@@ -251,8 +251,14 @@ __device__ inline int out_channel(int i, int m) {
 // 8 %); few query rows over d = 64 with a cap by vector instructions (65 %), of
 // which half turn int8 codes into bf16; a single short request by the chain of
 // a step (about 1 us).
+//   Every tile of a part is walked, those of list entries that are none, of pages
+// past a length and of pages outside lr among them (masked, with block 0's rows): a
+// list costs what it has room for (48 requests of 300 to 1,000 rows, 32 / 8 heads, d = 128:
+// without a list 21 us, with their pages in lists of 16 pages of 64 rows 26, of 64 60).
 //   W = 4 with at most 128 registers (d = 128, up to eight query rows), four
-// wavefronts a SIMD: a step's loads need only be one step ahead.  Two steps ahead
+// wavefronts a SIMD: a step's loads need only be one step ahead.  (fp16 of d = 128 and
+// up to four query rows spills 1 to 9 registers there: 32 requests to 8,000 rows, 32 / 8
+// heads, 73 us with the join, bf16 65.5.)  Two steps ahead
 // took 78 us for 77 (chosen pages) and 11.2 for 10.4 (1,001 rows); W = 8 and 16 for
 // long requests 5 to 20 % more, W = 2 the same for twice the parts.
 template <typename T, bool INT8, int D, bool PLAIN, int E, int NQ, int W>

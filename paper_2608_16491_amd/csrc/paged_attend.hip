@@ -93,7 +93,10 @@ PagedPlan plan_of(const frog_attend_paged_t& a) {
     p.waves = 4;
     p.parts = 1;
     // one launch for up to 1,024 rows (the host's time for two is above what the
-    // device saves: 1,001 rows of 4 kv heads 10.4 us, in parts 5.7 + 3.8)
+    // device saves: 1,001 rows of 4 kv heads 10.4 us, in parts 5.7 + 3.8); with two
+    // column tiles, whose steps are longer and whose workgroups have four wavefronts
+    // for eight, for up to 256, the least part (64 / 1 heads, d = 128, on the device: 1,000
+    // rows in parts 12.2 us, whole 16.5; 500 rows 12.1 and 11.5; 250 rows 9.1)
     if (p.tiles <= (p.wide ? 0 : 64)) {
         p.waves = p.wide ? 4 : 8;
         p.chunk = 64;
@@ -110,8 +113,13 @@ PagedPlan plan_of(const frog_attend_paged_t& a) {
     }
     // Else a workgroup begins (about 4 us) for 16 to 64 tiles (1 us for 8), more of
     // them where there is more to do, since the longest request decides and the
-    // parts are read again; of very large calls for 128.  Tiles a part, us of a
-    // call (bf16, e4m3, requests of all lengths up to the one named):
+    // parts are read again; of very large calls for 128.  A call is cut by the width of
+    // its table (its lists), since the lengths are on the device: parts past a
+    // request's rows end at once, but they count in this rule, and in the workspace
+    // (48 to 4,000 rows, 16 / 2 heads: 19.3 us, in a table of 32,000 rows 32).
+    // Tiles a part, us of a call (bf16, e4m3, requests of all lengths up to the one
+    // named; fp16 and fp32 are cut alike, and at these sizes within 14 % of their
+    // own best, bf16 within 12 %):
     //   rows, requests, heads, d       16     24     32     48     64     96    128
     //   60,000   1  32 / 8   128     36.4   32.8   31.0   31.5   28.5   30.0   30.0
     //   10,000   1  32 / 8   128     14.8   15.3   15.3   16.6   18.2   21.7   25.3

@@ -1,8 +1,11 @@
 // Rows into a cache in 8-bit pages and back (include/frog.h: frog_cache_write,
 // frog_cache_read).  Both move every byte once and are bound by HBM: prompts of
 // 104,000 rows of 8 heads, d = 128, bf16 to e4m3 639 MB in 127 us (5.0 TB/s); 1.08 GB
-// back in 209 (5.1).  d = 96 (rows of 12 lanes' pieces) and 32 (a byte of power for 32
-// of codes) reach 0.75 and 0.6 of that.  A few rows take a chain of five loads: 5.4 us.
+// back in 209 (5.1); fp32 rows 1.06 GB in 222 (4.8).  Prompts of 8 x 8,000 rows at d = 128,
+// 96, 64 and 32: 49, 46, 26.5 and 18 us, 0.91, 0.72, 0.84 and 0.62 of a copy's rate.  (d = 96
+// has 8 lanes of 12 values a row, whose pieces of 24 bytes leave gaps in each load; d = 32
+// 4 lanes, one of which stores a byte of power for 32 of codes; what each costs is not
+// measured.)  A few rows take a chain of five loads: 5.4 us.
 
 #include "paged.h"
 

@@ -131,7 +131,7 @@ def cache_write(cache, k, v, pages, lengths, *, starts=None, stream=None):
     in order; lengths int32 [batch]: the requests' rows with the new ones.
     starts int32 [batch + 1]: request b's new rows are starts[b] .. starts[b + 1]
     - 1, its last ones (None: tokens / batch each).  A page belongs to the
-    request that writes it.  The bounds of a page written from its row 0 on are
+    request that writes it, which lists it once.  The bounds of a page written from its row 0 on are
     those of the new rows, else they widen the old ones."""
     _no_gradient(("k", "v"), (k, v))
     kind = _values(("k", "v"), (k, v), (3, 3))
@@ -180,7 +180,8 @@ def select_pages(q, cache, pages, lengths, keep, *, first=0, recent=1, stream=No
     the largest bound on the head's scores, q [batch, heads, d], summed over the
     heads that share the kv head (equal: the lower page).  Returns int32 [batch,
     kv_heads, keep]: numbers of pages within the request, ascending, -1 behind
-    them, for ``chosen`` of :func:`attend_paged`."""
+    them, for ``chosen`` of :func:`attend_paged`.  The bound is one of q . k: a
+    distance bias, an ``lr`` or a negative scale of that call is not in it."""
     _no_gradient(("q",), (q,))
     table, rows, b, width = _table(cache, pages, lengths)
     kind = _query(q, cache, b)
@@ -206,7 +207,8 @@ def select_pages(q, cache, pages, lengths, keep, *, first=0, recent=1, stream=No
 def attend_paged(q, cache, pages, lengths, *, chosen=None, lr=None, scale=None, cap=0.0, slopes=None, return_lse=False, stream=None):
     """Attention of one token per request, q [batch, heads, d], over the rows of
     its pages, or over the ``chosen`` ones (int32 [batch, kv_heads, n], as
-    :func:`select_pages` gives them).  lr int32 [batch, 2]: the interval of rows
+    :func:`select_pages` gives them; an entry of -1 takes as long as a page).  A
+    table much wider than the longest request costs time.  lr int32 [batch, 2]: the interval of rows
     a request sees (None: all).  scale, cap and slopes [heads] as for
     :func:`attend`; the query stands on the request's last row.  Several tokens
     of one request at once are several requests of the same pages with lengths
