@@ -557,7 +557,8 @@ int frog_select_pages(const frog_select_pages_t* a, void* stream);
  * that is none, or whose rows are not seen, takes as long as a page.  Codes and
  * powers enter the products exactly; queries, weights and sums are as exact as
  * 32 bits for fp32 queries, and for 16-bit ones weights are held to 2^-16.  The
- * rows' magnitudes must stay below 2^100, those behind a length may be anything. */
+ * rows' and the queries' magnitudes must stay below 2^100 (rows behind a length
+ * may be anything). */
 typedef struct {
     frog_cache_t cache;
     const void* q; int64_t q_stride[2];        /* [batch, heads, d]: request, head */

@@ -226,3 +226,59 @@ def test_requests_of_many_pairs_are_whole(kind, h, kv, d, page, width):
         want, err, lw, le = ref.attend(q[at], pages[at], n[at], **{x: y[at] if x == "lr" else y for x, y in kw.items()})
         near(out[at].cpu(), want, err, f"out {list(kw)}")
         near(lse[at].cpu(), lw, le, f"lse {list(kw)}")
+
+
+# ------------------------------------------------------------------ more workgroups than a launch takes
+
+def test_attention_and_selection_in_several_launches():
+    """2^21 requests of 8 kv heads over a few pages: 2^33 threads and more, against the same requests in a call of 4,096."""
+    g = torch.Generator(device="cuda").manual_seed(0)
+    kv, d, page, few, b = 8, 32, 16, 4096, 2 ** 21 + 7
+    say("several launches", b)
+    cache = F.PagedCache.empty(64, kv, d, page=page)
+    k, v = (torch.randn((64 * page, kv, d), generator=g, device="cuda") for _ in range(2))
+    every = torch.arange(64, dtype=torch.int32, device="cuda").view(1, -1)
+    F.cache_write(cache, k, v, every, torch.full((1,), 64 * page, dtype=torch.int32, device="cuda"))
+    pages = torch.randint(0, 64, (few, 3), generator=g, device="cuda", dtype=torch.int32)
+    n = torch.randint(0, 3 * page + 1, (few,), generator=g, device="cuda", dtype=torch.int32)
+    q = torch.randn((few, 2 * kv, d), generator=g, device="cuda").bfloat16()
+    at = torch.randint(0, few, (b,), generator=g, device="cuda")
+    want, lse = F.attend_paged(q, cache, pages, n, return_lse=True)
+    chosen = F.select_pages(q, cache, pages, n, 2)
+    out, got = F.attend_paged(q[at], cache, pages[at], n[at], return_lse=True)
+    assert torch.equal(out, want[at]) and torch.equal(got, lse[at])
+    assert torch.equal(F.select_pages(q[at], cache, pages[at], n[at], 2), chosen[at])
+
+
+def test_rows_in_several_launches():
+    """2^21 requests of a row of 16 heads written, 2^24 blocks of 16 rows read, against parts of them in calls of their own."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+    kv, d, b = 16, 32, 2 ** 21 + 3
+    say("rows in several launches", b)
+    cache = F.PagedCache.empty(b, kv, d, page=16, storage="int8")
+    x = torch.randn((b, kv, d), generator=g, device="cuda").bfloat16()
+    pages = torch.randperm(b, generator=g, device="cuda").to(torch.int32).view(b, 1)
+    one = torch.ones(b, dtype=torch.int32, device="cuda")
+    F.cache_write(cache, x, -x, pages, one)
+    small = F.PagedCache.empty(1000, kv, d, page=16, storage="int8")
+    own = torch.arange(1000, dtype=torch.int32, device="cuda").view(-1, 1)
+    for i in (0, b // 2, b - 1000):
+        F.cache_write(small, x[i:i + 1000], -x[i:i + 1000], own, one[:1000])
+        where = pages[i:i + 1000, 0].long()
+        for name in ("k", "v", "k_exp", "v_exp", "bounds"):
+            assert torch.equal(getattr(cache, name)[where], getattr(small, name)), (name, i)
+    k, v = F.cache_read(cache, pages, one, 1)
+    # (a code is off by half a step of at most 1 / 63.5 of the largest magnitude: what it is above, half the limit)
+    assert ((k[:, 0].float() - x.float()).abs().amax(-1) <= x.float().abs().amax(-1) / 127).all() and torch.equal(k, -v)
+    del cache, small, x, k, v, pages, one
+    b, width = 2 ** 20 + 5, 17
+    cache = F.PagedCache.empty(64, 1, d, page=16)
+    k = torch.randn((1024, 1, d), generator=g, device="cuda")
+    every = torch.arange(64, dtype=torch.int32, device="cuda").view(1, -1)
+    F.cache_write(cache, k, -k, every, torch.full((1,), 1024, dtype=torch.int32, device="cuda"))
+    pages = torch.randint(0, 64, (b, width), generator=g, device="cuda", dtype=torch.int32)
+    n = torch.randint(0, 16 * width + 1, (b,), generator=g, device="cuda", dtype=torch.int32)
+    k, v = F.cache_read(cache, pages, n, 16 * width)
+    for i in (0, b // 2, 2 ** 24 // width - 1000, b - 2000):
+        some = F.cache_read(cache, pages[i:i + 2000], n[i:i + 2000], 16 * width)
+        assert torch.equal(k[i:i + 2000], some[0]) and torch.equal(v[i:i + 2000], some[1]), i
